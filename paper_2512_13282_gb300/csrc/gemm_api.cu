@@ -1175,6 +1175,43 @@ void gemm_profile_events(void *start_event, void *stop_event) {
 
 namespace gb300 {
 
+gemm_status_t op_context(cudaStream_t st, OpContext *c) {
+  DeviceState *d = nullptr;
+  const gemm_status_t s = device_state(&d);
+  if (s != GEMM_OK) return s;
+  *c = OpContext{d->sms, d->err, wait_limit_ns(), st};
+  return GEMM_OK;
+}
+
+gemm_status_t with_scratch(cudaStream_t st, gemm_status_t (*body)(const OpContext &, void *), void *arg) {
+  DeviceState *d = nullptr;
+  const gemm_status_t s = device_state(&d);
+  if (s != GEMM_OK) return s;
+  const ScratchLease lease(*d, st);
+  return body(OpContext{d->sms, d->err, wait_limit_ns(), st}, arg);
+}
+
+gemm_status_t op_workspace(size_t bytes, cudaStream_t st, void **ws) {
+  const gemm_status_t s = ensure_workspace(bytes, st);
+  *ws = s == GEMM_OK ? scratch_ws() : nullptr;
+  return s;
+}
+
+void count_launches(int n) { g_launches.fetch_add((uint64_t)n); }
+
+bool bf16_box_map(CUtensorMap *map, const void *base, uint64_t inner, uint64_t outer, uint64_t ld, uint32_t box_inner,
+                  uint32_t box_outer) {
+  return encode_bf16_2d(map, base, inner, outer, ld, box_inner, box_outer);
+}
+
+bool float_out_map(CUtensorMap *map, bool bf16, const void *base, uint64_t N, uint64_t M, uint64_t ld,
+                   uint64_t splits) {
+  return encode_out(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, bf16 ? 2 : 4, base,
+                    N, M, ld, splits);
+}
+
+bool tma_store_enabled() { return overrides().tma_store; }
+
 gemm_status_t validate_s8(int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, const void *B,
                           int64_t ldb, int b_layout, const void *C, int64_t ldc) {
   gemm_status_t s = check_common(M, N, K, A, lda, B, ldb, b_layout, C, ldc);

@@ -47,6 +47,37 @@ cudaError_t launch_ex(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem
   return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...);
 }
 
+// What an operator's call works with on the current device.
+struct OpContext {
+  int sms;
+  uint32_t *err;  // device error word
+  uint64_t wait_limit_ns;
+  cudaStream_t st;
+};
+// Looks up the current device (gemm_api.cu); GEMM_ERR_UNSUPPORTED where it
+// is not sm_103.
+gemm_status_t op_context(cudaStream_t st, OpContext *c);
+// The same, holding the stream's scratch while `body(context, arg)` runs;
+// op_workspace() within it grows the scratch to `bytes` (stream-ordered; in a
+// capture it must be large enough already) and returns it.
+gemm_status_t with_scratch(cudaStream_t st, gemm_status_t (*body)(const OpContext &, void *), void *arg);
+template <typename F>
+gemm_status_t with_scratch(cudaStream_t st, F &&f) {
+  return with_scratch(st, [](const OpContext &c, void *arg) { return (*static_cast<F *>(arg))(c); }, &f);
+}
+gemm_status_t op_workspace(size_t bytes, cudaStream_t st, void **ws);
+// Counts kernels for gemm_launch_count().
+void count_launches(int n);
+// Tensor maps: a bf16 matrix read in boxes (rows of `inner` contiguous
+// elements, 128-byte swizzle), and an output written in boxes of 32 rows x 32
+// columns (fp32 or bf16; splits > 1: planes of partials).
+bool bf16_box_map(CUtensorMap *map, const void *base, uint64_t inner, uint64_t outer, uint64_t ld, uint32_t box_inner,
+                  uint32_t box_outer);
+bool float_out_map(CUtensorMap *map, bool bf16, const void *base, uint64_t N, uint64_t M, uint64_t ld,
+                   uint64_t splits);
+// Whether outputs are to go through TMA stores (GB300_GEMM_TMA_STORE).
+bool tma_store_enabled();
+
 // One compiled variant of the tcgen05 kernel.
 struct TcVariant {
   int bn;        // tile width (see the instantiation files for the compiled set)

@@ -1,0 +1,100 @@
+// layer_internal.h -- host-side declarations of the layer operators
+// (layer_api.cu, layer_rows.cu, wgrad.cu); not part of the public ABI.
+#pragma once
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "gb300_layer.h"
+#include "gemm_internal.h"
+
+namespace gb300 {
+
+constexpr int kQ8Block = GEMM_Q8_BLOCK;
+
+// A checkpoint: signed bytes q (pitch ldq) and block exponents e (pitch lde).
+struct Q8Ref {
+  int8_t *q;
+  int64_t ldq;
+  uint8_t *e;
+  int64_t lde;
+};
+
+struct LnForward {
+  int64_t rows;
+  int cols;
+  const void *x;
+  int64_t ldx;
+  int x_type;
+  const void *gamma, *beta;  // either may be null: ones, zeros
+  int param_type;
+  float eps;
+  void *y;
+  int64_t ldy;
+  int y_type;
+  float *mean, *rstd;  // either may be null
+  Q8Ref ck;            // checkpoint of y, or ck.q null
+};
+cudaError_t launch_ln_forward(const LnForward &p, int sms, cudaStream_t st);
+
+struct LnBackward {
+  int64_t rows;
+  int cols;
+  const void *x;  // null: x is read from ck
+  int64_t ldx;
+  int x_type;     // of x; where x is null, of nothing
+  Q8Ref ck;
+  const void *gamma;  // null: ones
+  int param_type;
+  const float *mean, *rstd;
+  const void *dy;
+  int64_t lddy;
+  int dy_type;
+  void *dx;
+  int64_t lddx;
+  int dx_type;
+  float *dgamma, *dbeta;  // either may be null
+  float *partials;        // ln_backward_partials() floats
+};
+// Floats of workspace a backward pass wants for its partial parameter
+// gradients, and the launches it makes (filled in by the launcher).
+size_t ln_backward_partials(const LnBackward &p, int sms);
+cudaError_t launch_ln_backward(const LnBackward &p, int sms, cudaStream_t st, int *launches);
+
+cudaError_t launch_q8_save(const void *x, int64_t ldx, int x_type, int64_t rows, int64_t cols, const Q8Ref &ck,
+                           cudaStream_t st);
+cudaError_t launch_q8_restore(const Q8Ref &ck, void *x, int64_t ldx, int x_type, int64_t rows, int64_t cols,
+                              cudaStream_t st);
+
+// C[m][n] = base[m][n] + sum_t A[t][m] * B[t][n] with bf16 A (T x M) and B
+// (T x N), both read with their rows (t) outermost (wgrad.cu).
+struct WgradParams {
+  TcParams tc;  // M, N, K = T; tiling, split tail, C, ldc, partials, error word
+  const void *base;  // null: none
+  int64_t ldbase;
+  int out_bf16;      // type of C and base
+};
+// One compiled tile shape of the kernel.
+struct WgradTile {
+  bool pair;  // a CTA pair per 256-row tile, or one CTA per 128-row tile
+  int bn;     // tile width
+};
+// Tile shape, split tail and grid for an M x N result summed over T rows.
+struct WgradPlan {
+  WgradTile tile;
+  int tiles_m, tiles_n, num_kb;
+  int tail_first, tail_splits, tail_kb_per;
+  int grid;
+};
+WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t T, int sms, int pairs);
+// Bytes of partial sums a plan's split tail writes (0: none).
+size_t wgrad_partial_bytes(const WgradPlan &pl);
+cudaError_t launch_wgrad(const WgradTile &tile, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out,
+                         const CUtensorMap &ws, const WgradParams &p, int grid, cudaStream_t st);
+// T == 0: C = base, or zero.
+cudaError_t launch_wgrad_base(const WgradParams &p, int sms, cudaStream_t st);
+// The split tail's tiles: partials summed in split order, base added, rounded
+// and stored.
+cudaError_t launch_wgrad_reduce(const WgradTile &tile, const WgradParams &p, cudaStream_t st);
+
+}  // namespace gb300

@@ -1,0 +1,169 @@
+// wgrad.cu -- planning and launches of the weight gradient's tensor-core
+// kernel (wgrad_tc.cuh), and the reduction of its split tail.
+#include "wgrad_tc.cuh"
+
+namespace gb300 {
+
+namespace {
+
+inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Longest chain of tensor-core additions of a float32 result, in k-blocks
+// of 64 tokens.  Measured error of dW against 64 bits (2-norm, 1000 tokens of
+// 777 x 1501): 8.1e-8, 1.1e-7, 2.2e-7 and 5.1e-7 with slabs of 2, 4, 8 and 16
+// k-blocks; 16 also breaks the header's bound per element.
+constexpr int kSlabKb = 8;
+
+template <int BN, bool PAIR>
+cudaError_t launch_tile(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const CUtensorMap &ws,
+                        const WgradParams &p, int grid, cudaStream_t st) {
+  using Cfg = WgCfg<BN, PAIR>;
+  auto kern = wgrad_kernel<BN, PAIR>;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
+  if (e != cudaSuccess) return e;
+  return launch_ex(kern, dim3((unsigned)grid), dim3(kWgThreads), Cfg::kSmemBytes, st, PAIR ? 2 : 1, a, b, out, ws, p);
+}
+
+// Split tail: element group t (4 columns of a row) of the compact partials,
+// over the tail tiles' rows.
+__global__ void __launch_bounds__(256) wgrad_reduce_kernel(const WgradParams wp, int bn, int tile_m, int64_t groups) {
+  griddep_launch_dependents();
+  griddep_wait();
+  const TcParams &p = wp.tc;
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (t >= groups) return;
+  const int per_row = bn / 4;
+  const int64_t prow = t / per_row;
+  const int pc = (int)(t - prow * per_row) * 4;
+  const int slot = (int)(prow / tile_m);
+  int tm, tn;
+  raster_tile(p.tail_first + slot, p.tiles_m, p.tiles_n, p.group_m, &tm, &tn);
+  const int64_t row = (int64_t)tm * tile_m + (prow - (int64_t)slot * tile_m);
+  const int64_t col = (int64_t)tn * bn + pc;
+  if (row >= p.M || col >= p.N) return;
+  const int64_t plane = (int64_t)(p.tiles_m * p.tiles_n - p.tail_first) * tile_m * bn;
+  const float *src = static_cast<const float *>(p.ws) + prow * bn + pc;
+  float4 s = *reinterpret_cast<const float4 *>(src);
+  for (int k = 1; k < p.tail_splits; ++k) {
+    const float4 v = *reinterpret_cast<const float4 *>(src + k * plane);
+    s.x += v.x;
+    s.y += v.y;
+    s.z += v.z;
+    s.w += v.w;
+  }
+  const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (col + i >= p.N) break;
+    float r = v[i];
+    if (wp.out_bf16) {
+      if (wp.base)
+        r += __bfloat162float(static_cast<const __nv_bfloat16 *>(wp.base)[row * wp.ldbase + col + i]);
+      static_cast<__nv_bfloat16 *>(p.C)[row * p.ldc + col + i] = __float2bfloat16_rn(r);
+    } else {
+      if (wp.base) r += static_cast<const float *>(wp.base)[row * wp.ldbase + col + i];
+      static_cast<float *>(p.C)[row * p.ldc + col + i] = r;
+    }
+  }
+}
+
+// T == 0: C = base, or zero.
+__global__ void __launch_bounds__(256) wgrad_base_kernel(const WgradParams wp) {
+  griddep_launch_dependents();
+  griddep_wait();
+  const TcParams &p = wp.tc;
+  const int64_t n = (int64_t)p.M * p.N;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / p.N, c = i - r * p.N;
+    if (wp.out_bf16)
+      static_cast<uint16_t *>(p.C)[r * p.ldc + c] =
+          wp.base ? static_cast<const uint16_t *>(wp.base)[r * wp.ldbase + c] : (uint16_t)0;
+    else
+      static_cast<float *>(p.C)[r * p.ldc + c] =
+          wp.base ? static_cast<const float *>(wp.base)[r * wp.ldbase + c] : 0.f;
+  }
+}
+
+// Modelled cost of a tile shape: microseconds per k-block and per unit
+// (start, accumulator drain).
+struct TileCost {
+  WgradTile tile;
+  double kb_us, unit_us;
+};
+constexpr TileCost kTiles[] = {{{true, 256}, 0.28, 1.0}, {{true, 128}, 0.16, 0.7}, {{false, 128}, 0.16, 0.7}};
+constexpr double kTailFixedUs = 3.0, kTailUsPerMB = 0.4;
+
+}  // namespace
+
+WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t T, int sms, int pairs) {
+  WgradPlan best{};
+  double best_us = -1;
+  const int64_t num_kb = ceil_div64(T, kBK);
+  for (const TileCost &tc : kTiles) {
+    const int64_t slots = tc.tile.pair ? pairs : sms;
+    if (slots <= 0) continue;
+    const int tile_m = tc.tile.pair ? 2 * kBM : kBM;
+    const int64_t tiles_m = ceil_div64(M, tile_m), tiles_n = ceil_div64(N, tc.tile.bn), tiles = tiles_m * tiles_n;
+    const int64_t full = tiles / slots, rem = tiles % slots;
+    const double whole = num_kb * tc.kb_us + tc.unit_us;
+    for (int64_t s = 1; s <= 16; ++s) {
+      int64_t kb_per = num_kb, parts = 1;
+      if (s > 1) {
+        if (rem == 0 || rem * s > slots) break;
+        kb_per = ceil_div64(num_kb, s);
+        parts = ceil_div64(num_kb, kb_per);  // no part is empty
+        if (parts != s || kb_per < 4) continue;
+      }
+      double us = full * whole;
+      if (rem > 0) us += kb_per * tc.kb_us + tc.unit_us;
+      if (parts > 1) us += kTailFixedUs + kTailUsPerMB * (double)parts * rem * tile_m * tc.tile.bn * 4e-6;
+      if (best_us < 0 || us < best_us) {
+        best_us = us;
+        best.tile = tc.tile;
+        best.tiles_m = (int)tiles_m;
+        best.tiles_n = (int)tiles_n;
+        best.num_kb = (int)num_kb;
+        best.tail_first = parts > 1 ? (int)(full * slots) : 0;
+        best.tail_splits = parts > 1 ? (int)parts : 0;
+        best.tail_kb_per = parts > 1 ? (int)kb_per : 0;
+        const int64_t units = parts > 1 ? full * slots + rem * parts : tiles;
+        best.grid = (int)(units < slots ? units : slots) * (tc.tile.pair ? 2 : 1);
+      }
+    }
+  }
+  return best;
+}
+
+size_t wgrad_partial_bytes(const WgradPlan &pl) {
+  if (pl.tail_splits < 2) return 0;
+  const size_t tail = (size_t)pl.tiles_m * pl.tiles_n - pl.tail_first;
+  return (size_t)pl.tail_splits * tail * (pl.tile.pair ? 2 * kBM : kBM) * pl.tile.bn * 4;
+}
+
+cudaError_t launch_wgrad(const WgradTile &tile, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out,
+                         const CUtensorMap &ws, const WgradParams &p, int grid, cudaStream_t st) {
+  WgradParams q = p;
+  q.tc.slab_kb = p.out_bf16 ? p.tc.num_kb : kSlabKb;
+  if (tile.pair) {
+    if (tile.bn == 256) return launch_tile<256, true>(a, b, out, ws, q, grid, st);
+    if (tile.bn == 128) return launch_tile<128, true>(a, b, out, ws, q, grid, st);
+  } else if (tile.bn == 128) {
+    return launch_tile<128, false>(a, b, out, ws, q, grid, st);
+  }
+  return cudaErrorInvalidValue;
+}
+
+cudaError_t launch_wgrad_base(const WgradParams &p, int sms, cudaStream_t st) {
+  const int64_t want = ceil_div64((int64_t)p.tc.M * p.tc.N, 1024), cap = (int64_t)sms * 8;
+  return launch_ex(wgrad_base_kernel, dim3((unsigned)(want < cap ? want : cap)), dim3(256), 0, st, 1, p);
+}
+
+cudaError_t launch_wgrad_reduce(const WgradTile &tile, const WgradParams &p, cudaStream_t st) {
+  const int tile_m = tile.pair ? 2 * kBM : kBM;
+  const int64_t tail = (int64_t)p.tc.tiles_m * p.tc.tiles_n - p.tc.tail_first;
+  const int64_t groups = tail * tile_m * (tile.bn / 4);
+  return launch_ex(wgrad_reduce_kernel, dim3((unsigned)ceil_div64(groups, 256)), dim3(256), 0, st, 1, p, tile.bn, tile_m,
+                   groups);
+}
+
+}  // namespace gb300
