@@ -1,5 +1,6 @@
 // layer_internal.h -- host-side declarations of the layer operators
-// (layer_api.cu, layer_rows.cu, wgrad.cu); not part of the public ABI.
+// (layer_api.cu, layer_ln_fwd.cu, layer_ln_bwd.cu, layer_q8.cu,
+// wgrad.cu); not part of the public ABI.
 #pragma once
 #include <cuda_runtime.h>
 

@@ -1,5 +1,5 @@
-// layer_rows.cu -- the layer operators that walk a matrix by rows: layer norm
-// forward and backward, and the 8-bit checkpoint's save and restore.
+// layer_ln_bwd.cu -- layer norm backward: dx, and the reduction of dgamma and
+// dbeta over the rows.
 #include "layer_rows.cuh"
 
 namespace gb300 {
@@ -10,56 +10,6 @@ constexpr int kRowThreads = 256;
 
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int grid_cap(int64_t want, int64_t cap) { return (int)(want < 1 ? 1 : (want > cap ? cap : want)); }
-
-// ------------------------------------------------------- layer norm forward
-
-// Any width, pitch and alignment: a block per row, the row read three times
-// (mean, variance, result), the second and third time from L1 or L2.
-template <typename TX, typename TY>
-__global__ void __launch_bounds__(kRowThreads) ln_forward_any_kernel(const LnForward p) {
-  __shared__ float2 sm[2][32];
-  griddep_launch_dependents();
-  griddep_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const float inv_n = 1.0f / (float)p.cols;
-  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
-    const TX *x = static_cast<const TX *>(p.x) + r * p.ldx;
-    float s = 0.f;
-    for (int c = threadIdx.x; c < p.cols; c += kRowThreads) s += load_value<TX>(x, c);
-    const float mean = block_sum2(s, 0.f, sm, 0).x * inv_n;
-    float v = 0.f;
-    for (int c = threadIdx.x; c < p.cols; c += kRowThreads) {
-      const float d = load_value<TX>(x, c) - mean;
-      v = fmaf(d, d, v);
-    }
-    const float rstd = 1.0f / sqrtf(block_sum2(v, 0.f, sm, 1).x * inv_n + p.eps);
-    if (threadIdx.x == 0) {
-      if (p.mean) p.mean[r] = mean;
-      if (p.rstd) p.rstd[r] = rstd;
-    }
-    TY *y = static_cast<TY *>(p.y) + r * p.ldy;
-    // each warp takes whole blocks of 32 columns, so that a checkpoint block
-    // is the warp's 32 lanes
-    for (int c0 = warp * 32; c0 < p.cols; c0 += kRowThreads) {
-      const int c = c0 + lane;
-      float out = 0.f;
-      if (c < p.cols) {
-        out = fmaf((load_value<TX>(x, c) - mean) * rstd, load_param(p.gamma, p.param_type, c, 1.f),
-                   load_param(p.beta, p.param_type, c, 0.f));
-        store_value<TY>(y, c, out);
-      }
-      if (p.ck.q) {
-        out = as_stored<TY>(out);
-        const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(out) & 0x7FFFFFFFu);
-        const uint32_t e = q8_exponent(top);
-        if (c < p.cols) p.ck.q[r * p.ck.ldq + c] = (int8_t)q8_quantise(out, q8_inverse(e), e);
-        if (lane == 0) p.ck.e[r * p.ck.lde + (c0 >> 5)] = (uint8_t)e;
-      }
-    }
-  }
-}
-
-// ------------------------------------------------------ layer norm backward
 
 // Value c of row r of the forward pass's input: of type TX, or (Q8) held in
 // the checkpoint.
@@ -159,40 +109,6 @@ __global__ void __launch_bounds__(1024) ln_param_sum_kernel(const float *partial
   if (i == 0 && cj < cols) out[cj] = t;
 }
 
-// ------------------------------------------------------------- checkpoints
-
-// Any width, pitch and alignment: a warp per block of 32 values.
-template <typename TX>
-__global__ void __launch_bounds__(kRowThreads)
-    q8_save_any_kernel(const void *x, int64_t ldx, int64_t rows, int64_t cols, Q8Ref ck) {
-  griddep_launch_dependents();
-  griddep_wait();
-  const int lane = threadIdx.x & 31;
-  const int64_t blocks = (cols + 31) / 32, items = rows * blocks;
-  const int64_t step = (int64_t)gridDim.x * (kRowThreads / 32);
-  for (int64_t t = (int64_t)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5); t < items; t += step) {
-    const int64_t r = t / blocks, b = t - r * blocks, c = b * 32 + lane;
-    const float v = c < cols ? load_value<TX>(x, r * ldx + c) : 0.f;
-    const uint32_t e = q8_exponent(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7FFFFFFFu));
-    if (c < cols) ck.q[r * ck.ldq + c] = (int8_t)q8_quantise(v, q8_inverse(e), e);
-    if (lane == 0) ck.e[r * ck.lde + b] = (uint8_t)e;
-  }
-}
-
-template <typename TX>
-__global__ void __launch_bounds__(kRowThreads)
-    q8_restore_any_kernel(Q8Ref ck, void *x, int64_t ldx, int64_t rows, int64_t cols) {
-  griddep_launch_dependents();
-  griddep_wait();
-  const int lane = threadIdx.x & 31;
-  const int64_t blocks = (cols + 31) / 32, items = rows * blocks;
-  const int64_t step = (int64_t)gridDim.x * (kRowThreads / 32);
-  for (int64_t t = (int64_t)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5); t < items; t += step) {
-    const int64_t r = t / blocks, b = t - r * blocks, c = b * 32 + lane;
-    if (c < cols) store_value<TX>(x, r * ldx + c, (float)ck.q[r * ck.ldq + c] * q8_scale(ck.e[r * ck.lde + b]));
-  }
-}
-
 template <typename TX, typename TDY, typename TDX>
 cudaError_t ln_backward_any(const LnBackward &p, int sms, cudaStream_t st, int *launches) {
   cudaError_t e = cudaSuccess;
@@ -216,15 +132,6 @@ cudaError_t ln_backward_any(const LnBackward &p, int sms, cudaStream_t st, int *
 
 }  // namespace
 
-cudaError_t launch_ln_forward(const LnForward &p, int sms, cudaStream_t st) {
-  const dim3 grid(grid_cap(p.rows, (int64_t)sms * 8)), block(kRowThreads);
-  const bool xb = p.x_type == GEMM_TYPE_BF16, yb = p.y_type == GEMM_TYPE_BF16;
-  if (xb && yb) return launch_ex(ln_forward_any_kernel<bf16, bf16>, grid, block, 0, st, 1, p);
-  if (xb) return launch_ex(ln_forward_any_kernel<bf16, float>, grid, block, 0, st, 1, p);
-  if (yb) return launch_ex(ln_forward_any_kernel<float, bf16>, grid, block, 0, st, 1, p);
-  return launch_ex(ln_forward_any_kernel<float, float>, grid, block, 0, st, 1, p);
-}
-
 // Rows of partial sums: enough blocks of 32 columns x 8 rows at a time to
 // fill the device several times over, no more than there are groups of rows.
 size_t ln_backward_partials(const LnBackward &p, int sms) {
@@ -241,23 +148,6 @@ cudaError_t launch_ln_backward(const LnBackward &p, int sms, cudaStream_t st, in
   }
   if (ob) return gb ? ln_backward_any<bf16, bf16, bf16>(p, sms, st, launches) : ln_backward_any<bf16, float, bf16>(p, sms, st, launches);
   return gb ? ln_backward_any<float, bf16, float>(p, sms, st, launches) : ln_backward_any<float, float, float>(p, sms, st, launches);
-}
-
-cudaError_t launch_q8_save(const void *x, int64_t ldx, int x_type, int64_t rows, int64_t cols, const Q8Ref &ck,
-                           cudaStream_t st) {
-  const int64_t items = rows * ceil_div64(cols, 32);
-  const dim3 grid(grid_cap(ceil_div64(items, kRowThreads / 32), 1 << 20)), block(kRowThreads);
-  return x_type == GEMM_TYPE_BF16 ? launch_ex(q8_save_any_kernel<bf16>, grid, block, 0, st, 1, x, ldx, rows, cols, ck)
-                                  : launch_ex(q8_save_any_kernel<float>, grid, block, 0, st, 1, x, ldx, rows, cols, ck);
-}
-
-cudaError_t launch_q8_restore(const Q8Ref &ck, void *x, int64_t ldx, int x_type, int64_t rows, int64_t cols,
-                              cudaStream_t st) {
-  const int64_t items = rows * ceil_div64(cols, 32);
-  const dim3 grid(grid_cap(ceil_div64(items, kRowThreads / 32), 1 << 20)), block(kRowThreads);
-  return x_type == GEMM_TYPE_BF16
-             ? launch_ex(q8_restore_any_kernel<bf16>, grid, block, 0, st, 1, ck, x, ldx, rows, cols)
-             : launch_ex(q8_restore_any_kernel<float>, grid, block, 0, st, 1, ck, x, ldx, rows, cols);
 }
 
 }  // namespace gb300

@@ -1,5 +1,6 @@
 // layer_rows.cuh -- element access and row sums shared by the layer
-// operators' kernels (layer_rows.cu).
+// operators' kernels (layer_ln_fwd.cu, layer_ln_bwd.cu,
+// layer_q8.cu).
 #pragma once
 #include <cuda_bf16.h>
 
@@ -8,7 +9,9 @@
 namespace gb300 {
 
 using bf16 = __nv_bfloat16;
-struct Q8 {};  // element type tag: a value held in a checkpoint
+struct Q8 {     // element type: a value held in a checkpoint, as its byte
+  int8_t byte;
+};
 
 // 2^(e - 127) of a block exponent: e = 255 stands for NaN.
 __device__ __forceinline__ float q8_scale(uint32_t e) {
@@ -39,6 +42,32 @@ __device__ __forceinline__ int q8_quantise(float x, float inverse, uint32_t e) {
   return v;
 }
 
+// The same for four values, packed (v[0] in the low byte).  Added to 1.5 *
+// 2^23, where a float's unit in the last place is 1, the exact product
+// x * inverse is rounded to an integer, ties to even, which is then the low
+// byte of the sum: no conversion instructions (a quarter of the rate).
+__device__ __forceinline__ uint32_t q8_pack4(const float *v, float inverse, uint32_t e) {
+  constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23
+  uint32_t b[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(fmaf(v[i], inverse, kMagic));
+  uint32_t w = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+  if (e >= 249u) {
+    w = 0;
+    if (e == 249u) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w |= (uint32_t)(q8_quantise(v[i], inverse, e) & 0xFF) << (8 * i);
+    }
+  }
+  return w;
+}
+
+// Byte i of w as a float (see s8x4_to_bf16x4 for the arithmetic).
+__device__ __forceinline__ float s8_to_float(uint32_t w, int i) {
+  const uint32_t u = w ^ 0x80808080u;
+  return __fsub_rn(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7650 + i)), 8388736.0f);
+}
+
 template <typename T>
 __device__ __forceinline__ float load_value(const void *p, int64_t i) {
   if constexpr (sizeof(T) == 4)
@@ -62,6 +91,89 @@ __device__ __forceinline__ float as_stored(float v) {
     return __bfloat162float(__float2bfloat16_rn(v));
 }
 
+// V consecutive elements of a row as they are in memory, loaded with the
+// widest loads V allows (the address is a multiple of V elements), so that a
+// row can be fetched ahead of its use in half the registers.
+template <typename T, int V>
+struct Chunk {
+  static constexpr int kBytes = V * (int)sizeof(T), kWords = kBytes < 4 ? 1 : kBytes / 4;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const void *row, int64_t c) {
+    const char *p = static_cast<const char *>(row) + c * (int64_t)sizeof(T);
+    if constexpr (kBytes >= 16) {
+#pragma unroll
+      for (int i = 0; i < kBytes / 16; ++i) {
+        const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
+        w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+      }
+    } else if constexpr (kBytes == 8) {
+      const uint2 v = *reinterpret_cast<const uint2 *>(p);
+      w[0] = v.x, w[1] = v.y;
+    } else if constexpr (kBytes == 4) {
+      w[0] = *reinterpret_cast<const uint32_t *>(p);
+    } else if constexpr (kBytes == 2) {
+      w[0] = *reinterpret_cast<const uint16_t *>(p);
+    } else {
+      w[0] = *reinterpret_cast<const uint8_t *>(p);
+    }
+  }
+  // The first n of the chunk's elements, one by one.
+  __device__ __forceinline__ void load_part(const void *row, int64_t c, int n) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < n) {
+        if constexpr (sizeof(T) == 4)
+          w[i] = static_cast<const uint32_t *>(row)[c + i];
+        else if constexpr (sizeof(T) == 2)
+          w[i / 2] |= (uint32_t) static_cast<const uint16_t *>(row)[c + i] << (16 * (i & 1));
+        else
+          w[i / 4] |= (uint32_t) static_cast<const uint8_t *>(row)[c + i] << (8 * (i & 3));
+      }
+  }
+  // Element i (of a checkpoint: its byte, unscaled).
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (sizeof(T) == 4)
+      return __uint_as_float(w[i]);
+    else if constexpr (sizeof(T) == 2)
+      return __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    else
+      return s8_to_float(w[i / 4], i & 3);
+  }
+};
+
+// V consecutive results rounded to T and stored (address a multiple of V
+// elements); the first n of them, one by one, where n < V.
+template <typename T, int V>
+__device__ __forceinline__ void store_chunk(void *row, int64_t c, const float *v, int n) {
+  if (n < V) {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < n) store_value<T>(row, c + i, v[i]);
+    return;
+  }
+  if constexpr (V == 1) {
+    store_value<T>(row, c, v[0]);
+  } else if constexpr (sizeof(T) == 4) {
+    float4 *d = reinterpret_cast<float4 *>(static_cast<float *>(row) + c);
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) d[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+  } else {
+    uint32_t h[V / 2];
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) h[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    char *d = static_cast<char *>(row) + c * 2;
+    if constexpr (V == 4) {
+      *reinterpret_cast<uint2 *>(d) = make_uint2(h[0], h[1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V / 8; ++i)
+        reinterpret_cast<uint4 *>(d)[i] = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
+    }
+  }
+}
+
 // A parameter vector of either type, or absent.
 __device__ __forceinline__ float load_param(const void *p, int type, int c, float absent) {
   if (!p) return absent;
@@ -72,6 +184,17 @@ __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
+}
+
+// Sum over the block (a whole number of warps, at most 32); every thread
+// receives it.  See block_sum2.
+__device__ __forceinline__ float block_sum(float a, float *sm) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  a = warp_sum(a);
+  if (warps == 1) return a;
+  if (lane == 0) sm[warp] = a;
+  __syncthreads();
+  return warp_sum(lane < warps ? sm[lane] : 0.f);
 }
 
 // Sum of a pair over the block (a whole number of warps, at most 32); every
