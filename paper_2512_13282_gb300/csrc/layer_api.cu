@@ -83,14 +83,14 @@ gemm_status_t gemm_layernorm_backward(int64_t rows, int64_t cols, const void *x,
                Q8Ref{const_cast<int8_t *>(q), ldq, const_cast<uint8_t *>(e), lde}, gamma, param_type, mean, rstd, dy,
                lddy, dy_type, dx, lddx, dx_type, dgamma, dbeta, nullptr};
   return with_scratch(reinterpret_cast<cudaStream_t>(stream), [&](const OpContext &c) -> gemm_status_t {
-    if (dgamma || dbeta) {
+    if (const size_t partials = ln_backward_partials(p, c.sms)) {
       void *ws = nullptr;
-      const gemm_status_t w = op_workspace(ln_backward_partials(p, c.sms) * sizeof(float), c.st, &ws);
+      const gemm_status_t w = op_workspace(partials * sizeof(float), c.st, &ws);
       if (w != GEMM_OK) return w;
       p.partials = static_cast<float *>(ws);
     }
     int launches = 0;
-    const cudaError_t err = launch_ln_backward(p, c.sms, c.st, &launches);
+    const cudaError_t err = launch_ln_backward(p, c, &launches);
     count_launches(launches);
     return launched(err);
   });

@@ -55,12 +55,13 @@ struct LnBackward {
   int64_t lddx;
   int dx_type;
   float *dgamma, *dbeta;  // either may be null
-  float *partials;        // ln_backward_partials() floats
+  float *partials;        // ln_backward_partials() floats, or null
 };
 // Floats of workspace a backward pass wants for its partial parameter
-// gradients, and the launches it makes (filled in by the launcher).
+// gradients (0: it computes none).
 size_t ln_backward_partials(const LnBackward &p, int sms);
-cudaError_t launch_ln_backward(const LnBackward &p, int sms, cudaStream_t st, int *launches);
+// *launches is increased by the kernels launched.
+cudaError_t launch_ln_backward(const LnBackward &p, const OpContext &c, int *launches);
 
 cudaError_t launch_q8_save(const void *x, int64_t ldx, int x_type, int64_t rows, int64_t cols, const Q8Ref &ck,
                            cudaStream_t st);

@@ -7,6 +7,9 @@ namespace gb300 {
 namespace {
 
 constexpr int kRowThreads = 256;
+constexpr int kRingThreads = 512;     // most threads a block of the register-resident kernels has
+constexpr int kMaxStages = 8;
+constexpr int64_t kRingBytes = 200 * 1024;  // shared memory of an SM's rings together
 
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int grid_cap(int64_t want, int64_t cap) { return (int)(want < 1 ? 1 : (want > cap ? cap : want)); }
@@ -109,45 +112,395 @@ __global__ void __launch_bounds__(1024) ln_param_sum_kernel(const float *partial
   if (i == 0 && cj < cols) out[cj] = t;
 }
 
+// Row r's mean and 1/std as the factors of xh = x * rstd - mean * rstd.
+struct RowStats {
+  float rstd, shift;
+  __device__ __forceinline__ void load(const LnBackward &p, int64_t r) {
+    rstd = p.rstd[r];
+    shift = -p.mean[r] * rstd;
+  }
+};
+
+// Rows whose x and dy are whole 16-byte pieces, up to 512 * NV * 8 values.
+// A block walks rows gridDim.x apart.  Their x and dy come through a ring of
+// `stages` row slots in shared memory, filled by bulk copies that run as far
+// ahead as the ring is deep: dgamma and dbeta are summed in registers (16
+// values a thread and NV), which leaves none for rows in flight.  A row is
+// read from its slot twice, for the two averages and for the results; the
+// block-wide barrier between, passed by every thread once it has finished
+// with the row before, also frees that row's slot, which thread 0 refills.
+// One partial row of dgamma and dbeta a block goes to the workspace.
+template <typename TX, typename TDY, typename TDX, int NV>
+__global__ void __launch_bounds__(kRingThreads, NV == 1 ? 2 : 1)
+    ln_backward_ring_kernel(const LnBackward p, const int stages, const uint32_t x_bytes, const uint32_t dy_bytes,
+                            uint32_t *err, const uint64_t wait_limit_ns) {
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ float2 sm[2][32];
+  __shared__ __align__(8) uint64_t bars[kMaxStages];
+  __shared__ volatile uint32_t abort_flag;
+  griddep_launch_dependents();
+  const int T = blockDim.x;
+  const uint32_t slot_bytes = x_bytes + dy_bytes;
+  const uint32_t ring_addr = smem_addr(ring), bar0 = smem_addr(bars);
+  const float inv_n = 1.0f / (float)p.cols;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) mbar_init(bar0 + 8 * s, 1);
+    abort_flag = 0;
+    fence_mbar_init();
+  }
+  __syncthreads();
+  griddep_wait();
+  const int64_t mine = (p.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // rows of this block, at least one
+  const auto row_of = [&](int64_t i) { return (int64_t)blockIdx.x + i * gridDim.x; };
+  const auto fill = [&](int64_t i) {
+    const uint32_t s = (uint32_t)(i % stages), dst = ring_addr + s * slot_bytes, bar = bar0 + 8 * s;
+    const int64_t r = row_of(i);
+    mbar_arrive_expect_tx(bar, slot_bytes);
+    if constexpr (sizeof(TX) == 1)
+      bulk_load(dst, p.ck.q + r * p.ck.ldq, x_bytes, bar);
+    else
+      bulk_load(dst, static_cast<const TX *>(p.x) + r * p.ldx, x_bytes, bar);
+    bulk_load(dst + x_bytes, static_cast<const TDY *>(p.dy) + r * p.lddy, dy_bytes, bar);
+  };
+  if (threadIdx.x == 0)
+    for (int64_t i = 0; i < stages && i < mine; ++i) fill(i);
+
+  float gamma[NV * 8], dg[NV * 8], db[NV * 8];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = (v * T + (int)threadIdx.x) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      gamma[v * 8 + i] = c < p.cols ? load_param(p.gamma, p.param_type, c + i, 1.f) : 0.f;
+      dg[v * 8 + i] = db[v * 8 + i] = 0.f;
+    }
+  }
+  // the row's statistics and block exponents, fetched a row ahead
+  RowStats st, st_next;
+  uint32_t ex[NV], ex_next[NV];
+  const auto fetch = [&](int64_t i) {
+    const int64_t r = row_of(i);
+    st_next.load(p, r);
+    if constexpr (sizeof(TX) == 1) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int c = (v * T + (int)threadIdx.x) * 8;
+        ex_next[v] = c < p.cols ? p.ck.e[r * p.ck.lde + (c >> 5)] : 0;
+      }
+    }
+  };
+  fetch(0);
+  bool ok = true;
+  int64_t filled = mine < stages ? mine : stages;
+  for (int64_t i = 0; i < mine; ++i) {
+    const uint8_t *slot = ring + (i % stages) * slot_bytes;
+    st = st_next;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) ex[v] = ex_next[v];
+    if (i + 1 < mine) fetch(i + 1);
+    ok = mbar_wait(bar0 + 8 * (uint32_t)(i % stages), (uint32_t)(i / stages) & 1u, &abort_flag, err, wait_limit_ns);
+    float a = 0.f, b = 0.f;
+    // xh and g of chunk v, from the slot
+    const auto load = [&](int v, float(&xh)[8], float(&g)[8], float(&d)[8]) {
+      const int c = (v * T + (int)threadIdx.x) * 8;
+      Chunk<TX, 8> x;
+      Chunk<TDY, 8> y;
+      x.load(slot, c);
+      y.load(slot + x_bytes, c);
+      float scale = st.rstd;
+      if constexpr (sizeof(TX) == 1) scale *= q8_scale(ex[v]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        xh[j] = fmaf(x.get(j), scale, st.shift);
+        d[j] = y.get(j);
+        g[j] = d[j] * gamma[v * 8 + j];
+      }
+    };
+    if (ok) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        if ((v * T + (int)threadIdx.x) * 8 < p.cols) {
+          float xh[8], g[8], d[8];
+          load(v, xh, g, d);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            a += g[j];
+            b = fmaf(g[j], xh[j], b);
+          }
+        }
+      }
+    }
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = T >> 5;
+    a = warp_sum(a);
+    b = warp_sum(b);
+    if (lane == 0) sm[i & 1][warp] = make_float2(a, b);
+    // every wait of the block succeeded, or the block gives up together
+    if (!__syncthreads_and(ok)) {
+      ok = false;
+      break;
+    }
+    if (threadIdx.x == 0 && i > 0 && i - 1 + stages < mine) {
+      fill(i - 1 + stages);
+      filled = i + stages;
+    }
+    const float2 part = lane < warps ? sm[i & 1][lane] : make_float2(0.f, 0.f);
+    const float ga = warp_sum(part.x) * inv_n * st.rstd, gx = warp_sum(part.y) * inv_n * st.rstd;
+    TDX *dx = static_cast<TDX *>(p.dx) + row_of(i) * p.lddx;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = (v * T + (int)threadIdx.x) * 8;
+      if (c < p.cols) {
+        float xh[8], g[8], d[8], o[8];
+        load(v, xh, g, d);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          dg[v * 8 + j] = fmaf(d[j], xh[j], dg[v * 8 + j]);
+          db[v * 8 + j] += d[j];
+          o[j] = fmaf(g[j], st.rstd, -fmaf(xh[j], gx, ga));
+        }
+        store_chunk<TDX, 8>(dx, c, o, 8);
+      }
+    }
+  }
+  if (!ok) {  // let the copies in flight land before the block's memory is given up
+    if (threadIdx.x == 0)
+      for (int64_t i = filled > stages ? filled - stages : 0; i < filled; ++i)
+        mbar_wait_drain(bar0 + 8 * (uint32_t)(i % stages), (uint32_t)(i / stages) & 1u, 200ull * 1000 * 1000);
+    return;
+  }
+  if (!p.partials) return;
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = (v * T + (int)threadIdx.x) * 8;
+    if (c < p.cols) {
+      store_chunk<float, 8>(p.partials + (int64_t)blockIdx.x * p.cols, c, dg + v * 8, 8);
+      store_chunk<float, 8>(p.partials + (int64_t)(gridDim.x + blockIdx.x) * p.cols, c, db + v * 8, 8);
+    }
+  }
+}
+
+// Any alignment, up to 512 * NV * 8 values a row: x and dy are read straight
+// into registers, in chunks of V values (V = 4 where the rows of every matrix
+// start on a multiple of four values, else 1: neighbouring lanes still share
+// sectors), and kept there between the two averages and the results.
+template <typename TX, typename TDY, typename TDX, int NV, int V>
+__global__ void __launch_bounds__(kRingThreads) ln_backward_regs_kernel(const LnBackward p) {
+  constexpr int C = NV * 8 / V;
+  __shared__ float2 sm[2][32];
+  griddep_launch_dependents();
+  griddep_wait();
+  const int T = blockDim.x;
+  const float inv_n = 1.0f / (float)p.cols;
+  const auto col = [&](int k) { return (k * T + (int)threadIdx.x) * V; };
+  const auto valid = [&](int k) { return max(0, min(V, p.cols - col(k))); };
+  float gamma[C * V], dg[C * V], db[C * V];
+#pragma unroll
+  for (int k = 0; k < C; ++k)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      gamma[k * V + i] = i < valid(k) ? load_param(p.gamma, p.param_type, col(k) + i, 1.f) : 0.f;
+      dg[k * V + i] = db[k * V + i] = 0.f;
+    }
+  int buf = 0;
+  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+    RowStats st;
+    st.load(p, r);
+    Chunk<TX, V> x[C];
+    Chunk<TDY, V> y[C];
+    uint32_t ex[C];
+    const void *xr;
+    if constexpr (sizeof(TX) == 1)
+      xr = p.ck.q + r * p.ck.ldq;
+    else
+      xr = static_cast<const TX *>(p.x) + r * p.ldx;
+    const TDY *yr = static_cast<const TDY *>(p.dy) + r * p.lddy;
+#pragma unroll
+    for (int k = 0; k < C; ++k) {
+      const int n = valid(k), c = col(k);
+      if (n == V) {
+        x[k].load(xr, c);
+        y[k].load(yr, c);
+      } else {
+        x[k].load_part(xr, c, n);
+        y[k].load_part(yr, c, n);
+      }
+      if constexpr (sizeof(TX) == 1) ex[k] = n > 0 ? p.ck.e[r * p.ck.lde + (c >> 5)] : 0;
+    }
+    float a = 0.f, b = 0.f;
+    const auto xhat = [&](int k, int i) {
+      float scale = st.rstd;
+      if constexpr (sizeof(TX) == 1) scale *= q8_scale(ex[k]);
+      return fmaf(x[k].get(i), scale, st.shift);
+    };
+#pragma unroll
+    for (int k = 0; k < C; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if (i < valid(k)) {
+          const float g = y[k].get(i) * gamma[k * V + i];
+          a += g;
+          b = fmaf(g, xhat(k, i), b);
+        }
+      }
+    const float2 s = block_sum2(a, b, sm, buf);
+    buf ^= 1;
+    const float ga = s.x * inv_n * st.rstd, gx = s.y * inv_n * st.rstd;
+    TDX *dx = static_cast<TDX *>(p.dx) + r * p.lddx;
+#pragma unroll
+    for (int k = 0; k < C; ++k) {
+      const int n = valid(k);
+      float o[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float d = y[k].get(i), xh = xhat(k, i);
+        if (i < n) {
+          dg[k * V + i] = fmaf(d, xh, dg[k * V + i]);
+          db[k * V + i] += d;
+        }
+        o[i] = fmaf(d * gamma[k * V + i], st.rstd, -fmaf(xh, gx, ga));
+      }
+      store_chunk<TDX, V>(dx, col(k), o, n);
+    }
+  }
+  if (!p.partials) return;
+#pragma unroll
+  for (int k = 0; k < C; ++k)
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < valid(k)) {
+        p.partials[(int64_t)blockIdx.x * p.cols + col(k) + i] = dg[k * V + i];
+        p.partials[(int64_t)(gridDim.x + blockIdx.x) * p.cols + col(k) + i] = db[k * V + i];
+      }
+}
+
+// How a backward pass runs.
+enum LnPath { kLnAny, kLnRegs, kLnRing };
+struct LnPlan {
+  LnPath path;
+  int nv, threads, grid;
+  int chunk;                    // kLnRegs: V
+  int stages;                   // kLnRing
+  uint32_t x_bytes, dy_bytes;   // kLnRing: bytes of a row
+  int parts;                    // partial rows of the parameter gradients
+};
+
+// Whether rows of elements of `size` bytes at p, pitch ld, all start on a
+// multiple of `align` bytes.
+bool rows_on(const void *p, int64_t ld, int size, int align) {
+  return (reinterpret_cast<uintptr_t>(p) & (align - 1)) == 0 && ld * size % align == 0;
+}
+
+// Blocks that walk `rows` rows, `per_sm` at a time on an SM: every SM one
+// while there are few rows, more only where each has at least eight rows to
+// set against the partial row that it writes and another kernel reads.
+int row_blocks(int64_t rows, int sms, int per_sm) {
+  const int64_t few = rows < sms ? rows : sms, many = ceil_div64(rows, 8), most = (int64_t)sms * per_sm;
+  const int64_t want = many > few ? many : few;
+  return (int)(want < most ? want : most);
+}
+
+LnPlan plan_ln_backward(const LnBackward &p, int sms) {
+  LnPlan l{};
+  const int sx = !p.x ? 1 : p.x_type == GEMM_TYPE_BF16 ? 2 : 4, sg = p.dy_type == GEMM_TYPE_BF16 ? 2 : 4,
+            so = p.dx_type == GEMM_TYPE_BF16 ? 2 : 4;
+  const void *x = p.x ? p.x : (const void *)p.ck.q;
+  const int64_t ldx = p.x ? p.ldx : p.ck.ldq;
+  const int64_t eights = ceil_div64(p.cols, 8);
+  l.nv = (int)ceil_div64(eights, kRingThreads);
+  l.threads = (int)ceil_div64(ceil_div64(eights, l.nv), 32) * 32;
+  const bool pieces = (int64_t)p.cols * sx % 16 == 0 && (int64_t)p.cols * sg % 16 == 0 && p.cols % 8 == 0;
+  if (p.rows > 0 && l.nv <= 4 && pieces && rows_on(x, ldx, sx, 16) && rows_on(p.dy, p.lddy, sg, 16) &&
+      rows_on(p.dx, p.lddx, so, 16)) {
+    l.x_bytes = (uint32_t)p.cols * sx;
+    l.dy_bytes = (uint32_t)p.cols * sg;
+    int per_sm = (l.nv == 1 ? 2 : 1) * (kRingThreads / l.threads);
+    per_sm = per_sm > 4 ? 4 : per_sm;
+    int64_t stages = kRingBytes / per_sm / (l.x_bytes + l.dy_bytes);
+    if (stages < 2) {
+      per_sm = 1;
+      stages = kRingBytes / (l.x_bytes + l.dy_bytes);
+    }
+    if (stages >= 2) {
+      l.path = kLnRing;
+      l.stages = (int)(stages < kMaxStages ? stages : kMaxStages);
+      l.grid = l.parts = row_blocks(p.rows, sms, per_sm);
+      return l;
+    }
+  }
+  if (p.rows > 0 && l.nv <= 2) {
+    l.path = kLnRegs;
+    l.chunk = rows_on(x, ldx, sx, 4 * sx) && rows_on(p.dy, p.lddy, sg, 4 * sg) && rows_on(p.dx, p.lddx, so, 4 * so) ? 4 : 1;
+    const int per_sm = kRingThreads / l.threads;
+    l.grid = l.parts = row_blocks(p.rows, sms, per_sm > 4 ? 4 : per_sm);
+    return l;
+  }
+  // dx by one kernel, partials by another: enough blocks of 32 columns x 8
+  // rows at a time to fill the device several times over, no more than there
+  // are groups of rows
+  l.path = kLnAny;
+  l.grid = grid_cap(p.rows, (int64_t)sms * 8);
+  l.parts = grid_cap(ceil_div64((int64_t)sms * 16, ceil_div64(p.cols, 32)), ceil_div64(p.rows < 1 ? 1 : p.rows, 8));
+  return l;
+}
+
+template <typename TX, typename TDY, typename TDX, int NV>
+cudaError_t run_ring(const LnBackward &p, const LnPlan &l, const OpContext &c) {
+  const auto kern = ln_backward_ring_kernel<TX, TDY, TDX, NV>;
+  const size_t smem = (size_t)l.stages * (l.x_bytes + l.dy_bytes);
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
+  if (e != cudaSuccess) return e;
+  return launch_ex(kern, dim3(l.grid), dim3(l.threads), smem, c.st, 1, p, l.stages, l.x_bytes, l.dy_bytes, c.err,
+                   c.wait_limit_ns);
+}
+
 template <typename TX, typename TDY, typename TDX>
-cudaError_t ln_backward_any(const LnBackward &p, int sms, cudaStream_t st, int *launches) {
+cudaError_t run_types(const LnBackward &p, const OpContext &c, int *launches) {
+  const LnPlan l = plan_ln_backward(p, c.sms);
+  const dim3 grid(l.grid), block(l.threads);
   cudaError_t e = cudaSuccess;
   if (p.rows > 0) {
-    e = launch_ex(ln_backward_any_kernel<TX, TDY, TDX>, dim3(grid_cap(p.rows, (int64_t)sms * 8)), dim3(kRowThreads), 0,
-                  st, 1, p);
     ++*launches;
+    if (l.path == kLnRing)
+      e = l.nv == 1   ? run_ring<TX, TDY, TDX, 1>(p, l, c)
+          : l.nv == 2 ? run_ring<TX, TDY, TDX, 2>(p, l, c)
+          : l.nv == 3 ? run_ring<TX, TDY, TDX, 3>(p, l, c)
+                      : run_ring<TX, TDY, TDX, 4>(p, l, c);
+    else if (l.path == kLnRegs && l.nv == 1)
+      e = l.chunk == 4 ? launch_ex(ln_backward_regs_kernel<TX, TDY, TDX, 1, 4>, grid, block, 0, c.st, 1, p)
+                       : launch_ex(ln_backward_regs_kernel<TX, TDY, TDX, 1, 1>, grid, block, 0, c.st, 1, p);
+    else if (l.path == kLnRegs)
+      e = l.chunk == 4 ? launch_ex(ln_backward_regs_kernel<TX, TDY, TDX, 2, 4>, grid, block, 0, c.st, 1, p)
+                       : launch_ex(ln_backward_regs_kernel<TX, TDY, TDX, 2, 1>, grid, block, 0, c.st, 1, p);
+    else
+      e = launch_ex(ln_backward_any_kernel<TX, TDY, TDX>, grid, dim3(kRowThreads), 0, c.st, 1, p);
     if (e != cudaSuccess) return e;
   }
-  if (!p.dgamma && !p.dbeta) return e;
+  if (!p.partials) return e;
   const int strips = (int)ceil_div64(p.cols, 32);
-  const int parts = (int)(ln_backward_partials(p, sms) / 2 / p.cols);
-  e = launch_ex(ln_param_partials_kernel<TX, TDY>, dim3(strips, parts), dim3(kRowThreads), 0, st, 1, p);
+  if (l.path == kLnAny) {
+    ++*launches;
+    e = launch_ex(ln_param_partials_kernel<TX, TDY>, dim3(strips, l.parts), dim3(kRowThreads), 0, c.st, 1, p);
+    if (e != cudaSuccess) return e;
+  }
   ++*launches;
-  if (e != cudaSuccess) return e;
-  e = launch_ex(ln_param_sum_kernel, dim3(strips, 2), dim3(1024), 0, st, 1, (const float *)p.partials, parts, p.cols,
-                p.dgamma, p.dbeta);
-  ++*launches;
-  return e;
+  return launch_ex(ln_param_sum_kernel, dim3(strips, 2), dim3(1024), 0, c.st, 1, (const float *)p.partials, l.parts,
+                   p.cols, p.dgamma, p.dbeta);
 }
 
 }  // namespace
 
-// Rows of partial sums: enough blocks of 32 columns x 8 rows at a time to
-// fill the device several times over, no more than there are groups of rows.
 size_t ln_backward_partials(const LnBackward &p, int sms) {
-  const int64_t strips = ceil_div64(p.cols, 32);
-  const int64_t parts = grid_cap(ceil_div64((int64_t)sms * 16, strips), ceil_div64(p.rows < 1 ? 1 : p.rows, 8));
-  return (size_t)(2 * parts * p.cols);
+  return p.dgamma || p.dbeta ? (size_t)2 * plan_ln_backward(p, sms).parts * p.cols : 0;
 }
 
-cudaError_t launch_ln_backward(const LnBackward &p, int sms, cudaStream_t st, int *launches) {
+cudaError_t launch_ln_backward(const LnBackward &p, const OpContext &c, int *launches) {
   const bool gb = p.dy_type == GEMM_TYPE_BF16, ob = p.dx_type == GEMM_TYPE_BF16;
   if (!p.x) {
-    if (ob) return gb ? ln_backward_any<Q8, bf16, bf16>(p, sms, st, launches) : ln_backward_any<Q8, float, bf16>(p, sms, st, launches);
-    return gb ? ln_backward_any<Q8, bf16, float>(p, sms, st, launches) : ln_backward_any<Q8, float, float>(p, sms, st, launches);
+    if (ob) return gb ? run_types<Q8, bf16, bf16>(p, c, launches) : run_types<Q8, float, bf16>(p, c, launches);
+    return gb ? run_types<Q8, bf16, float>(p, c, launches) : run_types<Q8, float, float>(p, c, launches);
   }
-  if (ob) return gb ? ln_backward_any<bf16, bf16, bf16>(p, sms, st, launches) : ln_backward_any<bf16, float, bf16>(p, sms, st, launches);
-  return gb ? ln_backward_any<float, bf16, float>(p, sms, st, launches) : ln_backward_any<float, float, float>(p, sms, st, launches);
+  if (ob) return gb ? run_types<bf16, bf16, bf16>(p, c, launches) : run_types<bf16, float, bf16>(p, c, launches);
+  return gb ? run_types<float, bf16, float>(p, c, launches) : run_types<float, float, float>(p, c, launches);
 }
 
 }  // namespace gb300
