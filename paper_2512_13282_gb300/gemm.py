@@ -104,7 +104,9 @@ def _ptr(x) -> int:
 def _stream(s) -> int:
     if s is None:
         import torch
-        return int(torch.cuda.current_stream().cuda_stream)
+        # the handle itself: a torch.cuda.Stream object around it costs 2.8 us
+        # a call on GB300's host, a third of a small call's time, this 0.3 us
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(s, int):
         return s
     return int(s.cuda_stream)
