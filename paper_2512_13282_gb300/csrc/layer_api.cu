@@ -56,7 +56,7 @@ gemm_status_t gemm_layernorm_forward(int64_t rows, int64_t cols, const void *x, 
   const LnForward p{rows, (int)cols, x, ldx, x_type, gamma, beta, param_type, eps, y, ldy, y_type, mean, rstd,
                     Q8Ref{q, ldq, e, lde}};
   count_launches(1);
-  return launched(launch_ln_forward(p, c.sms, c.st));
+  return launched(launch_ln_forward(p, c));
 }
 
 gemm_status_t gemm_layernorm_backward(int64_t rows, int64_t cols, const void *x, int64_t ldx, int x_type,

@@ -36,7 +36,7 @@ struct LnForward {
   float *mean, *rstd;  // either may be null
   Q8Ref ck;            // checkpoint of y, or ck.q null
 };
-cudaError_t launch_ln_forward(const LnForward &p, int sms, cudaStream_t st);
+cudaError_t launch_ln_forward(const LnForward &p, const OpContext &c);
 
 struct LnBackward {
   int64_t rows;

@@ -8,8 +8,8 @@ namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int kRingThreads = 512;     // most threads a block of the register-resident kernels has
-constexpr int kMaxStages = 8;
-constexpr int64_t kRingBytes = 200 * 1024;  // shared memory of an SM's rings together
+// Threads of the ring kernel with NV eights of values each.
+__host__ __device__ constexpr int ring_threads(int nv) { return nv == 1 ? 128 : kRingThreads; }
 
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int grid_cap(int64_t want, int64_t cap) { return (int)(want < 1 ? 1 : (want > cap ? cap : want)); }
@@ -115,46 +115,46 @@ __global__ void __launch_bounds__(1024) ln_param_sum_kernel(const float *partial
 // Row r's mean and 1/std as the factors of xh = x * rstd - mean * rstd.
 struct RowStats {
   float rstd, shift;
-  __device__ __forceinline__ void load(const LnBackward &p, int64_t r) {
-    rstd = p.rstd[r];
-    shift = -p.mean[r] * rstd;
-  }
+  __device__ __forceinline__ explicit RowStats(float2 mean_rstd)
+      : rstd(mean_rstd.y), shift(-mean_rstd.x * mean_rstd.y) {}
 };
 
 // Rows whose x and dy are whole 16-byte pieces, up to 512 * NV * 8 values.
 // A block walks rows gridDim.x apart.  Their x and dy come through a ring of
-// `stages` row slots in shared memory, filled by bulk copies that run as far
-// ahead as the ring is deep: dgamma and dbeta are summed in registers (16
-// values a thread and NV), which leaves none for rows in flight.  A row is
-// read from its slot twice, for the two averages and for the results; the
-// block-wide barrier between, passed by every thread once it has finished
-// with the row before, also frees that row's slot, which thread 0 refills.
-// One partial row of dgamma and dbeta a block goes to the workspace.
+// row slots in shared memory, filled by bulk copies that run as far ahead as
+// the ring is deep: dgamma and dbeta are summed in registers (16 values a
+// thread and NV), which leaves none for rows in flight.  A row is read from
+// its slot twice, for the two averages and for the results; the block-wide
+// barrier between, passed by every thread once it has finished with the row
+// before, also frees that row's slot, which thread 0 refills.  One partial
+// row of dgamma and of dbeta a block goes to the workspace.
 template <typename TX, typename TDY, typename TDX, int NV>
-__global__ void __launch_bounds__(kRingThreads, NV == 1 ? 2 : 1)
+__global__ void __launch_bounds__(ring_threads(NV), NV == 1 ? 8 : 1)
     ln_backward_ring_kernel(const LnBackward p, const int stages, const uint32_t x_bytes, const uint32_t dy_bytes,
                             uint32_t *err, const uint64_t wait_limit_ns) {
-  extern __shared__ __align__(128) uint8_t ring[];
-  __shared__ float2 sm[2][32];
+  extern __shared__ __align__(128) uint8_t slots[];
+  __shared__ __align__(16) float2 sm[2][16];
   __shared__ __align__(8) uint64_t bars[kMaxStages];
   __shared__ volatile uint32_t abort_flag;
   griddep_launch_dependents();
-  const int T = blockDim.x;
-  const uint32_t slot_bytes = x_bytes + dy_bytes;
-  const uint32_t ring_addr = smem_addr(ring), bar0 = smem_addr(bars);
+  const int T = blockDim.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t ring = smem_addr(slots), bar0 = smem_addr(bars), slot_bytes = x_bytes + dy_bytes;
+  RingPlace use, put;  // put: thread 0's
   const float inv_n = 1.0f / (float)p.cols;
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) mbar_init(bar0 + 8 * s, 1);
     abort_flag = 0;
     fence_mbar_init();
   }
+  if (threadIdx.x < 32) sm[threadIdx.x >> 4][threadIdx.x & 15] = make_float2(0.f, 0.f);
   __syncthreads();
   griddep_wait();
   const int64_t mine = (p.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // rows of this block, at least one
   const auto row_of = [&](int64_t i) { return (int64_t)blockIdx.x + i * gridDim.x; };
   const auto fill = [&](int64_t i) {
-    const uint32_t s = (uint32_t)(i % stages), dst = ring_addr + s * slot_bytes, bar = bar0 + 8 * s;
+    const uint32_t dst = ring + put.slot * slot_bytes, bar = bar0 + 8u * put.slot;
     const int64_t r = row_of(i);
+    put.advance(stages);
     mbar_arrive_expect_tx(bar, slot_bytes);
     if constexpr (sizeof(TX) == 1)
       bulk_load(dst, p.ck.q + r * p.ck.ldq, x_bytes, bar);
@@ -162,25 +162,16 @@ __global__ void __launch_bounds__(kRingThreads, NV == 1 ? 2 : 1)
       bulk_load(dst, static_cast<const TX *>(p.x) + r * p.ldx, x_bytes, bar);
     bulk_load(dst + x_bytes, static_cast<const TDY *>(p.dy) + r * p.lddy, dy_bytes, bar);
   };
+  int64_t filled = mine < stages ? mine : stages;
   if (threadIdx.x == 0)
-    for (int64_t i = 0; i < stages && i < mine; ++i) fill(i);
+    for (int64_t i = 0; i < filled; ++i) fill(i);
 
-  float gamma[NV * 8], dg[NV * 8], db[NV * 8];
-#pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int c = (v * T + (int)threadIdx.x) * 8;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      gamma[v * 8 + i] = c < p.cols ? load_param(p.gamma, p.param_type, c + i, 1.f) : 0.f;
-      dg[v * 8 + i] = db[v * 8 + i] = 0.f;
-    }
-  }
   // the row's statistics and block exponents, fetched a row ahead
-  RowStats st, st_next;
+  float2 st_next;
   uint32_t ex[NV], ex_next[NV];
   const auto fetch = [&](int64_t i) {
     const int64_t r = row_of(i);
-    st_next.load(p, r);
+    st_next = make_float2(p.mean[r], p.rstd[r]);
     if constexpr (sizeof(TX) == 1) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
@@ -190,82 +181,90 @@ __global__ void __launch_bounds__(kRingThreads, NV == 1 ? 2 : 1)
     }
   };
   fetch(0);
+  float2 gamma[NV * 4], dg[NV * 4], db[NV * 4];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = (v * T + (int)threadIdx.x) * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      gamma[v * 4 + i] = c < p.cols ? make_float2(load_param(p.gamma, p.param_type, c + 2 * i, 1.f),
+                                                  load_param(p.gamma, p.param_type, c + 2 * i + 1, 1.f))
+                                    : both(0.f);
+      dg[v * 4 + i] = db[v * 4 + i] = both(0.f);
+    }
+  }
   bool ok = true;
-  int64_t filled = mine < stages ? mine : stages;
-  for (int64_t i = 0; i < mine; ++i) {
-    const uint8_t *slot = ring + (i % stages) * slot_bytes;
-    st = st_next;
+  int64_t done = 0;
+  for (int64_t i = 0; i < mine; done = ++i, use.advance(stages)) {
+    const uint8_t *slot = slots + use.slot * slot_bytes;
+    const RowStats st(st_next);
 #pragma unroll
     for (int v = 0; v < NV; ++v) ex[v] = ex_next[v];
     if (i + 1 < mine) fetch(i + 1);
-    ok = mbar_wait(bar0 + 8 * (uint32_t)(i % stages), (uint32_t)(i / stages) & 1u, &abort_flag, err, wait_limit_ns);
-    float a = 0.f, b = 0.f;
-    // xh and g of chunk v, from the slot
-    const auto load = [&](int v, float(&xh)[8], float(&g)[8], float(&d)[8]) {
+    ok = mbar_wait(bar0 + 8u * use.slot, use.parity, &abort_flag, err, wait_limit_ns);
+    const auto load = [&](int v, Chunk<TX, 8> &x, Chunk<TDY, 8> &y, float2 &scale) {
       const int c = (v * T + (int)threadIdx.x) * 8;
-      Chunk<TX, 8> x;
-      Chunk<TDY, 8> y;
       x.load(slot, c);
       y.load(slot + x_bytes, c);
-      float scale = st.rstd;
-      if constexpr (sizeof(TX) == 1) scale *= q8_scale(ex[v]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        xh[j] = fmaf(x.get(j), scale, st.shift);
-        d[j] = y.get(j);
-        g[j] = d[j] * gamma[v * 8 + j];
-      }
+      if constexpr (sizeof(TX) == 1)
+        scale = both(st.rstd * q8_scale(ex[v]));
+      else
+        scale = both(st.rstd);
     };
+    const float2 shift = both(st.shift);
+    float2 a2 = both(0.f), b2 = both(0.f);
     if (ok) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         if ((v * T + (int)threadIdx.x) * 8 < p.cols) {
-          float xh[8], g[8], d[8];
-          load(v, xh, g, d);
+          Chunk<TX, 8> x;
+          Chunk<TDY, 8> y;
+          float2 scale;
+          load(v, x, y, scale);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            a += g[j];
-            b = fmaf(g[j], xh[j], b);
+          for (int j = 0; j < 4; ++j) {
+            const float2 g = mul2(y.get2(j), gamma[v * 4 + j]);
+            a2 = add2(a2, g);
+            b2 = fma2(g, fma2(x.get2(j), scale, shift), b2);
           }
         }
       }
     }
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = T >> 5;
-    a = warp_sum(a);
-    b = warp_sum(b);
+    const float a = warp_sum(a2.x + a2.y), b = warp_sum(b2.x + b2.y);
     if (lane == 0) sm[i & 1][warp] = make_float2(a, b);
     // every wait of the block succeeded, or the block gives up together
     if (!__syncthreads_and(ok)) {
       ok = false;
       break;
     }
-    if (threadIdx.x == 0 && i > 0 && i - 1 + stages < mine) {
-      fill(i - 1 + stages);
-      filled = i + stages;
-    }
-    const float2 part = lane < warps ? sm[i & 1][lane] : make_float2(0.f, 0.f);
-    const float ga = warp_sum(part.x) * inv_n * st.rstd, gx = warp_sum(part.y) * inv_n * st.rstd;
+    if (threadIdx.x == 0 && i > 0 && filled < mine) fill(filled++);  // the slot of row i - 1
+    const float2 s = sum_over_warps(sm[i & 1], T >> 5);
+    const float2 ga = both(-s.x * inv_n * st.rstd), gx = both(-s.y * inv_n * st.rstd), rstd = both(st.rstd);
     TDX *dx = static_cast<TDX *>(p.dx) + row_of(i) * p.lddx;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = (v * T + (int)threadIdx.x) * 8;
       if (c < p.cols) {
-        float xh[8], g[8], d[8], o[8];
-        load(v, xh, g, d);
+        Chunk<TX, 8> x;
+        Chunk<TDY, 8> y;
+        float2 scale;
+        load(v, x, y, scale);
+        float o[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          dg[v * 8 + j] = fmaf(d[j], xh[j], dg[v * 8 + j]);
-          db[v * 8 + j] += d[j];
-          o[j] = fmaf(g[j], st.rstd, -fmaf(xh[j], gx, ga));
+        for (int j = 0; j < 4; ++j) {
+          const float2 d = y.get2(j), xh = fma2(x.get2(j), scale, shift);
+          dg[v * 4 + j] = fma2(d, xh, dg[v * 4 + j]);
+          db[v * 4 + j] = add2(db[v * 4 + j], d);
+          const float2 r = fma2(mul2(d, gamma[v * 4 + j]), rstd, fma2(xh, gx, ga));
+          o[2 * j] = r.x;
+          o[2 * j + 1] = r.y;
         }
         store_chunk<TDX, 8>(dx, c, o, 8);
       }
     }
   }
-  if (!ok) {  // let the copies in flight land before the block's memory is given up
-    if (threadIdx.x == 0)
-      for (int64_t i = filled > stages ? filled - stages : 0; i < filled; ++i)
-        mbar_wait_drain(bar0 + 8 * (uint32_t)(i % stages), (uint32_t)(i / stages) & 1u, 200ull * 1000 * 1000);
+  if (!ok) {
+    if (threadIdx.x == 0) ring_drain(bar0, stages, use, filled - done);
     return;
   }
   if (!p.partials) return;
@@ -273,8 +272,9 @@ __global__ void __launch_bounds__(kRingThreads, NV == 1 ? 2 : 1)
   for (int v = 0; v < NV; ++v) {
     const int c = (v * T + (int)threadIdx.x) * 8;
     if (c < p.cols) {
-      store_chunk<float, 8>(p.partials + (int64_t)blockIdx.x * p.cols, c, dg + v * 8, 8);
-      store_chunk<float, 8>(p.partials + (int64_t)(gridDim.x + blockIdx.x) * p.cols, c, db + v * 8, 8);
+      store_chunk<float, 8>(p.partials + (int64_t)blockIdx.x * p.cols, c, reinterpret_cast<const float *>(dg + v * 4), 8);
+      store_chunk<float, 8>(p.partials + (int64_t)(gridDim.x + blockIdx.x) * p.cols, c,
+                            reinterpret_cast<const float *>(db + v * 4), 8);
     }
   }
 }
@@ -303,8 +303,7 @@ __global__ void __launch_bounds__(kRingThreads) ln_backward_regs_kernel(const Ln
     }
   int buf = 0;
   for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
-    RowStats st;
-    st.load(p, r);
+    const RowStats st(make_float2(p.mean[r], p.rstd[r]));
     Chunk<TX, V> x[C];
     Chunk<TDY, V> y[C];
     uint32_t ex[C];
@@ -384,12 +383,6 @@ struct LnPlan {
   int parts;                    // partial rows of the parameter gradients
 };
 
-// Whether rows of elements of `size` bytes at p, pitch ld, all start on a
-// multiple of `align` bytes.
-bool rows_on(const void *p, int64_t ld, int size, int align) {
-  return (reinterpret_cast<uintptr_t>(p) & (align - 1)) == 0 && ld * size % align == 0;
-}
-
 // Blocks that walk `rows` rows, `per_sm` at a time on an SM: every SM one
 // while there are few rows, more only where each has at least eight rows to
 // set against the partial row that it writes and another kernel reads.
@@ -406,15 +399,18 @@ LnPlan plan_ln_backward(const LnBackward &p, int sms) {
   const void *x = p.x ? p.x : (const void *)p.ck.q;
   const int64_t ldx = p.x ? p.ldx : p.ck.ldq;
   const int64_t eights = ceil_div64(p.cols, 8);
-  l.nv = (int)ceil_div64(eights, kRingThreads);
-  l.threads = (int)ceil_div64(ceil_div64(eights, l.nv), 32) * 32;
+  // few threads with more values each: a row's fixed costs (its barrier, the
+  // sums over lanes and warps) are paid by every warp
+  const int ring_nv = eights <= ring_threads(1) ? 1 : eights <= 2 * kRingThreads ? 2 : (int)ceil_div64(eights, kRingThreads);
   const bool pieces = (int64_t)p.cols * sx % 16 == 0 && (int64_t)p.cols * sg % 16 == 0 && p.cols % 8 == 0;
-  if (p.rows > 0 && l.nv <= 4 && pieces && rows_on(x, ldx, sx, 16) && rows_on(p.dy, p.lddy, sg, 16) &&
+  if (p.rows > 0 && ring_nv <= 4 && pieces && rows_on(x, ldx, sx, 16) && rows_on(p.dy, p.lddy, sg, 16) &&
       rows_on(p.dx, p.lddx, so, 16)) {
     l.x_bytes = (uint32_t)p.cols * sx;
     l.dy_bytes = (uint32_t)p.cols * sg;
+    l.nv = ring_nv;
+    l.threads = (int)ceil_div64(ceil_div64(eights, l.nv), 32) * 32;
     int per_sm = (l.nv == 1 ? 2 : 1) * (kRingThreads / l.threads);
-    per_sm = per_sm > 4 ? 4 : per_sm;
+    per_sm = per_sm > 8 ? 8 : per_sm;
     int64_t stages = kRingBytes / per_sm / (l.x_bytes + l.dy_bytes);
     if (stages < 2) {
       per_sm = 1;
@@ -427,8 +423,10 @@ LnPlan plan_ln_backward(const LnBackward &p, int sms) {
       return l;
     }
   }
-  if (p.rows > 0 && l.nv <= 2) {
+  if (p.rows > 0 && eights <= 2 * kRingThreads) {
     l.path = kLnRegs;
+    l.nv = (int)ceil_div64(eights, kRingThreads);
+    l.threads = (int)ceil_div64(ceil_div64(eights, l.nv), 32) * 32;
     l.chunk = rows_on(x, ldx, sx, 4 * sx) && rows_on(p.dy, p.lddy, sg, 4 * sg) && rows_on(p.dx, p.lddx, so, 4 * so) ? 4 : 1;
     const int per_sm = kRingThreads / l.threads;
     l.grid = l.parts = row_blocks(p.rows, sms, per_sm > 4 ? 4 : per_sm);

@@ -1,5 +1,7 @@
 // layer_ln_fwd.cu -- layer norm forward, optionally with the result's 8-bit
 // checkpoint.
+#include <atomic>
+
 #include "layer_rows.cuh"
 
 namespace gb300 {
@@ -56,6 +58,33 @@ __global__ void __launch_bounds__(kAnyThreads) ln_forward_any_kernel(const LnFor
 }
 
 
+// The checkpoint of a lane's 8 consecutive results (the first n of them; four
+// lanes hold a block) as y's type holds them.  All lanes of the warp call it.
+template <typename TY>
+__device__ __forceinline__ void save_eighth(const Q8Ref &ck, int64_t r, int c, const float (&y)[8], int n) {
+  float o[8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    o[i] = i < n ? as_stored<TY>(y[i]) : 0.f;
+    top = max(top, __float_as_uint(o[i]) & 0x7FFFFFFFu);
+  }
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  const uint32_t e = q8_exponent(top);
+  const float inverse = q8_inverse(e);
+  const uint32_t lo = q8_pack4(o, inverse, e), hi = q8_pack4(o + 4, inverse, e);
+  int8_t *q = ck.q + r * ck.ldq + c;
+  if (n == 8) {
+    *reinterpret_cast<uint2 *>(q) = make_uint2(lo, hi);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) q[i] = (int8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
+  }
+  if (n > 0 && (c & 31) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
+}
+
 // Rows of up to 512 * NV * 8 values, kept in registers from their one read to
 // their one write: a block of T threads walks rows gridDim.x apart, the next
 // row's values on their way (as they are in memory) while this row is
@@ -68,7 +97,7 @@ __global__ void __launch_bounds__(kAnyThreads) ln_forward_any_kernel(const LnFor
 // sectors, as the lanes of a warp are neighbours.  A checkpoint block is 4
 // lanes' chunks (V = 8) or the warp's 32 lanes (V = 1).
 template <typename TX, typename TY, int NV, int V>
-__global__ void __launch_bounds__(kMaxThreads) ln_forward_kernel(const LnForward p) {
+__global__ void __launch_bounds__(kMaxThreads, NV == 1 ? 2 : 1) ln_forward_kernel(const LnForward p) {
   constexpr int C = NV * 8 / V;  // chunks per thread
   constexpr bool kKeep = NV <= 2;
   __shared__ float sm[2][32];
@@ -143,85 +172,215 @@ __global__ void __launch_bounds__(kMaxThreads) ln_forward_kernel(const LnForward
         o[i] = fmaf(x[k * V + i] * rstd, g, b);
       }
       store_chunk<TY, V>(y, c, o, n);
-      if (p.ck.q) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          o[i] = i < n ? as_stored<TY>(o[i]) : 0.f;
-          top = max(top, __float_as_uint(o[i]) & 0x7FFFFFFFu);
-        }
-        if constexpr (V == 1) {
-          top = __reduce_max_sync(0xffffffffu, top);
-        } else {
-          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        }
-        const uint32_t e = q8_exponent(top);
-        const float inverse = q8_inverse(e);
-        int8_t *q = p.ck.q + r * p.ck.ldq + c;
-        if constexpr (V == 8) {
-          const uint32_t lo = q8_pack4(o, inverse, e), hi = q8_pack4(o + 4, inverse, e);
-          if (n == V) {
-            *reinterpret_cast<uint2 *>(q) = make_uint2(lo, hi);
-          } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-              if (i < n) q[i] = (int8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
-          }
-        } else if (n > 0) {
-          q[0] = (int8_t)q8_quantise(o[0], inverse, e);
-        }
+      if (!p.ck.q) continue;
+      if constexpr (V == 8) {
+        save_eighth<TY>(p.ck, r, c, o, n);
+      } else {
+        o[0] = n > 0 ? as_stored<TY>(o[0]) : 0.f;
+        const uint32_t e = q8_exponent(__reduce_max_sync(0xffffffffu, __float_as_uint(o[0]) & 0x7FFFFFFFu));
+        if (n > 0) p.ck.q[r * p.ck.ldq + c] = (int8_t)q8_quantise(o[0], q8_inverse(e), e);
         if (n > 0 && (c & 31) == 0) p.ck.e[r * p.ck.lde + (c >> 5)] = (uint8_t)e;
       }
     }
   }
 }
 
-// Whether rows of elements of `size` bytes at p, pitch ld, all start on a
-// multiple of `align` bytes.
-bool rows_on(const void *p, int64_t ld, int size, int align) {
-  return (reinterpret_cast<uintptr_t>(p) & (align - 1)) == 0 && ld * size % align == 0;
+// Rows whose x is whole 16-byte pieces (and y's and q's rows aligned), up to
+// 512 * NV * 8 values: as above, with the rows to come in a ring of slots that
+// bulk copies fill, since one row ahead in registers is not enough in flight
+// (3 blocks of 8 KB rows an SM: 24 KB, where the copy rate times the latency
+// asks for 40).  The first of a row's two barriers frees its slot.
+//
+// THREADS bounds the block, and with it the registers so that 24 warps share
+// an SM (32 with NV = 1, 16 with NV = 4).
+template <typename TX, typename TY, int NV, int THREADS>
+__global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 && THREADS <= 256 ? 768 / THREADS : 1)
+    ln_forward_ring_kernel(const LnForward p, const int stages, const uint32_t x_bytes, uint32_t *err,
+                           const uint64_t wait_limit_ns) {
+  constexpr bool kKeep = NV <= 2;
+  extern __shared__ __align__(128) uint8_t slots[];
+  __shared__ __align__(16) float sm[2][16];
+  __shared__ __align__(8) uint64_t bars[kMaxStages];
+  __shared__ volatile uint32_t abort_flag;
+  griddep_launch_dependents();
+  const int T = blockDim.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t ring = smem_addr(slots), bar0 = smem_addr(bars);
+  RingPlace use, put;  // put: thread 0's
+  const float inv_n = 1.0f / (float)p.cols;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) mbar_init(bar0 + 8 * s, 1);
+    abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (threadIdx.x < 32) sm[threadIdx.x >> 4][threadIdx.x & 15] = 0.f;
+  __syncthreads();
+  griddep_wait();
+  const int64_t mine = (p.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // rows of this block, at least one
+  const auto row_of = [&](int64_t i) { return (int64_t)blockIdx.x + i * gridDim.x; };
+  const auto fill = [&](int64_t i) {
+    const uint32_t dst = ring + put.slot * x_bytes, bar = bar0 + 8u * put.slot;
+    put.advance(stages);
+    mbar_arrive_expect_tx(bar, x_bytes);
+    bulk_load(dst, static_cast<const TX *>(p.x) + row_of(i) * p.ldx, x_bytes, bar);
+  };
+  int64_t filled = mine < stages ? mine : stages;
+  if (threadIdx.x == 0)
+    for (int64_t i = 0; i < filled; ++i) fill(i);
+  const auto col = [&](int v) { return (v * T + (int)threadIdx.x) * 8; };
+  const auto param = [&](const void *src, int c, float absent) {
+    return make_float2(load_param(src, p.param_type, c, absent), load_param(src, p.param_type, c + 1, absent));
+  };
+  float2 gamma[kKeep ? NV * 4 : 1], beta[kKeep ? NV * 4 : 1];
+  if constexpr (kKeep) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool in = col(v) < p.cols;
+        gamma[v * 4 + j] = in ? param(p.gamma, col(v) + 2 * j, 1.f) : both(0.f);
+        beta[v * 4 + j] = in ? param(p.beta, col(v) + 2 * j, 0.f) : both(0.f);
+      }
+  }
+  bool ok = true;
+  int64_t done = 0;
+  for (int64_t i = 0; i < mine; done = ++i, use.advance(stages)) {
+    const int64_t r = row_of(i);
+    ok = mbar_wait(bar0 + 8u * use.slot, use.parity, &abort_flag, err, wait_limit_ns);
+    float2 x[NV * 4], s2 = both(0.f);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if (ok && col(v) < p.cols) {
+        Chunk<TX, 8> raw;
+        raw.load(slots + use.slot * x_bytes, col(v));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[v * 4 + j] = raw.get2(j);
+          s2 = add2(s2, x[v * 4 + j]);
+        }
+      }
+    }
+    const float s = warp_sum(s2.x + s2.y);
+    if (lane == 0) sm[0][warp] = s;
+    // every wait of the block succeeded, or the block gives up together
+    if (!__syncthreads_and(ok)) {
+      ok = false;
+      break;
+    }
+    if (threadIdx.x == 0 && filled < mine) fill(filled++);  // this row's slot
+    const float mean = sum_over_warps(sm[0], T >> 5) * inv_n;
+    float2 v2 = both(0.f);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if (col(v) < p.cols) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[v * 4 + j] = add2(x[v * 4 + j], both(-mean));
+          v2 = fma2(x[v * 4 + j], x[v * 4 + j], v2);
+        }
+      }
+    }
+    const float var = warp_sum(v2.x + v2.y);
+    if (lane == 0) sm[1][warp] = var;
+    __syncthreads();
+    const float rstd = 1.0f / sqrtf(sum_over_warps(sm[1], T >> 5) * inv_n + p.eps);
+    if (threadIdx.x == 0) {
+      if (p.mean) p.mean[r] = mean;
+      if (p.rstd) p.rstd[r] = rstd;
+    }
+    TY *y = static_cast<TY *>(p.y) + r * p.ldy;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = col(v);
+      const bool in = c < p.cols;
+      float o[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 g = kKeep ? gamma[v * 4 + j] : in ? param(p.gamma, c + 2 * j, 1.f) : both(0.f);
+        const float2 b = kKeep ? beta[v * 4 + j] : in ? param(p.beta, c + 2 * j, 0.f) : both(0.f);
+        const float2 w = fma2(mul2(x[v * 4 + j], both(rstd)), g, b);
+        o[2 * j] = w.x;
+        o[2 * j + 1] = w.y;
+      }
+      if (in) store_chunk<TY, 8>(y, c, o, 8);
+      if (p.ck.q) save_eighth<TY>(p.ck, r, c, o, in ? 8 : 0);
+    }
+  }
+  if (!ok && threadIdx.x == 0) ring_drain(bar0, stages, use, filled - done);
+}
+
+// Blocks of a kernel that an SM holds at once, asked once a kernel, block
+// shape and shared memory size (the devices served are all the same).
+template <typename K>
+int blocks_per_sm(K kern, int threads, size_t smem, std::atomic<uint64_t> &known) {
+  const uint64_t key = (uint64_t)smem << 16 | (uint64_t)threads << 8;
+  const uint64_t k = known.load(std::memory_order_relaxed);
+  if ((k & ~(uint64_t)0xFF) == key && (k & 0xFF)) return (int)(k & 0xFF);
+  int n = 0;
+  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, threads, smem) != cudaSuccess || n < 1) n = 1;
+  known.store(key | (uint64_t)n, std::memory_order_relaxed);
+  return n;
 }
 
 // Blocks that fill the device once, no more than there are rows.
-template <typename K>
-unsigned persistent_grid(K kern, int threads, int64_t rows, int sms) {
-  int per_sm = 0;
-  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, threads, 0) != cudaSuccess || per_sm < 1) per_sm = 1;
+unsigned persistent_grid(int per_sm, int64_t rows, int sms) {
   const int64_t most = (int64_t)sms * per_sm;
   return (unsigned)(rows < most ? rows : most);
 }
 
 template <typename TX, typename TY, int NV, int V>
-cudaError_t run_rows(const LnForward &p, int threads, int sms, cudaStream_t st) {
+cudaError_t run_rows(const LnForward &p, int threads, const OpContext &c) {
+  static std::atomic<uint64_t> known{0};
   const auto kern = ln_forward_kernel<TX, TY, NV, V>;
-  return launch_ex(kern, dim3(persistent_grid(kern, threads, p.rows, sms)), dim3(threads), 0, st, 1, p);
+  return launch_ex(kern, dim3(persistent_grid(blocks_per_sm(kern, threads, 0, known), p.rows, c.sms)), dim3(threads), 0,
+                   c.st, 1, p);
+}
+
+template <typename TX, typename TY, int NV, int THREADS>
+cudaError_t run_ring(const LnForward &p, const OpContext &c) {
+  static std::atomic<uint64_t> known{0};
+  const auto kern = ln_forward_ring_kernel<TX, TY, NV, THREADS>;
+  const int eights = (p.cols + 7) / 8, threads = ((eights + NV - 1) / NV + 31) / 32 * 32;
+  const uint32_t x_bytes = (uint32_t)(p.cols * sizeof(TX));
+  // the rings of the blocks that registers allow share the memory
+  const int want = (NV == 1 ? 1024 : NV == 2 ? 768 : 512) / threads;
+  int64_t stages = kRingBytes / (want < 8 ? want : 8) / x_bytes;
+  stages = stages < 2 ? 2 : stages > kMaxStages ? kMaxStages : stages;
+  const size_t smem = (size_t)stages * x_bytes;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
+  if (e != cudaSuccess) return e;
+  return launch_ex(kern, dim3(persistent_grid(blocks_per_sm(kern, threads, smem, known), p.rows, c.sms)), dim3(threads),
+                   smem, c.st, 1, p, (int)stages, x_bytes, c.err, c.wait_limit_ns);
 }
 
 template <typename TX, typename TY>
-cudaError_t run_types(const LnForward &p, int sms, cudaStream_t st) {
+cudaError_t run_types(const LnForward &p, const OpContext &c) {
   const int eights = (p.cols + 7) / 8;
   const bool vec = rows_on(p.x, p.ldx, sizeof(TX), 16) && rows_on(p.y, p.ldy, sizeof(TY), 16) &&
                    (!p.ck.q || rows_on(p.ck.q, p.ck.ldq, 1, 8));
+  if (eights > 4 * kMaxThreads) {
+    const int64_t most = (int64_t)c.sms * 8;
+    return launch_ex(ln_forward_any_kernel<TX, TY>, dim3((unsigned)(p.rows < most ? p.rows : most)), dim3(kAnyThreads),
+                     0, c.st, 1, p);
+  }
+  if (vec && p.cols % 8 == 0) {
+    if (eights <= 128) return run_ring<TX, TY, 1, 128>(p, c);
+    if (eights <= 512) return run_ring<TX, TY, 2, 256>(p, c);
+    return eights <= 2 * kMaxThreads ? run_ring<TX, TY, 2, kMaxThreads>(p, c) : run_ring<TX, TY, 4, kMaxThreads>(p, c);
+  }
   // values per thread: 8 for rows of up to 256 threads, else 16, else 32
   const int nv = eights <= 256 ? 1 : eights <= 2 * kMaxThreads ? 2 : 4;
-  if (eights > nv * kMaxThreads) {
-    const int64_t most = (int64_t)sms * 8;
-    return launch_ex(ln_forward_any_kernel<TX, TY>, dim3((unsigned)(p.rows < most ? p.rows : most)), dim3(kAnyThreads),
-                     0, st, 1, p);
-  }
   const int threads = ((eights + nv - 1) / nv + 31) / 32 * 32;
-  if (nv == 1) return vec ? run_rows<TX, TY, 1, 8>(p, threads, sms, st) : run_rows<TX, TY, 1, 1>(p, threads, sms, st);
-  if (nv == 2) return vec ? run_rows<TX, TY, 2, 8>(p, threads, sms, st) : run_rows<TX, TY, 2, 1>(p, threads, sms, st);
-  return vec ? run_rows<TX, TY, 4, 8>(p, threads, sms, st) : run_rows<TX, TY, 4, 1>(p, threads, sms, st);
+  if (nv == 1) return vec ? run_rows<TX, TY, 1, 8>(p, threads, c) : run_rows<TX, TY, 1, 1>(p, threads, c);
+  if (nv == 2) return vec ? run_rows<TX, TY, 2, 8>(p, threads, c) : run_rows<TX, TY, 2, 1>(p, threads, c);
+  return vec ? run_rows<TX, TY, 4, 8>(p, threads, c) : run_rows<TX, TY, 4, 1>(p, threads, c);
 }
 
 }  // namespace
 
-cudaError_t launch_ln_forward(const LnForward &p, int sms, cudaStream_t st) {
+cudaError_t launch_ln_forward(const LnForward &p, const OpContext &c) {
   const bool xb = p.x_type == GEMM_TYPE_BF16, yb = p.y_type == GEMM_TYPE_BF16;
-  if (xb) return yb ? run_types<bf16, bf16>(p, sms, st) : run_types<bf16, float>(p, sms, st);
-  return yb ? run_types<float, bf16>(p, sms, st) : run_types<float, float>(p, sms, st);
+  if (xb) return yb ? run_types<bf16, bf16>(p, c) : run_types<bf16, float>(p, c);
+  return yb ? run_types<float, bf16>(p, c) : run_types<float, float>(p, c);
 }
 
 }  // namespace gb300

@@ -141,6 +141,7 @@ struct Chunk {
     else
       return s8_to_float(w[i / 4], i & 3);
   }
+  __device__ __forceinline__ float2 get2(int i) const { return make_float2(get(2 * i), get(2 * i + 1)); }
 };
 
 // V consecutive results rounded to T and stored (address a multiple of V
@@ -180,6 +181,32 @@ __device__ __forceinline__ float load_param(const void *p, int type, int c, floa
   return type == GEMM_TYPE_F32 ? static_cast<const float *>(p)[c] : __bfloat162float(static_cast<const bf16 *>(p)[c]);
 }
 
+// Pairs of float32 operations in one instruction each; both halves round as
+// the scalar ones do.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(d)
+      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)),
+        "l"(*reinterpret_cast<unsigned long long *>(&c)));
+  return *reinterpret_cast<float2 *>(&d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(d)
+      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
+  return *reinterpret_cast<float2 *>(&d);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(d)
+      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
+  return *reinterpret_cast<float2 *>(&d);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -209,6 +236,57 @@ __device__ __forceinline__ float2 block_sum2(float a, float b, float2 (*sm)[32],
   __syncthreads();
   const float2 v = lane < warps ? sm[buf][lane] : make_float2(0.f, 0.f);
   return make_float2(warp_sum(v.x), warp_sum(v.y));
+}
+
+// The second half of a block-wide sum, after the barrier: the sum of the
+// warps' values sm[0 .. warps), padded with zeros to a multiple of four, read
+// by broadcast (cheaper, and sooner done, than another tree of shuffles).
+__device__ __forceinline__ float2 sum_over_warps(const float2 *sm, int warps) {
+  float2 s = make_float2(0.f, 0.f), t = s;
+  for (int w = 0; w < warps; w += 4) {
+    const float4 a = *reinterpret_cast<const float4 *>(sm + w), b = *reinterpret_cast<const float4 *>(sm + w + 2);
+    s = add2(s, add2(make_float2(a.x, a.y), make_float2(a.z, a.w)));
+    t = add2(t, add2(make_float2(b.x, b.y), make_float2(b.z, b.w)));
+  }
+  return add2(s, t);
+}
+__device__ __forceinline__ float sum_over_warps(const float *sm, int warps) {
+  float s = 0.f;
+  for (int w = 0; w < warps; w += 4) {
+    const float4 a = *reinterpret_cast<const float4 *>(sm + w);
+    s += (a.x + a.y) + (a.z + a.w);
+  }
+  return s;
+}
+
+// A place in a ring of row slots in shared memory that bulk copies fill ahead
+// of their use: counted, not computed from the row's number (a division per
+// row and thread is a tenth of a row's instructions).
+struct RingPlace {
+  int slot = 0;
+  uint32_t parity = 0;
+  __device__ __forceinline__ void advance(int stages) {
+    if (++slot == stages) {
+      slot = 0;
+      parity ^= 1u;
+    }
+  }
+};
+// After giving up (thread 0): the fills issued and not waited for -- `use` is
+// the first of them, `pending` their number -- have landed before the block's
+// memory is given up.
+__device__ __forceinline__ void ring_drain(uint32_t bars, int stages, RingPlace use, int64_t pending) {
+  for (; pending > 0; --pending, use.advance(stages))
+    mbar_wait_drain(bars + 8u * use.slot, use.parity, 200ull * 1000 * 1000);
+}
+
+constexpr int kMaxStages = 8;
+constexpr int64_t kRingBytes = 200 * 1024;  // shared memory of an SM's rings together
+
+// Whether rows of elements of `size` bytes at p, pitch ld, all start on a
+// multiple of `align` bytes.
+inline bool rows_on(const void *p, int64_t ld, int size, int align) {
+  return (reinterpret_cast<uintptr_t>(p) & (align - 1)) == 0 && ld * size % align == 0;
 }
 
 }  // namespace gb300
