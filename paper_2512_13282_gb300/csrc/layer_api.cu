@@ -167,31 +167,32 @@ gemm_status_t gemm_q8_weight_grad(int64_t T, int64_t K, int64_t N, const int8_t 
     const gemm_status_t s = op_workspace(x_bytes + g_bytes + wgrad_partial_bytes(pl), c.st, &ws);
     if (s != GEMM_OK) return s;
     uint8_t *xs = static_cast<uint8_t *>(ws), *gs = xs + x_bytes, *parts = gs + g_bytes;
+    const Q8Ref ck{const_cast<int8_t *>(q), ldq, const_cast<uint8_t *>(e), lde};
+    const bool x16 = aligned_to(q, 16) && ldq % 16 == 0;
     count_launches(1);
-    if (launch_q8_restore(Q8Ref{const_cast<int8_t *>(q), ldq, const_cast<uint8_t *>(e), lde}, xs, ldk, GEMM_TYPE_BF16,
-                          T, K, c.st) != cudaSuccess)
+    if ((x16 && !pack ? launch_q8_restore(ck, xs, ldk, GEMM_TYPE_BF16, T, K, c.st)
+                      : launch_wgrad_stage(ck, T, K, reinterpret_cast<uint16_t *>(xs), ldk, pack ? dY : nullptr, lddy, N,
+                                           reinterpret_cast<uint16_t *>(gs), ldn, c.st)) != cudaSuccess)
       return GEMM_ERR_CUDA;
-    const void *g = dY;
-    int64_t ldg = lddy;
-    if (pack) {
-      count_launches(1);
-      if (launch_pack_u16(dY, T, N, lddy, reinterpret_cast<uint16_t *>(gs), ldn, c.sms, c.st) != cudaSuccess)
-        return GEMM_ERR_CUDA;
-      g = gs;
-      ldg = ldn;
-    }
+    const void *g = pack ? (const void *)gs : dY;
+    const int64_t ldg = pack ? ldn : lddy;
     CUtensorMap tx, tg, tout, tws;
     if (!bf16_box_map(&tx, xs, (uint64_t)K, (uint64_t)T, (uint64_t)ldk, 64, kBK) ||
         !bf16_box_map(&tg, g, (uint64_t)N, (uint64_t)T, (uint64_t)ldg, 64, kBK))
       return GEMM_ERR_CUDA;
     tout = tws = tx;
     // C through TMA where its base, pitch and row ends are multiples of 16
-    // bytes (a clipped TMA store would write into the row's padding)
+    // bytes (a clipped TMA store would write into the row's padding) and no
+    // base is added; with one in 16-byte pieces where both allow it
     const int64_t es = bf ? 2 : 4;
-    p.tc.out_tma = kOutDirect;
-    if (tma_store_enabled() && aligned_to(dW, 16) && ldw * es % 16 == 0 && cols * es % 16 == 0) {
+    const bool c16 = aligned_to(dW, 16) && ldw * es % 16 == 0 && cols * es % 16 == 0;
+    const bool base16 = base && aligned_to(base, 16) && ldbase * es % 16 == 0;
+    p.tc.out_tma = kBlockElements;
+    if (c16 && !base && tma_store_enabled()) {
       if (!float_out_map(&tout, bf, dW, (uint64_t)cols, (uint64_t)M, (uint64_t)ldw, 1)) return GEMM_ERR_CUDA;
-      p.tc.out_tma = kOutTmaC;
+      p.tc.out_tma = kBlockTma;
+    } else if (c16 && (!base || base16)) {
+      p.tc.out_tma = kBlockPieces;
     }
     p.tc.tiles_m = pl.tiles_m;
     p.tc.tiles_n = pl.tiles_n;

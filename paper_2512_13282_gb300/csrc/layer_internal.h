@@ -68,6 +68,17 @@ cudaError_t launch_q8_save(const void *x, int64_t ldx, int x_type, int64_t rows,
 cudaError_t launch_q8_restore(const Q8Ref &ck, void *x, int64_t ldx, int x_type, int64_t rows, int64_t cols,
                               cudaStream_t st);
 
+// Operands of the weight gradient that TMA cannot read as they are, in one
+// launch: the checkpoint restored to bf16 (T x K at x, pitch ldx) and, where g
+// is not null, the T x N bf16 matrix g copied to gx (pitch ldgx); x and gx have
+// 16-byte aligned rows, the sources any alignment (wgrad.cu).
+cudaError_t launch_wgrad_stage(const Q8Ref &ck, int64_t T, int64_t K, uint16_t *x, int64_t ldx, const uint16_t *g,
+                               int64_t ldg, int64_t N, uint16_t *gx, int64_t ldgx, cudaStream_t st);
+
+// How the epilogue of the weight gradient writes blocks of 32 x 32 results
+// (TcParams::out_tma): TMA stores, 16-byte pieces along rows, or elements.
+enum BlockAccess : int { kBlockTma = 0, kBlockPieces = 1, kBlockElements = 2 };
+
 // C[m][n] = base[m][n] + sum_t A[t][m] * B[t][n] with bf16 A (T x M) and B
 // (T x N), both read with their rows (t) outermost (wgrad.cu).
 struct WgradParams {

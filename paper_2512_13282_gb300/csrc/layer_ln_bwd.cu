@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(ring_threads(NV), NV == 1 ? 8 : 1)
       break;
     }
     if (threadIdx.x == 0 && i > 0 && filled < mine) fill(filled++);  // the slot of row i - 1
-    const float2 s = sum_over_warps(sm[i & 1], T >> 5);
+    const float2 s = sum_over_warps<ring_threads(NV) / 32>(sm[i & 1]);
     const float2 ga = both(-s.x * inv_n * st.rstd), gx = both(-s.y * inv_n * st.rstd), rstd = both(st.rstd);
     TDX *dx = static_cast<TDX *>(p.dx) + row_of(i) * p.lddx;
 #pragma unroll

@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(kAnyThreads) ln_forward_any_kernel(const LnFor
       const float d = load_value<TX>(x, c) - mean;
       v = fmaf(d, d, v);
     }
-    const float rstd = 1.0f / sqrtf(block_sum2(v, 0.f, sm, 1).x * inv_n + p.eps);
+    const float rstd = rsqrtf(block_sum2(v, 0.f, sm, 1).x * inv_n + p.eps);
     if (threadIdx.x == 0) {
       if (p.mean) p.mean[r] = mean;
       if (p.rstd) p.rstd[r] = rstd;
@@ -58,29 +58,57 @@ __global__ void __launch_bounds__(kAnyThreads) ln_forward_any_kernel(const LnFor
 }
 
 
-// The checkpoint of a lane's 8 consecutive results (the first n of them; four
-// lanes hold a block) as y's type holds them.  All lanes of the warp call it.
+// A lane's 8 consecutive results (the first n of them), rounded to y's type
+// and stored, and their part of the checkpoint of y as stored (four lanes hold
+// a block).  All lanes of the warp call it.
 template <typename TY>
-__device__ __forceinline__ void save_eighth(const Q8Ref &ck, int64_t r, int c, const float (&y)[8], int n) {
-  float o[8];
-  uint32_t top = 0;
+__device__ __forceinline__ void store_eighth(TY *y, const Q8Ref &ck, int64_t r, int c, const float2 (&v)[4], int n) {
+  float2 o[4];
+  uint32_t top;
+  if constexpr (sizeof(TY) == 2) {
+    uint32_t h[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    o[i] = i < n ? as_stored<TY>(y[i]) : 0.f;
-    top = max(top, __float_as_uint(o[i]) & 0x7FFFFFFFu);
+    for (int j = 0; j < 4; ++j) h[j] = pack_bf16x2(v[j].x, v[j].y);
+    if (n == 8) {
+      *reinterpret_cast<uint4 *>(y + c) = make_uint4(h[0], h[1], h[2], h[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (i < n)
+          reinterpret_cast<uint16_t *>(y)[c + i] = (uint16_t)(h[i / 2] >> (16 * (i & 1)));
+        else
+          h[i / 2] &= (i & 1) ? 0x0000FFFFu : 0xFFFF0000u;  // not in the block
+      }
+    }
+    if (!ck.q) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      o[j] = make_float2(__uint_as_float(h[j] << 16), __uint_as_float(h[j] & 0xFFFF0000u));
+    top = max_magnitude_bf16<4>(h);
+  } else {
+    float w[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[2 * j] = v[j].x, w[2 * j + 1] = v[j].y;
+    store_chunk<TY, 8>(y, c, w, n);
+    if (!ck.q) return;
+    top = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      o[j] = make_float2(2 * j < n ? v[j].x : 0.f, 2 * j + 1 < n ? v[j].y : 0.f);
+      top = max(top, max(__float_as_uint(o[j].x) & 0x7FFFFFFFu, __float_as_uint(o[j].y) & 0x7FFFFFFFu));
+    }
   }
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   const uint32_t e = q8_exponent(top);
-  const float inverse = q8_inverse(e);
-  const uint32_t lo = q8_pack4(o, inverse, e), hi = q8_pack4(o + 4, inverse, e);
+  const uint2 w = q8_pack8(o, e);
   int8_t *q = ck.q + r * ck.ldq + c;
   if (n == 8) {
-    *reinterpret_cast<uint2 *>(q) = make_uint2(lo, hi);
+    *reinterpret_cast<uint2 *>(q) = w;
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (i < n) q[i] = (int8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
+      if (i < n) q[i] = (int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
   }
   if (n > 0 && (c & 31) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
 }
@@ -155,7 +183,7 @@ __global__ void __launch_bounds__(kMaxThreads, NV == 1 ? 2 : 1) ln_forward_kerne
         if (i < n) v = fmaf(x[k * V + i], x[k * V + i], v);
       }
     }
-    const float rstd = 1.0f / sqrtf(block_sum(v, sm[1]) * inv_n + p.eps);
+    const float rstd = rsqrtf(block_sum(v, sm[1]) * inv_n + p.eps);
     if (threadIdx.x == 0) {
       if (p.mean) p.mean[r] = mean;
       if (p.rstd) p.rstd[r] = rstd;
@@ -171,11 +199,12 @@ __global__ void __launch_bounds__(kMaxThreads, NV == 1 ? 2 : 1) ln_forward_kerne
         const float b = kKeep ? beta[k * V + i] : i < n ? load_param(p.beta, p.param_type, c + i, 0.f) : 0.f;
         o[i] = fmaf(x[k * V + i] * rstd, g, b);
       }
-      store_chunk<TY, V>(y, c, o, n);
-      if (!p.ck.q) continue;
       if constexpr (V == 8) {
-        save_eighth<TY>(p.ck, r, c, o, n);
+        const float2 w[4] = {{o[0], o[1]}, {o[2], o[3]}, {o[4], o[5]}, {o[6], o[7]}};
+        store_eighth<TY>(y, p.ck, r, c, w, n);
       } else {
+        store_chunk<TY, V>(y, c, o, n);
+        if (!p.ck.q) continue;
         o[0] = n > 0 ? as_stored<TY>(o[0]) : 0.f;
         const uint32_t e = q8_exponent(__reduce_max_sync(0xffffffffu, __float_as_uint(o[0]) & 0x7FFFFFFFu));
         if (n > 0) p.ck.q[r * p.ck.ldq + c] = (int8_t)q8_quantise(o[0], q8_inverse(e), e);
@@ -249,15 +278,15 @@ __global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 &&
     float2 x[NV * 4], s2 = both(0.f);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      if (ok && col(v) < p.cols) {
-        Chunk<TX, 8> raw;
-        raw.load(slots + use.slot * x_bytes, col(v));
+      Chunk<TX, 8> raw;  // past the row's end: column 0, left out of the sums
+      raw.load(slots + use.slot * x_bytes, col(v) < p.cols ? col(v) : 0);
+      float2 t = both(0.f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          x[v * 4 + j] = raw.get2(j);
-          s2 = add2(s2, x[v * 4 + j]);
-        }
+      for (int j = 0; j < 4; ++j) {
+        x[v * 4 + j] = raw.get2(j);
+        t = add2(t, x[v * 4 + j]);
       }
+      s2 = add2(s2, col(v) < p.cols ? t : both(0.f));
     }
     const float s = warp_sum(s2.x + s2.y);
     if (lane == 0) sm[0][warp] = s;
@@ -267,22 +296,22 @@ __global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 &&
       break;
     }
     if (threadIdx.x == 0 && filled < mine) fill(filled++);  // this row's slot
-    const float mean = sum_over_warps(sm[0], T >> 5) * inv_n;
+    const float mean = sum_over_warps<THREADS / 32>(sm[0]) * inv_n;
     float2 v2 = both(0.f);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      if (col(v) < p.cols) {
+      float2 t = both(0.f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          x[v * 4 + j] = add2(x[v * 4 + j], both(-mean));
-          v2 = fma2(x[v * 4 + j], x[v * 4 + j], v2);
-        }
+      for (int j = 0; j < 4; ++j) {
+        x[v * 4 + j] = add2(x[v * 4 + j], both(-mean));
+        t = fma2(x[v * 4 + j], x[v * 4 + j], t);
       }
+      v2 = add2(v2, col(v) < p.cols ? t : both(0.f));
     }
     const float var = warp_sum(v2.x + v2.y);
     if (lane == 0) sm[1][warp] = var;
     __syncthreads();
-    const float rstd = 1.0f / sqrtf(sum_over_warps(sm[1], T >> 5) * inv_n + p.eps);
+    const float rstd = rsqrtf(sum_over_warps<THREADS / 32>(sm[1]) * inv_n + p.eps);
     if (threadIdx.x == 0) {
       if (p.mean) p.mean[r] = mean;
       if (p.rstd) p.rstd[r] = rstd;
@@ -292,17 +321,14 @@ __global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 &&
     for (int v = 0; v < NV; ++v) {
       const int c = col(v);
       const bool in = c < p.cols;
-      float o[8];
+      float2 o[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float2 g = kKeep ? gamma[v * 4 + j] : in ? param(p.gamma, c + 2 * j, 1.f) : both(0.f);
         const float2 b = kKeep ? beta[v * 4 + j] : in ? param(p.beta, c + 2 * j, 0.f) : both(0.f);
-        const float2 w = fma2(mul2(x[v * 4 + j], both(rstd)), g, b);
-        o[2 * j] = w.x;
-        o[2 * j + 1] = w.y;
+        o[j] = fma2(mul2(x[v * 4 + j], both(rstd)), g, b);
       }
-      if (in) store_chunk<TY, 8>(y, c, o, 8);
-      if (p.ck.q) save_eighth<TY>(p.ck, r, c, o, in ? 8 : 0);
+      store_eighth<TY>(y, p.ck, r, c, o, in ? 8 : 0);
     }
   }
   if (!ok && threadIdx.x == 0) ring_drain(bar0, stages, use, filled - done);

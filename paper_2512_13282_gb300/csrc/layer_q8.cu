@@ -48,19 +48,20 @@ __global__ void __launch_bounds__(kQ8Threads)
       raw.load(row, c);
     else
       raw.load_part(row, c, n);
-    float v[16];
     uint32_t top = 0;
+    if constexpr (sizeof(TX) == 2) {
+      top = max_magnitude_bf16<8>(raw.w);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      v[i] = raw.get(i);
-      top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+      for (int i = 0; i < 16; ++i) top = max(top, raw.w[i] & 0x7FFFFFFFu);
     }
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     const uint32_t e = q8_exponent(top);
-    const float inverse = q8_inverse(e);
-    uint32_t w[4];
+    float2 lo[4], hi[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = q8_pack4(v + 4 * i, inverse, e);
+    for (int j = 0; j < 4; ++j) lo[j] = raw.get2(j), hi[j] = raw.get2(4 + j);
+    const uint2 wl = q8_pack8(lo, e), wh = q8_pack8(hi, e);
+    const uint32_t w[4] = {wl.x, wl.y, wh.x, wh.y};
     int8_t *q = ck.q + r * ck.ldq + c;
     if (VEC && n == 16) {
       *reinterpret_cast<uint4 *>(q) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -71,13 +72,6 @@ __global__ void __launch_bounds__(kQ8Threads)
     }
     if (live && (h & 1) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
   }
-}
-
-// Scaling by 2^E in bf16 arithmetic is exact: a byte has at most 8
-// significant bits, and no product with E >= -126 is subnormal.
-__device__ __forceinline__ uint32_t scale_bf16x2(uint32_t v, __nv_bfloat162 s) {
-  const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&v), s);
-  return *reinterpret_cast<const uint32_t *>(&p);
 }
 
 template <typename TX, bool VEC>

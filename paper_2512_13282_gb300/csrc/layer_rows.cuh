@@ -13,6 +13,32 @@ struct Q8 {     // element type: a value held in a checkpoint, as its byte
   int8_t byte;
 };
 
+// Pairs of float32 operations in one instruction each; both halves round as
+// the scalar ones do.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(d)
+      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)),
+        "l"(*reinterpret_cast<unsigned long long *>(&c)));
+  return *reinterpret_cast<float2 *>(&d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(d)
+      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
+  return *reinterpret_cast<float2 *>(&d);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(d)
+      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
+  return *reinterpret_cast<float2 *>(&d);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
 // 2^(e - 127) of a block exponent: e = 255 stands for NaN.
 __device__ __forceinline__ float q8_scale(uint32_t e) {
   return __uint_as_float(e == 255u ? 0x7FC00000u : e << 23);
@@ -33,6 +59,24 @@ __device__ __forceinline__ uint32_t q8_exponent(uint32_t top) {
 // rounding; 0 for a block of NaN, whose bytes are 0.  E lies in -126 .. 122.
 __device__ __forceinline__ float q8_inverse(uint32_t e) { return __uint_as_float((254u - e) << 23); }
 
+// Float bits of the largest magnitude among 2 * N bf16 values, two to a word;
+// a NaN if there is one.
+template <int N>
+__device__ __forceinline__ uint32_t max_magnitude_bf16(const uint32_t (&w)[N]) {
+  __nv_bfloat162 m[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t a = w[i] & 0x7FFF7FFFu;
+    m[i] = *reinterpret_cast<const __nv_bfloat162 *>(&a);
+  }
+#pragma unroll
+  for (int n = N; n > 1; n /= 2)
+#pragma unroll
+    for (int i = 0; i < n / 2; ++i) m[i] = __hmax2_nan(m[i], m[i + n / 2]);
+  const uint32_t t = *reinterpret_cast<const uint32_t *>(m);
+  return max(t << 16, t & 0xFFFF0000u);
+}
+
 // round_half_even(x * inverse) of a finite block; 0 where the block holds a
 // NaN or an infinity; limited to 63 at the largest exponent (E = 122), where
 // 64 * 2^122 would be past float32.
@@ -42,21 +86,33 @@ __device__ __forceinline__ int q8_quantise(float x, float inverse, uint32_t e) {
   return v;
 }
 
-// The same for four values, packed (v[0] in the low byte).  Added to 1.5 *
-// 2^23, where a float's unit in the last place is 1, the exact product
-// x * inverse is rounded to an integer, ties to even, which is then the low
-// byte of the sum: no conversion instructions (a quarter of the rate).
-__device__ __forceinline__ uint32_t q8_pack4(const float *v, float inverse, uint32_t e) {
-  constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23
-  uint32_t b[4];
+// The same for eight values of a block below the largest exponent, packed
+// (v[0].x in the low byte of `lo`).  Added to 1.5 * 2^23, where a float's unit
+// in the last place is 1, the exact product x * inverse is rounded to an
+// integer, ties to even, which is then the low byte of the sum: no conversion
+// instructions (a quarter of the rate).
+__device__ __forceinline__ uint2 q8_pack8(const float2 (&v)[4], float inverse) {
+  const float2 scale = both(inverse), magic = both(12582912.0f);
+  uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(fmaf(v[i], inverse, kMagic));
-  uint32_t w = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+  for (int i = 0; i < 2; ++i) {
+    const float2 a = fma2(v[2 * i], scale, magic), b = fma2(v[2 * i + 1], scale, magic);
+    const uint32_t lo = __byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040);
+    const uint32_t hi = __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040);
+    w[i] = __byte_perm(lo, hi, 0x5410);
+  }
+  return make_uint2(w[0], w[1]);
+}
+// ... and of any block: zeros where e = 255; at e = 249, where no value is past
+// 64, bytes of 64 (0x40) become 63 and bytes of -64 (0xC0) -63, four at a time.
+__device__ __forceinline__ uint2 q8_pack8(const float2 (&v)[4], uint32_t e) {
+  uint2 w = q8_pack8(v, q8_inverse(e));
   if (e >= 249u) {
-    w = 0;
     if (e == 249u) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w |= (uint32_t)(q8_quantise(v[i], inverse, e) & 0xFF) << (8 * i);
+      w.x += (__vcmpeq4(w.x, 0xC0C0C0C0u) & 0x01010101u) - (__vcmpeq4(w.x, 0x40404040u) & 0x01010101u);
+      w.y += (__vcmpeq4(w.y, 0xC0C0C0C0u) & 0x01010101u) - (__vcmpeq4(w.y, 0x40404040u) & 0x01010101u);
+    } else {
+      w = make_uint2(0, 0);
     }
   }
   return w;
@@ -66,6 +122,13 @@ __device__ __forceinline__ uint32_t q8_pack4(const float *v, float inverse, uint
 __device__ __forceinline__ float s8_to_float(uint32_t w, int i) {
   const uint32_t u = w ^ 0x80808080u;
   return __fsub_rn(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7650 + i)), 8388736.0f);
+}
+
+// Scaling by 2^E in bf16 arithmetic is exact: a byte has at most 8
+// significant bits, and no product with E >= -126 is subnormal.
+__device__ __forceinline__ uint32_t scale_bf16x2(uint32_t v, __nv_bfloat162 s) {
+  const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&v), s);
+  return *reinterpret_cast<const uint32_t *>(&p);
 }
 
 template <typename T>
@@ -181,32 +244,6 @@ __device__ __forceinline__ float load_param(const void *p, int type, int c, floa
   return type == GEMM_TYPE_F32 ? static_cast<const float *>(p)[c] : __bfloat162float(static_cast<const bf16 *>(p)[c]);
 }
 
-// Pairs of float32 operations in one instruction each; both halves round as
-// the scalar ones do.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  unsigned long long d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;"
-      : "=l"(d)
-      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)),
-        "l"(*reinterpret_cast<unsigned long long *>(&c)));
-  return *reinterpret_cast<float2 *>(&d);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  unsigned long long d;
-  asm("add.rn.f32x2 %0, %1, %2;"
-      : "=l"(d)
-      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
-  return *reinterpret_cast<float2 *>(&d);
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  unsigned long long d;
-  asm("mul.rn.f32x2 %0, %1, %2;"
-      : "=l"(d)
-      : "l"(*reinterpret_cast<unsigned long long *>(&a)), "l"(*reinterpret_cast<unsigned long long *>(&b)));
-  return *reinterpret_cast<float2 *>(&d);
-}
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
-
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -239,20 +276,24 @@ __device__ __forceinline__ float2 block_sum2(float a, float b, float2 (*sm)[32],
 }
 
 // The second half of a block-wide sum, after the barrier: the sum of the
-// warps' values sm[0 .. warps), padded with zeros to a multiple of four, read
-// by broadcast (cheaper, and sooner done, than another tree of shuffles).
-__device__ __forceinline__ float2 sum_over_warps(const float2 *sm, int warps) {
-  float2 s = make_float2(0.f, 0.f), t = s;
-  for (int w = 0; w < warps; w += 4) {
+// values of up to WARPS warps (a multiple of four; absent ones zero), read by
+// broadcast (cheaper, and sooner done, than another tree of shuffles).
+template <int WARPS>
+__device__ __forceinline__ float2 sum_over_warps(const float2 *sm) {
+  float2 s = both(0.f), t = s;
+#pragma unroll
+  for (int w = 0; w < WARPS; w += 4) {
     const float4 a = *reinterpret_cast<const float4 *>(sm + w), b = *reinterpret_cast<const float4 *>(sm + w + 2);
     s = add2(s, add2(make_float2(a.x, a.y), make_float2(a.z, a.w)));
     t = add2(t, add2(make_float2(b.x, b.y), make_float2(b.z, b.w)));
   }
   return add2(s, t);
 }
-__device__ __forceinline__ float sum_over_warps(const float *sm, int warps) {
+template <int WARPS>
+__device__ __forceinline__ float sum_over_warps(const float *sm) {
   float s = 0.f;
-  for (int w = 0; w < warps; w += 4) {
+#pragma unroll
+  for (int w = 0; w < WARPS; w += 4) {
     const float4 a = *reinterpret_cast<const float4 *>(sm + w);
     s += (a.x + a.y) + (a.z + a.w);
   }

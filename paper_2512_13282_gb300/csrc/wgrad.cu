@@ -1,5 +1,6 @@
 // wgrad.cu -- planning and launches of the weight gradient's tensor-core
 // kernel (wgrad_tc.cuh), and the reduction of its split tail.
+#include "layer_rows.cuh"
 #include "wgrad_tc.cuh"
 
 namespace gb300 {
@@ -18,7 +19,8 @@ template <int BN, bool PAIR>
 cudaError_t launch_tile(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const CUtensorMap &ws,
                         const WgradParams &p, int grid, cudaStream_t st) {
   using Cfg = WgCfg<BN, PAIR>;
-  auto kern = wgrad_kernel<BN, PAIR>;
+  const bool slabs = p.tc.num_kb > p.tc.slab_kb;
+  auto kern = slabs ? wgrad_kernel<BN, PAIR, true> : wgrad_kernel<BN, PAIR, false>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
   if (e != cudaSuccess) return e;
   return launch_ex(kern, dim3((unsigned)grid), dim3(kWgThreads), Cfg::kSmemBytes, st, PAIR ? 2 : 1, a, b, out, ws, p);
@@ -64,6 +66,72 @@ __global__ void __launch_bounds__(256) wgrad_reduce_kernel(const WgradParams wp,
       if (wp.base) r += static_cast<const float *>(wp.base)[row * wp.ldbase + col + i];
       static_cast<float *>(p.C)[row * p.ldc + col + i] = r;
     }
+  }
+}
+
+// 32-bit words that hold the bytes from p on, p any address: BYTES / 4 of
+// them, from aligned words (one more than that is read where p is not
+// aligned: up to 3 bytes before p and after the last byte asked for).
+template <int BYTES>
+__device__ __forceinline__ void load_shifted(const void *p, uint32_t (&w)[BYTES / 4]) {
+  const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(p) & 3u;
+  const uint32_t *a = reinterpret_cast<const uint32_t *>(reinterpret_cast<uintptr_t>(p) - off);
+  uint32_t v[BYTES / 4 + 1];
+#pragma unroll
+  for (int i = 0; i < BYTES / 4; ++i) v[i] = a[i];
+  v[BYTES / 4] = off ? a[BYTES / 4] : 0;
+#pragma unroll
+  for (int i = 0; i < BYTES / 4; ++i) w[i] = __funnelshift_r(v[i], v[i + 1], off * 8);
+}
+
+// A thread writes 8 values (16 bytes) of a row of the restored X or, past
+// them, of the copied gradient.  The source's words are read aligned and
+// shifted into place; within 8 values of a row's ends, where such a word may
+// reach outside the matrix, its elements are read one by one.
+__global__ void __launch_bounds__(256)
+    wgrad_stage_kernel(Q8Ref ck, int64_t T, int64_t K, uint16_t *x, int64_t ldx, const uint16_t *g, int64_t ldg, int64_t N,
+                       uint16_t *gx, int64_t ldgx) {
+  griddep_launch_dependents();
+  griddep_wait();
+  const int64_t xe = ldx / 8, ge = g ? ldgx / 8 : 0, x_items = T * xe, items = x_items + T * ge;
+  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < items; t += (int64_t)gridDim.x * 256) {
+    const bool is_x = t < x_items;
+    const int64_t u = is_x ? t : t - x_items, per = is_x ? xe : ge;
+    const int64_t r = u <= 0xFFFFFFFFll ? (int64_t)((uint32_t)u / (uint32_t)per) : u / per;
+    const int64_t c = (u - r * per) * 8, cols = is_x ? K : N;
+    const bool inside = c >= 8 && c + 16 <= cols;
+    const int n = (int)min((int64_t)8, cols - c);
+    uint32_t o[4];
+    if (is_x) {
+      const int8_t *src = ck.q + r * ck.ldq + c;
+      uint32_t w[2] = {0, 0};
+      if (inside) {
+        load_shifted<8>(src, w);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < n) w[i / 4] |= (uint32_t)(uint8_t)src[i] << (8 * (i & 3));
+      }
+      const __nv_bfloat162 s = __float2bfloat162_rn(q8_scale(ck.e[r * ck.lde + (c >> 5)]));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        s8x4_to_bf16x4(w[i], o[2 * i], o[2 * i + 1]);
+        o[2 * i] = scale_bf16x2(o[2 * i], s);
+        o[2 * i + 1] = scale_bf16x2(o[2 * i + 1], s);
+      }
+    } else {
+      const uint16_t *src = g + r * ldg + c;
+      if (inside) {
+        load_shifted<16>(src, o);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < n) o[i / 2] |= (uint32_t)src[i] << (16 * (i & 1));
+      }
+    }
+    *reinterpret_cast<uint4 *>((is_x ? x + r * ldx : gx + r * ldgx) + c) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
 
@@ -151,6 +219,13 @@ cudaError_t launch_wgrad(const WgradTile &tile, const CUtensorMap &a, const CUte
     return launch_tile<128, false>(a, b, out, ws, q, grid, st);
   }
   return cudaErrorInvalidValue;
+}
+
+cudaError_t launch_wgrad_stage(const Q8Ref &ck, int64_t T, int64_t K, uint16_t *x, int64_t ldx, const uint16_t *g,
+                               int64_t ldg, int64_t N, uint16_t *gx, int64_t ldgx, cudaStream_t st) {
+  const int64_t blocks = ceil_div64(T * (ldx / 8 + (g ? ldgx / 8 : 0)), 256);
+  return launch_ex(wgrad_stage_kernel, dim3((unsigned)(blocks < (1 << 30) ? blocks : (1 << 30))), dim3(256), 0, st, 1, ck,
+                   T, K, x, ldx, g, ldg, N, gx, ldgx);
 }
 
 cudaError_t launch_wgrad_base(const WgradParams &p, int sms, cudaStream_t st) {

@@ -25,8 +25,25 @@
 namespace gb300 {
 
 constexpr int kWgEpiWarps = 8;
-constexpr int kWgThreads = (2 + kWgEpiWarps) * 32;
+// Warps 0 (TMA) and 1 (MMA) of the first warpgroup work, the epilogue is the
+// other two warpgroups.
+constexpr int kWgThreads = (4 + kWgEpiWarps) * 32;
 constexpr uint32_t kWgBoxBytes = 64 * kBK * 2;  // one 64-column x 64-token box
+
+// Registers a thread when the sums of slabs are kept in them: the block is
+// launched with 384 x 168; the first warpgroup gives up all but 40 of its own,
+// and the epilogue's threads (128 sums each) take them: 128 x 40 + 256 x 232 =
+// 384 x 168.
+constexpr int kWgLaunchRegs = 168, kWgIssueRegs = 40, kWgEpiRegs = 232;
+static_assert(128 * kWgIssueRegs + kWgEpiWarps * 32 * kWgEpiRegs <= kWgThreads * kWgLaunchRegs, "the shares fit");
+template <int N>
+__device__ __forceinline__ void regs_give() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_take() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
 
 template <int BN, bool PAIR>
 struct WgCfg {
@@ -47,51 +64,110 @@ struct WgCfg {
   static_assert(kTmemCols <= 512, "TMEM has 512 columns");
 };
 
-// 32 columns of one row of base added to v; clipped at column N.  base may be
-// the result itself, so these are plain loads; this thread's block of C is
-// written after them.
-__device__ __forceinline__ void add_base32(const WgradParams &p, int64_t row, int col, uint32_t (&v)[32]) {
+// The way a 32 x 32 block of results leaves an epilogue warp where it does not
+// go through TMA (a base to add, or rows TMA cannot take): the block is turned
+// in the warp's shared memory, so that the lanes read base and write C along
+// rows.  A lane's own row would be 32 lines touched by every access of the
+// warp; along rows it is four (16-byte pieces) or one or two.
+
+// Base's values that this lane will add to the block at (y0, x), fetched ahead:
+// 16-byte pieces only (kBlockPieces; the block's rows and columns come in whole
+// pieces there).  b[8] words a lane for bf16 pieces use the first half.
+__device__ __forceinline__ void fetch_base(const WgradParams &p, int64_t y0, int x, int lane, uint4 (&b)[8]) {
   if (p.out_bf16) {
-    const uint16_t *src = static_cast<const uint16_t *>(p.base) + row * p.ldbase + col;
-    if (col + 32 <= p.tc.N && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
+    const int c = x + (lane & 3) * 8;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint4 w = reinterpret_cast<const uint4 *>(src)[i];
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[8 * i + 2 * j] = __float_as_uint(__uint_as_float(v[8 * i + 2 * j]) + __uint_as_float(u[j] << 16));
-          v[8 * i + 2 * j + 1] =
-              __float_as_uint(__uint_as_float(v[8 * i + 2 * j + 1]) + __uint_as_float(u[j] & 0xFFFF0000u));
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (col + i < p.tc.N)
-          v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float((uint32_t)src[i] << 16));
+    for (int i = 0; i < 4; ++i) {
+      const int64_t r = y0 + i * 8 + (lane >> 2);
+      if (r < p.tc.M && c < p.tc.N)
+        b[i] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.base) + r * p.ldbase + c);
     }
   } else {
-    const float *src = static_cast<const float *>(p.base) + row * p.ldbase + col;
-    if (col + 32 <= p.tc.N && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
+    const int c = x + (lane & 7) * 4;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float4 w = reinterpret_cast<const float4 *>(src)[i];
-        v[4 * i] = __float_as_uint(__uint_as_float(v[4 * i]) + w.x);
-        v[4 * i + 1] = __float_as_uint(__uint_as_float(v[4 * i + 1]) + w.y);
-        v[4 * i + 2] = __float_as_uint(__uint_as_float(v[4 * i + 2]) + w.z);
-        v[4 * i + 3] = __float_as_uint(__uint_as_float(v[4 * i + 3]) + w.w);
+    for (int i = 0; i < 8; ++i) {
+      const int64_t r = y0 + i * 4 + (lane >> 3);
+      if (r < p.tc.M && c < p.tc.N)
+        b[i] = *reinterpret_cast<const uint4 *>(static_cast<const float *>(p.base) + r * p.ldbase + c);
+    }
+  }
+}
+
+__device__ __forceinline__ float4 as_float4(uint4 v) {
+  return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+}
+__device__ __forceinline__ float4 operator+(float4 a, float4 b) {
+  return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+}
+
+// Block of sums v (lane = row, 32 columns) at (y0, x) of C, base added,
+// rounded once and stored along rows.  AHEAD: b is as fetch_base left it; else
+// base is fetched here, once v's registers are free.
+template <bool AHEAD>
+__device__ __forceinline__ void store_block(const WgradParams &p, uint32_t buf, int lane, const uint32_t (&v)[32],
+                                            uint4 (&b)[8], int64_t y0, int x, bool pieces) {
+  __syncwarp();  // the block before has been read
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    st_shared_v4(buf + lane * 128 + ((j ^ (lane & 7)) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+  __syncwarp();
+  if (!AHEAD && pieces && p.base) fetch_base(p, y0, x, lane, b);
+  const auto piece = [&](int row, int j) { return as_float4(ld_shared_v4(buf + row * 128 + ((j ^ (row & 7)) << 4))); };
+  if (pieces && p.out_bf16) {
+    const int j = lane & 3, c = x + j * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = i * 8 + (lane >> 2);
+      const int64_t r = y0 + row;
+      if (r < p.tc.M && c < p.tc.N) {
+        float4 lo = piece(row, 2 * j), hi = piece(row, 2 * j + 1);
+        if (p.base) {
+          lo = lo + make_float4(__uint_as_float(b[i].x << 16), __uint_as_float(b[i].x & 0xFFFF0000u),
+                                __uint_as_float(b[i].y << 16), __uint_as_float(b[i].y & 0xFFFF0000u));
+          hi = hi + make_float4(__uint_as_float(b[i].z << 16), __uint_as_float(b[i].z & 0xFFFF0000u),
+                                __uint_as_float(b[i].w << 16), __uint_as_float(b[i].w & 0xFFFF0000u));
+        }
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.tc.C) + r * p.tc.ldc + c) =
+            make_uint4(pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y),
+                       pack_bf16x2(hi.z, hi.w));
       }
-    } else {
+    }
+  } else if (pieces) {
+    const int j = lane & 7, c = x + j * 4;
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (col + i < p.tc.N) v[i] = __float_as_uint(__uint_as_float(v[i]) + src[i]);
+    for (int i = 0; i < 8; ++i) {
+      const int row = i * 4 + (lane >> 3);
+      const int64_t r = y0 + row;
+      if (r < p.tc.M && c < p.tc.N) {
+        float4 f = piece(row, j);
+        if (p.base) f = f + as_float4(b[i]);
+        *reinterpret_cast<float4 *>(static_cast<float *>(p.tc.C) + r * p.tc.ldc + c) = f;
+      }
+    }
+  } else {  // lane = column
+    const int c = x + lane;
+    const int rows = (int)min((int64_t)32, p.tc.M - y0);
+    if (c < p.tc.N) {
+#pragma unroll 8
+      for (int row = 0; row < rows; ++row) {
+        const int64_t r = y0 + row;
+        float f = __uint_as_float(ld_shared_u32(buf + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4));
+        if (p.out_bf16) {
+          if (p.base) f += __uint_as_float((uint32_t) static_cast<const uint16_t *>(p.base)[r * p.ldbase + c] << 16);
+          static_cast<__nv_bfloat16 *>(p.tc.C)[r * p.tc.ldc + c] = __float2bfloat16_rn(f);
+        } else {
+          if (p.base) f += static_cast<const float *>(p.base)[r * p.ldbase + c];
+          static_cast<float *>(p.tc.C)[r * p.tc.ldc + c] = f;
+        }
+      }
     }
   }
 }
 
 // Launch with cluster dimensions (2,1,1) and an even grid when PAIR.
-template <int BN, bool PAIR>
+// SLABS: the sums of several slabs are added in registers (the reduction is
+// longer than one slab); else every unit is one slab.
+template <int BN, bool PAIR, bool SLABS>
 __global__ void __launch_bounds__(kWgThreads, 1)
     wgrad_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                  const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ CUtensorMap tmWs,
@@ -136,7 +212,7 @@ __global__ void __launch_bounds__(kWgThreads, 1)
     fence_mbar_init();
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
-    if (p.out_tma != kOutDirect) tma_prefetch_desc(&tmOut);
+    if (p.out_tma == kBlockTma) tma_prefetch_desc(&tmOut);
     if (p.tail_splits > 0) tma_prefetch_desc(&tmWs);
   }
   __syncwarp();
@@ -160,150 +236,150 @@ __global__ void __launch_bounds__(kWgThreads, 1)
   const int num_units = tc_num_units(p);
   constexpr uint64_t kDrainNs = 200ull * 1000 * 1000;
 
-  if (warp == 0) {
-    // ------------------------------------------------------ TMA producer
-    if (lane == 0) {
-      uint32_t g = 0;
-      bool ok = true;
-      for (int u = first_unit; ok && u < num_units; u += unit_step) {
-        const Unit w = decode_unit(p, u);
-        const int m0 = w.tm * Cfg::kTileM + (int)rank * kBM;
-        const int n0 = w.tn * BN + (int)rank * Cfg::kCtaN;
-        for (int kb = w.kb0; kb < w.kb1; ++kb) {
-          const uint32_t s = g % STAGES, ph = (g / STAGES) & 1u;
-          if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.err, p.wait_limit_ns)) {
-            ok = false;
-            break;
-          }
-          if (leader) mbar_arrive_expect_tx(full_bar(s), (PAIR ? 2 : 1) * Cfg::kStageBytes);
-          const uint32_t a_dst = sA + s * kABytes, b_dst = sB + s * Cfg::kBBytes;
-          if constexpr (PAIR) {
-            const uint32_t fb = mapa_shared(full_bar(s), 0);
-#pragma unroll
-            for (int j = 0; j < kBM / 64; ++j)
-              tma_load_2d_pair(a_dst + j * kWgBoxBytes, &tmA, m0 + 64 * j, kb * kBK, fb);
-#pragma unroll
-            for (int j = 0; j < Cfg::kCtaN / 64; ++j)
-              tma_load_2d_pair(b_dst + j * kWgBoxBytes, &tmB, n0 + 64 * j, kb * kBK, fb);
-          } else {
-#pragma unroll
-            for (int j = 0; j < kBM / 64; ++j)
-              tma_load_2d(a_dst + j * kWgBoxBytes, &tmA, m0 + 64 * j, kb * kBK, full_bar(s));
-#pragma unroll
-            for (int j = 0; j < Cfg::kCtaN / 64; ++j)
-              tma_load_2d(b_dst + j * kWgBoxBytes, &tmB, n0 + 64 * j, kb * kBK, full_bar(s));
-          }
-          ++g;
-        }
-      }
-      // Every load has landed before the CTA may exit (the peer's loads
-      // complete on the leader's barriers: it waits until their stages have
-      // been released).
-      const uint32_t first = g > (uint32_t)STAGES ? g - STAGES : 0u;
-      for (uint32_t i = first; i < g; ++i)
-        mbar_wait_drain(leader ? full_bar(i % STAGES) : empty_bar(i % STAGES), (i / STAGES) & 1u, kDrainNs);
-    }
-    __syncwarp();
-  } else if (warp == 1) {
-    // ------------------------------------------------ MMA issuer (leader)
-    if (lane == 0 && leader) {
-      // both operands MN-major: bit 15 is A's, bit 16 B's
-      constexpr uint32_t idesc = idesc_bf16_f32(Cfg::kTileM, BN, true) | (1u << 15);
-      uint32_t g = 0, acc_cnt = 0;
-      bool ok = true;
-      for (int u = first_unit; ok && u < num_units; u += unit_step) {
-        const Unit w = decode_unit(p, u);
-        for (int kb_s = w.kb0; ok && kb_s < w.kb1; kb_s += p.slab_kb) {
-          const int kb_e = min(w.kb1, kb_s + p.slab_kb);
-          const uint32_t b = acc_cnt & 1u, aph = (acc_cnt >> 1) & 1u;
-          if (!mbar_wait(acce_bar(b), aph ^ 1u, abort_flag, p.err, p.wait_limit_ns)) {
-            ok = false;
-            break;
-          }
-          tc_fence_after_sync();
-          const uint32_t d_tmem = tmem_base + b * BN;
-          for (int kb = kb_s; kb < kb_e; ++kb) {
+  if (warp < 4) {
+    if constexpr (SLABS) regs_give<kWgIssueRegs>();
+    if (warp == 0) {
+      // ------------------------------------------------------ TMA producer
+      if (lane == 0) {
+        uint32_t g = 0;
+        bool ok = true;
+        for (int u = first_unit; ok && u < num_units; u += unit_step) {
+          const Unit w = decode_unit(p, u);
+          const int m0 = w.tm * Cfg::kTileM + (int)rank * kBM;
+          const int n0 = w.tn * BN + (int)rank * Cfg::kCtaN;
+          for (int kb = w.kb0; kb < w.kb1; ++kb) {
             const uint32_t s = g % STAGES, ph = (g / STAGES) & 1u;
-            if (!mbar_wait(full_bar(s), ph, abort_flag, p.err, p.wait_limit_ns)) {
+            if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.err, p.wait_limit_ns)) {
+              ok = false;
+              break;
+            }
+            if (leader) mbar_arrive_expect_tx(full_bar(s), (PAIR ? 2 : 1) * Cfg::kStageBytes);
+            const uint32_t a_dst = sA + s * kABytes, b_dst = sB + s * Cfg::kBBytes;
+            if constexpr (PAIR) {
+              const uint32_t fb = mapa_shared(full_bar(s), 0);
+#pragma unroll
+              for (int j = 0; j < kBM / 64; ++j)
+                tma_load_2d_pair(a_dst + j * kWgBoxBytes, &tmA, m0 + 64 * j, kb * kBK, fb);
+#pragma unroll
+              for (int j = 0; j < Cfg::kCtaN / 64; ++j)
+                tma_load_2d_pair(b_dst + j * kWgBoxBytes, &tmB, n0 + 64 * j, kb * kBK, fb);
+            } else {
+#pragma unroll
+              for (int j = 0; j < kBM / 64; ++j)
+                tma_load_2d(a_dst + j * kWgBoxBytes, &tmA, m0 + 64 * j, kb * kBK, full_bar(s));
+#pragma unroll
+              for (int j = 0; j < Cfg::kCtaN / 64; ++j)
+                tma_load_2d(b_dst + j * kWgBoxBytes, &tmB, n0 + 64 * j, kb * kBK, full_bar(s));
+            }
+            ++g;
+          }
+        }
+        // Every load has landed before the CTA may exit (the peer's loads
+        // complete on the leader's barriers: it waits until their stages have
+        // been released).
+        const uint32_t first = g > (uint32_t)STAGES ? g - STAGES : 0u;
+        for (uint32_t i = first; i < g; ++i)
+          mbar_wait_drain(leader ? full_bar(i % STAGES) : empty_bar(i % STAGES), (i / STAGES) & 1u, kDrainNs);
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      // ------------------------------------------------ MMA issuer (leader)
+      if (lane == 0 && leader) {
+        // both operands MN-major: bit 15 is A's, bit 16 B's
+        constexpr uint32_t idesc = idesc_bf16_f32(Cfg::kTileM, BN, true) | (1u << 15);
+        uint32_t g = 0, acc_cnt = 0;
+        bool ok = true;
+        for (int u = first_unit; ok && u < num_units; u += unit_step) {
+          const Unit w = decode_unit(p, u);
+          for (int kb_s = w.kb0; ok && kb_s < w.kb1; kb_s += p.slab_kb) {
+            const int kb_e = min(w.kb1, kb_s + p.slab_kb);
+            const uint32_t b = acc_cnt & 1u, aph = (acc_cnt >> 1) & 1u;
+            if (!mbar_wait(acce_bar(b), aph ^ 1u, abort_flag, p.err, p.wait_limit_ns)) {
               ok = false;
               break;
             }
             tc_fence_after_sync();
-            const uint32_t a0 = sA + s * kABytes;
-            const uint32_t b0 = sB + s * Cfg::kBBytes;
+            const uint32_t d_tmem = tmem_base + b * BN;
+            for (int kb = kb_s; kb < kb_e; ++kb) {
+              const uint32_t s = g % STAGES, ph = (g / STAGES) & 1u;
+              if (!mbar_wait(full_bar(s), ph, abort_flag, p.err, p.wait_limit_ns)) {
+                ok = false;
+                break;
+              }
+              tc_fence_after_sync();
+              const uint32_t a0 = sA + s * kABytes;
+              const uint32_t b0 = sB + s * Cfg::kBBytes;
 #pragma unroll
-            for (int k = 0; k < kBK / 16; ++k) {
-              // 64-wide chunks one box apart (LBO), groups of 8 tokens 1024
-              // bytes apart (SBO); a step of 16 tokens is 2048 bytes
-              const uint64_t ad = smem_desc_sw128(a0 + k * 2048, kWgBoxBytes, 1024);
-              const uint64_t bd = smem_desc_sw128(b0 + k * 2048, kWgBoxBytes, 1024);
-              const uint32_t acc = (kb > kb_s || k > 0) ? 1u : 0u;
+              for (int k = 0; k < kBK / 16; ++k) {
+                // 64-wide chunks one box apart (LBO), groups of 8 tokens 1024
+                // bytes apart (SBO); a step of 16 tokens is 2048 bytes
+                const uint64_t ad = smem_desc_sw128(a0 + k * 2048, kWgBoxBytes, 1024);
+                const uint64_t bd = smem_desc_sw128(b0 + k * 2048, kWgBoxBytes, 1024);
+                const uint32_t acc = (kb > kb_s || k > 0) ? 1u : 0u;
+                if constexpr (PAIR)
+                  tc_mma_bf16_pair(d_tmem, ad, bd, idesc, acc);
+                else
+                  tc_mma_bf16(d_tmem, ad, bd, idesc, acc);
+              }
               if constexpr (PAIR)
-                tc_mma_bf16_pair(d_tmem, ad, bd, idesc, acc);
+                tc_commit_pair_multicast(empty_bar(s));
               else
-                tc_mma_bf16(d_tmem, ad, bd, idesc, acc);
+                tc_commit(empty_bar(s));
+              ++g;
             }
+            if (!ok) break;
             if constexpr (PAIR)
-              tc_commit_pair_multicast(empty_bar(s));
+              tc_commit_pair_multicast(accf_bar(b));
             else
-              tc_commit(empty_bar(s));
-            ++g;
+              tc_commit(accf_bar(b));
+            ++acc_cnt;
           }
-          if (!ok) break;
-          if constexpr (PAIR)
-            tc_commit_pair_multicast(accf_bar(b));
-          else
-            tc_commit(accf_bar(b));
-          ++acc_cnt;
         }
+        // all MMAs complete before TMEM is released
+        if constexpr (PAIR)
+          tc_commit_pair_multicast(drain_bar);
+        else
+          tc_commit(drain_bar);
+        mbar_wait_drain(drain_bar, 0, kDrainNs);
       }
-      // all MMAs complete before TMEM is released
-      if constexpr (PAIR)
-        tc_commit_pair_multicast(drain_bar);
-      else
-        tc_commit(drain_bar);
-      mbar_wait_drain(drain_bar, 0, kDrainNs);
+      __syncwarp();
     }
-    __syncwarp();
   } else {
+    if constexpr (SLABS) regs_take<kWgEpiRegs>();
     // --------------------------------------------------------- epilogue
     constexpr int CPT = Cfg::kColsPerThread;
-    const int ew = warp - 2;
+    const int ew = warp - 4;
     const int quad = warp & 3;  // a warp may only touch TMEM lanes 32*(warp%4) ..
     const int colpart = ew >> 2;
     const uint32_t ebuf = base + Cfg::kEpiOffset + ew * 4096u;
     uint32_t acc_cnt = 0;
     bool ok = true;
+    bool stored_tma = false;  // lane 0: the last block left through TMA
     for (int u = first_unit; ok && u < num_units; u += unit_step) {
       const Unit w = decode_unit(p, u);
       const bool split = w.part != 0;  // partials of a split-tail tile, not C
       const int y0 = w.tm * Cfg::kTileM + (int)rank * kBM + quad * 32;  // first row of this warp
-      const int64_t row = (int64_t)y0 + lane;
-      const bool row_ok = row < p.M;
       const int col0 = w.tn * BN + colpart * CPT;
-      // Writes 32 columns of sums, with base added and rounded once: of C
-      // through TMA where its rows allow, else directly; of the partials
-      // (compact blocks: tail tile `slot`, row pitch BN) through TMA.
-      auto emit = [&](uint32_t(&v)[32], int c) {
+      const bool pieces = p.out_tma == kBlockPieces && wp.base != nullptr && !split && y0 < p.M;
+      // Writes 32 columns of sums: of C through TMA where its rows allow and
+      // there is no base, else along rows (store_block); of a tail tile's
+      // partials (compact blocks: tile `slot`, row pitch BN) through TMA.
+      auto emit = [&](uint32_t(&v)[32], uint4(&base_words)[8], int c) {
         const int x = col0 + c * 32;
+        const bool in_range = y0 < p.M && x < p.N;
         if (split) {
           tma_out_words32<true>(&tmWs, ebuf, lane, v, colpart * CPT + c * 32,
                                 w.slot * Cfg::kTileM + (int)rank * kBM + quad * 32, w.split, true);
-          return;
-        }
-        if (wp.base && row_ok && x < p.N) add_base32(wp, row, x, v);
-        const bool in_range = y0 < p.M && x < p.N;
-        if (p.out_tma == kOutTmaC) {
+        } else if (p.out_tma == kBlockTma) {
           if (wp.out_bf16)
             tma_out_bf16x32(&tmOut, ebuf, lane, v, x, y0, in_range);
           else
             tma_out_words32<false>(&tmOut, ebuf, lane, v, x, y0, 0, in_range);
-        } else if (row_ok) {
-          if (wp.out_bf16)
-            store_bf16<32>(static_cast<uint16_t *>(p.C) + row * p.ldc, x, p.N, true, v);
-          else
-            store_words<32>(static_cast<uint32_t *>(p.C) + row * p.ldc, x, p.N, true, v);
+        } else if (in_range) {
+          if (stored_tma) bulk_wait_read_all();  // partials may still be leaving the buffer
+          store_block<!SLABS>(wp, ebuf, lane, v, base_words, y0, x, p.out_tma == kBlockPieces);
         }
+        stored_tma = split && lane == 0;
       };
       auto release = [&](uint32_t b) {
         tc_fence_before_sync();
@@ -314,8 +390,11 @@ __global__ void __launch_bounds__(kWgThreads, 1)
         ++acc_cnt;
       };
       const uint32_t t_lane = (uint32_t)(quad * 32) << 16;
-      if (w.kb1 - w.kb0 <= p.slab_kb) {
-        // one slab: its sums are the result, streamed 32 columns at a time
+      if constexpr (!SLABS) {
+        // one slab: its sums are the result, streamed 32 columns at a time,
+        // base's next block on its way meanwhile
+        uint4 ahead[8] = {};
+        if (pieces) fetch_base(wp, y0, col0, lane, ahead);
         const uint32_t b = acc_cnt & 1u, aph = (acc_cnt >> 1) & 1u;
         if (!__all_sync(0xffffffffu, mbar_wait(accf_bar(b), aph, abort_flag, p.err, p.wait_limit_ns))) {
           ok = false;
@@ -324,41 +403,46 @@ __global__ void __launch_bounds__(kWgThreads, 1)
         tc_fence_after_sync();
 #pragma unroll 1
         for (int c = 0; c < CPT / 32; ++c) {
+          uint4 base_words[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) base_words[i] = ahead[i];
           uint32_t v[32];
           tmem_ld<32>(tmem_base + b * BN + t_lane + colpart * CPT + c * 32, v);
+          if (pieces && c + 1 < CPT / 32) fetch_base(wp, y0, col0 + (c + 1) * 32, lane, ahead);
           tmem_ld_wait();
-          emit(v, c);
+          emit(v, base_words, c);
         }
         release(b);
-        continue;
-      }
-      float acc[CPT];
+      } else {
+        float acc[CPT];
 #pragma unroll
-      for (int i = 0; i < CPT; ++i) acc[i] = 0.f;
-      for (int kb_s = w.kb0; kb_s < w.kb1; kb_s += p.slab_kb) {
-        const uint32_t b = acc_cnt & 1u, aph = (acc_cnt >> 1) & 1u;
-        if (!__all_sync(0xffffffffu, mbar_wait(accf_bar(b), aph, abort_flag, p.err, p.wait_limit_ns))) {
-          ok = false;
-          break;
+        for (int i = 0; i < CPT; ++i) acc[i] = 0.f;
+        for (int kb_s = w.kb0; kb_s < w.kb1; kb_s += p.slab_kb) {
+          const uint32_t b = acc_cnt & 1u, aph = (acc_cnt >> 1) & 1u;
+          if (!__all_sync(0xffffffffu, mbar_wait(accf_bar(b), aph, abort_flag, p.err, p.wait_limit_ns))) {
+            ok = false;
+            break;
+          }
+          tc_fence_after_sync();
+#pragma unroll
+          for (int c = 0; c < CPT / 16; ++c) {
+            uint32_t v[16];
+            tmem_ld<16>(tmem_base + b * BN + t_lane + colpart * CPT + c * 16, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[c * 16 + i] += __uint_as_float(v[i]);
+          }
+          release(b);
         }
-        tc_fence_after_sync();
+        if (!ok) break;
 #pragma unroll
         for (int c = 0; c < CPT / 32; ++c) {
           uint32_t v[32];
-          tmem_ld<32>(tmem_base + b * BN + t_lane + colpart * CPT + c * 32, v);
-          tmem_ld_wait();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) acc[c * 32 + i] += __uint_as_float(v[i]);
+          for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(acc[c * 32 + i]);
+          uint4 base_words[8];
+          emit(v, base_words, c);
         }
-        release(b);
-      }
-      if (!ok) break;
-#pragma unroll
-      for (int c = 0; c < CPT / 32; ++c) {
-        uint32_t v[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(acc[c * 32 + i]);
-        emit(v, c);
       }
     }
     if (lane == 0) bulk_wait_all();  // this warp's TMA stores have landed
