@@ -155,7 +155,7 @@ gemm_status_t gemm_q8_weight_grad(int64_t T, int64_t K, int64_t N, const int8_t 
       count_launches(1);
       return launched(launch_wgrad_base(p, c.sms, c.st));
     }
-    const WgradPlan pl = plan_wgrad(M, cols, T, c.sms, pair_slots());
+    const WgradPlan pl = plan_wgrad(M, cols, T, bf ? 2 : 4, base != nullptr, c.sms, pair_slots());
     if (pl.grid <= 0) return GEMM_ERR_CUDA;
     // scratch: X restored to bf16 with 16-byte aligned rows, dY re-pitched
     // where TMA cannot read it, the split tail's partials
@@ -182,17 +182,14 @@ gemm_status_t gemm_q8_weight_grad(int64_t T, int64_t K, int64_t N, const int8_t 
       return GEMM_ERR_CUDA;
     tout = tws = tx;
     // C through TMA where its base, pitch and row ends are multiples of 16
-    // bytes (a clipped TMA store would write into the row's padding) and no
-    // base is added; with one in 16-byte pieces where both allow it
+    // bytes (a clipped TMA store would write into the row's padding), and the
+    // base, read in 16-byte pieces then, likewise
     const int64_t es = bf ? 2 : 4;
-    const bool c16 = aligned_to(dW, 16) && ldw * es % 16 == 0 && cols * es % 16 == 0;
-    const bool base16 = base && aligned_to(base, 16) && ldbase * es % 16 == 0;
-    p.tc.out_tma = kBlockElements;
-    if (c16 && !base && tma_store_enabled()) {
+    p.tc.out_tma = kOutDirect;
+    if (tma_store_enabled() && aligned_to(dW, 16) && ldw * es % 16 == 0 && cols * es % 16 == 0 &&
+        (!base || (aligned_to(base, 16) && ldbase * es % 16 == 0))) {
       if (!float_out_map(&tout, bf, dW, (uint64_t)cols, (uint64_t)M, (uint64_t)ldw, 1)) return GEMM_ERR_CUDA;
-      p.tc.out_tma = kBlockTma;
-    } else if (c16 && (!base || base16)) {
-      p.tc.out_tma = kBlockPieces;
+      p.tc.out_tma = kOutTmaC;
     }
     p.tc.tiles_m = pl.tiles_m;
     p.tc.tiles_n = pl.tiles_n;

@@ -75,10 +75,6 @@ cudaError_t launch_q8_restore(const Q8Ref &ck, void *x, int64_t ldx, int x_type,
 cudaError_t launch_wgrad_stage(const Q8Ref &ck, int64_t T, int64_t K, uint16_t *x, int64_t ldx, const uint16_t *g,
                                int64_t ldg, int64_t N, uint16_t *gx, int64_t ldgx, cudaStream_t st);
 
-// How the epilogue of the weight gradient writes blocks of 32 x 32 results
-// (TcParams::out_tma): TMA stores, 16-byte pieces along rows, or elements.
-enum BlockAccess : int { kBlockTma = 0, kBlockPieces = 1, kBlockElements = 2 };
-
 // C[m][n] = base[m][n] + sum_t A[t][m] * B[t][n] with bf16 A (T x M) and B
 // (T x N), both read with their rows (t) outermost (wgrad.cu).
 struct WgradParams {
@@ -87,19 +83,20 @@ struct WgradParams {
   int64_t ldbase;
   int out_bf16;      // type of C and base
 };
-// One compiled tile shape of the kernel.
+// A compiled tile shape of the kernel.
 struct WgradTile {
-  bool pair;  // a CTA pair per 256-row tile, or one CTA per 128-row tile
-  int bn;     // tile width
+  bool pair;  // a CTA pair per 256-row tile (256 wide), or one CTA per 128-row tile
+  int bn;     // tile width: 256, or 128 or 64
 };
-// Tile shape, split tail and grid for an M x N result summed over T rows.
+// Tile shape, split tail and grid for an M x N result of out_bytes each summed
+// over T rows, with or without a base to read: the least modelled time.
 struct WgradPlan {
   WgradTile tile;
   int tiles_m, tiles_n, num_kb;
   int tail_first, tail_splits, tail_kb_per;
   int grid;
 };
-WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t T, int sms, int pairs);
+WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t T, int out_bytes, bool base, int sms, int pairs);
 // Bytes of partial sums a plan's split tail writes (0: none).
 size_t wgrad_partial_bytes(const WgradPlan &pl);
 cudaError_t launch_wgrad(const WgradTile &tile, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out,

@@ -1,5 +1,7 @@
 // wgrad.cu -- planning and launches of the weight gradient's tensor-core
 // kernel (wgrad_tc.cuh), and the reduction of its split tail.
+#include <cmath>
+
 #include "layer_rows.cuh"
 #include "wgrad_tc.cuh"
 
@@ -152,18 +154,28 @@ __global__ void __launch_bounds__(256) wgrad_base_kernel(const WgradParams wp) {
   }
 }
 
-// Modelled cost of a tile shape: microseconds per k-block and per unit
-// (start, accumulator drain).
+// Modelled cost of a tile shape, fitted to forced plans on GB300 (T from 16
+// to 8192, K and N from 256 to 12288, every shape and split): microseconds per
+// k-block of 64 tokens and per unit besides, and what a unit takes at least to
+// write its tile (and read base's): its latency, and the bytes at a slot's
+// share of the memory.  The narrow tiles move twice and four times the operand
+// bytes a flop, which shared memory paces; with few tokens, where the output
+// sets the time, they fill the device in rounds that leave less of it idle
+// (128 tokens, 4096 x 4096 float32 with base: 36.8 us, pairs 40.2; 2048
+// tokens: 85 us, pairs 62).
 struct TileCost {
   WgradTile tile;
-  double kb_us, unit_us;
+  double kb_us, unit_us, least_us, bytes_per_us;
 };
-constexpr TileCost kTiles[] = {{{true, 256}, 0.28, 1.0}, {{true, 128}, 0.16, 0.7}, {{false, 128}, 0.16, 0.7}};
-constexpr double kTailFixedUs = 3.0, kTailUsPerMB = 0.4;
+constexpr TileCost kTiles[] = {{{true, 256}, 0.36, 1.2, 3.2, 65e3},
+                               {{false, 128}, 0.33, 0.5, 1.45, 35e3},
+                               {{false, 64}, 0.30, 0.4, 0.9, 35e3}};
+// A split tail's reduction: its launch, and the partials written and read.
+constexpr double kTailFixedUs = 3.5, kTailUsPerMB = 0.36;
 
 }  // namespace
 
-WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t T, int sms, int pairs) {
+WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t T, int out_bytes, bool base, int sms, int pairs) {
   WgradPlan best{};
   double best_us = -1;
   const int64_t num_kb = ceil_div64(T, kBK);
@@ -173,7 +185,11 @@ WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t T, int sms, int pairs) {
     const int tile_m = tc.tile.pair ? 2 * kBM : kBM;
     const int64_t tiles_m = ceil_div64(M, tile_m), tiles_n = ceil_div64(N, tc.tile.bn), tiles = tiles_m * tiles_n;
     const int64_t full = tiles / slots, rem = tiles % slots;
-    const double whole = num_kb * tc.kb_us + tc.unit_us;
+    const double tile_bytes = (double)tile_m * tc.tile.bn;
+    const auto unit_us = [&](int64_t kb, double bytes) {
+      return fmax(kb * tc.kb_us + tc.unit_us, fmax(tc.least_us, bytes / tc.bytes_per_us));
+    };
+    const double out = tile_bytes * out_bytes * (base ? 2 : 1), whole = unit_us(num_kb, out);
     for (int64_t s = 1; s <= 16; ++s) {
       int64_t kb_per = num_kb, parts = 1;
       if (s > 1) {
@@ -183,8 +199,8 @@ WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t T, int sms, int pairs) {
         if (parts != s || kb_per < 4) continue;
       }
       double us = full * whole;
-      if (rem > 0) us += kb_per * tc.kb_us + tc.unit_us;
-      if (parts > 1) us += kTailFixedUs + kTailUsPerMB * (double)parts * rem * tile_m * tc.tile.bn * 4e-6;
+      if (rem > 0) us += parts > 1 ? unit_us(kb_per, tile_bytes * 4) : whole;
+      if (parts > 1) us += kTailFixedUs + kTailUsPerMB * (double)parts * rem * tile_bytes * 4e-6;
       if (best_us < 0 || us < best_us) {
         best_us = us;
         best.tile = tc.tile;
@@ -212,13 +228,9 @@ cudaError_t launch_wgrad(const WgradTile &tile, const CUtensorMap &a, const CUte
                          const CUtensorMap &ws, const WgradParams &p, int grid, cudaStream_t st) {
   WgradParams q = p;
   q.tc.slab_kb = p.out_bf16 ? p.tc.num_kb : kSlabKb;
-  if (tile.pair) {
-    if (tile.bn == 256) return launch_tile<256, true>(a, b, out, ws, q, grid, st);
-    if (tile.bn == 128) return launch_tile<128, true>(a, b, out, ws, q, grid, st);
-  } else if (tile.bn == 128) {
-    return launch_tile<128, false>(a, b, out, ws, q, grid, st);
-  }
-  return cudaErrorInvalidValue;
+  if (tile.pair) return launch_tile<256, true>(a, b, out, ws, q, grid, st);
+  return tile.bn == 128 ? launch_tile<128, false>(a, b, out, ws, q, grid, st)
+                        : launch_tile<64, false>(a, b, out, ws, q, grid, st);
 }
 
 cudaError_t launch_wgrad_stage(const Q8Ref &ck, int64_t T, int64_t K, uint16_t *x, int64_t ldx, const uint16_t *g,

@@ -64,15 +64,14 @@ struct WgCfg {
   static_assert(kTmemCols <= 512, "TMEM has 512 columns");
 };
 
-// The way a 32 x 32 block of results leaves an epilogue warp where it does not
-// go through TMA (a base to add, or rows TMA cannot take): the block is turned
-// in the warp's shared memory, so that the lanes read base and write C along
-// rows.  A lane's own row would be 32 lines touched by every access of the
-// warp; along rows it is four (16-byte pieces) or one or two.
+// Where a base is added, and where C's rows rule TMA out, a 32 x 32 block of
+// results is turned in the epilogue warp's shared memory, so that the lanes
+// read base and write C along rows: a lane's own row would be 32 lines touched
+// by every access of the warp, along rows it is four (16-byte pieces) or one
+// or two (elements).
 
-// Base's values that this lane will add to the block at (y0, x), fetched ahead:
-// 16-byte pieces only (kBlockPieces; the block's rows and columns come in whole
-// pieces there).  b[8] words a lane for bf16 pieces use the first half.
+// Base's values that this lane adds to the block at (y0, x), in 16-byte pieces
+// (base's rows come in whole ones): four words of bf16, eight of float32.
 __device__ __forceinline__ void fetch_base(const WgradParams &p, int64_t y0, int x, int lane, uint4 (&b)[8]) {
   if (p.out_bf16) {
     const int c = x + (lane & 3) * 8;
@@ -99,72 +98,103 @@ __device__ __forceinline__ float4 as_float4(uint4 v) {
 __device__ __forceinline__ float4 operator+(float4 a, float4 b) {
   return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
 }
-
-// Block of sums v (lane = row, 32 columns) at (y0, x) of C, base added,
-// rounded once and stored along rows.  AHEAD: b is as fetch_base left it; else
-// base is fetched here, once v's registers are free.
-template <bool AHEAD>
-__device__ __forceinline__ void store_block(const WgradParams &p, uint32_t buf, int lane, const uint32_t (&v)[32],
-                                            uint4 (&b)[8], int64_t y0, int x, bool pieces) {
-  __syncwarp();  // the block before has been read
+__device__ __forceinline__ uint32_t block_piece(uint32_t buf, int row, int j) {
+  return buf + row * 128 + ((j ^ (row & 7)) << 4);
+}
+// A block of sums (lane = row, 32 columns) into the warp's shared memory, in
+// the layout of TMA's 128-byte swizzle.
+__device__ __forceinline__ void stage_block(uint32_t buf, int lane, const uint32_t (&v)[32]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    st_shared_v4(buf + lane * 128 + ((j ^ (lane & 7)) << 4), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+  for (int j = 0; j < 8; ++j) st_shared_v4(block_piece(buf, lane, j), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+}
+
+// The block at (y0, x): base added, rounded once, stored by TMA.  AHEAD: b is
+// as fetch_base left it; else base is fetched here, once v's registers are
+// free.
+template <bool AHEAD>
+__device__ __forceinline__ void tma_out_with_base(const WgradParams &p, const CUtensorMap *tm, uint32_t buf, int lane,
+                                                  const uint32_t (&v)[32], uint4 (&b)[8], int y0, int x) {
+  if (lane == 0) bulk_wait_read_all();
   __syncwarp();
-  if (!AHEAD && pieces && p.base) fetch_base(p, y0, x, lane, b);
-  const auto piece = [&](int row, int j) { return as_float4(ld_shared_v4(buf + row * 128 + ((j ^ (row & 7)) << 4))); };
-  if (pieces && p.out_bf16) {
-    const int j = lane & 3, c = x + j * 8;
+  stage_block(buf, lane, v);
+  if (!AHEAD) fetch_base(p, y0, x, lane, b);
+  __syncwarp();
+  if (p.out_bf16) {
+    const int j = lane & 3;
+    uint4 o[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = i * 8 + (lane >> 2);
-      const int64_t r = y0 + row;
-      if (r < p.tc.M && c < p.tc.N) {
-        float4 lo = piece(row, 2 * j), hi = piece(row, 2 * j + 1);
-        if (p.base) {
-          lo = lo + make_float4(__uint_as_float(b[i].x << 16), __uint_as_float(b[i].x & 0xFFFF0000u),
-                                __uint_as_float(b[i].y << 16), __uint_as_float(b[i].y & 0xFFFF0000u));
-          hi = hi + make_float4(__uint_as_float(b[i].z << 16), __uint_as_float(b[i].z & 0xFFFF0000u),
-                                __uint_as_float(b[i].w << 16), __uint_as_float(b[i].w & 0xFFFF0000u));
-        }
-        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.tc.C) + r * p.tc.ldc + c) =
-            make_uint4(pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y),
-                       pack_bf16x2(hi.z, hi.w));
-      }
+      const float4 lo = as_float4(ld_shared_v4(block_piece(buf, row, 2 * j))) +
+                        make_float4(__uint_as_float(b[i].x << 16), __uint_as_float(b[i].x & 0xFFFF0000u),
+                                    __uint_as_float(b[i].y << 16), __uint_as_float(b[i].y & 0xFFFF0000u));
+      const float4 hi = as_float4(ld_shared_v4(block_piece(buf, row, 2 * j + 1))) +
+                        make_float4(__uint_as_float(b[i].z << 16), __uint_as_float(b[i].z & 0xFFFF0000u),
+                                    __uint_as_float(b[i].w << 16), __uint_as_float(b[i].w & 0xFFFF0000u));
+      o[i] = make_uint4(pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y),
+                        pack_bf16x2(hi.z, hi.w));
     }
-  } else if (pieces) {
-    const int j = lane & 7, c = x + j * 4;
+    __syncwarp();
+    // 64-byte rows, 64-byte swizzle: chunk j of row r at chunk j ^ ((r / 2) % 4)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = i * 8 + (lane >> 2);
+      st_shared_v4(buf + row * 64 + ((j ^ ((row >> 1) & 3)) << 4), o[i].x, o[i].y, o[i].z, o[i].w);
+    }
+  } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int row = i * 4 + (lane >> 3);
-      const int64_t r = y0 + row;
-      if (r < p.tc.M && c < p.tc.N) {
-        float4 f = piece(row, j);
-        if (p.base) f = f + as_float4(b[i]);
-        *reinterpret_cast<float4 *>(static_cast<float *>(p.tc.C) + r * p.tc.ldc + c) = f;
-      }
+      const uint32_t at = block_piece(buf, i * 4 + (lane >> 3), lane & 7);
+      const float4 f = as_float4(ld_shared_v4(at)) + as_float4(b[i]);
+      st_shared_v4(at, __float_as_uint(f.x), __float_as_uint(f.y), __float_as_uint(f.z), __float_as_uint(f.w));
     }
-  } else {  // lane = column
-    const int c = x + lane;
-    const int rows = (int)min((int64_t)32, p.tc.M - y0);
-    if (c < p.tc.N) {
-#pragma unroll 8
-      for (int row = 0; row < rows; ++row) {
-        const int64_t r = y0 + row;
-        float f = __uint_as_float(ld_shared_u32(buf + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4));
-        if (p.out_bf16) {
-          if (p.base) f += __uint_as_float((uint32_t) static_cast<const uint16_t *>(p.base)[r * p.ldbase + c] << 16);
-          static_cast<__nv_bfloat16 *>(p.tc.C)[r * p.tc.ldc + c] = __float2bfloat16_rn(f);
-        } else {
-          if (p.base) f += static_cast<const float *>(p.base)[r * p.ldbase + c];
-          static_cast<float *>(p.tc.C)[r * p.tc.ldc + c] = f;
-        }
-      }
-    }
+  }
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    tma_store_2d(tm, buf, x, y0);
+    bulk_commit();
   }
 }
 
-// Launch with cluster dimensions (2,1,1) and an even grid when PAIR.
+// The block at (y0, x) with any base and C: base added, rounded once, stored
+// element by element along rows (lane = column).
+__device__ __forceinline__ void store_elements(const WgradParams &p, uint32_t buf, int lane, const uint32_t (&v)[32],
+                                               int y0, int x) {
+  if (lane == 0) bulk_wait_read_all();  // partials may still be leaving the buffer
+  __syncwarp();
+  stage_block(buf, lane, v);
+  __syncwarp();
+  const int c = x + lane, rows = min(32, p.tc.M - y0);
+  if (c >= p.tc.N) return;
+  // base may be C itself, so loads cannot move above stores by themselves:
+  // eight rows are read before the first of them is written
+  for (int r0 = 0; r0 < rows; r0 += 8) {
+    float f[8], o[8] = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(ld_shared_u32(block_piece(buf, r0 + i, lane >> 2) + (lane & 3) * 4));
+    if (p.base) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r0 + i < rows) {
+          const int64_t at = (int64_t)(y0 + r0 + i) * p.ldbase + c;
+          o[i] = p.out_bf16 ? __uint_as_float((uint32_t) static_cast<const uint16_t *>(p.base)[at] << 16)
+                            : static_cast<const float *>(p.base)[at];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (r0 + i < rows) {
+        const int64_t at = (int64_t)(y0 + r0 + i) * p.tc.ldc + c;
+        if (p.base) f[i] += o[i];
+        if (p.out_bf16)
+          static_cast<__nv_bfloat16 *>(p.tc.C)[at] = __float2bfloat16_rn(f[i]);
+        else
+          static_cast<float *>(p.tc.C)[at] = f[i];
+      }
+  }
+}
+
 // SLABS: the sums of several slabs are added in registers (the reduction is
 // longer than one slab); else every unit is one slab.
 template <int BN, bool PAIR, bool SLABS>
@@ -212,7 +242,7 @@ __global__ void __launch_bounds__(kWgThreads, 1)
     fence_mbar_init();
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
-    if (p.out_tma == kBlockTma) tma_prefetch_desc(&tmOut);
+    if (p.out_tma == kOutTmaC) tma_prefetch_desc(&tmOut);
     if (p.tail_splits > 0) tma_prefetch_desc(&tmWs);
   }
   __syncwarp();
@@ -354,32 +384,30 @@ __global__ void __launch_bounds__(kWgThreads, 1)
     const uint32_t ebuf = base + Cfg::kEpiOffset + ew * 4096u;
     uint32_t acc_cnt = 0;
     bool ok = true;
-    bool stored_tma = false;  // lane 0: the last block left through TMA
     for (int u = first_unit; ok && u < num_units; u += unit_step) {
       const Unit w = decode_unit(p, u);
       const bool split = w.part != 0;  // partials of a split-tail tile, not C
       const int y0 = w.tm * Cfg::kTileM + (int)rank * kBM + quad * 32;  // first row of this warp
       const int col0 = w.tn * BN + colpart * CPT;
-      const bool pieces = p.out_tma == kBlockPieces && wp.base != nullptr && !split && y0 < p.M;
-      // Writes 32 columns of sums: of C through TMA where its rows allow and
-      // there is no base, else along rows (store_block); of a tail tile's
-      // partials (compact blocks: tile `slot`, row pitch BN) through TMA.
+      const bool with_base = p.out_tma == kOutTmaC && wp.base != nullptr && !split;
+      // Writes 32 columns of sums: of C, or of a tail tile's partials (compact
+      // blocks: tile `slot`, row pitch BN).
       auto emit = [&](uint32_t(&v)[32], uint4(&base_words)[8], int c) {
         const int x = col0 + c * 32;
         const bool in_range = y0 < p.M && x < p.N;
         if (split) {
           tma_out_words32<true>(&tmWs, ebuf, lane, v, colpart * CPT + c * 32,
                                 w.slot * Cfg::kTileM + (int)rank * kBM + quad * 32, w.split, true);
-        } else if (p.out_tma == kBlockTma) {
+        } else if (with_base) {
+          if (in_range) tma_out_with_base<!SLABS>(wp, &tmOut, ebuf, lane, v, base_words, y0, x);
+        } else if (p.out_tma == kOutTmaC) {
           if (wp.out_bf16)
             tma_out_bf16x32(&tmOut, ebuf, lane, v, x, y0, in_range);
           else
             tma_out_words32<false>(&tmOut, ebuf, lane, v, x, y0, 0, in_range);
         } else if (in_range) {
-          if (stored_tma) bulk_wait_read_all();  // partials may still be leaving the buffer
-          store_block<!SLABS>(wp, ebuf, lane, v, base_words, y0, x, p.out_tma == kBlockPieces);
+          store_elements(wp, ebuf, lane, v, y0, x);
         }
-        stored_tma = split && lane == 0;
       };
       auto release = [&](uint32_t b) {
         tc_fence_before_sync();
@@ -392,25 +420,25 @@ __global__ void __launch_bounds__(kWgThreads, 1)
       const uint32_t t_lane = (uint32_t)(quad * 32) << 16;
       if constexpr (!SLABS) {
         // one slab: its sums are the result, streamed 32 columns at a time,
-        // base's next block on its way meanwhile
-        uint4 ahead[8] = {};
-        if (pieces) fetch_base(wp, y0, col0, lane, ahead);
+        // the next two blocks of base on their way meanwhile
+        constexpr int kChunks = CPT / 32, kAhead = kChunks < 2 ? kChunks : 2;
+        uint4 ahead[kAhead][8] = {};
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c)
+          if (with_base) fetch_base(wp, y0, col0 + c * 32, lane, ahead[c]);
         const uint32_t b = acc_cnt & 1u, aph = (acc_cnt >> 1) & 1u;
         if (!__all_sync(0xffffffffu, mbar_wait(accf_bar(b), aph, abort_flag, p.err, p.wait_limit_ns))) {
           ok = false;
           break;
         }
         tc_fence_after_sync();
-#pragma unroll 1
-        for (int c = 0; c < CPT / 32; ++c) {
-          uint4 base_words[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) base_words[i] = ahead[i];
+        for (int c = 0; c < kChunks; ++c) {
           uint32_t v[32];
           tmem_ld<32>(tmem_base + b * BN + t_lane + colpart * CPT + c * 32, v);
-          if (pieces && c + 1 < CPT / 32) fetch_base(wp, y0, col0 + (c + 1) * 32, lane, ahead);
           tmem_ld_wait();
-          emit(v, base_words, c);
+          emit(v, ahead[c % kAhead], c);
+          if (with_base && c + kAhead < kChunks) fetch_base(wp, y0, col0 + (c + kAhead) * 32, lane, ahead[c % kAhead]);
         }
         release(b);
       } else {
