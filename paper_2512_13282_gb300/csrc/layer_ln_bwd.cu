@@ -8,8 +8,11 @@ namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int kRingThreads = 512;     // most threads a block of the register-resident kernels has
-// Threads of the ring kernel with NV eights of values each.
-__host__ __device__ constexpr int ring_threads(int nv) { return nv == 1 ? 128 : kRingThreads; }
+// Blocks of the ring kernel that its registers are to leave room for: 1024
+// threads an SM with 8 values each (768 at any alignment), else 512.
+__host__ __device__ constexpr int ring_blocks(int nv, int v, int threads) {
+  return (nv > 1 ? 512 : v == 8 ? 1024 : 768) / threads;
+}
 
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int grid_cap(int64_t want, int64_t cap) { return (int)(want < 1 ? 1 : (want > cap ? cap : want)); }
@@ -119,26 +122,30 @@ struct RowStats {
       : rstd(mean_rstd.y), shift(-mean_rstd.x * mean_rstd.y) {}
 };
 
-// Rows whose x and dy are whole 16-byte pieces, up to 512 * NV * 8 values.
-// A block walks rows gridDim.x apart.  Their x and dy come through a ring of
-// row slots in shared memory, filled by bulk copies that run as far ahead as
-// the ring is deep: dgamma and dbeta are summed in registers (16 values a
-// thread and NV), which leaves none for rows in flight.  A row is read from
-// its slot twice, for the two averages and for the results; the block-wide
-// barrier between, passed by every thread once it has finished with the row
-// before, also frees that row's slot, which thread 0 refills.  One partial
-// row of dgamma and of dbeta a block goes to the workspace.
-template <typename TX, typename TDY, typename TDX, int NV>
-__global__ void __launch_bounds__(ring_threads(NV), NV == 1 ? 8 : 1)
+// Rows of up to 512 * NV * 8 values, at least 64 where V = 1.  A block walks
+// rows gridDim.x apart.  Their x and dy come through a ring of row slots in shared memory, filled by bulk
+// copies that run as far ahead as the ring is deep (SlotRow): dgamma and dbeta
+// are summed in registers (16 values a thread and NV), which leaves none for
+// rows in flight.  A row is read from its slot twice, for the two averages and
+// for the results; the block-wide barrier between, passed by every thread once
+// it has finished with the row before, also frees that row's slot, which
+// thread 0 refills.  One partial row of dgamma and of dbeta a block goes to the
+// workspace.
+template <typename TX, typename TDY, typename TDX, int NV, int V, int THREADS>
+__global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
     ln_backward_ring_kernel(const LnBackward p, const int stages, const uint32_t x_bytes, const uint32_t dy_bytes,
                             uint32_t *err, const uint64_t wait_limit_ns) {
+  constexpr bool kQ8 = sizeof(TX) == 1;
   extern __shared__ __align__(128) uint8_t slots[];
   __shared__ __align__(16) float2 sm[2][16];
+  // block exponents of three rows: being read, still being read by a thread
+  // that is behind, and being written
+  __shared__ uint8_t exps[kQ8 ? 3 : 1][kQ8 ? 512 : 1];
   __shared__ __align__(8) uint64_t bars[kMaxStages];
   __shared__ volatile uint32_t abort_flag;
   griddep_launch_dependents();
-  const int T = blockDim.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t ring = smem_addr(slots), bar0 = smem_addr(bars), slot_bytes = x_bytes + dy_bytes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t ring = smem_addr(slots), bar0 = smem_addr(bars), both_bytes = x_bytes + dy_bytes;
   RingPlace use, put;  // put: thread 0's
   const float inv_n = 1.0f / (float)p.cols;
   if (threadIdx.x == 0) {
@@ -151,84 +158,111 @@ __global__ void __launch_bounds__(ring_threads(NV), NV == 1 ? 8 : 1)
   griddep_wait();
   const int64_t mine = (p.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // rows of this block, at least one
   const auto row_of = [&](int64_t i) { return (int64_t)blockIdx.x + i * gridDim.x; };
-  const auto fill = [&](int64_t i) {
-    const uint32_t dst = ring + put.slot * slot_bytes, bar = bar0 + 8u * put.slot;
-    const int64_t r = row_of(i);
-    put.advance(stages);
-    mbar_arrive_expect_tx(bar, slot_bytes);
-    if constexpr (sizeof(TX) == 1)
-      bulk_load(dst, p.ck.q + r * p.ck.ldq, x_bytes, bar);
+  const auto x_row = [&](int64_t i) -> const void * {
+    if constexpr (kQ8)
+      return p.ck.q + row_of(i) * p.ck.ldq;
     else
-      bulk_load(dst, static_cast<const TX *>(p.x) + r * p.ldx, x_bytes, bar);
-    bulk_load(dst + x_bytes, static_cast<const TDY *>(p.dy) + r * p.lddy, dy_bytes, bar);
+      return static_cast<const TX *>(p.x) + row_of(i) * p.ldx;
+  };
+  const auto dy_row = [&](int64_t i) { return static_cast<const TDY *>(p.dy) + row_of(i) * p.lddy; };
+  const auto fill = [&](int64_t i) {
+    const uint32_t dst = ring + put.slot * both_bytes, bar = bar0 + 8u * put.slot;
+    put.advance(stages);
+    const uint32_t xb = SlotRow<TX, V, THREADS>::copy_bytes(x_row(i), p.cols), yb = SlotRow<TDY, V, THREADS>::copy_bytes(dy_row(i), p.cols);
+    mbar_arrive_expect_tx(bar, xb + yb);
+    SlotRow<TX, V, THREADS>::copy(dst, x_row(i), xb, bar);
+    SlotRow<TDY, V, THREADS>::copy(dst + x_bytes, dy_row(i), yb, bar);
   };
   int64_t filled = mine < stages ? mine : stages;
   if (threadIdx.x == 0)
     for (int64_t i = 0; i < filled; ++i) fill(i);
 
-  // the row's statistics and block exponents, fetched a row ahead
-  float2 st_next;
-  uint32_t ex[NV], ex_next[NV];
-  const auto fetch = [&](int64_t i) {
-    const int64_t r = row_of(i);
-    st_next = make_float2(p.mean[r], p.rstd[r]);
-    if constexpr (sizeof(TX) == 1) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int c = (v * T + (int)threadIdx.x) * 8;
-        ex_next[v] = c < p.cols ? p.ck.e[r * p.ck.lde + (c >> 5)] : 0;
-      }
-    }
+  // fetched a row ahead: the statistics and the rows' ends; two rows ahead, on
+  // their way through shared memory: the block exponents
+  SlotRow<TX, V, THREADS> xr;
+  SlotRow<TDY, V, THREADS> yr;
+  xr.init(p.cols);
+  yr.init(p.cols);
+  float2 st_next = make_float2(p.mean[row_of(0)], p.rstd[row_of(0)]);
+  xr.fetch_ends(x_row(0));
+  yr.fetch_ends(dy_row(0));
+  const int blocks = (p.cols + 31) / 32;  // at most one a thread
+  const auto exp_at = [&](int64_t i) -> uint32_t {
+    return kQ8 && i < mine && (int)threadIdx.x < blocks ? p.ck.e[row_of(i) * p.ck.lde + threadIdx.x] : 0u;
   };
-  fetch(0);
+  uint32_t exp_next = 0;
+  int exp_use = 0;
+  if constexpr (kQ8) {
+    if ((int)threadIdx.x < blocks) exps[0][threadIdx.x] = (uint8_t)exp_at(0);
+    exp_next = exp_at(1);
+    __syncthreads();
+  }
   float2 gamma[NV * 4], dg[NV * 4], db[NV * 4];
+  const auto gamma_at = [&](int c) { return c < p.cols ? load_param(p.gamma, p.param_type, c, 1.f) : 0.f; };
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int c = (v * T + (int)threadIdx.x) * 8;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      gamma[v * 4 + i] = c < p.cols ? make_float2(load_param(p.gamma, p.param_type, c + 2 * i, 1.f),
-                                                  load_param(p.gamma, p.param_type, c + 2 * i + 1, 1.f))
-                                    : both(0.f);
-      dg[v * 4 + i] = db[v * 4 + i] = both(0.f);
+    for (int j = 0; j < 4; ++j) {
+      gamma[v * 4 + j] = make_float2(gamma_at(group_col<V, THREADS>(v, 2 * j)), gamma_at(group_col<V, THREADS>(v, 2 * j + 1)));
+      dg[v * 4 + j] = db[v * 4 + j] = both(0.f);
     }
   }
   bool ok = true;
   int64_t done = 0;
   for (int64_t i = 0; i < mine; done = ++i, use.advance(stages)) {
-    const uint8_t *slot = slots + use.slot * slot_bytes;
+    uint8_t *slot = slots + use.slot * both_bytes;
     const RowStats st(st_next);
-#pragma unroll
-    for (int v = 0; v < NV; ++v) ex[v] = ex_next[v];
-    if (i + 1 < mine) fetch(i + 1);
+    const uint32_t x_off = xr.offset(x_row(i)), y_off = yr.offset(dy_row(i));
     ok = mbar_wait(bar0 + 8u * use.slot, use.parity, &abort_flag, err, wait_limit_ns);
-    const auto load = [&](int v, Chunk<TX, 8> &x, Chunk<TDY, 8> &y, float2 &scale) {
-      const int c = (v * T + (int)threadIdx.x) * 8;
-      x.load(slot, c);
-      y.load(slot + x_bytes, c);
-      if constexpr (sizeof(TX) == 1)
-        scale = both(st.rstd * q8_scale(ex[v]));
-      else
-        scale = both(st.rstd);
-    };
-    const float2 shift = both(st.shift);
-    float2 a2 = both(0.f), b2 = both(0.f);
     if (ok) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        if ((v * T + (int)threadIdx.x) * 8 < p.cols) {
-          Chunk<TX, 8> x;
-          Chunk<TDY, 8> y;
-          float2 scale;
-          load(v, x, y, scale);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 g = mul2(y.get2(j), gamma[v * 4 + j]);
-            a2 = add2(a2, g);
-            b2 = fma2(g, fma2(x.get2(j), scale, shift), b2);
-          }
-        }
+      xr.put_ends(slot, x_off);
+      yr.put_ends(slot + x_bytes, y_off);
+    }
+    if (i + 1 < mine) {
+      st_next = make_float2(p.mean[row_of(i + 1)], p.rstd[row_of(i + 1)]);
+      xr.fetch_ends(x_row(i + 1));
+      yr.fetch_ends(dy_row(i + 1));
+    }
+    const uint8_t *exp_row = exps[0];
+    if constexpr (kQ8) {
+      exp_row = exps[exp_use];
+      exp_use = exp_use == 2 ? 0 : exp_use + 1;
+      if ((int)threadIdx.x < blocks) exps[exp_use][threadIdx.x] = (uint8_t)exp_next;
+      exp_next = exp_at(i + 2);
+    }
+    // x as xh and dy of group v
+    const auto load = [&](int v, float2(&xh)[4], float2(&d)[4]) {
+      xr.load(slot, x_off, v, p.cols, xh);
+      yr.load(slot + x_bytes, y_off, v, p.cols, d);
+      float2 scale = both(st.rstd);
+      if constexpr (kQ8 && V == 8) {
+        const int c = group_col<V, THREADS>(v, 0);
+        scale = both(st.rstd * q8_scale(exp_row[c < p.cols ? c >> 5 : 0]));
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (kQ8 && V == 1) {
+          const int c = group_col<V, THREADS>(v, 2 * j), e = group_col<V, THREADS>(v, 2 * j + 1);
+          scale = make_float2(st.rstd * q8_scale(exp_row[c < p.cols ? c >> 5 : 0]),
+                              st.rstd * q8_scale(exp_row[e < p.cols ? e >> 5 : 0]));
+        }
+        xh[j] = fma2(xh[j], scale, both(st.shift));
+      }
+    };
+    float2 a2 = both(0.f), b2 = both(0.f);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float2 xh[4], d[4], a = both(0.f), b = both(0.f);
+      load(v, xh, d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 g = mul2(d[j], gamma[v * 4 + j]);
+        a = add2(a, g);
+        b = fma2(g, xh[j], b);
+      }
+      const bool in = V == 1 || group_col<V, THREADS>(v, 0) < p.cols;
+      a2 = add2(a2, in ? a : both(0.f));
+      b2 = add2(b2, in ? b : both(0.f));
     }
     const float a = warp_sum(a2.x + a2.y), b = warp_sum(b2.x + b2.y);
     if (lane == 0) sm[i & 1][warp] = make_float2(a, b);
@@ -238,28 +272,31 @@ __global__ void __launch_bounds__(ring_threads(NV), NV == 1 ? 8 : 1)
       break;
     }
     if (threadIdx.x == 0 && i > 0 && filled < mine) fill(filled++);  // the slot of row i - 1
-    const float2 s = sum_over_warps<ring_threads(NV) / 32>(sm[i & 1]);
+    const float2 s = sum_over_warps<THREADS / 32>(sm[i & 1]);
     const float2 ga = both(-s.x * inv_n * st.rstd), gx = both(-s.y * inv_n * st.rstd), rstd = both(st.rstd);
     TDX *dx = static_cast<TDX *>(p.dx) + row_of(i) * p.lddx;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = (v * T + (int)threadIdx.x) * 8;
-      if (c < p.cols) {
-        Chunk<TX, 8> x;
-        Chunk<TDY, 8> y;
-        float2 scale;
-        load(v, x, y, scale);
-        float o[8];
+      float2 xh[4], d[4];
+      float o[8];
+      load(v, xh, d);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 d = y.get2(j), xh = fma2(x.get2(j), scale, shift);
-          dg[v * 4 + j] = fma2(d, xh, dg[v * 4 + j]);
-          db[v * 4 + j] = add2(db[v * 4 + j], d);
-          const float2 r = fma2(mul2(d, gamma[v * 4 + j]), rstd, fma2(xh, gx, ga));
-          o[2 * j] = r.x;
-          o[2 * j + 1] = r.y;
+      for (int j = 0; j < 4; ++j) {
+        dg[v * 4 + j] = fma2(d[j], xh[j], dg[v * 4 + j]);
+        db[v * 4 + j] = add2(db[v * 4 + j], d[j]);
+        const float2 r = fma2(mul2(d[j], gamma[v * 4 + j]), rstd, fma2(xh[j], gx, ga));
+        o[2 * j] = r.x;
+        o[2 * j + 1] = r.y;
+      }
+      if constexpr (V == 8) {
+        const int c = group_col<V, THREADS>(v, 0);
+        if (c < p.cols) store_chunk<TDX, 8>(dx, c, o, 8);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int c = group_col<V, THREADS>(v, k);
+          if (c < p.cols) store_value<TDX>(dx, c, o[k]);
         }
-        store_chunk<TDX, 8>(dx, c, o, 8);
       }
     }
   }
@@ -268,126 +305,45 @@ __global__ void __launch_bounds__(ring_threads(NV), NV == 1 ? 8 : 1)
     return;
   }
   if (!p.partials) return;
+  float *dg_out = p.partials + (int64_t)blockIdx.x * p.cols, *db_out = dg_out + (int64_t)gridDim.x * p.cols;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int c = (v * T + (int)threadIdx.x) * 8;
-    if (c < p.cols) {
-      store_chunk<float, 8>(p.partials + (int64_t)blockIdx.x * p.cols, c, reinterpret_cast<const float *>(dg + v * 4), 8);
-      store_chunk<float, 8>(p.partials + (int64_t)(gridDim.x + blockIdx.x) * p.cols, c,
-                            reinterpret_cast<const float *>(db + v * 4), 8);
-    }
-  }
-}
-
-// Any alignment, up to 512 * NV * 8 values a row: x and dy are read straight
-// into registers, in chunks of V values (V = 4 where the rows of every matrix
-// start on a multiple of four values, else 1: neighbouring lanes still share
-// sectors), and kept there between the two averages and the results.
-template <typename TX, typename TDY, typename TDX, int NV, int V>
-__global__ void __launch_bounds__(kRingThreads) ln_backward_regs_kernel(const LnBackward p) {
-  constexpr int C = NV * 8 / V;
-  __shared__ float2 sm[2][32];
-  griddep_launch_dependents();
-  griddep_wait();
-  const int T = blockDim.x;
-  const float inv_n = 1.0f / (float)p.cols;
-  const auto col = [&](int k) { return (k * T + (int)threadIdx.x) * V; };
-  const auto valid = [&](int k) { return max(0, min(V, p.cols - col(k))); };
-  float gamma[C * V], dg[C * V], db[C * V];
-#pragma unroll
-  for (int k = 0; k < C; ++k)
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      gamma[k * V + i] = i < valid(k) ? load_param(p.gamma, p.param_type, col(k) + i, 1.f) : 0.f;
-      dg[k * V + i] = db[k * V + i] = 0.f;
-    }
-  int buf = 0;
-  for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
-    const RowStats st(make_float2(p.mean[r], p.rstd[r]));
-    Chunk<TX, V> x[C];
-    Chunk<TDY, V> y[C];
-    uint32_t ex[C];
-    const void *xr;
-    if constexpr (sizeof(TX) == 1)
-      xr = p.ck.q + r * p.ck.ldq;
-    else
-      xr = static_cast<const TX *>(p.x) + r * p.ldx;
-    const TDY *yr = static_cast<const TDY *>(p.dy) + r * p.lddy;
-#pragma unroll
-    for (int k = 0; k < C; ++k) {
-      const int n = valid(k), c = col(k);
-      if (n == V) {
-        x[k].load(xr, c);
-        y[k].load(yr, c);
-      } else {
-        x[k].load_part(xr, c, n);
-        y[k].load_part(yr, c, n);
+    if constexpr (V == 8) {
+      const int c = group_col<V, THREADS>(v, 0);
+      if (c < p.cols) {
+        store_chunk<float, 8>(dg_out, c, reinterpret_cast<const float *>(dg + v * 4), 8);
+        store_chunk<float, 8>(db_out, c, reinterpret_cast<const float *>(db + v * 4), 8);
       }
-      if constexpr (sizeof(TX) == 1) ex[k] = n > 0 ? p.ck.e[r * p.ck.lde + (c >> 5)] : 0;
-    }
-    float a = 0.f, b = 0.f;
-    const auto xhat = [&](int k, int i) {
-      float scale = st.rstd;
-      if constexpr (sizeof(TX) == 1) scale *= q8_scale(ex[k]);
-      return fmaf(x[k].get(i), scale, st.shift);
-    };
+    } else {
 #pragma unroll
-    for (int k = 0; k < C; ++k)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if (i < valid(k)) {
-          const float g = y[k].get(i) * gamma[k * V + i];
-          a += g;
-          b = fmaf(g, xhat(k, i), b);
+      for (int k = 0; k < 8; ++k) {
+        const int c = group_col<V, THREADS>(v, k);
+        if (c < p.cols) {
+          dg_out[c] = (k & 1) ? dg[v * 4 + (k >> 1)].y : dg[v * 4 + (k >> 1)].x;
+          db_out[c] = (k & 1) ? db[v * 4 + (k >> 1)].y : db[v * 4 + (k >> 1)].x;
         }
       }
-    const float2 s = block_sum2(a, b, sm, buf);
-    buf ^= 1;
-    const float ga = s.x * inv_n * st.rstd, gx = s.y * inv_n * st.rstd;
-    TDX *dx = static_cast<TDX *>(p.dx) + r * p.lddx;
-#pragma unroll
-    for (int k = 0; k < C; ++k) {
-      const int n = valid(k);
-      float o[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float d = y[k].get(i), xh = xhat(k, i);
-        if (i < n) {
-          dg[k * V + i] = fmaf(d, xh, dg[k * V + i]);
-          db[k * V + i] += d;
-        }
-        o[i] = fmaf(d * gamma[k * V + i], st.rstd, -fmaf(xh, gx, ga));
-      }
-      store_chunk<TDX, V>(dx, col(k), o, n);
     }
   }
-  if (!p.partials) return;
-#pragma unroll
-  for (int k = 0; k < C; ++k)
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < valid(k)) {
-        p.partials[(int64_t)blockIdx.x * p.cols + col(k) + i] = dg[k * V + i];
-        p.partials[(int64_t)(gridDim.x + blockIdx.x) * p.cols + col(k) + i] = db[k * V + i];
-      }
 }
 
 // How a backward pass runs.
-enum LnPath { kLnAny, kLnRegs, kLnRing };
+enum LnPath { kLnAny, kLnRing };
 struct LnPlan {
   LnPath path;
-  int nv, threads, grid;
-  int chunk;                    // kLnRegs: V
-  int stages;                   // kLnRing
-  uint32_t x_bytes, dy_bytes;   // kLnRing: bytes of a row
-  int parts;                    // partial rows of the parameter gradients
+  int grid, parts;  // blocks; partial rows of the parameter gradients
+  // kLnRing
+  int nv, threads, stages;
+  bool aligned;                // V = 8, else 1
+  uint32_t x_bytes, dy_bytes;  // of a slot
 };
 
 // Blocks that walk `rows` rows, `per_sm` at a time on an SM: every SM one
-// while there are few rows, more only where each has at least eight rows to
-// set against the partial row that it writes and another kernel reads.
+// while there are few rows, more where each still has two rows to set against
+// the partial row that it writes and another kernel reads (1000 rows of 1500
+// from a checkpoint: XX us with 152 blocks, YY with 500).
 int row_blocks(int64_t rows, int sms, int per_sm) {
-  const int64_t few = rows < sms ? rows : sms, many = ceil_div64(rows, 8), most = (int64_t)sms * per_sm;
+  const int64_t few = rows < sms ? rows : sms, many = ceil_div64(rows, 2), most = (int64_t)sms * per_sm;
   const int64_t want = many > few ? many : few;
   return (int)(want < most ? want : most);
 }
@@ -401,15 +357,18 @@ LnPlan plan_ln_backward(const LnBackward &p, int sms) {
   const int64_t eights = ceil_div64(p.cols, 8);
   // few threads with more values each: a row's fixed costs (its barrier, the
   // sums over lanes and warps) are paid by every warp
-  const int ring_nv = eights <= ring_threads(1) ? 1 : eights <= 2 * kRingThreads ? 2 : (int)ceil_div64(eights, kRingThreads);
-  const bool pieces = (int64_t)p.cols * sx % 16 == 0 && (int64_t)p.cols * sg % 16 == 0 && p.cols % 8 == 0;
-  if (p.rows > 0 && ring_nv <= 4 && pieces && rows_on(x, ldx, sx, 16) && rows_on(p.dy, p.lddy, sg, 16) &&
-      rows_on(p.dx, p.lddx, so, 16)) {
-    l.x_bytes = (uint32_t)p.cols * sx;
-    l.dy_bytes = (uint32_t)p.cols * sg;
-    l.nv = ring_nv;
+  l.nv = eights <= 128 ? 1 : eights <= 2 * kRingThreads ? 2 : (int)ceil_div64(eights, kRingThreads);
+  l.aligned = (int64_t)p.cols * sx % 16 == 0 && (int64_t)p.cols * sg % 16 == 0 && p.cols % 8 == 0 &&
+              rows_on(x, ldx, sx, 16) && rows_on(p.dy, p.lddy, sg, 16) && rows_on(p.dx, p.lddx, so, 16);
+  if (p.rows > 0 && l.nv <= 4 && (l.aligned || p.cols >= 64)) {
+    l.x_bytes = slot_bytes(p.cols, sx, l.aligned);
+    l.dy_bytes = slot_bytes(p.cols, sg, l.aligned);
     l.threads = (int)ceil_div64(ceil_div64(eights, l.nv), 32) * 32;
-    int per_sm = (l.nv == 1 ? 2 : 1) * (kRingThreads / l.threads);
+    if (!l.aligned) {  // one of the block sizes compiled
+      l.threads = l.threads <= 128 ? 128 : l.threads <= 256 && l.nv == 2 ? 256 : 512;
+      if (l.nv == 3) l.nv = 4;
+    }
+    int per_sm = ring_blocks(l.nv, l.aligned ? 8 : 1, l.threads);
     per_sm = per_sm > 8 ? 8 : per_sm;
     int64_t stages = kRingBytes / per_sm / (l.x_bytes + l.dy_bytes);
     if (stages < 2) {
@@ -423,15 +382,6 @@ LnPlan plan_ln_backward(const LnBackward &p, int sms) {
       return l;
     }
   }
-  if (p.rows > 0 && eights <= 2 * kRingThreads) {
-    l.path = kLnRegs;
-    l.nv = (int)ceil_div64(eights, kRingThreads);
-    l.threads = (int)ceil_div64(ceil_div64(eights, l.nv), 32) * 32;
-    l.chunk = rows_on(x, ldx, sx, 4 * sx) && rows_on(p.dy, p.lddy, sg, 4 * sg) && rows_on(p.dx, p.lddx, so, 4 * so) ? 4 : 1;
-    const int per_sm = kRingThreads / l.threads;
-    l.grid = l.parts = row_blocks(p.rows, sms, per_sm > 4 ? 4 : per_sm);
-    return l;
-  }
   // dx by one kernel, partials by another: enough blocks of 32 columns x 8
   // rows at a time to fill the device several times over, no more than there
   // are groups of rows
@@ -441,9 +391,9 @@ LnPlan plan_ln_backward(const LnBackward &p, int sms) {
   return l;
 }
 
-template <typename TX, typename TDY, typename TDX, int NV>
+template <typename TX, typename TDY, typename TDX, int NV, int V, int THREADS>
 cudaError_t run_ring(const LnBackward &p, const LnPlan &l, const OpContext &c) {
-  const auto kern = ln_backward_ring_kernel<TX, TDY, TDX, NV>;
+  const auto kern = ln_backward_ring_kernel<TX, TDY, TDX, NV, V, THREADS>;
   const size_t smem = (size_t)l.stages * (l.x_bytes + l.dy_bytes);
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
   if (e != cudaSuccess) return e;
@@ -452,23 +402,28 @@ cudaError_t run_ring(const LnBackward &p, const LnPlan &l, const OpContext &c) {
 }
 
 template <typename TX, typename TDY, typename TDX>
+cudaError_t run_width(const LnBackward &p, const LnPlan &l, const OpContext &c) {
+  if (l.aligned)
+    return l.nv == 1   ? run_ring<TX, TDY, TDX, 1, 8, 128>(p, l, c)
+           : l.nv == 2 ? run_ring<TX, TDY, TDX, 2, 8, 512>(p, l, c)
+           : l.nv == 3 ? run_ring<TX, TDY, TDX, 3, 8, 512>(p, l, c)
+                       : run_ring<TX, TDY, TDX, 4, 8, 512>(p, l, c);
+  if (l.nv == 1) return run_ring<TX, TDY, TDX, 1, 1, 128>(p, l, c);
+  if (l.nv == 4) return run_ring<TX, TDY, TDX, 4, 1, 512>(p, l, c);
+  return l.threads == 128   ? run_ring<TX, TDY, TDX, 2, 1, 128>(p, l, c)
+         : l.threads == 256 ? run_ring<TX, TDY, TDX, 2, 1, 256>(p, l, c)
+                            : run_ring<TX, TDY, TDX, 2, 1, 512>(p, l, c);
+}
+
+template <typename TX, typename TDY, typename TDX>
 cudaError_t run_types(const LnBackward &p, const OpContext &c, int *launches) {
   const LnPlan l = plan_ln_backward(p, c.sms);
-  const dim3 grid(l.grid), block(l.threads);
+  const dim3 grid(l.grid);
   cudaError_t e = cudaSuccess;
   if (p.rows > 0) {
     ++*launches;
     if (l.path == kLnRing)
-      e = l.nv == 1   ? run_ring<TX, TDY, TDX, 1>(p, l, c)
-          : l.nv == 2 ? run_ring<TX, TDY, TDX, 2>(p, l, c)
-          : l.nv == 3 ? run_ring<TX, TDY, TDX, 3>(p, l, c)
-                      : run_ring<TX, TDY, TDX, 4>(p, l, c);
-    else if (l.path == kLnRegs && l.nv == 1)
-      e = l.chunk == 4 ? launch_ex(ln_backward_regs_kernel<TX, TDY, TDX, 1, 4>, grid, block, 0, c.st, 1, p)
-                       : launch_ex(ln_backward_regs_kernel<TX, TDY, TDX, 1, 1>, grid, block, 0, c.st, 1, p);
-    else if (l.path == kLnRegs)
-      e = l.chunk == 4 ? launch_ex(ln_backward_regs_kernel<TX, TDY, TDX, 2, 4>, grid, block, 0, c.st, 1, p)
-                       : launch_ex(ln_backward_regs_kernel<TX, TDY, TDX, 2, 1>, grid, block, 0, c.st, 1, p);
+      e = run_width<TX, TDY, TDX>(p, l, c);
     else
       e = launch_ex(ln_backward_any_kernel<TX, TDY, TDX>, grid, dim3(kRowThreads), 0, c.st, 1, p);
     if (e != cudaSuccess) return e;

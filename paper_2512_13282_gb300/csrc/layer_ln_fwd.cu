@@ -9,7 +9,6 @@ namespace gb300 {
 namespace {
 
 constexpr int kAnyThreads = 256;
-constexpr int kMaxThreads = 512;
 
 // Any width, pitch and alignment: a block per row, the row read three times
 // (mean, variance, result), the second and third time from L1 or L2.
@@ -50,7 +49,7 @@ __global__ void __launch_bounds__(kAnyThreads) ln_forward_any_kernel(const LnFor
         out = as_stored<TY>(out);
         const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(out) & 0x7FFFFFFFu);
         const uint32_t e = q8_exponent(top);
-        if (c < p.cols) p.ck.q[r * p.ck.ldq + c] = (int8_t)q8_quantise(out, q8_inverse(e), e);
+        if (c < p.cols) p.ck.q[r * p.ck.ldq + c] = (int8_t)q8_byte(out, q8_inverse(e), e);
         if (lane == 0) p.ck.e[r * p.ck.lde + (c0 >> 5)] = (uint8_t)e;
       }
     }
@@ -113,127 +112,30 @@ __device__ __forceinline__ void store_eighth(TY *y, const Q8Ref &ck, int64_t r, 
   if (n > 0 && (c & 31) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
 }
 
-// Rows of up to 512 * NV * 8 values, kept in registers from their one read to
-// their one write: a block of T threads walks rows gridDim.x apart, the next
-// row's values on their way (as they are in memory) while this row is
-// reduced, so that the loads never wait for the two block-wide sums.  gamma
-// and beta stay in registers where they fit (NV <= 2).
-//
-// A thread holds NV * 8 / V chunks of V consecutive values, chunk k at column
-// (k * T + t) * V: V = 8 where every row of x, y and q starts on 16 (q: 8)
-// bytes, else V = 1, which any alignment allows and which still fills whole
-// sectors, as the lanes of a warp are neighbours.  A checkpoint block is 4
-// lanes' chunks (V = 8) or the warp's 32 lanes (V = 1).
-template <typename TX, typename TY, int NV, int V>
-__global__ void __launch_bounds__(kMaxThreads, NV == 1 ? 2 : 1) ln_forward_kernel(const LnForward p) {
-  constexpr int C = NV * 8 / V;  // chunks per thread
-  constexpr bool kKeep = NV <= 2;
-  __shared__ float sm[2][32];
-  griddep_launch_dependents();
-  const int T = blockDim.x;
-  int64_t r = blockIdx.x;
-  const float inv_n = 1.0f / (float)p.cols;
-  const auto col = [&](int k) { return (k * T + (int)threadIdx.x) * V; };
-  // valid values of chunk k
-  const auto valid = [&](int k) { return max(0, min(V, p.cols - col(k))); };
-  const auto fetch = [&](Chunk<TX, V>(&raw)[C], int64_t row) {
-    const TX *x = static_cast<const TX *>(p.x) + row * p.ldx;
-#pragma unroll
-    for (int k = 0; k < C; ++k) {
-      const int n = valid(k);
-      if (n == V)
-        raw[k].load(x, col(k));
-      else
-        raw[k].load_part(x, col(k), n);
-    }
-  };
-  griddep_wait();
-  Chunk<TX, V> raw[C];
-  fetch(raw, r);
-  float gamma[kKeep ? C * V : 1], beta[kKeep ? C * V : 1];
-  if constexpr (kKeep) {
-#pragma unroll
-    for (int k = 0; k < C; ++k)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const bool in = col(k) + i < p.cols;
-        gamma[k * V + i] = in ? load_param(p.gamma, p.param_type, col(k) + i, 1.f) : 0.f;
-        beta[k * V + i] = in ? load_param(p.beta, p.param_type, col(k) + i, 0.f) : 0.f;
-      }
-  }
-  for (; r < p.rows; r += gridDim.x) {
-    float x[C * V];
-    float s = 0.f;
-#pragma unroll
-    for (int k = 0; k < C; ++k)
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        x[k * V + i] = raw[k].get(i);
-        s += x[k * V + i];  // zero past the row's end
-      }
-    if (r + gridDim.x < p.rows) fetch(raw, r + gridDim.x);
-    const float mean = block_sum(s, sm[0]) * inv_n;
-    float v = 0.f;
-#pragma unroll
-    for (int k = 0; k < C; ++k) {
-      const int n = valid(k);
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        x[k * V + i] -= mean;
-        if (i < n) v = fmaf(x[k * V + i], x[k * V + i], v);
-      }
-    }
-    const float rstd = rsqrtf(block_sum(v, sm[1]) * inv_n + p.eps);
-    if (threadIdx.x == 0) {
-      if (p.mean) p.mean[r] = mean;
-      if (p.rstd) p.rstd[r] = rstd;
-    }
-    TY *y = static_cast<TY *>(p.y) + r * p.ldy;
-#pragma unroll
-    for (int k = 0; k < C; ++k) {
-      const int n = valid(k), c = col(k);
-      float o[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float g = kKeep ? gamma[k * V + i] : i < n ? load_param(p.gamma, p.param_type, c + i, 1.f) : 0.f;
-        const float b = kKeep ? beta[k * V + i] : i < n ? load_param(p.beta, p.param_type, c + i, 0.f) : 0.f;
-        o[i] = fmaf(x[k * V + i] * rstd, g, b);
-      }
-      if constexpr (V == 8) {
-        const float2 w[4] = {{o[0], o[1]}, {o[2], o[3]}, {o[4], o[5]}, {o[6], o[7]}};
-        store_eighth<TY>(y, p.ck, r, c, w, n);
-      } else {
-        store_chunk<TY, V>(y, c, o, n);
-        if (!p.ck.q) continue;
-        o[0] = n > 0 ? as_stored<TY>(o[0]) : 0.f;
-        const uint32_t e = q8_exponent(__reduce_max_sync(0xffffffffu, __float_as_uint(o[0]) & 0x7FFFFFFFu));
-        if (n > 0) p.ck.q[r * p.ck.ldq + c] = (int8_t)q8_quantise(o[0], q8_inverse(e), e);
-        if (n > 0 && (c & 31) == 0) p.ck.e[r * p.ck.lde + (c >> 5)] = (uint8_t)e;
-      }
-    }
-  }
-}
-
-// Rows whose x is whole 16-byte pieces (and y's and q's rows aligned), up to
-// 512 * NV * 8 values: as above, with the rows to come in a ring of slots that
-// bulk copies fill, since one row ahead in registers is not enough in flight
-// (3 blocks of 8 KB rows an SM: 24 KB, where the copy rate times the latency
-// asks for 40).  The first of a row's two barriers frees its slot.
+// Rows of up to 512 * NV * 8 values, at least 64, read once and kept in
+// registers until they are written.  A block of threads walks rows gridDim.x
+// apart, which come through a ring of slots that bulk copies fill (SlotRow);
+// one row ahead in registers instead was not enough in flight (3 blocks of
+// 8 KB rows an SM: 24 KB, where the copy rate times the latency asks for 40).
+// The first of a row's two barriers, the sums for its mean and its variance,
+// frees its slot.  gamma and beta stay in registers (NV <= 2) or in shared
+// memory as float32 (params_shared), else they are read again a row.
 //
 // THREADS bounds the block, and with it the registers so that 24 warps share
 // an SM (32 with NV = 1, 16 with NV = 4).
-template <typename TX, typename TY, int NV, int THREADS>
+template <typename TX, typename TY, int NV, int THREADS, int V>
 __global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 && THREADS <= 256 ? 768 / THREADS : 1)
-    ln_forward_ring_kernel(const LnForward p, const int stages, const uint32_t x_bytes, uint32_t *err,
-                           const uint64_t wait_limit_ns) {
+    ln_forward_ring_kernel(const LnForward p, const int stages, const uint32_t x_bytes, const int params_shared,
+                           uint32_t *err, const uint64_t wait_limit_ns) {
   constexpr bool kKeep = NV <= 2;
   extern __shared__ __align__(128) uint8_t slots[];
   __shared__ __align__(16) float sm[2][16];
   __shared__ __align__(8) uint64_t bars[kMaxStages];
   __shared__ volatile uint32_t abort_flag;
   griddep_launch_dependents();
-  const int T = blockDim.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t ring = smem_addr(slots), bar0 = smem_addr(bars);
+  float *shared_gamma = reinterpret_cast<float *>(slots + stages * x_bytes), *shared_beta = shared_gamma + p.cols;
   RingPlace use, put;  // put: thread 0's
   const float inv_n = 1.0f / (float)p.cols;
   if (threadIdx.x == 0) {
@@ -246,47 +148,70 @@ __global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 &&
   griddep_wait();
   const int64_t mine = (p.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // rows of this block, at least one
   const auto row_of = [&](int64_t i) { return (int64_t)blockIdx.x + i * gridDim.x; };
+  const auto x_row = [&](int64_t i) { return static_cast<const TX *>(p.x) + row_of(i) * p.ldx; };
   const auto fill = [&](int64_t i) {
     const uint32_t dst = ring + put.slot * x_bytes, bar = bar0 + 8u * put.slot;
     put.advance(stages);
-    mbar_arrive_expect_tx(bar, x_bytes);
-    bulk_load(dst, static_cast<const TX *>(p.x) + row_of(i) * p.ldx, x_bytes, bar);
+    const uint32_t bytes = SlotRow<TX, V, THREADS>::copy_bytes(x_row(i), p.cols);
+    mbar_arrive_expect_tx(bar, bytes);
+    SlotRow<TX, V, THREADS>::copy(dst, x_row(i), bytes, bar);
   };
   int64_t filled = mine < stages ? mine : stages;
   if (threadIdx.x == 0)
     for (int64_t i = 0; i < filled; ++i) fill(i);
-  const auto col = [&](int v) { return (v * T + (int)threadIdx.x) * 8; };
-  const auto param = [&](const void *src, int c, float absent) {
-    return make_float2(load_param(src, p.param_type, c, absent), load_param(src, p.param_type, c + 1, absent));
-  };
+  SlotRow<TX, V, THREADS> xr;
+  xr.init(p.cols);
+  xr.fetch_ends(x_row(0));
+  const auto gamma_at = [&](int c) { return c < p.cols ? load_param(p.gamma, p.param_type, c, 1.f) : 0.f; };
+  const auto beta_at = [&](int c) { return c < p.cols ? load_param(p.beta, p.param_type, c, 0.f) : 0.f; };
   float2 gamma[kKeep ? NV * 4 : 1], beta[kKeep ? NV * 4 : 1];
   if constexpr (kKeep) {
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const bool in = col(v) < p.cols;
-        gamma[v * 4 + j] = in ? param(p.gamma, col(v) + 2 * j, 1.f) : both(0.f);
-        beta[v * 4 + j] = in ? param(p.beta, col(v) + 2 * j, 0.f) : both(0.f);
+        const int c = group_col<V, THREADS>(v, 2 * j), d = group_col<V, THREADS>(v, 2 * j + 1);
+        gamma[v * 4 + j] = make_float2(gamma_at(c), gamma_at(d));
+        beta[v * 4 + j] = make_float2(beta_at(c), beta_at(d));
       }
+  } else if (params_shared) {
+    // read past the first row's barriers; eight columns in flight a thread
+    for (int c0 = threadIdx.x; c0 < p.cols; c0 += 8 * blockDim.x) {
+      float g[8], b[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        g[k] = gamma_at(c0 + k * blockDim.x);
+        b[k] = beta_at(c0 + k * blockDim.x);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int c = c0 + k * (int)blockDim.x;
+        if (c < p.cols) shared_gamma[c] = g[k], shared_beta[c] = b[k];
+      }
+    }
   }
   bool ok = true;
   int64_t done = 0;
   for (int64_t i = 0; i < mine; done = ++i, use.advance(stages)) {
     const int64_t r = row_of(i);
     ok = mbar_wait(bar0 + 8u * use.slot, use.parity, &abort_flag, err, wait_limit_ns);
+    uint8_t *slot = slots + use.slot * x_bytes;
+    const uint32_t off = xr.offset(x_row(i));
+    if constexpr (V == 1) {
+      if (ok) xr.put_ends(slot, off);
+      if (i + 1 < mine) xr.fetch_ends(x_row(i + 1));
+    }
     float2 x[NV * 4], s2 = both(0.f);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      Chunk<TX, 8> raw;  // past the row's end: column 0, left out of the sums
-      raw.load(slots + use.slot * x_bytes, col(v) < p.cols ? col(v) : 0);
-      float2 t = both(0.f);
+      float2 e[4], t = both(0.f);
+      xr.load(slot, off, v, p.cols, e);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        x[v * 4 + j] = raw.get2(j);
-        t = add2(t, x[v * 4 + j]);
+        x[v * 4 + j] = e[j];
+        t = add2(t, e[j]);
       }
-      s2 = add2(s2, col(v) < p.cols ? t : both(0.f));
+      s2 = add2(s2, V == 1 || group_col<V, THREADS>(v, 0) < p.cols ? t : both(0.f));
     }
     const float s = warp_sum(s2.x + s2.y);
     if (lane == 0) sm[0][warp] = s;
@@ -303,10 +228,15 @@ __global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 &&
       float2 t = both(0.f);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        x[v * 4 + j] = add2(x[v * 4 + j], both(-mean));
-        t = fma2(x[v * 4 + j], x[v * 4 + j], t);
+        float2 d = add2(x[v * 4 + j], both(-mean));
+        if constexpr (V == 1) {
+          if (group_col<V, THREADS>(v, 2 * j) >= p.cols) d.x = 0.f;
+          if (group_col<V, THREADS>(v, 2 * j + 1) >= p.cols) d.y = 0.f;
+        }
+        x[v * 4 + j] = d;
+        t = fma2(d, d, t);
       }
-      v2 = add2(v2, col(v) < p.cols ? t : both(0.f));
+      v2 = add2(v2, V == 1 || group_col<V, THREADS>(v, 0) < p.cols ? t : both(0.f));
     }
     const float var = warp_sum(v2.x + v2.y);
     if (lane == 0) sm[1][warp] = var;
@@ -317,18 +247,42 @@ __global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 &&
       if (p.rstd) p.rstd[r] = rstd;
     }
     TY *y = static_cast<TY *>(p.y) + r * p.ldy;
+    int8_t *q_row = p.ck.q + r * p.ck.ldq;
+    uint8_t *e_row = p.ck.e + r * p.ck.lde;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = col(v);
-      const bool in = c < p.cols;
-      float2 o[4];
+      const int c0 = group_col<V, THREADS>(v, 0);
+      float2 g[4], b[4], o[4];
+      if constexpr (kKeep) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 g = kKeep ? gamma[v * 4 + j] : in ? param(p.gamma, c + 2 * j, 1.f) : both(0.f);
-        const float2 b = kKeep ? beta[v * 4 + j] : in ? param(p.beta, c + 2 * j, 0.f) : both(0.f);
-        o[j] = fma2(mul2(x[v * 4 + j], both(rstd)), g, b);
+        for (int j = 0; j < 4; ++j) g[j] = gamma[v * 4 + j], b[j] = beta[v * 4 + j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int c = group_col<V, THREADS>(v, 2 * j), d = group_col<V, THREADS>(v, 2 * j + 1);
+          const int cs = c < p.cols ? c : 0, ds = d < p.cols ? d : 0;
+          g[j] = params_shared ? make_float2(shared_gamma[cs], shared_gamma[ds]) : make_float2(gamma_at(c), gamma_at(d));
+          b[j] = params_shared ? make_float2(shared_beta[cs], shared_beta[ds]) : make_float2(beta_at(c), beta_at(d));
+        }
       }
-      store_eighth<TY>(y, p.ck, r, c, o, in ? 8 : 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = fma2(mul2(x[v * 4 + j], both(rstd)), g[j], b[j]);
+      if constexpr (V == 8) {
+        store_eighth<TY>(y, p.ck, r, c0, o, c0 < p.cols ? 8 : 0);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int c = group_col<V, THREADS>(v, k);
+          const float w = (k & 1) ? o[k >> 1].y : o[k >> 1].x;
+          if (c < p.cols) store_value<TY>(y, c, w);
+          if (p.ck.q && c - lane < p.cols) {  // the warp's 32 columns are a block
+            const float h = c < p.cols ? as_stored<TY>(w) : 0.f;
+            const uint32_t e = q8_exponent(__reduce_max_sync(0xffffffffu, __float_as_uint(h) & 0x7FFFFFFFu));
+            if (c < p.cols) q_row[c] = (int8_t)q8_byte(h, q8_inverse(e), e);
+            if (lane == 0) e_row[c >> 5] = (uint8_t)e;
+          }
+        }
+      }
     }
   }
   if (!ok && threadIdx.x == 0) ring_drain(bar0, stages, use, filled - done);
@@ -353,52 +307,46 @@ unsigned persistent_grid(int per_sm, int64_t rows, int sms) {
   return (unsigned)(rows < most ? rows : most);
 }
 
-template <typename TX, typename TY, int NV, int V>
-cudaError_t run_rows(const LnForward &p, int threads, const OpContext &c) {
-  static std::atomic<uint64_t> known{0};
-  const auto kern = ln_forward_kernel<TX, TY, NV, V>;
-  return launch_ex(kern, dim3(persistent_grid(blocks_per_sm(kern, threads, 0, known), p.rows, c.sms)), dim3(threads), 0,
-                   c.st, 1, p);
-}
-
-template <typename TX, typename TY, int NV, int THREADS>
+template <typename TX, typename TY, int NV, int THREADS, int V>
 cudaError_t run_ring(const LnForward &p, const OpContext &c) {
   static std::atomic<uint64_t> known{0};
-  const auto kern = ln_forward_ring_kernel<TX, TY, NV, THREADS>;
-  const int eights = (p.cols + 7) / 8, threads = ((eights + NV - 1) / NV + 31) / 32 * 32;
-  const uint32_t x_bytes = (uint32_t)(p.cols * sizeof(TX));
-  // the rings of the blocks that registers allow share the memory
-  const int want = (NV == 1 ? 1024 : NV == 2 ? 768 : 512) / threads;
-  int64_t stages = kRingBytes / (want < 8 ? want : 8) / x_bytes;
+  const auto kern = ln_forward_ring_kernel<TX, TY, NV, THREADS, V>;
+  const int eights = (p.cols + 7) / 8, threads = V == 1 ? THREADS : ((eights + NV - 1) / NV + 31) / 32 * 32;
+  const uint32_t x_bytes = slot_bytes(p.cols, sizeof(TX), V == 8);
+  // the rings of the blocks that registers allow share the memory, with the
+  // parameters where those stay in it and two slots still fit
+  int want = (NV == 1 ? 1024 : NV == 2 ? 768 : 512) / threads;
+  want = want < 1 ? 1 : want > 8 ? 8 : want;
+  int64_t room = kRingBytes / want;
+  const int64_t param_bytes = NV > 2 && room - 8 * (int64_t)p.cols >= 2 * (int64_t)x_bytes ? 8 * (int64_t)p.cols : 0;
+  int64_t stages = (room - param_bytes) / x_bytes;
   stages = stages < 2 ? 2 : stages > kMaxStages ? kMaxStages : stages;
-  const size_t smem = (size_t)stages * x_bytes;
+  const size_t smem = (size_t)(stages * x_bytes + param_bytes);
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
   if (e != cudaSuccess) return e;
   return launch_ex(kern, dim3(persistent_grid(blocks_per_sm(kern, threads, smem, known), p.rows, c.sms)), dim3(threads),
-                   smem, c.st, 1, p, (int)stages, x_bytes, c.err, c.wait_limit_ns);
+                   smem, c.st, 1, p, (int)stages, x_bytes, param_bytes ? 1 : 0, c.err, c.wait_limit_ns);
+}
+
+template <typename TX, typename TY, int V>
+cudaError_t run_width(const LnForward &p, const OpContext &c) {
+  const int eights = (p.cols + 7) / 8;
+  if (eights <= 128) return run_ring<TX, TY, 1, 128, V>(p, c);
+  if (V == 1 && eights <= 256) return run_ring<TX, TY, 2, 128, 1>(p, c);
+  if (eights <= 512) return run_ring<TX, TY, 2, 256, V>(p, c);
+  return eights <= 1024 ? run_ring<TX, TY, 2, 512, V>(p, c) : run_ring<TX, TY, 4, 512, V>(p, c);
 }
 
 template <typename TX, typename TY>
 cudaError_t run_types(const LnForward &p, const OpContext &c) {
-  const int eights = (p.cols + 7) / 8;
-  const bool vec = rows_on(p.x, p.ldx, sizeof(TX), 16) && rows_on(p.y, p.ldy, sizeof(TY), 16) &&
+  const bool vec = p.cols % 8 == 0 && rows_on(p.x, p.ldx, sizeof(TX), 16) && rows_on(p.y, p.ldy, sizeof(TY), 16) &&
                    (!p.ck.q || rows_on(p.ck.q, p.ck.ldq, 1, 8));
-  if (eights > 4 * kMaxThreads) {
+  if (p.cols > 16384 || (!vec && p.cols < 64)) {
     const int64_t most = (int64_t)c.sms * 8;
     return launch_ex(ln_forward_any_kernel<TX, TY>, dim3((unsigned)(p.rows < most ? p.rows : most)), dim3(kAnyThreads),
                      0, c.st, 1, p);
   }
-  if (vec && p.cols % 8 == 0) {
-    if (eights <= 128) return run_ring<TX, TY, 1, 128>(p, c);
-    if (eights <= 512) return run_ring<TX, TY, 2, 256>(p, c);
-    return eights <= 2 * kMaxThreads ? run_ring<TX, TY, 2, kMaxThreads>(p, c) : run_ring<TX, TY, 4, kMaxThreads>(p, c);
-  }
-  // values per thread: 8 for rows of up to 256 threads, else 16, else 32
-  const int nv = eights <= 256 ? 1 : eights <= 2 * kMaxThreads ? 2 : 4;
-  const int threads = ((eights + nv - 1) / nv + 31) / 32 * 32;
-  if (nv == 1) return vec ? run_rows<TX, TY, 1, 8>(p, threads, c) : run_rows<TX, TY, 1, 1>(p, threads, c);
-  if (nv == 2) return vec ? run_rows<TX, TY, 2, 8>(p, threads, c) : run_rows<TX, TY, 2, 1>(p, threads, c);
-  return vec ? run_rows<TX, TY, 4, 8>(p, threads, c) : run_rows<TX, TY, 4, 1>(p, threads, c);
+  return vec ? run_width<TX, TY, 8>(p, c) : run_width<TX, TY, 1>(p, c);
 }
 
 }  // namespace

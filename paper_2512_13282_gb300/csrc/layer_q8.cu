@@ -28,8 +28,8 @@ __device__ __forceinline__ void half_block(int64_t h, int64_t halves, int64_t *r
   *c = (h - row * halves) * 16;
 }
 
-// VEC: rows of x start on 16 bytes and rows of q on 16; else any alignment.
-template <typename TX, bool VEC>
+// Rows of x and of q start on 16 bytes.
+template <typename TX>
 __global__ void __launch_bounds__(kQ8Threads)
     q8_save_kernel(const void *x, int64_t ldx, int64_t rows, int64_t cols, Q8Ref ck) {
   griddep_launch_dependents();
@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(kQ8Threads)
     const int n = !live || c >= cols ? 0 : (int)min((int64_t)16, cols - c);
     const TX *row = static_cast<const TX *>(x) + r * ldx;
     Chunk<TX, 16> raw;
-    if (VEC && n == 16)
+    if (n == 16)
       raw.load(row, c);
     else
       raw.load_part(row, c, n);
@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kQ8Threads)
     const uint2 wl = q8_pack8(lo, e), wh = q8_pack8(hi, e);
     const uint32_t w[4] = {wl.x, wl.y, wh.x, wh.y};
     int8_t *q = ck.q + r * ck.ldq + c;
-    if (VEC && n == 16) {
+    if (n == 16) {
       *reinterpret_cast<uint4 *>(q) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
 #pragma unroll
@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(kQ8Threads)
   }
 }
 
-template <typename TX, bool VEC>
+template <typename TX>
 __global__ void __launch_bounds__(kQ8Threads)
     q8_restore_kernel(Q8Ref ck, void *x, int64_t ldx, int64_t rows, int64_t cols) {
   griddep_launch_dependents();
@@ -88,13 +88,13 @@ __global__ void __launch_bounds__(kQ8Threads)
     const int8_t *q = ck.q + r * ck.ldq;
     const float scale = q8_scale(ck.e[r * ck.lde + (c >> 5)]);
     Chunk<Q8, 16> raw;
-    if (VEC && n == 16)
+    if (n == 16)
       raw.load(q, c);
     else
       raw.load_part(q, c, n);
     TX *row = static_cast<TX *>(x) + r * ldx;
     if constexpr (sizeof(TX) == 2) {
-      if (VEC && n == 16) {
+      if (n == 16) {
         const __nv_bfloat162 s = __float2bfloat162_rn(scale);
         uint32_t o[8];
 #pragma unroll
@@ -112,19 +112,64 @@ __global__ void __launch_bounds__(kQ8Threads)
     float v[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = raw.get(i) * scale;
-    if constexpr (VEC)
-      store_chunk<TX, 16>(row, c, v, n);
-    else
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i < n) store_value<TX>(row, c + i, v[i]);
+    store_chunk<TX, 16>(row, c, v, n);
   }
 }
 
-// Whether a matrix's rows, and with it a vector access per 16 elements, start
-// on 16-byte boundaries.
-bool rows16(const void *p, int64_t ld, int size) {
-  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * size % 16 == 0;
+// Any alignment: a warp takes kRun blocks of a row, a lane one value of each,
+// so that neighbouring lanes are neighbours in memory and kRun loads are in
+// flight a lane; a block's largest magnitude is one reduction over the warp.
+constexpr int kRun = 8;
+
+template <typename TX>
+__global__ void __launch_bounds__(kQ8Threads)
+    q8_save_any_kernel(const void *x, int64_t ldx, int64_t rows, int64_t cols, Q8Ref ck) {
+  griddep_launch_dependents();
+  griddep_wait();
+  const int lane = threadIdx.x & 31;
+  const int64_t runs = (cols + 32 * kRun - 1) / (32 * kRun), items = rows * runs;
+  const int64_t step = (int64_t)gridDim.x * (kQ8Threads / 32);
+  for (int64_t t = (int64_t)blockIdx.x * (kQ8Threads / 32) + (threadIdx.x >> 5); t < items; t += step) {
+    const int64_t r = t / runs, c0 = (t - r * runs) * (32 * kRun) + lane;
+    float v[kRun];
+#pragma unroll
+    for (int k = 0; k < kRun; ++k) v[k] = c0 + 32 * k < cols ? load_value<TX>(x, r * ldx + c0 + 32 * k) : 0.f;
+    int8_t *q = ck.q + r * ck.ldq;
+    uint8_t *ex = ck.e + r * ck.lde;
+#pragma unroll
+    for (int k = 0; k < kRun; ++k) {
+      const int64_t c = c0 + 32 * k;
+      const uint32_t e = q8_exponent(__reduce_max_sync(0xffffffffu, __float_as_uint(v[k]) & 0x7FFFFFFFu));
+      if (c < cols) q[c] = (int8_t)q8_byte(v[k], q8_inverse(e), e);
+      if (lane == 0 && c < cols) ex[c >> 5] = (uint8_t)e;
+    }
+  }
+}
+
+template <typename TX>
+__global__ void __launch_bounds__(kQ8Threads)
+    q8_restore_any_kernel(Q8Ref ck, void *x, int64_t ldx, int64_t rows, int64_t cols) {
+  griddep_launch_dependents();
+  griddep_wait();
+  const int lane = threadIdx.x & 31;
+  const int64_t runs = (cols + 32 * kRun - 1) / (32 * kRun), items = rows * runs;
+  const int64_t step = (int64_t)gridDim.x * (kQ8Threads / 32);
+  for (int64_t t = (int64_t)blockIdx.x * (kQ8Threads / 32) + (threadIdx.x >> 5); t < items; t += step) {
+    const int64_t r = t / runs, c0 = (t - r * runs) * (32 * kRun) + lane;
+    const int8_t *q = ck.q + r * ck.ldq;
+    const uint8_t *ex = ck.e + r * ck.lde;
+    float v[kRun];
+    uint32_t e[kRun];
+#pragma unroll
+    for (int k = 0; k < kRun; ++k) {
+      const int64_t c = c0 + 32 * k;
+      v[k] = c < cols ? (float)q[c] : 0.f;
+      e[k] = c < cols ? ex[c >> 5] : 0u;
+    }
+#pragma unroll
+    for (int k = 0; k < kRun; ++k)
+      if (c0 + 32 * k < cols) store_value<TX>(x, r * ldx + c0 + 32 * k, v[k] * q8_scale(e[k]));
+  }
 }
 
 struct Q8Launch {
@@ -133,13 +178,15 @@ struct Q8Launch {
   dim3 grid;
 };
 Q8Launch plan_q8(const Q8Ref &ck, const void *x, int64_t ldx, int x_type, int64_t rows, int64_t cols) {
-  Q8Launch l{rows, cols, rows16(x, ldx, x_type == GEMM_TYPE_BF16 ? 2 : 4) && rows16(ck.q, ck.ldq, 1), dim3(1)};
+  Q8Launch l{rows, cols, rows_on(x, ldx, x_type == GEMM_TYPE_BF16 ? 2 : 4, 16) && rows_on(ck.q, ck.ldq, 1, 16), dim3(1)};
   // rows that follow one another without a gap, in whole blocks: one long row
   if (cols % kQ8Block == 0 && ldx == cols && ck.ldq == cols && ck.lde == cols / kQ8Block) {
     l.cols = rows * cols;
     l.rows = 1;
   }
-  const int64_t items = l.rows * ((l.cols + 31) / 32 * 2), blocks = (items + kQ8Threads - 1) / kQ8Threads;
+  const int64_t items = l.vec ? l.rows * ((l.cols + 31) / 32 * 2)
+                              : l.rows * ((l.cols + 32 * kRun - 1) / (32 * kRun)) * 32;
+  const int64_t blocks = (items + kQ8Threads - 1) / kQ8Threads;
   l.grid.x = (unsigned)(blocks < (1 << 30) ? blocks : (1 << 30));
   return l;
 }
@@ -149,23 +196,19 @@ Q8Launch plan_q8(const Q8Ref &ck, const void *x, int64_t ldx, int x_type, int64_
 cudaError_t launch_q8_save(const void *x, int64_t ldx, int x_type, int64_t rows, int64_t cols, const Q8Ref &ck,
                            cudaStream_t st) {
   const Q8Launch l = plan_q8(ck, x, ldx, x_type, rows, cols);
-  const dim3 block(kQ8Threads);
-  if (x_type == GEMM_TYPE_BF16)
-    return l.vec ? launch_ex(q8_save_kernel<bf16, true>, l.grid, block, 0, st, 1, x, ldx, l.rows, l.cols, ck)
-                 : launch_ex(q8_save_kernel<bf16, false>, l.grid, block, 0, st, 1, x, ldx, l.rows, l.cols, ck);
-  return l.vec ? launch_ex(q8_save_kernel<float, true>, l.grid, block, 0, st, 1, x, ldx, l.rows, l.cols, ck)
-               : launch_ex(q8_save_kernel<float, false>, l.grid, block, 0, st, 1, x, ldx, l.rows, l.cols, ck);
+  const bool bf = x_type == GEMM_TYPE_BF16;
+  const auto kern = l.vec ? bf ? q8_save_kernel<bf16> : q8_save_kernel<float>
+                          : bf ? q8_save_any_kernel<bf16> : q8_save_any_kernel<float>;
+  return launch_ex(kern, l.grid, dim3(kQ8Threads), 0, st, 1, x, ldx, l.rows, l.cols, ck);
 }
 
 cudaError_t launch_q8_restore(const Q8Ref &ck, void *x, int64_t ldx, int x_type, int64_t rows, int64_t cols,
                               cudaStream_t st) {
   const Q8Launch l = plan_q8(ck, x, ldx, x_type, rows, cols);
-  const dim3 block(kQ8Threads);
-  if (x_type == GEMM_TYPE_BF16)
-    return l.vec ? launch_ex(q8_restore_kernel<bf16, true>, l.grid, block, 0, st, 1, ck, x, ldx, l.rows, l.cols)
-                 : launch_ex(q8_restore_kernel<bf16, false>, l.grid, block, 0, st, 1, ck, x, ldx, l.rows, l.cols);
-  return l.vec ? launch_ex(q8_restore_kernel<float, true>, l.grid, block, 0, st, 1, ck, x, ldx, l.rows, l.cols)
-               : launch_ex(q8_restore_kernel<float, false>, l.grid, block, 0, st, 1, ck, x, ldx, l.rows, l.cols);
+  const bool bf = x_type == GEMM_TYPE_BF16;
+  const auto kern = l.vec ? bf ? q8_restore_kernel<bf16> : q8_restore_kernel<float>
+                          : bf ? q8_restore_any_kernel<bf16> : q8_restore_any_kernel<float>;
+  return launch_ex(kern, l.grid, dim3(kQ8Threads), 0, st, 1, ck, x, ldx, l.rows, l.cols);
 }
 
 }  // namespace gb300

@@ -77,20 +77,20 @@ __device__ __forceinline__ uint32_t max_magnitude_bf16(const uint32_t (&w)[N]) {
   return max(t << 16, t & 0xFFFF0000u);
 }
 
-// round_half_even(x * inverse) of a finite block; 0 where the block holds a
-// NaN or an infinity; limited to 63 at the largest exponent (E = 122), where
-// 64 * 2^122 would be past float32.
-__device__ __forceinline__ int q8_quantise(float x, float inverse, uint32_t e) {
-  int v = __float2int_rn(x * inverse);
-  if (e >= 249u) v = e == 255u ? 0 : min(max(v, -63), 63);
-  return v;
+// The byte of a value of a block with exponent e: round_half_even(x * inverse),
+// 0 where the block holds a NaN or an infinity, limited to 63 at the largest
+// exponent (E = 122), where 64 * 2^122 would be past float32.  Rounded by
+// adding 1.5 * 2^23, where a float's unit in the last place is 1; what is left
+// in the sum's low byte is the result.  (min and max drop a NaN.)
+__device__ __forceinline__ uint32_t q8_byte(float x, float inverse, uint32_t e) {
+  constexpr float kMagic = 12582912.0f;
+  const float limit = e == 255u ? 0.f : e == 249u ? 63.f : 127.f;
+  const float v = fminf(fmaxf(fmaf(x, inverse, kMagic) - kMagic, -limit), limit);
+  return __float_as_uint(v + kMagic) & 0xFFu;
 }
 
 // The same for eight values of a block below the largest exponent, packed
-// (v[0].x in the low byte of `lo`).  Added to 1.5 * 2^23, where a float's unit
-// in the last place is 1, the exact product x * inverse is rounded to an
-// integer, ties to even, which is then the low byte of the sum: no conversion
-// instructions (a quarter of the rate).
+// (v[0].x in the low byte of x); rounded as in q8_byte.
 __device__ __forceinline__ uint2 q8_pack8(const float2 (&v)[4], float inverse) {
   const float2 scale = both(inverse), magic = both(12582912.0f);
   uint32_t w[2];
@@ -319,6 +319,107 @@ struct RingPlace {
 __device__ __forceinline__ void ring_drain(uint32_t bars, int stages, RingPlace use, int64_t pending) {
   for (; pending > 0; --pending, use.advance(stages))
     mbar_wait_drain(bars + 8u * use.slot, use.parity, 200ull * 1000 * 1000);
+}
+
+// A row of T values on its way through a ring slot, its elements taken in
+// groups of eight a thread.
+//
+// V = 8: rows start on 16 bytes and are whole 16-byte pieces.  The slot is the
+// row, group v of thread t the eight values from column (v * threads + t) * 8.
+//
+// V = 1: any alignment.  The slot keeps the row's place within 16 bytes, so
+// that a bulk copy brings the aligned pieces that lie wholly inside the row;
+// the ends, up to kEdge values on each side, are read by the threads that own
+// them, a row ahead, and put into the slot by them: a thread reads only its
+// own columns from a slot, so that takes no barrier.  Value i of group v is
+// column (v * 8 + i) * threads + t, neighbouring lanes being neighbours in
+// memory.  Rows have at least 2 * kEdge values.  Its blocks have exactly THREADS
+// threads, which makes every address of a thread's values a constant distance
+// from its first (the many small accesses of V = 1 cost instructions, not
+// bytes); with V = 8 THREADS is only the most.
+template <typename T, int V, int THREADS>
+struct SlotRow {
+  static constexpr int kSize = (int)sizeof(T), kEdge = 16 / kSize;
+  uint32_t head, tail;  // the ends' bits, fetched ahead
+  int tail_col;         // column of the tail value that this thread owns, or -1
+  __device__ __forceinline__ void init(int cols) {
+    const int c0 = cols - kEdge, d = ((int)threadIdx.x - c0 % THREADS + THREADS) % THREADS;
+    tail_col = d < kEdge ? c0 + d : -1;
+  }
+  __device__ __forceinline__ static uint32_t offset(const void *row) {
+    return V == 1 ? (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u : 0u;
+  }
+  // Thread 0: the copy into the slot at `dst`; bytes to expect.
+  __device__ __forceinline__ static uint32_t copy_bytes(const void *row, int cols) {
+    if constexpr (V != 1) return (uint32_t)cols * kSize;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(row), lo = (a + 15) & ~(uintptr_t)15;
+    return (uint32_t)(((a + (uintptr_t)cols * kSize) & ~(uintptr_t)15) - lo);
+  }
+  __device__ __forceinline__ static void copy(uint32_t dst, const void *row, uint32_t bytes, uint32_t bar) {
+    const uint32_t skip = (16u - offset(row)) & 15u;
+    bulk_load(dst + (skip ? 16u : 0u), static_cast<const char *>(row) + skip, bytes, bar);
+  }
+  __device__ __forceinline__ static uint32_t bits(const void *row, int c) {
+    if constexpr (kSize == 4) return static_cast<const uint32_t *>(row)[c];
+    if constexpr (kSize == 2) return static_cast<const uint16_t *>(row)[c];
+    return static_cast<const uint8_t *>(row)[c];
+  }
+  __device__ __forceinline__ static void put(uint8_t *at, uint32_t b) {
+    if constexpr (kSize == 4)
+      *reinterpret_cast<uint32_t *>(at) = b;
+    else if constexpr (kSize == 2)
+      *reinterpret_cast<uint16_t *>(at) = (uint16_t)b;
+    else
+      *at = (uint8_t)b;
+  }
+  __device__ __forceinline__ void fetch_ends(const void *row) {
+    if constexpr (V == 1) {
+      head = threadIdx.x < kEdge ? bits(row, threadIdx.x) : 0;
+      tail = tail_col >= 0 ? bits(row, tail_col) : 0;
+    }
+  }
+  // After the copy into the slot has been waited for.  The fence orders these
+  // writes before the copy that will refill the slot.
+  __device__ __forceinline__ void put_ends(uint8_t *slot, uint32_t off) const {
+    if constexpr (V == 1) {
+      if (threadIdx.x < kEdge) put(slot + off + threadIdx.x * kSize, head);
+      if (tail_col >= 0) put(slot + off + tail_col * kSize, tail);
+      if (threadIdx.x < kEdge || tail_col >= 0) fence_proxy_async_smem();
+    }
+  }
+  // Group v of the row; zero past the row's end (V = 8: the group at column 0
+  // instead, for the caller to leave out).
+  __device__ __forceinline__ static void load(const uint8_t *slot, uint32_t off, int v, int cols, float2 (&x)[4]) {
+    const int t = (int)threadIdx.x;
+    if constexpr (V == 8) {
+      const int c = (v * (int)blockDim.x + t) * 8;
+      Chunk<T, 8> raw;
+      raw.load(slot, c < cols ? c : 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = raw.get2(j);
+    } else {
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int c = (v * 8 + i) * THREADS + t;
+        Chunk<T, 1> raw;
+        raw.w[0] = 0;
+        if (c < cols) raw.load(slot + off, c);
+        e[i] = c < cols ? raw.get(0) : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = make_float2(e[2 * j], e[2 * j + 1]);
+    }
+  }
+};
+// Column of value i of group v (see SlotRow).
+template <int V, int THREADS>
+__device__ __forceinline__ int group_col(int v, int i) {
+  return V == 8 ? (v * (int)blockDim.x + (int)threadIdx.x) * 8 + i : (v * 8 + i) * THREADS + (int)threadIdx.x;
+}
+// Bytes of a slot for a row of cols values of `size` bytes.
+inline uint32_t slot_bytes(int64_t cols, int size, bool aligned) {
+  return (uint32_t)(aligned ? cols * size : (cols * size + 30) / 16 * 16);
 }
 
 constexpr int kMaxStages = 8;
