@@ -104,8 +104,10 @@ __global__ void __launch_bounds__(1024) ln_param_sum_kernel(const float *partial
   const int64_t c = (int64_t)blockIdx.x * 32 + i;
   const float *src = partials + (int64_t)blockIdx.y * parts * cols + c;
   float s = 0.f;
-  if (c < cols)
+  if (c < cols) {
+#pragma unroll 8
     for (int k = j; k < parts; k += 32) s += src[(int64_t)k * cols];
+  }
   sm[j][i] = s;
   __syncthreads();
   // warp j adds up column j: the 32 sums are added pairwise, in an order the
@@ -236,8 +238,7 @@ __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
       yr.load(slot + x_bytes, y_off, v, p.cols, d);
       float2 scale = both(st.rstd);
       if constexpr (kQ8 && V == 8) {
-        const int c = group_col<V, THREADS>(v, 0);
-        scale = both(st.rstd * q8_scale(exp_row[c < p.cols ? c >> 5 : 0]));
+        scale = both(st.rstd * q8_scale(exp_row[group_col<V, THREADS>(v, 0) >> 5]));
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -252,17 +253,15 @@ __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
     float2 a2 = both(0.f), b2 = both(0.f);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      float2 xh[4], d[4], a = both(0.f), b = both(0.f);
+      if (V == 8 && group_col<V, THREADS>(v, 0) >= p.cols) continue;
+      float2 xh[4], d[4];
       load(v, xh, d);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float2 g = mul2(d[j], gamma[v * 4 + j]);
-        a = add2(a, g);
-        b = fma2(g, xh[j], b);
+        a2 = add2(a2, g);
+        b2 = fma2(g, xh[j], b2);
       }
-      const bool in = V == 1 || group_col<V, THREADS>(v, 0) < p.cols;
-      a2 = add2(a2, in ? a : both(0.f));
-      b2 = add2(b2, in ? b : both(0.f));
     }
     const float a = warp_sum(a2.x + a2.y), b = warp_sum(b2.x + b2.y);
     if (lane == 0) sm[i & 1][warp] = make_float2(a, b);
@@ -277,6 +276,7 @@ __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
     TDX *dx = static_cast<TDX *>(p.dx) + row_of(i) * p.lddx;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
+      if (V == 8 && group_col<V, THREADS>(v, 0) >= p.cols) continue;
       float2 xh[4], d[4];
       float o[8];
       load(v, xh, d);
@@ -289,8 +289,7 @@ __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
         o[2 * j + 1] = r.y;
       }
       if constexpr (V == 8) {
-        const int c = group_col<V, THREADS>(v, 0);
-        if (c < p.cols) store_chunk<TDX, 8>(dx, c, o, 8);
+        store_chunk<TDX, 8>(dx, group_col<V, THREADS>(v, 0), o, 8);
       } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {

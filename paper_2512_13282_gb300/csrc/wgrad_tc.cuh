@@ -70,8 +70,26 @@ struct WgCfg {
 // by every access of the warp, along rows it is four (16-byte pieces) or one
 // or two (elements).
 
-// Base's values that this lane adds to the block at (y0, x), in 16-byte pieces
-// (base's rows come in whole ones): four words of bf16, eight of float32.
+// Base's values that this lane adds to the block at (y0, x) by elements (lane =
+// column): word i is row y0 + i.
+__device__ __forceinline__ void fetch_base_elements(const WgradParams &p, int64_t y0, int x, int lane, uint4 (&b)[8]) {
+  const int c = x + lane;
+  if (c >= p.tc.N) return;
+  uint32_t w[32] = {};
+  const int rows = (int)min((int64_t)32, p.tc.M - y0);
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (i < rows) {
+      const int64_t at = (y0 + i) * p.ldbase + c;
+      w[i] = p.out_bf16 ? (uint32_t) static_cast<const uint16_t *>(p.base)[at] << 16
+                        : static_cast<const uint32_t *>(p.base)[at];
+    }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
+
+// The same in 16-byte pieces (base's rows come in whole ones): four words of
+// bf16, eight of float32.
 __device__ __forceinline__ void fetch_base(const WgradParams &p, int64_t y0, int x, int lane, uint4 (&b)[8]) {
   if (p.out_bf16) {
     const int c = x + (lane & 3) * 8;
@@ -158,9 +176,11 @@ __device__ __forceinline__ void tma_out_with_base(const WgradParams &p, const CU
 }
 
 // The block at (y0, x) with any base and C: base added, rounded once, stored
-// element by element along rows (lane = column).
+// element by element along rows (lane = column).  AHEAD: b is as
+// fetch_base_elements left it.
+template <bool AHEAD>
 __device__ __forceinline__ void store_elements(const WgradParams &p, uint32_t buf, int lane, const uint32_t (&v)[32],
-                                               int y0, int x) {
+                                               const uint4 (&b)[8], int y0, int x) {
   if (lane == 0) bulk_wait_read_all();  // partials may still be leaving the buffer
   __syncwarp();
   stage_block(buf, lane, v);
@@ -169,11 +189,17 @@ __device__ __forceinline__ void store_elements(const WgradParams &p, uint32_t bu
   if (c >= p.tc.N) return;
   // base may be C itself, so loads cannot move above stores by themselves:
   // eight rows are read before the first of them is written
-  for (int r0 = 0; r0 < rows; r0 += 8) {
+#pragma unroll
+  for (int r0 = 0; r0 < 32; r0 += 8) {
+    if (r0 >= rows) break;
     float f[8], o[8] = {};
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(ld_shared_u32(block_piece(buf, r0 + i, lane >> 2) + (lane & 3) * 4));
-    if (p.base) {
+    if (AHEAD) {
+      const uint4 lo = b[r0 / 4], hi = b[r0 / 4 + 1];
+      const float4 l = as_float4(lo), h = as_float4(hi);
+      o[0] = l.x, o[1] = l.y, o[2] = l.z, o[3] = l.w, o[4] = h.x, o[5] = h.y, o[6] = h.z, o[7] = h.w;
+    } else if (p.base) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if (r0 + i < rows) {
@@ -389,7 +415,7 @@ __global__ void __launch_bounds__(kWgThreads, 1)
       const bool split = w.part != 0;  // partials of a split-tail tile, not C
       const int y0 = w.tm * Cfg::kTileM + (int)rank * kBM + quad * 32;  // first row of this warp
       const int col0 = w.tn * BN + colpart * CPT;
-      const bool with_base = p.out_tma == kOutTmaC && wp.base != nullptr && !split;
+      const bool with_base = wp.base != nullptr && !split && y0 < p.M;
       // Writes 32 columns of sums: of C, or of a tail tile's partials (compact
       // blocks: tile `slot`, row pitch BN).
       auto emit = [&](uint32_t(&v)[32], uint4(&base_words)[8], int c) {
@@ -398,7 +424,7 @@ __global__ void __launch_bounds__(kWgThreads, 1)
         if (split) {
           tma_out_words32<true>(&tmWs, ebuf, lane, v, colpart * CPT + c * 32,
                                 w.slot * Cfg::kTileM + (int)rank * kBM + quad * 32, w.split, true);
-        } else if (with_base) {
+        } else if (p.out_tma == kOutTmaC && wp.base) {
           if (in_range) tma_out_with_base<!SLABS>(wp, &tmOut, ebuf, lane, v, base_words, y0, x);
         } else if (p.out_tma == kOutTmaC) {
           if (wp.out_bf16)
@@ -406,7 +432,7 @@ __global__ void __launch_bounds__(kWgThreads, 1)
           else
             tma_out_words32<false>(&tmOut, ebuf, lane, v, x, y0, 0, in_range);
         } else if (in_range) {
-          store_elements(wp, ebuf, lane, v, y0, x);
+          store_elements<!SLABS>(wp, ebuf, lane, v, base_words, y0, x);
         }
       };
       auto release = [&](uint32_t b) {
@@ -423,9 +449,15 @@ __global__ void __launch_bounds__(kWgThreads, 1)
         // the next two blocks of base on their way meanwhile
         constexpr int kChunks = CPT / 32, kAhead = kChunks < 2 ? kChunks : 2;
         uint4 ahead[kAhead][8] = {};
+        const auto fetch = [&](int x, uint4(&b)[8]) {
+          if (p.out_tma == kOutTmaC)
+            fetch_base(wp, y0, x, lane, b);
+          else
+            fetch_base_elements(wp, y0, x, lane, b);
+        };
 #pragma unroll
         for (int c = 0; c < kAhead; ++c)
-          if (with_base) fetch_base(wp, y0, col0 + c * 32, lane, ahead[c]);
+          if (with_base) fetch(col0 + c * 32, ahead[c]);
         const uint32_t b = acc_cnt & 1u, aph = (acc_cnt >> 1) & 1u;
         if (!__all_sync(0xffffffffu, mbar_wait(accf_bar(b), aph, abort_flag, p.err, p.wait_limit_ns))) {
           ok = false;
@@ -438,7 +470,7 @@ __global__ void __launch_bounds__(kWgThreads, 1)
           tmem_ld<32>(tmem_base + b * BN + t_lane + colpart * CPT + c * 32, v);
           tmem_ld_wait();
           emit(v, ahead[c % kAhead], c);
-          if (with_base && c + kAhead < kChunks) fetch_base(wp, y0, col0 + (c + kAhead) * 32, lane, ahead[c % kAhead]);
+          if (with_base && c + kAhead < kChunks) fetch(col0 + (c + kAhead) * 32, ahead[c % kAhead]);
         }
         release(b);
       } else {
