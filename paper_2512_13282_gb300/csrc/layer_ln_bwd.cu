@@ -368,7 +368,7 @@ LnPlan plan_ln_backward(const LnBackward &p, int sms) {
       if (l.nv == 3) l.nv = 4;
     }
     int per_sm = ring_blocks(l.nv, l.aligned ? 8 : 1, l.threads);
-    per_sm = per_sm > 8 ? 8 : per_sm;
+    per_sm = per_sm > 16 ? 16 : per_sm;
     int64_t stages = kRingBytes / per_sm / (l.x_bytes + l.dy_bytes);
     if (stages < 2) {
       per_sm = 1;

@@ -112,24 +112,23 @@ __device__ __forceinline__ void store_eighth(TY *y, const Q8Ref &ck, int64_t r, 
   if (n > 0 && (c & 31) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
 }
 
-// Rows of up to 512 * NV * 8 values, at least 64, read once and kept in
-// registers until they are written.  A block of threads walks rows gridDim.x
-// apart, which come through a ring of slots that bulk copies fill (SlotRow);
-// one row ahead in registers instead was not enough in flight (3 blocks of
-// 8 KB rows an SM: 24 KB, where the copy rate times the latency asks for 40).
-// The first of a row's two barriers, the sums for its mean and its variance,
-// frees its slot.  gamma and beta stay in registers (NV <= 2) or in shared
-// memory as float32 (params_shared), else they are read again a row.
-//
-// THREADS bounds the block, and with it the registers so that 24 warps share
-// an SM (32 with NV = 1, 16 with NV = 4).
+// Rows of up to THREADS * NV * 8 values, at least 64 where V = 1, read once and
+// kept in registers until they are written.  A block of threads walks rows
+// gridDim.x apart, which come through a ring of slots that bulk copies fill
+// (SlotRow); one row ahead in registers instead was not enough in flight (3
+// blocks of 8 KB rows an SM: 24 KB, where the copy rate times the latency asks
+// for 40).  The first of a row's two barriers, the sums for its mean and its
+// variance, frees its slot.  gamma and beta stay in registers (NV = 1), else in
+// shared memory as float32 where the rings leave room (params_shared), so that
+// 1024 threads share an SM whatever the width: with 16 parameters a thread in
+// registers half as many fit (12288 wide: 96 us, now YY).
 template <typename TX, typename TY, int NV, int THREADS, int V>
-__global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 && THREADS <= 256 ? 768 / THREADS : 1)
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS)
     ln_forward_ring_kernel(const LnForward p, const int stages, const uint32_t x_bytes, const int params_shared,
                            uint32_t *err, const uint64_t wait_limit_ns) {
-  constexpr bool kKeep = NV <= 2;
+  constexpr bool kKeep = NV == 1;
   extern __shared__ __align__(128) uint8_t slots[];
-  __shared__ __align__(16) float sm[2][16];
+  __shared__ __align__(16) float sm[2][32];
   __shared__ __align__(8) uint64_t bars[kMaxStages];
   __shared__ volatile uint32_t abort_flag;
   griddep_launch_dependents();
@@ -143,7 +142,7 @@ __global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 &&
     abort_flag = 0;
     fence_mbar_init();
   }
-  if (threadIdx.x < 32) sm[threadIdx.x >> 4][threadIdx.x & 15] = 0.f;
+  if (threadIdx.x < 32) sm[0][threadIdx.x] = sm[1][threadIdx.x] = 0.f;
   __syncthreads();
   griddep_wait();
   const int64_t mine = (p.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // rows of this block, at least one
@@ -163,6 +162,10 @@ __global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 &&
   xr.init(p.cols);
   xr.fetch_ends(x_row(0));
   const auto gamma_at = [&](int c) { return c < p.cols ? load_param(p.gamma, p.param_type, c, 1.f) : 0.f; };
+  // place of column c's parameters in shared memory: where a lane takes eight,
+  // the first four of every eight and then the others, so that a warp's 16-byte
+  // reads follow one another
+  const auto param_at = [&](int c) { return V == 8 ? ((c >> 2) & 1) * (p.cols / 2) + (c >> 3) * 4 + (c & 3) : c; };
   const auto beta_at = [&](int c) { return c < p.cols ? load_param(p.beta, p.param_type, c, 0.f) : 0.f; };
   float2 gamma[kKeep ? NV * 4 : 1], beta[kKeep ? NV * 4 : 1];
   if constexpr (kKeep) {
@@ -186,7 +189,7 @@ __global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 &&
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const int c = c0 + k * (int)blockDim.x;
-        if (c < p.cols) shared_gamma[c] = g[k], shared_beta[c] = b[k];
+        if (c < p.cols) shared_gamma[param_at(c)] = g[k], shared_beta[param_at(c)] = b[k];
       }
     }
   }
@@ -257,12 +260,23 @@ __global__ void __launch_bounds__(THREADS, NV == 1 ? 1024 / THREADS : NV == 2 &&
 #pragma unroll
         for (int j = 0; j < 4; ++j) g[j] = gamma[v * 4 + j], b[j] = beta[v * 4 + j];
       } else {
+        if (V == 8 && params_shared) {
+          const int at = c0 < p.cols ? param_at(c0) : 0, half = p.cols / 2;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int c = group_col<V, THREADS>(v, 2 * j), d = group_col<V, THREADS>(v, 2 * j + 1);
-          const int cs = c < p.cols ? c : 0, ds = d < p.cols ? d : 0;
-          g[j] = params_shared ? make_float2(shared_gamma[cs], shared_gamma[ds]) : make_float2(gamma_at(c), gamma_at(d));
-          b[j] = params_shared ? make_float2(shared_beta[cs], shared_beta[ds]) : make_float2(beta_at(c), beta_at(d));
+          for (int h = 0; h < 2; ++h) {
+            const float4 gq = *reinterpret_cast<const float4 *>(shared_gamma + at + h * half);
+            const float4 bq = *reinterpret_cast<const float4 *>(shared_beta + at + h * half);
+            g[2 * h] = make_float2(gq.x, gq.y), g[2 * h + 1] = make_float2(gq.z, gq.w);
+            b[2 * h] = make_float2(bq.x, bq.y), b[2 * h + 1] = make_float2(bq.z, bq.w);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int c = group_col<V, THREADS>(v, 2 * j), d = group_col<V, THREADS>(v, 2 * j + 1);
+            const int cs = c < p.cols ? c : 0, ds = d < p.cols ? d : 0;
+            g[j] = params_shared ? make_float2(shared_gamma[cs], shared_gamma[ds]) : make_float2(gamma_at(c), gamma_at(d));
+            b[j] = params_shared ? make_float2(shared_beta[cs], shared_beta[ds]) : make_float2(beta_at(c), beta_at(d));
+          }
         }
       }
 #pragma unroll
@@ -315,10 +329,9 @@ cudaError_t run_ring(const LnForward &p, const OpContext &c) {
   const uint32_t x_bytes = slot_bytes(p.cols, sizeof(TX), V == 8);
   // the rings of the blocks that registers allow share the memory, with the
   // parameters where those stay in it and two slots still fit
-  int want = (NV == 1 ? 1024 : NV == 2 ? 768 : 512) / threads;
-  want = want < 1 ? 1 : want > 8 ? 8 : want;
-  int64_t room = kRingBytes / want;
-  const int64_t param_bytes = NV > 2 && room - 8 * (int64_t)p.cols >= 2 * (int64_t)x_bytes ? 8 * (int64_t)p.cols : 0;
+  const int want = 1024 / threads;
+  const int64_t room = kRingBytes / (want < 16 ? want : 16);
+  const int64_t param_bytes = NV > 1 && room - 8 * (int64_t)p.cols >= 2 * (int64_t)x_bytes ? 8 * (int64_t)p.cols : 0;
   int64_t stages = (room - param_bytes) / x_bytes;
   stages = stages < 2 ? 2 : stages > kMaxStages ? kMaxStages : stages;
   const size_t smem = (size_t)(stages * x_bytes + param_bytes);
@@ -334,7 +347,7 @@ cudaError_t run_width(const LnForward &p, const OpContext &c) {
   if (eights <= 128) return run_ring<TX, TY, 1, 128, V>(p, c);
   if (V == 1 && eights <= 256) return run_ring<TX, TY, 2, 128, 1>(p, c);
   if (eights <= 512) return run_ring<TX, TY, 2, 256, V>(p, c);
-  return eights <= 1024 ? run_ring<TX, TY, 2, 512, V>(p, c) : run_ring<TX, TY, 4, 512, V>(p, c);
+  return eights <= 1024 ? run_ring<TX, TY, 2, 512, V>(p, c) : run_ring<TX, TY, 2, 1024, V>(p, c);
 }
 
 template <typename TX, typename TY>

@@ -103,9 +103,7 @@ __global__ void __launch_bounds__(kQ8Threads)
           o[2 * i] = scale_bf16x2(o[2 * i], s);
           o[2 * i + 1] = scale_bf16x2(o[2 * i + 1], s);
         }
-        uint4 *d = reinterpret_cast<uint4 *>(row + c);
-        d[0] = make_uint4(o[0], o[1], o[2], o[3]);
-        d[1] = make_uint4(o[4], o[5], o[6], o[7]);
+        store_32_bytes(row + c, o);
         continue;
       }
     }

@@ -207,6 +207,20 @@ struct Chunk {
   __device__ __forceinline__ float2 get2(int i) const { return make_float2(get(2 * i), get(2 * i + 1)); }
 };
 
+// 32 bytes as eight words (any address that is a multiple of 16; one access
+// where it is one of 32).
+__device__ __forceinline__ void store_32_bytes(void *p, const uint32_t (&w)[8]) {
+  if ((reinterpret_cast<uintptr_t>(p) & 31) == 0) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(__cvta_generic_to_global(p)), "r"(w[0]),
+                 "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else {
+    uint4 *d = static_cast<uint4 *>(p);
+    d[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    d[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+
 // V consecutive results rounded to T and stored (address a multiple of V
 // elements); the first n of them, one by one, where n < V.
 template <typename T, int V>
