@@ -9,9 +9,10 @@ namespace {
 constexpr int kRowThreads = 256;
 constexpr int kRingThreads = 512;     // most threads a block of the register-resident kernels has
 // Blocks of the ring kernel that its registers are to leave room for: 1024
-// threads an SM with 8 values each (768 at any alignment), else 512.
+// threads an SM with 8 values each (768 at any alignment), else 512, or 384
+// with 32 values each.
 __host__ __device__ constexpr int ring_blocks(int nv, int v, int threads) {
-  return (nv > 1 ? 512 : v == 8 ? 1024 : 768) / threads;
+  return (nv == 4 && threads <= 128 ? 384 : nv > 1 ? 512 : v == 8 ? 1024 : 768) / threads;
 }
 
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -340,7 +341,7 @@ struct LnPlan {
 // Blocks that walk `rows` rows, `per_sm` at a time on an SM: every SM one
 // while there are few rows, more where each still has two rows to set against
 // the partial row that it writes and another kernel reads (1000 rows of 1500
-// from a checkpoint: XX us with 152 blocks, YY with 500).
+// from a checkpoint: 36 us with 152 blocks, 17.5 with 500).
 int row_blocks(int64_t rows, int sms, int per_sm) {
   const int64_t few = rows < sms ? rows : sms, many = ceil_div64(rows, 2), most = (int64_t)sms * per_sm;
   const int64_t want = many > few ? many : few;
@@ -354,18 +355,21 @@ LnPlan plan_ln_backward(const LnBackward &p, int sms) {
   const void *x = p.x ? p.x : (const void *)p.ck.q;
   const int64_t ldx = p.x ? p.ldx : p.ck.ldq;
   const int64_t eights = ceil_div64(p.cols, 8);
-  // few threads with more values each: a row's fixed costs (its barrier, the
-  // sums over lanes and warps) are paid by every warp
-  l.nv = eights <= 128 ? 1 : eights <= 2 * kRingThreads ? 2 : (int)ceil_div64(eights, kRingThreads);
   l.aligned = (int64_t)p.cols * sx % 16 == 0 && (int64_t)p.cols * sg % 16 == 0 && p.cols % 8 == 0 &&
               rows_on(x, ldx, sx, 16) && rows_on(p.dy, p.lddy, sg, 16) && rows_on(p.dx, p.lddx, so, 16);
+  // few threads with more values each: a row's fixed costs (its barrier, the
+  // sums over lanes and warps) are paid by every warp.  32768 x 1024: 51 us
+  // with 8 values a thread, 44 with 16; 32768 x 4096: 131 us with 16, 126 with
+  // 32, which take three blocks an SM where 16 take two, and so many rows that
+  // the third's partial sums do not matter (2048 x 4096: 19.8 and 21.5 us).
+  l.nv = eights <= (l.aligned ? 32 : 128) ? 1 : eights <= 2 * kRingThreads ? 2 : (int)ceil_div64(eights, kRingThreads);
+  if (l.aligned && eights > 256 && eights <= 512 && p.rows >= (int64_t)32 * sms) l.nv = 4;
   if (p.rows > 0 && l.nv <= 4 && (l.aligned || p.cols >= 64)) {
     l.x_bytes = slot_bytes(p.cols, sx, l.aligned);
     l.dy_bytes = slot_bytes(p.cols, sg, l.aligned);
     l.threads = (int)ceil_div64(ceil_div64(eights, l.nv), 32) * 32;
     if (!l.aligned) {  // one of the block sizes compiled
       l.threads = l.threads <= 128 ? 128 : l.threads <= 256 && l.nv == 2 ? 256 : 512;
-      if (l.nv == 3) l.nv = 4;
     }
     int per_sm = ring_blocks(l.nv, l.aligned ? 8 : 1, l.threads);
     per_sm = per_sm > 16 ? 16 : per_sm;
@@ -406,8 +410,10 @@ cudaError_t run_width(const LnBackward &p, const LnPlan &l, const OpContext &c) 
     return l.nv == 1   ? run_ring<TX, TDY, TDX, 1, 8, 128>(p, l, c)
            : l.nv == 2 ? run_ring<TX, TDY, TDX, 2, 8, 512>(p, l, c)
            : l.nv == 3 ? run_ring<TX, TDY, TDX, 3, 8, 512>(p, l, c)
-                       : run_ring<TX, TDY, TDX, 4, 8, 512>(p, l, c);
+           : l.threads <= 128 ? run_ring<TX, TDY, TDX, 4, 8, 128>(p, l, c)
+                              : run_ring<TX, TDY, TDX, 4, 8, 512>(p, l, c);
   if (l.nv == 1) return run_ring<TX, TDY, TDX, 1, 1, 128>(p, l, c);
+  if (l.nv == 3) return run_ring<TX, TDY, TDX, 3, 1, 512>(p, l, c);
   if (l.nv == 4) return run_ring<TX, TDY, TDX, 4, 1, 512>(p, l, c);
   return l.threads == 128   ? run_ring<TX, TDY, TDX, 2, 1, 128>(p, l, c)
          : l.threads == 256 ? run_ring<TX, TDY, TDX, 2, 1, 256>(p, l, c)
