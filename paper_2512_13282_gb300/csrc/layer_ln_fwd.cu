@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
 // shape and shared memory size (the devices served are all the same).
 template <typename K>
 int blocks_per_sm(K kern, int threads, size_t smem, std::atomic<uint64_t> &known) {
-  const uint64_t key = (uint64_t)smem << 16 | (uint64_t)threads << 8;
+  const uint64_t key = (uint64_t)smem << 24 | (uint64_t)threads << 8;
   const uint64_t k = known.load(std::memory_order_relaxed);
   if ((k & ~(uint64_t)0xFF) == key && (k & 0xFF)) return (int)(k & 0xFF);
   int n = 0;
