@@ -8,6 +8,9 @@ namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int kRingThreads = 512;     // most threads a block of the register-resident kernels has
+// Floats from one partial row to the next: whole strips of 32 columns.
+__host__ __device__ constexpr int partial_pitch(int cols) { return (cols + 31) / 32 * 32; }
+
 // Blocks of the ring kernel that its registers are to leave room for: 1024
 // threads an SM with 8 values each (768 at any alignment), else 512, or 384
 // with 32 values each.
@@ -62,7 +65,7 @@ __global__ void __launch_bounds__(kRowThreads) ln_backward_any_kernel(const LnBa
 // Partial dgamma and dbeta of a strip of 32 columns over every gridDim.y-th
 // group of 8 rows: thread (i, j) walks column i of rows j, j + 8 gridDim.y,
 // ...; the eight partial sums are added in order.  Partials: gridDim.y rows
-// of dgamma, then as many of dbeta, cols floats each.
+// of dgamma, then as many of dbeta, pitch partial_pitch(cols).
 template <typename TX, typename TDY>
 __global__ void __launch_bounds__(kRowThreads) ln_param_partials_kernel(const LnBackward p) {
   __shared__ float2 sm[8][32];
@@ -86,36 +89,51 @@ __global__ void __launch_bounds__(kRowThreads) ln_param_partials_kernel(const Ln
       dg += sm[k][i].x;
       db += sm[k][i].y;
     }
-    p.partials[(int64_t)blockIdx.y * p.cols + c] = dg;
-    p.partials[(int64_t)(gridDim.y + blockIdx.y) * p.cols + c] = db;
+    const int64_t pitch = partial_pitch(p.cols);
+    p.partials[blockIdx.y * pitch + c] = dg;
+    p.partials[(gridDim.y + blockIdx.y) * pitch + c] = db;
   }
 }
 
-// dgamma (blockIdx.y 0) or dbeta (1): `parts` rows of partials summed.  A
-// block takes 32 columns; its 32 warps each add every 32nd row, and the 32
-// sums are added in order.
-__global__ void __launch_bounds__(1024) ln_param_sum_kernel(const float *partials, int parts, int cols, float *dgamma,
-                                                            float *dbeta) {
-  __shared__ float sm[32][33];
+// dgamma (blockIdx.y 0) or dbeta (1): `parts` rows of partials (pitch
+// partial_pitch) summed.  A block takes 32 columns; a warp reads four rows at a
+// time, eight lanes a row in 16-byte pieces, the block 128 rows.  Blocks are
+// large on purpose: launched while the kernel before is ending, small ones
+// crowd on the SMs that it leaves first (8192 x 4096: 52 us a backward pass
+// with blocks of 256, 38 with these).  The sums are joined in an order that the
+// lanes' and warps' numbers fix.
+constexpr int kSumThreads = 1024;
+__global__ void __launch_bounds__(kSumThreads) ln_param_sum_kernel(const float *partials, int parts, int cols, int pitch,
+                                                                   float *dgamma, float *dbeta) {
+  __shared__ float sm[32][33];  // [warp][column]
   griddep_launch_dependents();
   griddep_wait();
   float *out = blockIdx.y == 0 ? dgamma : dbeta;
   if (!out) return;
-  const int i = threadIdx.x & 31, j = threadIdx.x >> 5;
-  const int64_t c = (int64_t)blockIdx.x * 32 + i;
-  const float *src = partials + (int64_t)blockIdx.y * parts * cols + c;
-  float s = 0.f;
-  if (c < cols) {
-#pragma unroll 8
-    for (int k = j; k < parts; k += 32) s += src[(int64_t)k * cols];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane & 7;
+  const float4 *src =
+      reinterpret_cast<const float4 *>(partials + (int64_t)blockIdx.y * parts * pitch + (int64_t)blockIdx.x * 32) + piece;
+  float2 lo = both(0.f), hi = lo;
+#pragma unroll 4
+  for (int k = warp * 4 + (lane >> 3); k < parts; k += kSumThreads / 8) {
+    const float4 v = src[(int64_t)k * (pitch / 4)];
+    lo = add2(lo, make_float2(v.x, v.y));
+    hi = add2(hi, make_float2(v.z, v.w));
   }
-  sm[j][i] = s;
+#pragma unroll
+  for (int o = 8; o <= 16; o <<= 1) {
+    lo = add2(lo, make_float2(__shfl_xor_sync(0xffffffffu, lo.x, o), __shfl_xor_sync(0xffffffffu, lo.y, o)));
+    hi = add2(hi, make_float2(__shfl_xor_sync(0xffffffffu, hi.x, o), __shfl_xor_sync(0xffffffffu, hi.y, o)));
+  }
+  if (lane < 8) {
+    float *at = &sm[warp][piece * 4];
+    at[0] = lo.x, at[1] = lo.y, at[2] = hi.x, at[3] = hi.y;
+  }
   __syncthreads();
-  // warp j adds up column j: the 32 sums are added pairwise, in an order the
-  // lane numbers fix
-  const float t = warp_sum(sm[i][j]);
-  const int64_t cj = (int64_t)blockIdx.x * 32 + j;
-  if (i == 0 && cj < cols) out[cj] = t;
+  // warp w adds up column w
+  const float s = warp_sum(sm[lane][warp]);
+  const int64_t c = (int64_t)blockIdx.x * 32 + warp;
+  if (lane == 0 && c < cols) out[c] = s;
 }
 
 // Row r's mean and 1/std as the factors of xh = x * rstd - mean * rstd.
@@ -305,7 +323,8 @@ __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
     return;
   }
   if (!p.partials) return;
-  float *dg_out = p.partials + (int64_t)blockIdx.x * p.cols, *db_out = dg_out + (int64_t)gridDim.x * p.cols;
+  float *dg_out = p.partials + (int64_t)blockIdx.x * partial_pitch(p.cols);
+  float *db_out = dg_out + (int64_t)gridDim.x * partial_pitch(p.cols);
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     if constexpr (V == 8) {
@@ -441,14 +460,14 @@ cudaError_t run_types(const LnBackward &p, const OpContext &c, int *launches) {
     if (e != cudaSuccess) return e;
   }
   ++*launches;
-  return launch_ex(ln_param_sum_kernel, dim3(strips, 2), dim3(1024), 0, c.st, 1, (const float *)p.partials, l.parts,
-                   p.cols, p.dgamma, p.dbeta);
+  return launch_ex(ln_param_sum_kernel, dim3(strips, 2), dim3(kSumThreads), 0, c.st, 1, (const float *)p.partials,
+                   l.parts, p.cols, partial_pitch(p.cols), p.dgamma, p.dbeta);
 }
 
 }  // namespace
 
 size_t ln_backward_partials(const LnBackward &p, int sms) {
-  return p.dgamma || p.dbeta ? (size_t)2 * plan_ln_backward(p, sms).parts * p.cols : 0;
+  return p.dgamma || p.dbeta ? (size_t)2 * plan_ln_backward(p, sms).parts * partial_pitch(p.cols) : 0;
 }
 
 cudaError_t launch_ln_backward(const LnBackward &p, const OpContext &c, int *launches) {
