@@ -8,6 +8,10 @@ namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int kRingThreads = 512;     // most threads a block of the register-resident kernels has
+// Rows that the ring kernel takes at a time, between two barriers, where the
+// ring has slots for twice as many: two where registers allow.
+__host__ __device__ constexpr int most_rows(int nv, int v) { return v == 8 && nv <= 2 ? 2 : 1; }
+
 // Floats from one partial row to the next: whole strips of 32 columns.
 __host__ __device__ constexpr int partial_pitch(int cols) { return (cols + 31) / 32 * 32; }
 
@@ -97,14 +101,16 @@ __global__ void __launch_bounds__(kRowThreads) ln_param_partials_kernel(const Ln
 
 // dgamma (blockIdx.y 0) or dbeta (1): `parts` rows of partials (pitch
 // partial_pitch) summed.  A block takes 32 columns; a warp reads four rows at a
-// time, eight lanes a row in 16-byte pieces, the block 128 rows.  Blocks are
-// large on purpose: launched while the kernel before is ending, small ones
-// crowd on the SMs that it leaves first (8192 x 4096: 52 us a backward pass
-// with blocks of 256, 38 with these).  The sums are joined in an order that the
+// time, eight lanes a row in 16-byte pieces.  Many partial rows want the large
+// blocks: launched while the kernel before is ending, small ones crowd on the
+// SMs that it leaves first (8192 x 4096, 456 partial rows: 52 us a backward
+// pass with blocks of 256, 38 of 1024); one partial row an SM wants the small
+// ones (8192 x 12288: 95 and 98 us).  The sums are joined in an order that the
 // lanes' and warps' numbers fix.
-constexpr int kSumThreads = 1024;
-__global__ void __launch_bounds__(kSumThreads) ln_param_sum_kernel(const float *partials, int parts, int cols, int pitch,
-                                                                   float *dgamma, float *dbeta) {
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) ln_param_sum_kernel(const float *partials, int parts, int cols, int pitch,
+                                                               float *dgamma, float *dbeta) {
+  constexpr int kWarps = THREADS / 32;
   __shared__ float sm[32][33];  // [warp][column]
   griddep_launch_dependents();
   griddep_wait();
@@ -115,7 +121,7 @@ __global__ void __launch_bounds__(kSumThreads) ln_param_sum_kernel(const float *
       reinterpret_cast<const float4 *>(partials + (int64_t)blockIdx.y * parts * pitch + (int64_t)blockIdx.x * 32) + piece;
   float2 lo = both(0.f), hi = lo;
 #pragma unroll 4
-  for (int k = warp * 4 + (lane >> 3); k < parts; k += kSumThreads / 8) {
+  for (int k = warp * 4 + (lane >> 3); k < parts; k += THREADS / 8) {
     const float4 v = src[(int64_t)k * (pitch / 4)];
     lo = add2(lo, make_float2(v.x, v.y));
     hi = add2(hi, make_float2(v.z, v.w));
@@ -130,10 +136,13 @@ __global__ void __launch_bounds__(kSumThreads) ln_param_sum_kernel(const float *
     at[0] = lo.x, at[1] = lo.y, at[2] = hi.x, at[3] = hi.y;
   }
   __syncthreads();
-  // warp w adds up column w
-  const float s = warp_sum(sm[lane][warp]);
-  const int64_t c = (int64_t)blockIdx.x * 32 + warp;
-  if (lane == 0 && c < cols) out[c] = s;
+  // warp w adds up columns w, w + kWarps, ...
+#pragma unroll
+  for (int w = warp; w < 32; w += kWarps) {
+    const float s = warp_sum(lane < kWarps ? sm[lane][w] : 0.f);
+    const int64_t c = (int64_t)blockIdx.x * 32 + w;
+    if (lane == 0 && c < cols) out[c] = s;
+  }
 }
 
 // Row r's mean and 1/std as the factors of xh = x * rstd - mean * rstd.
@@ -150,18 +159,19 @@ struct RowStats {
 // rows in flight.  A row is read from its slot twice, for the two averages and
 // for the results; the block-wide barrier between, passed by every thread once
 // it has finished with the row before, also frees that row's slot, which
-// thread 0 refills.  One partial row of dgamma and of dbeta a block goes to the
+// thread 0 refills.  `step` rows are taken between two barriers.  One partial row of dgamma and of dbeta a block goes to the
 // workspace.
 template <typename TX, typename TDY, typename TDX, int NV, int V, int THREADS>
 __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
-    ln_backward_ring_kernel(const LnBackward p, const int stages, const uint32_t x_bytes, const uint32_t dy_bytes,
-                            uint32_t *err, const uint64_t wait_limit_ns) {
+    ln_backward_ring_kernel(const LnBackward p, const int stages, const int step, const uint32_t x_bytes,
+                            const uint32_t dy_bytes, uint32_t *err, const uint64_t wait_limit_ns) {
   constexpr bool kQ8 = sizeof(TX) == 1;
+  constexpr int R = most_rows(NV, V);  // step is at most that
   extern __shared__ __align__(128) uint8_t slots[];
-  __shared__ __align__(16) float2 sm[2][16];
-  // block exponents of three rows: being read, still being read by a thread
-  // that is behind, and being written
-  __shared__ uint8_t exps[kQ8 ? 3 : 1][kQ8 ? 512 : 1];
+  __shared__ __align__(16) float2 sm[2][R][16];
+  // block exponents of three steps' rows: being read, still being read by a
+  // thread that is behind, and being written
+  __shared__ uint8_t exps[kQ8 ? 3 : 1][R][kQ8 ? 512 : 1];
   __shared__ __align__(8) uint64_t bars[kMaxStages];
   __shared__ volatile uint32_t abort_flag;
   griddep_launch_dependents();
@@ -174,7 +184,7 @@ __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
     abort_flag = 0;
     fence_mbar_init();
   }
-  if (threadIdx.x < 32) sm[threadIdx.x >> 4][threadIdx.x & 15] = make_float2(0.f, 0.f);
+  for (int i = threadIdx.x; i < 2 * R * 16; i += blockDim.x) (&sm[0][0][0])[i] = make_float2(0.f, 0.f);
   __syncthreads();
   griddep_wait();
   const int64_t mine = (p.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // rows of this block, at least one
@@ -198,24 +208,36 @@ __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
   if (threadIdx.x == 0)
     for (int64_t i = 0; i < filled; ++i) fill(i);
 
-  // fetched a row ahead: the statistics and the rows' ends; two rows ahead, on
-  // their way through shared memory: the block exponents
+  // fetched a step ahead: the statistics and the rows' ends; two steps ahead,
+  // on their way through shared memory: the block exponents
   SlotRow<TX, V, THREADS> xr;
   SlotRow<TDY, V, THREADS> yr;
   xr.init(p.cols);
   yr.init(p.cols);
-  float2 st_next = make_float2(p.mean[row_of(0)], p.rstd[row_of(0)]);
-  xr.fetch_ends(x_row(0));
-  yr.fetch_ends(dy_row(0));
+  float2 st_next[R];
+  const auto fetch = [&](int64_t i) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (r < step && i + r < mine) st_next[r] = make_float2(p.mean[row_of(i + r)], p.rstd[row_of(i + r)]);
+    if (V == 1 && i < mine) {  // one row a step
+      xr.fetch_ends(x_row(i));
+      yr.fetch_ends(dy_row(i));
+    }
+  };
+  fetch(0);
   const int blocks = (p.cols + 31) / 32;  // at most one a thread
   const auto exp_at = [&](int64_t i) -> uint32_t {
     return kQ8 && i < mine && (int)threadIdx.x < blocks ? p.ck.e[row_of(i) * p.ck.lde + threadIdx.x] : 0u;
   };
-  uint32_t exp_next = 0;
+  uint32_t exp_next[R] = {};
   int exp_use = 0;
   if constexpr (kQ8) {
-    if ((int)threadIdx.x < blocks) exps[0][threadIdx.x] = (uint8_t)exp_at(0);
-    exp_next = exp_at(1);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r >= step) break;
+      if ((int)threadIdx.x < blocks) exps[0][r][threadIdx.x] = (uint8_t)exp_at(r);
+      exp_next[r] = exp_at(step + r);
+    }
     __syncthreads();
   }
   float2 gamma[NV * 4], dg[NV * 4], db[NV * 4];
@@ -230,90 +252,131 @@ __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
   }
   bool ok = true;
   int64_t done = 0;
-  for (int64_t i = 0; i < mine; done = ++i, use.advance(stages)) {
-    uint8_t *slot = slots + use.slot * both_bytes;
-    const RowStats st(st_next);
-    const uint32_t x_off = xr.offset(x_row(i)), y_off = yr.offset(dy_row(i));
-    ok = mbar_wait(bar0 + 8u * use.slot, use.parity, &abort_flag, err, wait_limit_ns);
-    if (ok) {
-      xr.put_ends(slot, x_off);
-      yr.put_ends(slot + x_bytes, y_off);
+  int buf = 0;
+  for (int64_t i = 0; i < mine; i += step, done = i, buf ^= 1) {
+    // rows i .. i + step - 1: their slots, statistics and what is past the end
+    uint8_t *slot[R];
+    uint32_t x_off[R], y_off[R];
+    bool here[R];
+    float2 st[R];
+    RingPlace place = use;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      here[r] = r < step && i + r < mine;
+      st[r] = st_next[r];
+      slot[r] = slots + place.slot * both_bytes;
+      x_off[r] = y_off[r] = 0;
+      if (!here[r]) continue;
+      ok = mbar_wait(bar0 + 8u * place.slot, place.parity, &abort_flag, err, wait_limit_ns) && ok;
+      place.advance(stages);
+      if constexpr (V == 1) {
+        x_off[r] = xr.offset(x_row(i));
+        y_off[r] = yr.offset(dy_row(i));
+        if (ok) {
+          xr.put_ends(slot[r], x_off[r]);
+          yr.put_ends(slot[r] + x_bytes, y_off[r]);
+        }
+      }
     }
-    if (i + 1 < mine) {
-      st_next = make_float2(p.mean[row_of(i + 1)], p.rstd[row_of(i + 1)]);
-      xr.fetch_ends(x_row(i + 1));
-      yr.fetch_ends(dy_row(i + 1));
-    }
-    const uint8_t *exp_row = exps[0];
+    fetch(i + step);
+    const uint8_t(*exp_rows)[kQ8 ? 512 : 1] = exps[0];
     if constexpr (kQ8) {
-      exp_row = exps[exp_use];
+      exp_rows = exps[exp_use];
       exp_use = exp_use == 2 ? 0 : exp_use + 1;
-      if ((int)threadIdx.x < blocks) exps[exp_use][threadIdx.x] = (uint8_t)exp_next;
-      exp_next = exp_at(i + 2);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (r >= step) break;
+        if ((int)threadIdx.x < blocks) exps[exp_use][r][threadIdx.x] = (uint8_t)exp_next[r];
+        exp_next[r] = exp_at(i + 2 * step + r);
+      }
     }
-    // x as xh and dy of group v
-    const auto load = [&](int v, float2(&xh)[4], float2(&d)[4]) {
-      xr.load(slot, x_off, v, p.cols, xh);
-      yr.load(slot + x_bytes, y_off, v, p.cols, d);
-      float2 scale = both(st.rstd);
+    // x as xh and dy of group v of row r of the step
+    const auto load = [&](int r, int v, float2(&xh)[4], float2(&d)[4]) {
+      const RowStats stats(st[r]);
+      xr.load(slot[r], x_off[r], v, p.cols, xh);
+      yr.load(slot[r] + x_bytes, y_off[r], v, p.cols, d);
+      float2 scale = both(stats.rstd);
       if constexpr (kQ8 && V == 8) {
-        scale = both(st.rstd * q8_scale(exp_row[group_col<V, THREADS>(v, 0) >> 5]));
+        scale = both(stats.rstd * q8_scale(exp_rows[r][group_col<V, THREADS>(v, 0) >> 5]));
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if constexpr (kQ8 && V == 1) {
           const int c = group_col<V, THREADS>(v, 2 * j), e = group_col<V, THREADS>(v, 2 * j + 1);
-          scale = make_float2(st.rstd * q8_scale(exp_row[c < p.cols ? c >> 5 : 0]),
-                              st.rstd * q8_scale(exp_row[e < p.cols ? e >> 5 : 0]));
+          scale = make_float2(stats.rstd * q8_scale(exp_rows[r][c < p.cols ? c >> 5 : 0]),
+                              stats.rstd * q8_scale(exp_rows[r][e < p.cols ? e >> 5 : 0]));
         }
-        xh[j] = fma2(xh[j], scale, both(st.shift));
+        xh[j] = fma2(xh[j], scale, both(stats.shift));
       }
     };
-    float2 a2 = both(0.f), b2 = both(0.f);
+    float a[R], b[R];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (V == 8 && group_col<V, THREADS>(v, 0) >= p.cols) continue;
-      float2 xh[4], d[4];
-      load(v, xh, d);
+    for (int r = 0; r < R; ++r) {
+      float2 a2 = both(0.f), b2 = both(0.f);
+      if (here[r]) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 g = mul2(d[j], gamma[v * 4 + j]);
-        a2 = add2(a2, g);
-        b2 = fma2(g, xh[j], b2);
+        for (int v = 0; v < NV; ++v) {
+          if (V == 8 && group_col<V, THREADS>(v, 0) >= p.cols) continue;
+          float2 xh[4], d[4];
+          load(r, v, xh, d);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 g = mul2(d[j], gamma[v * 4 + j]);
+            a2 = add2(a2, g);
+            b2 = fma2(g, xh[j], b2);
+          }
+        }
       }
+      a[r] = a2.x + a2.y;
+      b[r] = b2.x + b2.y;
     }
-    const float a = warp_sum(a2.x + a2.y), b = warp_sum(b2.x + b2.y);
-    if (lane == 0) sm[i & 1][warp] = make_float2(a, b);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        a[r] += __shfl_xor_sync(0xffffffffu, a[r], o);
+        b[r] += __shfl_xor_sync(0xffffffffu, b[r], o);
+      }
+    if (lane == 0) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) sm[buf][r][warp] = make_float2(a[r], b[r]);
+    }
     // every wait of the block succeeded, or the block gives up together
     if (!__syncthreads_and(ok)) {
       ok = false;
       break;
     }
-    if (threadIdx.x == 0 && i > 0 && filled < mine) fill(filled++);  // the slot of row i - 1
-    const float2 s = sum_over_warps<THREADS / 32>(sm[i & 1]);
-    const float2 ga = both(-s.x * inv_n * st.rstd), gx = both(-s.y * inv_n * st.rstd), rstd = both(st.rstd);
-    TDX *dx = static_cast<TDX *>(p.dx) + row_of(i) * p.lddx;
+    if (threadIdx.x == 0 && i > 0)  // the slots of the step before
+      for (int r = 0; r < step && filled < mine; ++r) fill(filled++);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (V == 8 && group_col<V, THREADS>(v, 0) >= p.cols) continue;
-      float2 xh[4], d[4];
-      float o[8];
-      load(v, xh, d);
+    for (int r = 0; r < R; ++r) {
+      if (!here[r]) continue;
+      use.advance(stages);
+      const float2 s = sum_over_warps<THREADS / 32>(sm[buf][r]);
+      const float2 ga = both(-s.x * inv_n * st[r].y), gx = both(-s.y * inv_n * st[r].y), rstd = both(st[r].y);
+      TDX *dx = static_cast<TDX *>(p.dx) + row_of(i + r) * p.lddx;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        dg[v * 4 + j] = fma2(d[j], xh[j], dg[v * 4 + j]);
-        db[v * 4 + j] = add2(db[v * 4 + j], d[j]);
-        const float2 r = fma2(mul2(d[j], gamma[v * 4 + j]), rstd, fma2(xh[j], gx, ga));
-        o[2 * j] = r.x;
-        o[2 * j + 1] = r.y;
-      }
-      if constexpr (V == 8) {
-        store_chunk<TDX, 8>(dx, group_col<V, THREADS>(v, 0), o, 8);
-      } else {
+      for (int v = 0; v < NV; ++v) {
+        if (V == 8 && group_col<V, THREADS>(v, 0) >= p.cols) continue;
+        float2 xh[4], d[4];
+        float o[8];
+        load(r, v, xh, d);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int c = group_col<V, THREADS>(v, k);
-          if (c < p.cols) store_value<TDX>(dx, c, o[k]);
+        for (int j = 0; j < 4; ++j) {
+          dg[v * 4 + j] = fma2(d[j], xh[j], dg[v * 4 + j]);
+          db[v * 4 + j] = add2(db[v * 4 + j], d[j]);
+          const float2 w = fma2(mul2(d[j], gamma[v * 4 + j]), rstd, fma2(xh[j], gx, ga));
+          o[2 * j] = w.x;
+          o[2 * j + 1] = w.y;
+        }
+        if constexpr (V == 8) {
+          store_chunk<TDX, 8>(dx, group_col<V, THREADS>(v, 0), o, 8);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int c = group_col<V, THREADS>(v, k);
+            if (c < p.cols) store_value<TDX>(dx, c, o[k]);
+          }
         }
       }
     }
@@ -352,7 +415,7 @@ struct LnPlan {
   LnPath path;
   int grid, parts;  // blocks; partial rows of the parameter gradients
   // kLnRing
-  int nv, threads, stages;
+  int nv, threads, stages, step;
   bool aligned;                // V = 8, else 1
   uint32_t x_bytes, dy_bytes;  // of a slot
 };
@@ -400,6 +463,7 @@ LnPlan plan_ln_backward(const LnBackward &p, int sms) {
     if (stages >= 2) {
       l.path = kLnRing;
       l.stages = (int)(stages < kMaxStages ? stages : kMaxStages);
+      l.step = l.stages >= 4 ? most_rows(l.nv, l.aligned ? 8 : 1) : 1;
       l.grid = l.parts = row_blocks(p.rows, sms, per_sm);
       return l;
     }
@@ -419,8 +483,8 @@ cudaError_t run_ring(const LnBackward &p, const LnPlan &l, const OpContext &c) {
   const size_t smem = (size_t)l.stages * (l.x_bytes + l.dy_bytes);
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
   if (e != cudaSuccess) return e;
-  return launch_ex(kern, dim3(l.grid), dim3(l.threads), smem, c.st, 1, p, l.stages, l.x_bytes, l.dy_bytes, c.err,
-                   c.wait_limit_ns);
+  return launch_ex(kern, dim3(l.grid), dim3(l.threads), smem, c.st, 1, p, l.stages, l.step, l.x_bytes, l.dy_bytes,
+                   c.err, c.wait_limit_ns);
 }
 
 template <typename TX, typename TDY, typename TDX>
@@ -460,8 +524,9 @@ cudaError_t run_types(const LnBackward &p, const OpContext &c, int *launches) {
     if (e != cudaSuccess) return e;
   }
   ++*launches;
-  return launch_ex(ln_param_sum_kernel, dim3(strips, 2), dim3(kSumThreads), 0, c.st, 1, (const float *)p.partials,
-                   l.parts, p.cols, partial_pitch(p.cols), p.dgamma, p.dbeta);
+  const bool few = l.parts <= c.sms;
+  return launch_ex(few ? ln_param_sum_kernel<256> : ln_param_sum_kernel<1024>, dim3(strips, 2), dim3(few ? 256 : 1024), 0, c.st, 1,
+                   (const float *)p.partials, l.parts, p.cols, partial_pitch(p.cols), p.dgamma, p.dbeta);
 }
 
 }  // namespace
