@@ -451,7 +451,10 @@ LnPlan plan_ln_backward(const LnBackward &p, int sms) {
     l.dy_bytes = slot_bytes(p.cols, sg, l.aligned);
     l.threads = (int)ceil_div64(ceil_div64(eights, l.nv), 32) * 32;
     if (!l.aligned) {  // one of the block sizes compiled
-      l.threads = l.threads <= 128 ? 128 : l.threads <= 256 && l.nv == 2 ? 256 : 512;
+      l.threads = l.nv == 1              ? l.threads <= 32 ? 32 : l.threads <= 64 ? 64 : 128
+                  : l.threads <= 128     ? 128
+                  : l.threads <= 256 && l.nv == 2 ? 256
+                                         : 512;
     }
     int per_sm = ring_blocks(l.nv, l.aligned ? 8 : 1, l.threads);
     per_sm = per_sm > 16 ? 16 : per_sm;
@@ -495,7 +498,10 @@ cudaError_t run_width(const LnBackward &p, const LnPlan &l, const OpContext &c) 
            : l.nv == 3 ? run_ring<TX, TDY, TDX, 3, 8, 512>(p, l, c)
            : l.threads <= 128 ? run_ring<TX, TDY, TDX, 4, 8, 128>(p, l, c)
                               : run_ring<TX, TDY, TDX, 4, 8, 512>(p, l, c);
-  if (l.nv == 1) return run_ring<TX, TDY, TDX, 1, 1, 128>(p, l, c);
+  if (l.nv == 1)
+    return l.threads == 32   ? run_ring<TX, TDY, TDX, 1, 1, 32>(p, l, c)
+           : l.threads == 64 ? run_ring<TX, TDY, TDX, 1, 1, 64>(p, l, c)
+                             : run_ring<TX, TDY, TDX, 1, 1, 128>(p, l, c);
   if (l.nv == 3) return run_ring<TX, TDY, TDX, 3, 1, 512>(p, l, c);
   if (l.nv == 4) return run_ring<TX, TDY, TDX, 4, 1, 512>(p, l, c);
   return l.threads == 128   ? run_ring<TX, TDY, TDX, 2, 1, 128>(p, l, c)

@@ -344,6 +344,8 @@ cudaError_t run_ring(const LnForward &p, const OpContext &c) {
 template <typename TX, typename TY, int V>
 cudaError_t run_width(const LnForward &p, const OpContext &c) {
   const int eights = (p.cols + 7) / 8;
+  if (V == 1 && eights <= 32) return run_ring<TX, TY, 1, 32, 1>(p, c);
+  if (V == 1 && eights <= 64) return run_ring<TX, TY, 1, 64, 1>(p, c);
   if (eights <= 128) return run_ring<TX, TY, 1, 128, V>(p, c);
   if (V == 1 && eights <= 256) return run_ring<TX, TY, 2, 128, 1>(p, c);
   if (eights <= 512) return run_ring<TX, TY, 2, 256, V>(p, c);

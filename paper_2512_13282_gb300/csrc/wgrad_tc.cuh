@@ -187,37 +187,47 @@ __device__ __forceinline__ void store_elements(const WgradParams &p, uint32_t bu
   __syncwarp();
   const int c = x + lane, rows = min(32, p.tc.M - y0);
   if (c >= p.tc.N) return;
-  // base may be C itself, so loads cannot move above stores by themselves:
-  // eight rows are read before the first of them is written
+  // base may be C itself, so loads cannot move above stores by themselves: a
+  // batch of rows is read before the first of them is written
+  constexpr int kBatch = AHEAD ? 32 : 8;
 #pragma unroll
-  for (int r0 = 0; r0 < 32; r0 += 8) {
+  for (int r0 = 0; r0 < 32; r0 += kBatch) {
     if (r0 >= rows) break;
-    float f[8], o[8] = {};
+    float f[kBatch];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(ld_shared_u32(block_piece(buf, r0 + i, lane >> 2) + (lane & 3) * 4));
-    if (AHEAD) {
-      const uint4 lo = b[r0 / 4], hi = b[r0 / 4 + 1];
-      const float4 l = as_float4(lo), h = as_float4(hi);
-      o[0] = l.x, o[1] = l.y, o[2] = l.z, o[3] = l.w, o[4] = h.x, o[5] = h.y, o[6] = h.z, o[7] = h.w;
-    } else if (p.base) {
+    for (int i = 0; i < kBatch; ++i)
+      f[i] = __uint_as_float(ld_shared_u32(block_piece(buf, r0 + i, lane >> 2) + (lane & 3) * 4));
+    if (p.base) {
+      float o[kBatch] = {};
+      if constexpr (AHEAD) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (r0 + i < rows) {
-          const int64_t at = (int64_t)(y0 + r0 + i) * p.ldbase + c;
-          o[i] = p.out_bf16 ? __uint_as_float((uint32_t) static_cast<const uint16_t *>(p.base)[at] << 16)
-                            : static_cast<const float *>(p.base)[at];
+        for (int i = 0; i < 8; ++i) {
+          const float4 l = as_float4(b[i]);
+          o[4 * i] = l.x, o[4 * i + 1] = l.y, o[4 * i + 2] = l.z, o[4 * i + 3] = l.w;
         }
-    }
+      } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (r0 + i < rows) {
-        const int64_t at = (int64_t)(y0 + r0 + i) * p.tc.ldc + c;
-        if (p.base) f[i] += o[i];
-        if (p.out_bf16)
-          static_cast<__nv_bfloat16 *>(p.tc.C)[at] = __float2bfloat16_rn(f[i]);
-        else
-          static_cast<float *>(p.tc.C)[at] = f[i];
+        for (int i = 0; i < kBatch; ++i)
+          if (r0 + i < rows) {
+            const int64_t at = (int64_t)(y0 + r0 + i) * p.ldbase + c;
+            o[i] = p.out_bf16 ? __uint_as_float((uint32_t) static_cast<const uint16_t *>(p.base)[at] << 16)
+                              : static_cast<const float *>(p.base)[at];
+          }
       }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) f[i] += o[i];
+    }
+    if (p.out_bf16) {
+      __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.tc.C) + (int64_t)(y0 + r0) * p.tc.ldc + c;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i, dst += p.tc.ldc)
+        if (r0 + i < rows) *dst = __float2bfloat16_rn(f[i]);
+    } else {
+      float *dst = static_cast<float *>(p.tc.C) + (int64_t)(y0 + r0) * p.tc.ldc + c;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i, dst += p.tc.ldc)
+        if (r0 + i < rows) *dst = f[i];
+    }
   }
 }
 

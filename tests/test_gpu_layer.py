@@ -187,6 +187,69 @@ def test_layernorm_backward(rows, cols, xt, gt, ot, pt):
         within(O2.host(), R.ln_backward(x, m, s, one, dy)[0], R.ln_backward_bounds(x, m, s, one, dy, ot)[0])
 
 
+@pytest.mark.parametrize("rows,cols", [(4900, 2304), (5000, 4096), (20000, 100), (9000, 141)])
+@pytest.mark.parametrize("xt,gt,ot", [("bf16", "bf16", "bf16"), ("q8", "bf16", "f32")])
+def test_layernorm_backward_of_many_rows(rows, cols, xt, gt, ot):
+    """Enough rows that every block walks many of them, the rings go round
+    several times and there are many partial sums."""
+    rng = np.random.default_rng(rows + cols)
+    x = rng.normal(size=(rows, cols)).astype(np.float32) * 2 + 0.5
+    X = Q = E = None
+    if xt == "q8":
+        q = rng.integers(-127, 128, size=(rows, cols)).astype(np.int8)
+        e = rng.integers(118, 123, size=(rows, -(-cols // 32))).astype(np.uint8)
+        x = R.q8_values(q, e)
+        Q, E = Mat(rows, cols, "s8", fill=q), Mat(rows, -(-cols // 32), "u8", fill=e)
+    else:
+        x = as_kind(x, xt)
+        X = Mat(rows, cols, xt, fill=x)
+    gamma = as_kind(1 + 0.2 * rng.normal(size=cols), "f32")
+    _, m, s = R.ln_forward(x, gamma, 0, EPS)
+    m, s = m.astype(np.float32), s.astype(np.float32)
+    dy = as_kind(rng.normal(size=(rows, cols)), gt)
+    D, O = Mat(rows, cols, gt, fill=dy), Mat(rows, cols, ot)
+    dg, db = Mat(1, cols, "f32"), Mat(1, cols, "f32")
+    for _ in range(2):
+        done(L.gemm_layernorm_backward(
+            rows, cols, X.ptr if X else None, cols if X else 0, TYPES[ot], Q.ptr if Q else None, cols,
+            E.ptr if E else None, E.ld if E else 0, vec(gamma, "f32"), TYPES["f32"], vec(m, "f32"), vec(s, "f32"), D.ptr,
+            cols, TYPES[gt], O.ptr, cols, TYPES[ot], dg.ptr, db.ptr))
+        want = R.ln_backward(x, m, s, gamma, dy)
+        bound = R.ln_backward_bounds(x, m, s, gamma, dy, ot)
+        within(O.host(), want[0], bound[0])
+        within(dg.host()[0], want[1], bound[1])
+        within(db.host()[0], want[2], bound[2])
+    assert all(a.guarded() for a in (D, O, dg, db))
+
+
+@pytest.mark.parametrize("rows,cols,xt", [(5000, 1024, "bf16"), (3000, 130, "bf16"), (4000, 500, "f32")])
+def test_layernorm_forward_of_many_rows(rows, cols, xt):
+    rng = np.random.default_rng(rows + cols)
+    x = as_kind(rng.normal(size=(rows, cols)) * 3 - 1, xt)
+    gamma, beta = as_kind(1 + 0.2 * rng.normal(size=cols), "bf16"), as_kind(0.2 * rng.normal(size=cols), "bf16")
+    X, Y = Mat(rows, cols, xt, fill=x), Mat(rows, cols, "bf16")
+    Q, E = Mat(rows, cols, "s8"), Mat(rows, -(-cols // 32), "u8")
+    mean, rstd = Mat(1, rows, "f32"), Mat(1, rows, "f32")
+    done(L.gemm_layernorm_forward(rows, cols, X.ptr, cols, TYPES[xt], vec(gamma, "bf16"), vec(beta, "bf16"),
+                                  TYPES["bf16"], EPS, Y.ptr, cols, TYPES["bf16"], mean.ptr, rstd.ptr, Q.ptr, cols,
+                                  E.ptr, E.ld))
+    y, m, s = R.ln_forward(x, gamma, beta, EPS)
+    by, bm, bs = R.ln_forward_bounds(x, gamma, beta, EPS, "bf16")
+    within(Y.host(), y, by)
+    within(mean.host()[0], m, bm)
+    within(rstd.host()[0], s, bs)
+    # the checkpoint's values, against those of y as stored (the blocks are
+    # independent, so a sample of rows goes through the definition)
+    pick = np.r_[0:50, rows - 50:rows]
+    q, e = R.q8_save(Y.host()[pick])
+    assert np.array_equal(Q.host()[pick], q) and np.array_equal(E.host()[pick], e)
+    B = Mat(rows, cols, "f32")
+    done(L.gemm_q8_restore(rows, cols, Q.ptr, cols, E.ptr, E.ld, B.ptr, cols, TYPES["f32"]))
+    top = np.repeat(np.maximum.reduceat(np.abs(Y.host()), np.arange(0, cols, 32), axis=1), 32, axis=1)[:, :cols]
+    assert (np.abs(B.host() - Y.host()) <= top / 126).all()
+    assert all(a.guarded() for a in (X, Y, Q, E, mean, rstd))
+
+
 def test_layernorm_backward_of_no_rows_is_zero():
     dg, db = torch.full((50,), 7.0, device="cuda"), torch.full((50,), 7.0, device="cuda")
     done(L.gemm_layernorm_backward(0, 50, None, 0, 0, None, 0, None, 0, None, 0, None, None, None, 0, 0, None, 0, 0,
