@@ -170,10 +170,11 @@ gemm_status_t gemm_q8_weight_grad(int64_t T, int64_t K, int64_t N, const int8_t 
     const Q8Ref ck{const_cast<int8_t *>(q), ldq, const_cast<uint8_t *>(e), lde};
     const bool x16 = aligned_to(q, 16) && ldq % 16 == 0;
     count_launches(1);
-    if ((x16 && !pack ? launch_q8_restore(ck, xs, ldk, GEMM_TYPE_BF16, T, K, c.st)
-                      : launch_wgrad_stage(ck, T, K, reinterpret_cast<uint16_t *>(xs), ldk, pack ? dY : nullptr, lddy, N,
-                                           reinterpret_cast<uint16_t *>(gs), ldn, c.st)) != cudaSuccess)
-      return GEMM_ERR_CUDA;
+    uint16_t *x16s = reinterpret_cast<uint16_t *>(xs), *g16s = reinterpret_cast<uint16_t *>(gs);
+    const cudaError_t staged =
+        x16 && !pack ? launch_q8_restore(ck, xs, ldk, GEMM_TYPE_BF16, T, K, c.st)
+                     : launch_wgrad_stage(ck, T, K, x16s, ldk, pack ? dY : nullptr, lddy, N, g16s, ldn, c.st);
+    if (staged != cudaSuccess) return GEMM_ERR_CUDA;
     const void *g = pack ? (const void *)gs : dY;
     const int64_t ldg = pack ? ldn : lddy;
     CUtensorMap tx, tg, tout, tws;

@@ -1,5 +1,16 @@
 // layer_ln_fwd.cu -- layer norm forward, optionally with the result's 8-bit
-// checkpoint.
+// checkpoint:
+//     y = (x - mu) * rstd * gamma + beta,  rstd = 1 / sqrt(var + eps),
+// mu and var of a row, var from the differences x - mu (a second sum over the
+// row, held in registers, so that a mean far above the deviations costs no
+// digits).  Sums are float32; y is rounded once, to its type.
+//
+// HBM bounds it: each value read once and written once, 4 bytes in bf16, and 1
+// more for the checkpoint.  Measured, back to back, bf16, against a plain copy
+// of as many bytes: 8192 x 4096 28.3 us (4.7 TB/s; copy 23.1), with the
+// checkpoint 38.5 us; 32768 x 4096 96 us (5.6 TB/s; copy 82).  What is left is
+// issue: 22 instructions a value (32 with the checkpoint) keep the schedulers
+// two thirds busy.
 #include <atomic>
 
 #include "layer_rows.cuh"
@@ -11,7 +22,9 @@ namespace {
 constexpr int kAnyThreads = 256;
 
 // Any width, pitch and alignment: a block per row, the row read three times
-// (mean, variance, result), the second and third time from L1 or L2.
+// (mean, variance, result), the second and third time from L1 or L2.  For rows
+// above 16384 values and unaligned ones below 64 only: 8192 x 4096 with its
+// checkpoint takes 300 us here.
 template <typename TX, typename TY>
 __global__ void __launch_bounds__(kAnyThreads) ln_forward_any_kernel(const LnForward p) {
   __shared__ float2 sm[2][32];
@@ -57,59 +70,44 @@ __global__ void __launch_bounds__(kAnyThreads) ln_forward_any_kernel(const LnFor
 }
 
 
-// A lane's 8 consecutive results (the first n of them), rounded to y's type
-// and stored, and their part of the checkpoint of y as stored (four lanes hold
-// a block).  All lanes of the warp call it.
+// A lane's 8 consecutive results, rounded to y's type and stored, and their part
+// of the checkpoint of y as stored (four lanes hold a block).  All lanes of the
+// warp call it, those past the row's end with `in` false.
 template <typename TY>
-__device__ __forceinline__ void store_eighth(TY *y, const Q8Ref &ck, int64_t r, int c, const float2 (&v)[4], int n) {
+__device__ __forceinline__ void store_eighth(TY *y, const Q8Ref &ck, int64_t r, int c, const float2 (&v)[4], bool in) {
   float2 o[4];
   uint32_t top;
   if constexpr (sizeof(TY) == 2) {
     uint32_t h[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) h[j] = pack_bf16x2(v[j].x, v[j].y);
-    if (n == 8) {
-      *reinterpret_cast<uint4 *>(y + c) = make_uint4(h[0], h[1], h[2], h[3]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (i < n)
-          reinterpret_cast<uint16_t *>(y)[c + i] = (uint16_t)(h[i / 2] >> (16 * (i & 1)));
-        else
-          h[i / 2] &= (i & 1) ? 0x0000FFFFu : 0xFFFF0000u;  // not in the block
-      }
-    }
+    if (in) *reinterpret_cast<uint4 *>(y + c) = make_uint4(h[0], h[1], h[2], h[3]);
     if (!ck.q) return;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      o[j] = make_float2(__uint_as_float(h[j] << 16), __uint_as_float(h[j] & 0xFFFF0000u));
+    for (int j = 0; j < 4; ++j) o[j] = make_float2(__uint_as_float(h[j] << 16), __uint_as_float(h[j] & 0xFFFF0000u));
     top = max_magnitude_bf16<4>(h);
   } else {
-    float w[8];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[2 * j] = v[j].x, w[2 * j + 1] = v[j].y;
-    store_chunk<TY, 8>(y, c, w, n);
+    if (in) {
+      float4 *d = reinterpret_cast<float4 *>(y + c);
+      d[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+      d[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+    }
     if (!ck.q) return;
     top = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      o[j] = make_float2(2 * j < n ? v[j].x : 0.f, 2 * j + 1 < n ? v[j].y : 0.f);
-      top = max(top, max(__float_as_uint(o[j].x) & 0x7FFFFFFFu, __float_as_uint(o[j].y) & 0x7FFFFFFFu));
+      o[j] = v[j];
+      top = max(top, max(__float_as_uint(v[j].x) & 0x7FFFFFFFu, __float_as_uint(v[j].y) & 0x7FFFFFFFu));
     }
   }
+  if (!in) top = 0;  // not in the block
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   const uint32_t e = q8_exponent(top);
   const uint2 w = q8_pack8(o, e);
-  int8_t *q = ck.q + r * ck.ldq + c;
-  if (n == 8) {
-    *reinterpret_cast<uint2 *>(q) = w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) q[i] = (int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
-  }
-  if (n > 0 && (c & 31) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
+  if (!in) return;
+  *reinterpret_cast<uint2 *>(ck.q + r * ck.ldq + c) = w;
+  if ((c & 31) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
 }
 
 // Rows of up to THREADS * NV * 8 values, at least 64 where V = 1, read once and
@@ -274,15 +272,17 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
           for (int j = 0; j < 4; ++j) {
             const int c = group_col<V, THREADS>(v, 2 * j), d = group_col<V, THREADS>(v, 2 * j + 1);
             const int cs = c < p.cols ? c : 0, ds = d < p.cols ? d : 0;
-            g[j] = params_shared ? make_float2(shared_gamma[cs], shared_gamma[ds]) : make_float2(gamma_at(c), gamma_at(d));
-            b[j] = params_shared ? make_float2(shared_beta[cs], shared_beta[ds]) : make_float2(beta_at(c), beta_at(d));
+            g[j] = params_shared ? make_float2(shared_gamma[cs], shared_gamma[ds])
+                                 : make_float2(gamma_at(c), gamma_at(d));
+            b[j] = params_shared ? make_float2(shared_beta[cs], shared_beta[ds])
+                                 : make_float2(beta_at(c), beta_at(d));
           }
         }
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] = fma2(mul2(x[v * 4 + j], both(rstd)), g[j], b[j]);
       if constexpr (V == 8) {
-        store_eighth<TY>(y, p.ck, r, c0, o, c0 < p.cols ? 8 : 0);
+        store_eighth<TY>(y, p.ck, r, c0, o, c0 < p.cols);
       } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {

