@@ -62,6 +62,7 @@ std::mutex g_mu;
 DeviceState g_dev[kMaxDevices];
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
 std::atomic<uint64_t> g_launches{0};
+std::atomic<uint64_t> g_epoch{1};  // gemm_release_resources() calls so far, plus one
 cudaEvent_t g_prof_start = nullptr, g_prof_stop = nullptr;
 
 }  // namespace
@@ -1076,6 +1077,7 @@ void gemm_release_resources(void) {
     x = Scratch{};
   }
   d.ready = false;  // look the device's symbols up again at the next call
+  g_epoch.fetch_add(1);
   noalloc_forget_device(dev);
 }
 
@@ -1195,6 +1197,17 @@ gemm_status_t op_workspace(size_t bytes, cudaStream_t st, void **ws) {
   const gemm_status_t s = ensure_workspace(bytes, st);
   *ws = s == GEMM_OK ? scratch_ws() : nullptr;
   return s;
+}
+
+cudaError_t allow_shared_memory(const void *kern, size_t bytes, std::atomic<uint64_t> &done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t now = g_epoch.load() << 8 | (uint64_t)(dev & 0xFF);
+  if (done.load(std::memory_order_relaxed) == now) return cudaSuccess;
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess) done.store(now, std::memory_order_relaxed);
+  return e;
 }
 
 void count_launches(int n) { g_launches.fetch_add((uint64_t)n); }

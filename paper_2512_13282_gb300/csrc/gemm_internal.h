@@ -4,6 +4,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <utility>
 
@@ -66,6 +67,11 @@ gemm_status_t with_scratch(cudaStream_t st, F &&f) {
   return with_scratch(st, [](const OpContext &c, void *arg) { return (*static_cast<F *>(arg))(c); }, &f);
 }
 gemm_status_t op_workspace(size_t bytes, cudaStream_t st, void **ws);
+// Lets `kern` use `bytes` of dynamic shared memory on the current device: asked
+// of the runtime once (0.4 us a call otherwise), and again after
+// gemm_release_resources(), which a device reset calls for.  `done` is the
+// caller's, one per kernel, zero at first.
+cudaError_t allow_shared_memory(const void *kern, size_t bytes, std::atomic<uint64_t> &done);
 // Counts kernels for gemm_launch_count().
 void count_launches(int n);
 // Tensor maps: a bf16 matrix read in boxes (rows of `inner` contiguous

@@ -399,12 +399,14 @@ __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
     if (threadIdx.x == 0) ring_drain(bar0, stages, use, filled - done);
     return;
   }
-  if (!p.partials) return;
-  float *dg_out = p.partials + (int64_t)blockIdx.x * partial_pitch(p.cols);
-  float *db_out = dg_out + (int64_t)gridDim.x * partial_pitch(p.cols);
+  // the only block has the whole sums; else one partial row each of the block's
+  const bool whole = gridDim.x == 1;
+  if (!whole && !p.partials) return;
+  float *dg_out = whole ? p.dgamma : p.partials + (int64_t)blockIdx.x * partial_pitch(p.cols);
+  float *db_out = whole ? p.dbeta : p.partials + (int64_t)(gridDim.x + blockIdx.x) * partial_pitch(p.cols);
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    if constexpr (V == 8) {
+    if (V == 8 && !whole) {
       const int c = group_col<V, THREADS>(v, 0);
       if (c < p.cols) {
         store_chunk<float, 8>(dg_out, c, reinterpret_cast<const float *>(dg + v * 4), 8);
@@ -415,8 +417,8 @@ __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
       for (int k = 0; k < 8; ++k) {
         const int c = group_col<V, THREADS>(v, k);
         if (c < p.cols) {
-          dg_out[c] = (k & 1) ? dg[v * 4 + (k >> 1)].y : dg[v * 4 + (k >> 1)].x;
-          db_out[c] = (k & 1) ? db[v * 4 + (k >> 1)].y : db[v * 4 + (k >> 1)].x;
+          if (dg_out) dg_out[c] = (k & 1) ? dg[v * 4 + (k >> 1)].y : dg[v * 4 + (k >> 1)].x;
+          if (db_out) db_out[c] = (k & 1) ? db[v * 4 + (k >> 1)].y : db[v * 4 + (k >> 1)].x;
         }
       }
     }
@@ -438,7 +440,11 @@ struct LnPlan {
 // while there are few rows, more where each still has two rows to set against
 // the partial row that it writes and another kernel reads (1000 rows of 1500
 // from a checkpoint: 36 us with 152 blocks, 17.5 with 500).
+//
+// Up to four rows go to one block, which then has the whole sums: a launch less
+// is worth more than the rows' latencies side by side.
 int row_blocks(int64_t rows, int sms, int per_sm) {
+  if (rows <= 4) return 1;
   const int64_t few = rows < sms ? rows : sms, many = ceil_div64(rows, 2), most = (int64_t)sms * per_sm;
   const int64_t want = many > few ? many : few;
   return (int)(want < most ? want : most);
@@ -498,7 +504,8 @@ template <typename TX, typename TDY, typename TDX, int NV, int V, int THREADS>
 cudaError_t run_ring(const LnBackward &p, const LnPlan &l, const OpContext &c) {
   const auto kern = ln_backward_ring_kernel<TX, TDY, TDX, NV, V, THREADS>;
   const size_t smem = (size_t)l.stages * (l.x_bytes + l.dy_bytes);
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = allow_shared_memory((const void *)kern, kRingBytes, allowed);
   if (e != cudaSuccess) return e;
   return launch_ex(kern, dim3(l.grid), dim3(l.threads), smem, c.st, 1, p, l.stages, l.step, l.x_bytes, l.dy_bytes,
                    c.err, c.wait_limit_ns);
@@ -536,7 +543,7 @@ cudaError_t run_types(const LnBackward &p, const OpContext &c, int *launches) {
       e = launch_ex(ln_backward_any_kernel<TX, TDY, TDX>, grid, dim3(kRowThreads), 0, c.st, 1, p);
     if (e != cudaSuccess) return e;
   }
-  if (!p.partials) return e;
+  if (!p.partials || (l.path == kLnRing && l.grid == 1)) return e;
   const int strips = (int)ceil_div64(p.cols, 32);
   if (l.path == kLnAny) {
     ++*launches;

@@ -335,7 +335,8 @@ cudaError_t run_ring(const LnForward &p, const OpContext &c) {
   int64_t stages = (room - param_bytes) / x_bytes;
   stages = stages < 2 ? 2 : stages > kMaxStages ? kMaxStages : stages;
   const size_t smem = (size_t)(stages * x_bytes + param_bytes);
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = allow_shared_memory((const void *)kern, kRingBytes, allowed);
   if (e != cudaSuccess) return e;
   return launch_ex(kern, dim3(persistent_grid(blocks_per_sm(kern, threads, smem, known), p.rows, c.sms)), dim3(threads),
                    smem, c.st, 1, p, (int)stages, x_bytes, param_bytes ? 1 : 0, c.err, c.wait_limit_ns);

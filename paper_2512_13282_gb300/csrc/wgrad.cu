@@ -24,20 +24,21 @@ cudaError_t launch_tile(const CUtensorMap &a, const CUtensorMap &b, const CUtens
   using Cfg = WgCfg<BN, PAIR>;
   const bool slabs = p.tc.num_kb > p.tc.slab_kb;
   auto kern = slabs ? wgrad_kernel<BN, PAIR, true> : wgrad_kernel<BN, PAIR, false>;
+  static std::atomic<uint64_t> allowed[2];
+  const cudaError_t e = allow_shared_memory((const void *)kern, Cfg::kSmemBytes, allowed[slabs]);
+  if (e != cudaSuccess) return e;
   if (slabs) {
     // its epilogue takes registers over from the other warps, and would wait
     // for ever if the block were launched with fewer than that adds up to
     static std::atomic<int> regs{0};
     if (regs.load() == 0) {
       cudaFuncAttributes attr;
-      const cudaError_t e = cudaFuncGetAttributes(&attr, kern);
-      if (e != cudaSuccess) return e;
+      const cudaError_t f = cudaFuncGetAttributes(&attr, kern);
+      if (f != cudaSuccess) return f;
       regs.store(attr.numRegs);
     }
     if (regs.load() < kWgLaunchRegs) return cudaErrorLaunchOutOfResources;
   }
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmemBytes);
-  if (e != cudaSuccess) return e;
   return launch_ex(kern, dim3((unsigned)grid), dim3(kWgThreads), Cfg::kSmemBytes, st, PAIR ? 2 : 1, a, b, out, ws, p);
 }
 
