@@ -177,11 +177,12 @@ gemm_status_t gemm_q8_weight_grad(int64_t T, int64_t K, int64_t N, const int8_t 
     if (staged != cudaSuccess) return GEMM_ERR_CUDA;
     const void *g = pack ? (const void *)gs : dY;
     const int64_t ldg = pack ? ldn : lddy;
-    CUtensorMap tx, tg, tout, tws;
+    WgradMaps m;
+    CUtensorMap &tx = kn ? m.a : m.b, &tg = kn ? m.b : m.a;
     if (!bf16_box_map(&tx, xs, (uint64_t)K, (uint64_t)T, (uint64_t)ldk, 64, kBK) ||
         !bf16_box_map(&tg, g, (uint64_t)N, (uint64_t)T, (uint64_t)ldg, 64, kBK))
       return GEMM_ERR_CUDA;
-    tout = tws = tx;
+    m.out = m.partials = m.base = tx;
     // C through TMA where its base, pitch and row ends are multiples of 16
     // bytes (a clipped TMA store would write into the row's padding), and the
     // base, read in 16-byte pieces then, likewise
@@ -189,7 +190,9 @@ gemm_status_t gemm_q8_weight_grad(int64_t T, int64_t K, int64_t N, const int8_t 
     p.tc.out_tma = kOutDirect;
     if (tma_store_enabled() && aligned_to(dW, 16) && ldw * es % 16 == 0 && cols * es % 16 == 0 &&
         (!base || (aligned_to(base, 16) && ldbase * es % 16 == 0))) {
-      if (!float_out_map(&tout, bf, dW, (uint64_t)cols, (uint64_t)M, (uint64_t)ldw, 1)) return GEMM_ERR_CUDA;
+      if (!float_out_map(&m.out, bf, dW, (uint64_t)cols, (uint64_t)M, (uint64_t)ldw, 1) ||
+          (base && !float_out_map(&m.base, bf, base, (uint64_t)cols, (uint64_t)M, (uint64_t)ldbase, 1)))
+        return GEMM_ERR_CUDA;
       p.tc.out_tma = kOutTmaC;
     }
     p.tc.tiles_m = pl.tiles_m;
@@ -207,13 +210,12 @@ gemm_status_t gemm_q8_weight_grad(int64_t T, int64_t K, int64_t N, const int8_t 
       p.tc.ws = parts;
       const int tile_m = pl.tile.pair ? 2 * kBM : kBM;
       const int64_t tail_rows = ((int64_t)pl.tiles_m * pl.tiles_n - pl.tail_first) * tile_m;
-      if (!float_out_map(&tws, false, parts, (uint64_t)pl.tile.bn, (uint64_t)tail_rows, (uint64_t)pl.tile.bn,
+      if (!float_out_map(&m.partials, false, parts, (uint64_t)pl.tile.bn, (uint64_t)tail_rows, (uint64_t)pl.tile.bn,
                          (uint64_t)pl.tail_splits))
         return GEMM_ERR_CUDA;
     }
     count_launches(1);
-    if (launch_wgrad(pl.tile, kn ? tx : tg, kn ? tg : tx, tout, tws, p, pl.grid, c.st) != cudaSuccess)
-      return GEMM_ERR_CUDA;
+    if (launch_wgrad(pl.tile, m, p, pl.grid, c.st) != cudaSuccess) return GEMM_ERR_CUDA;
     if (pl.tail_splits > 0) {
       count_launches(1);
       return launched(launch_wgrad_reduce(pl.tile, p, c.st));

@@ -99,8 +99,12 @@ struct WgradPlan {
 WgradPlan plan_wgrad(int64_t M, int64_t N, int64_t T, int out_bytes, bool base, int sms, int pairs);
 // Bytes of partial sums a plan's split tail writes (0: none).
 size_t wgrad_partial_bytes(const WgradPlan &pl);
-cudaError_t launch_wgrad(const WgradTile &tile, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out,
-                         const CUtensorMap &ws, const WgradParams &p, int grid, cudaStream_t st);
+// Tensor maps of its operands; out and base where C goes through TMA, partials
+// with a split tail (any valid map else).
+struct WgradMaps {
+  CUtensorMap a, b, out, partials, base;
+};
+cudaError_t launch_wgrad(const WgradTile &tile, const WgradMaps &m, const WgradParams &p, int grid, cudaStream_t st);
 // T == 0: C = base, or zero.
 cudaError_t launch_wgrad_base(const WgradParams &p, int sms, cudaStream_t st);
 // The split tail's tiles: partials summed in split order, base added, rounded

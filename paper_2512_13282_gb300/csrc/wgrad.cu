@@ -18,16 +18,20 @@ inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // k-blocks; 16 also breaks the header's bound per element.
 constexpr int kSlabKb = 8;
 
-template <int BN, bool PAIR>
-cudaError_t launch_tile(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const CUtensorMap &ws,
-                        const WgradParams &p, int grid, cudaStream_t st) {
-  using Cfg = WgCfg<BN, PAIR>;
-  const bool slabs = p.tc.num_kb > p.tc.slab_kb;
-  auto kern = slabs ? wgrad_kernel<BN, PAIR, true> : wgrad_kernel<BN, PAIR, false>;
-  static std::atomic<uint64_t> allowed[2];
-  const cudaError_t e = allow_shared_memory((const void *)kern, Cfg::kSmemBytes, allowed[slabs]);
+// Most k-blocks for which base comes through shared memory: its blocks displace
+// two stages of operands, which longer reductions miss.  4096 x 4096 bf16 with
+// base, through registers / through shared memory: 768 tokens 34.7 / 33.4 us,
+// 1024 37.1 / 39.0, 2048 56.4 / 65.9.
+constexpr int kBaseKb = 12;
+
+template <int BN, bool PAIR, bool SLABS, bool BASE>
+cudaError_t launch_kernel(const WgradMaps &m, const WgradParams &p, int grid, cudaStream_t st) {
+  using Cfg = WgCfg<BN, PAIR, BASE>;
+  auto kern = wgrad_kernel<BN, PAIR, SLABS, BASE>;
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = allow_shared_memory((const void *)kern, Cfg::kSmemBytes, allowed);
   if (e != cudaSuccess) return e;
-  if (slabs) {
+  if (SLABS) {
     // its epilogue takes registers over from the other warps, and would wait
     // for ever if the block were launched with fewer than that adds up to
     static std::atomic<int> regs{0};
@@ -39,7 +43,16 @@ cudaError_t launch_tile(const CUtensorMap &a, const CUtensorMap &b, const CUtens
     }
     if (regs.load() < kWgLaunchRegs) return cudaErrorLaunchOutOfResources;
   }
-  return launch_ex(kern, dim3((unsigned)grid), dim3(kWgThreads), Cfg::kSmemBytes, st, PAIR ? 2 : 1, a, b, out, ws, p);
+  return launch_ex(kern, dim3((unsigned)grid), dim3(kWgThreads), Cfg::kSmemBytes, st, PAIR ? 2 : 1, m.a, m.b, m.out,
+                   m.partials, m.base, p);
+}
+
+template <int BN, bool PAIR>
+cudaError_t launch_tile(const WgradMaps &m, const WgradParams &p, int grid, cudaStream_t st) {
+  if (p.tc.num_kb > p.tc.slab_kb) return launch_kernel<BN, PAIR, true, false>(m, p, grid, st);
+  if (p.base && p.tc.out_tma == kOutTmaC && p.tc.num_kb <= kBaseKb)
+    return launch_kernel<BN, PAIR, false, true>(m, p, grid, st);
+  return launch_kernel<BN, PAIR, false, false>(m, p, grid, st);
 }
 
 // Split tail: element group t (4 columns of a row) of the compact partials,
@@ -241,13 +254,11 @@ size_t wgrad_partial_bytes(const WgradPlan &pl) {
   return (size_t)pl.tail_splits * tail * (pl.tile.pair ? 2 * kBM : kBM) * pl.tile.bn * 4;
 }
 
-cudaError_t launch_wgrad(const WgradTile &tile, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out,
-                         const CUtensorMap &ws, const WgradParams &p, int grid, cudaStream_t st) {
+cudaError_t launch_wgrad(const WgradTile &tile, const WgradMaps &m, const WgradParams &p, int grid, cudaStream_t st) {
   WgradParams q = p;
   q.tc.slab_kb = p.out_bf16 ? p.tc.num_kb : kSlabKb;
-  if (tile.pair) return launch_tile<256, true>(a, b, out, ws, q, grid, st);
-  return tile.bn == 128 ? launch_tile<128, false>(a, b, out, ws, q, grid, st)
-                        : launch_tile<64, false>(a, b, out, ws, q, grid, st);
+  if (tile.pair) return launch_tile<256, true>(m, q, grid, st);
+  return tile.bn == 128 ? launch_tile<128, false>(m, q, grid, st) : launch_tile<64, false>(m, q, grid, st);
 }
 
 cudaError_t launch_wgrad_stage(const Q8Ref &ck, int64_t T, int64_t K, uint16_t *x, int64_t ldx, const uint16_t *g,

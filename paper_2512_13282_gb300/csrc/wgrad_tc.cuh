@@ -22,7 +22,7 @@
 // The tensor cores bound it for many tokens (8192 tokens, 4096 x 11008,
 // float32: 417 us alone, 1.77 PFLOP/s; 475 us back to back with X's restore,
 // under the power cap), the output's bytes for few (128 tokens, 4096 x 4096
-// float32 with base: 36 us for 136 MB), and between the two the rounds of
+// float32 with base: 27 us for 136 MB), and between the two the rounds of
 // tiles over 76 pairs (2048 tokens, 4096 x 4096: 256 tiles are 3.4 rounds, run
 // as 4).
 #pragma once
@@ -52,20 +52,30 @@ __device__ __forceinline__ void regs_take() {
   asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
 }
 
-template <int BN, bool PAIR>
+// Blocks of base (32 x 32) in flight per epilogue warp of a kernel that brings
+// base in by TMA.
+constexpr int kBaseBlocks = 2;
+
+// BASE: the kernel has shared memory for blocks of base.
+template <int BN, bool PAIR, bool BASE>
 struct WgCfg {
   static constexpr int kTileM = PAIR ? 2 * kBM : kBM;
   static constexpr int kCtaN = PAIR ? BN / 2 : BN;  // columns of B a CTA loads
   static_assert(kCtaN % 64 == 0 && BN <= 256, "operands are assembled from 64-wide boxes");
   static constexpr uint32_t kBBytes = kCtaN * kRowBytes;
   static constexpr uint32_t kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = tc_max_stages(kCtaN, kWgEpiWarps, 1);
+  static constexpr uint32_t kBaseBytes = BASE ? kWgEpiWarps * kBaseBlocks * 4096u : 0u;
+  static constexpr int kBaseBars = BASE ? kWgEpiWarps * kBaseBlocks : 0;
+  // the deepest ring that the rest leaves room for
+  static constexpr int kStages =
+      tc_max_stages(kCtaN, kWgEpiWarps, 1) - (int)((kBaseBytes + kBaseBars * 8 + kStageBytes - 1) / kStageBytes);
   static constexpr uint32_t kTmemCols = pow2_at_least(2 * BN);
   static constexpr int kColsPerThread = BN / (kWgEpiWarps / 4);
   static_assert(kColsPerThread % 32 == 0, "the epilogue moves 32 columns at a time");
   static constexpr uint32_t kEpiOffset = kStages * kStageBytes;
-  static constexpr uint32_t kBarOffset = kEpiOffset + kWgEpiWarps * 4096;
-  static constexpr uint32_t kNumBars = 2 * kStages + 4 + 1;
+  static constexpr uint32_t kBaseOffset = kEpiOffset + kWgEpiWarps * 4096;
+  static constexpr uint32_t kBarOffset = kBaseOffset + kBaseBytes;
+  static constexpr uint32_t kNumBars = 2 * kStages + 4 + 1 + kBaseBars;
   static constexpr uint32_t kSmemBytes = kBarOffset + kNumBars * 8 + 16 + 1024;
   static_assert(kSmemBytes <= 232448, "shared memory per CTA is 227 KB");
   static_assert(kTmemCols <= 512, "TMEM has 512 columns");
@@ -183,6 +193,32 @@ __device__ __forceinline__ void tma_out_with_base(const WgradParams &p, const CU
   }
 }
 
+// A block of base in shared memory, as TMA brought it (the lane's row; 128-byte
+// swizzle for float32, 64-byte for bf16), added to v.
+__device__ __forceinline__ void add_base_block(uint32_t buf, int lane, bool bf, uint32_t (&v)[32]) {
+  if (bf) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint4 w = ld_shared_v4(buf + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4));
+      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t &lo = v[8 * j + 2 * k], &hi = v[8 * j + 2 * k + 1];
+        lo = __float_as_uint(__uint_as_float(lo) + __uint_as_float(u[k] << 16));
+        hi = __float_as_uint(__uint_as_float(hi) + __uint_as_float(u[k] & 0xFFFF0000u));
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float4 w = as_float4(ld_shared_v4(block_piece(buf, lane, j)));
+      const float u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[4 * j + k] = __float_as_uint(__uint_as_float(v[4 * j + k]) + u[k]);
+    }
+  }
+}
+
 // The block at (y0, x) with any base and C: base added, rounded once, stored
 // element by element along rows (lane = column).  AHEAD: b is as
 // fetch_base_elements left it.
@@ -241,12 +277,18 @@ __device__ __forceinline__ void store_elements(const WgradParams &p, uint32_t bu
 
 // SLABS: the sums of several slabs are added in registers (the reduction is
 // longer than one slab); else every unit is one slab.
-template <int BN, bool PAIR, bool SLABS>
+// BASE (without SLABS): base and C are TMA's; each epilogue warp keeps
+// kBaseBlocks blocks of base on their way in shared memory, the next unit's
+// among them, since with few tokens base and C are all the traffic and
+// registers hold base no further ahead than the unit (128 tokens, 4096 x 4096
+// float32: 36.0 us with registers, 27.4 so).
+template <int BN, bool PAIR, bool SLABS, bool BASE>
 __global__ void __launch_bounds__(kWgThreads, 1)
     wgrad_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                  const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ CUtensorMap tmWs,
-                 const WgradParams wp) {
-  using Cfg = WgCfg<BN, PAIR>;
+                 const __grid_constant__ CUtensorMap tmBase, const WgradParams wp) {
+  static_assert(!(SLABS && BASE), "slabs add base in registers");
+  using Cfg = WgCfg<BN, PAIR, BASE>;
   constexpr int STAGES = Cfg::kStages;
   const TcParams &p = wp.tc;
   extern __shared__ uint8_t smem_raw[];
@@ -264,6 +306,7 @@ __global__ void __launch_bounds__(kWgThreads, 1)
   auto accf_bar = [&](uint32_t b) { return bars + 8u * (2 * STAGES + b); };
   auto acce_bar = [&](uint32_t b) { return bars + 8u * (2 * STAGES + 2 + b); };
   const uint32_t drain_bar = bars + 8u * (2 * STAGES + 4);
+  const uint32_t base_bars = drain_bar + 8u;
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
@@ -282,11 +325,13 @@ __global__ void __launch_bounds__(kWgThreads, 1)
       mbar_init(acce_bar(b), (PAIR ? 2 : 1) * kWgEpiWarps * 32);
     }
     mbar_init(drain_bar, 1);
+    for (int b = 0; b < Cfg::kBaseBars; ++b) mbar_init(base_bars + 8u * b, 1);
     *abort_flag = 0u;
     fence_mbar_init();
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
     if (p.out_tma == kOutTmaC) tma_prefetch_desc(&tmOut);
+    if (BASE) tma_prefetch_desc(&tmBase);
     if (p.tail_splits > 0) tma_prefetch_desc(&tmWs);
   }
   __syncwarp();
@@ -428,12 +473,41 @@ __global__ void __launch_bounds__(kWgThreads, 1)
     const uint32_t ebuf = base + Cfg::kEpiOffset + ew * 4096u;
     uint32_t acc_cnt = 0;
     bool ok = true;
+    // BASE: blocks of base in the order in which they are added, those that
+    // exist; next_u, next_c: the next one to ask for
+    constexpr int kChunks = CPT / 32;
+    const uint32_t base_buf = base + Cfg::kBaseOffset + ew * (kBaseBlocks * 4096u);
+    const uint32_t base_bar = base_bars + 8u * (ew * kBaseBlocks);
+    uint32_t asked = 0, added = 0;
+    int next_u = first_unit, next_c = 0;
+    const auto ask = [&]() {
+      while (next_u < num_units) {
+        const Unit w = decode_unit(p, next_u);
+        const int y = w.tm * Cfg::kTileM + (int)rank * kBM + quad * 32, x = w.tn * BN + colpart * CPT + next_c * 32;
+        const bool here = w.part == 0 && y < p.M && x < p.N;
+        if (++next_c == kChunks || w.part != 0 || y >= p.M) {
+          next_c = 0;
+          next_u += unit_step;
+        }
+        if (!here) continue;
+        if (lane == 0) {
+          const uint32_t k = asked % kBaseBlocks;
+          mbar_arrive_expect_tx(base_bar + 8u * k, wp.out_bf16 ? 2048u : 4096u);
+          tma_load_2d(base_buf + k * 4096u, &tmBase, x, y, base_bar + 8u * k);
+        }
+        ++asked;
+        return;
+      }
+    };
+    if constexpr (BASE) {
+      for (int i = 0; i < kBaseBlocks; ++i) ask();
+    }
     for (int u = first_unit; ok && u < num_units; u += unit_step) {
       const Unit w = decode_unit(p, u);
       const bool split = w.part != 0;  // partials of a split-tail tile, not C
       const int y0 = w.tm * Cfg::kTileM + (int)rank * kBM + quad * 32;  // first row of this warp
       const int col0 = w.tn * BN + colpart * CPT;
-      const bool with_base = wp.base != nullptr && !split && y0 < p.M;
+      const bool with_base = !BASE && wp.base != nullptr && !split && y0 < p.M;
       // Writes 32 columns of sums: of C, or of a tail tile's partials (compact
       // blocks: tile `slot`, row pitch BN).
       auto emit = [&](uint32_t(&v)[32], uint4(&base_words)[8], int c) {
@@ -442,9 +516,20 @@ __global__ void __launch_bounds__(kWgThreads, 1)
         if (split) {
           tma_out_words32<true>(&tmWs, ebuf, lane, v, colpart * CPT + c * 32,
                                 w.slot * Cfg::kTileM + (int)rank * kBM + quad * 32, w.split, true);
-        } else if (p.out_tma == kOutTmaC && wp.base) {
+        } else if (!BASE && p.out_tma == kOutTmaC && wp.base) {
           if (in_range) tma_out_with_base<!SLABS>(wp, &tmOut, ebuf, lane, v, base_words, y0, x);
-        } else if (p.out_tma == kOutTmaC) {
+        } else if (BASE || p.out_tma == kOutTmaC) {
+          if (BASE && in_range) {
+            const uint32_t k = added % kBaseBlocks;
+            ok = __all_sync(0xffffffffu, mbar_wait(base_bar + 8u * k, (added / kBaseBlocks) & 1u, abort_flag, p.err,
+                                                   p.wait_limit_ns));
+            if (!ok) return;
+            ++added;
+            add_base_block(base_buf + k * 4096u, lane, wp.out_bf16 != 0, v);
+            fence_proxy_async_smem();
+            __syncwarp();
+            ask();  // into the block just read
+          }
           if (wp.out_bf16)
             tma_out_bf16x32(&tmOut, ebuf, lane, v, x, y0, in_range);
           else
@@ -463,15 +548,15 @@ __global__ void __launch_bounds__(kWgThreads, 1)
       };
       const uint32_t t_lane = (uint32_t)(quad * 32) << 16;
       if constexpr (!SLABS) {
-        // one slab: its sums are the result, streamed 32 columns at a time,
-        // the next two blocks of base on their way meanwhile
-        constexpr int kChunks = CPT / 32, kAhead = kChunks < 2 ? kChunks : 2;
+        // one slab: its sums are the result, streamed 32 columns at a time, base
+        // (without BASE) two blocks ahead in registers
+        constexpr int kAhead = kChunks < 2 ? kChunks : 2;
         uint4 ahead[kAhead][8] = {};
-        const auto fetch = [&](int x, uint4(&b)[8]) {
+        const auto fetch = [&](int x, uint4(&o)[8]) {
           if (p.out_tma == kOutTmaC)
-            fetch_base(wp, y0, x, lane, b);
+            fetch_base(wp, y0, x, lane, o);
           else
-            fetch_base_elements(wp, y0, x, lane, b);
+            fetch_base_elements(wp, y0, x, lane, o);
         };
 #pragma unroll
         for (int c = 0; c < kAhead; ++c)
@@ -488,8 +573,10 @@ __global__ void __launch_bounds__(kWgThreads, 1)
           tmem_ld<32>(tmem_base + b * BN + t_lane + colpart * CPT + c * 32, v);
           tmem_ld_wait();
           emit(v, ahead[c % kAhead], c);
+          if (!ok) break;
           if (with_base && c + kAhead < kChunks) fetch(col0 + (c + kAhead) * 32, ahead[c % kAhead]);
         }
+        if (!ok) break;
         release(b);
       } else {
         float acc[CPT];
@@ -523,7 +610,12 @@ __global__ void __launch_bounds__(kWgThreads, 1)
         }
       }
     }
-    if (lane == 0) bulk_wait_all();  // this warp's TMA stores have landed
+    if (lane == 0) {
+      // blocks of base asked for and not added (after giving up only) have landed
+      for (; BASE && added < asked; ++added)
+        mbar_wait_drain(base_bar + 8u * (added % kBaseBlocks), (added / kBaseBlocks) & 1u, kDrainNs);
+      bulk_wait_all();  // this warp's TMA stores have landed
+    }
   }
 
   griddep_launch_dependents();
