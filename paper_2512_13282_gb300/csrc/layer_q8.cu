@@ -30,6 +30,45 @@ __device__ __forceinline__ void half_block(int64_t h, int64_t halves, int64_t *r
   *c = (h - row * halves) * 16;
 }
 
+// A half block's bytes and its block's exponent (the other half is the
+// neighbouring lane's).
+struct Q8Half {
+  uint32_t w[4], e;
+};
+template <typename TX>
+__device__ __forceinline__ Q8Half q8_half(const Chunk<TX, 16> &raw) {
+  uint32_t top = 0;
+  if constexpr (sizeof(TX) == 2) {
+    top = max_magnitude_bf16<8>(raw.w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, raw.w[i] & 0x7FFFFFFFu);
+  }
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  const uint32_t e = q8_exponent(top);
+  float2 lo[4], hi[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) lo[j] = raw.get2(j), hi[j] = raw.get2(4 + j);
+  const uint2 wl = q8_pack8(lo, e), wh = q8_pack8(hi, e);
+  return Q8Half{{wl.x, wl.y, wh.x, wh.y}, e};
+}
+// The first n of a half block's bytes.
+__device__ __forceinline__ void store_bytes(int8_t *q, const uint32_t (&w)[4], int n) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (i < n) q[i] = (int8_t)(w[i / 4] >> (8 * (i & 3)));
+}
+// A half block's values in bf16.
+__device__ __forceinline__ void q8_restored(const Chunk<Q8, 16> &raw, float scale, uint32_t (&o)[8]) {
+  const __nv_bfloat162 s = __float2bfloat162_rn(scale);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    s8x4_to_bf16x4(raw.w[i], o[2 * i], o[2 * i + 1]);
+    o[2 * i] = scale_bf16x2(o[2 * i], s);
+    o[2 * i + 1] = scale_bf16x2(o[2 * i + 1], s);
+  }
+}
+
 // Rows of x and of q start on 16 bytes.
 template <typename TX>
 __global__ void __launch_bounds__(kQ8Threads)
@@ -50,29 +89,13 @@ __global__ void __launch_bounds__(kQ8Threads)
       raw.load(row, c);
     else
       raw.load_part(row, c, n);
-    uint32_t top = 0;
-    if constexpr (sizeof(TX) == 2) {
-      top = max_magnitude_bf16<8>(raw.w);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = max(top, raw.w[i] & 0x7FFFFFFFu);
-    }
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    const uint32_t e = q8_exponent(top);
-    float2 lo[4], hi[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) lo[j] = raw.get2(j), hi[j] = raw.get2(4 + j);
-    const uint2 wl = q8_pack8(lo, e), wh = q8_pack8(hi, e);
-    const uint32_t w[4] = {wl.x, wl.y, wh.x, wh.y};
+    const Q8Half b = q8_half(raw);
     int8_t *q = ck.q + r * ck.ldq + c;
-    if (n == 16) {
-      *reinterpret_cast<uint4 *>(q) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i < n) q[i] = (int8_t)(w[i / 4] >> (8 * (i & 3)));
-    }
-    if (live && (h & 1) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
+    if (n == 16)
+      *reinterpret_cast<uint4 *>(q) = make_uint4(b.w[0], b.w[1], b.w[2], b.w[3]);
+    else
+      store_bytes(q, b.w, n);
+    if (live && (h & 1) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)b.e;
   }
 }
 
@@ -97,14 +120,8 @@ __global__ void __launch_bounds__(kQ8Threads)
     TX *row = static_cast<TX *>(x) + r * ldx;
     if constexpr (sizeof(TX) == 2) {
       if (n == 16) {
-        const __nv_bfloat162 s = __float2bfloat162_rn(scale);
         uint32_t o[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s8x4_to_bf16x4(raw.w[i], o[2 * i], o[2 * i + 1]);
-          o[2 * i] = scale_bf16x2(o[2 * i], s);
-          o[2 * i + 1] = scale_bf16x2(o[2 * i + 1], s);
-        }
+        q8_restored(raw, scale, o);
         store_32_bytes(row + c, o);
         continue;
       }
@@ -116,35 +133,159 @@ __global__ void __launch_bounds__(kQ8Threads)
   }
 }
 
-// Any alignment: a warp takes kRun blocks of a row, a lane one value of each,
-// so that neighbouring lanes are neighbours in memory and kRun loads are in
-// flight a lane; a block's largest magnitude is one reduction over the warp.
-// Save and restore of 512 x 10216 float32 with a pitch of 10221: 20 us, which
-// a thread per half block with element accesses took 43 for.
-constexpr int kRun = 8;
+// Rows at any alignment: the same half blocks, their bytes shifted between
+// registers and the 16-byte pieces of memory that they lie in (one more than
+// fill them where the row does not start on 16 bytes).  A piece is read whole
+// where it lies inside the row, else (the row's ends) in 1, 2, 4 and 8 bytes.
+// A piece that two half blocks share is written by the later one's lane, which
+// has the earlier one's bytes from its neighbour; where there is no such
+// neighbour, both write their part.  1792 x 10471 bf16: save 16.5 us, restore
+// 15.3; a warp per 256 values of a row, a lane one value of each 32, took 36.4
+// and 23.6.
+
+// The words from byte `by` (0 .. 15) of w on.
+template <int W>
+__device__ __forceinline__ void shift_words(uint32_t (&w)[W + 4], uint32_t by) {
+#pragma unroll
+  for (int i = 0; i < W + 2; ++i) w[i] = by & 8u ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < W + 1; ++i) w[i] = by & 4u ? w[i + 1] : w[i];
+#pragma unroll
+  for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (by & 3u) * 8);
+}
+
+// Bytes [b, 16) and [0, b) of a 16-byte piece as naturally aligned runs of 1,
+// 2, 4 and 8: f(first byte, bytes).
+template <typename F>
+__device__ __forceinline__ void upper_runs(uint32_t b, F f) {
+#pragma unroll
+  for (uint32_t n = 1; n <= 8; n *= 2)
+    if (b & n) {
+      f(b, n);
+      b += n;
+    }
+}
+template <typename F>
+__device__ __forceinline__ void lower_runs(uint32_t b, F f) {
+  uint32_t at = 0;
+#pragma unroll
+  for (uint32_t n = 8; n >= 1; n /= 2)
+    if (b & n) {
+      f(at, n);
+      at += n;
+    }
+}
+
+// A run of the piece at p into its words w[AT ..] (zero before), and back.
+template <int AT, int N>
+__device__ __forceinline__ void load_run(const char *p, uint32_t at, uint32_t n, uint32_t (&w)[N]) {
+  uint2 v = make_uint2(0, 0);
+  if (n == 8)
+    v = *reinterpret_cast<const uint2 *>(p + at);
+  else
+    v.x = (n == 4   ? *reinterpret_cast<const uint32_t *>(p + at)
+           : n == 2 ? *reinterpret_cast<const uint16_t *>(p + at)
+                    : *reinterpret_cast<const uint8_t *>(p + at))
+          << (8 * (at & 3u));
+#pragma unroll
+  for (uint32_t k = 0; k < 4; ++k) w[AT + k] |= at >> 2 == k ? v.x : n == 8 && (at >> 2) + 1 == k ? v.y : 0u;
+}
+template <int AT, int N>
+__device__ __forceinline__ void store_run(char *p, uint32_t at, uint32_t n, const uint32_t (&w)[N]) {
+  const uint32_t i = at >> 2, lo = i & 1u ? w[AT + 1] : w[AT], hi = i & 1u ? w[AT + 3] : w[AT + 2];
+  const uint32_t v = (i & 2u ? hi : lo) >> (8 * (at & 3u));
+  if (n == 8)
+    *reinterpret_cast<uint2 *>(p + at) = at ? make_uint2(w[AT + 2], w[AT + 3]) : make_uint2(w[AT], w[AT + 1]);
+  else if (n == 4)
+    *reinterpret_cast<uint32_t *>(p + at) = v;
+  else if (n == 2)
+    *reinterpret_cast<uint16_t *>(p + at) = (uint16_t)v;
+  else
+    *reinterpret_cast<uint8_t *>(p + at) = (uint8_t)v;
+}
+
+// A half block's W words at src.  first: the row starts with it; after: bytes
+// of the row that follow it.
+template <int W>
+__device__ __forceinline__ void load_half(const void *src, bool first, int64_t after, uint32_t (&out)[W]) {
+  const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(src) & 15u;
+  const char *p = static_cast<const char *>(src) - off;
+  uint32_t w[W + 4] = {};
+#pragma unroll
+  for (int i = 0; i <= W / 4; ++i) {
+    if (i == 0 && first && off) {
+      upper_runs(off, [&](uint32_t at, uint32_t n) { load_run<0>(p, at, n, w); });
+    } else if (i == W / 4 && after < 16 - (int)off) {
+      lower_runs(off, [&](uint32_t at, uint32_t n) { load_run<W>(p + 4 * W, at, n, w); });
+    } else if (i < W / 4 || off) {
+      const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
+      w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+    }
+  }
+  shift_words<W>(w, off);
+#pragma unroll
+  for (int i = 0; i < W; ++i) out[i] = w[i];
+}
+
+// A half block's W words to dst; all lanes of the warp call it, the half
+// blocks of neighbouring ones following one another.  whole: the lane has one
+// to store; joined: the lane before has the one before it in its row; taken:
+// the lane after has the one after it, whole.
+template <int W>
+__device__ __forceinline__ void store_half(void *dst, bool whole, bool joined, bool taken, const uint32_t (&in)[W]) {
+  const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(dst) & 15u;
+  char *p = static_cast<char *>(dst) - off;
+  uint32_t w[W + 4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(0xffffffffu, in[W - 4 + i], 1);
+  if (!whole) return;
+#pragma unroll
+  for (int i = 0; i < W; ++i) w[4 + i] = in[i];
+  if (off == 0) {
+#pragma unroll
+    for (int i = 0; i < W / 4; ++i)
+      reinterpret_cast<uint4 *>(p)[i] = make_uint4(in[4 * i], in[4 * i + 1], in[4 * i + 2], in[4 * i + 3]);
+    return;
+  }
+  if (!taken) {  // bytes [0, off) of the last piece
+    uint32_t t[8] = {in[W - 4], in[W - 3], in[W - 2], in[W - 1]};
+    shift_words<4>(t, 16 - off);
+    lower_runs(off, [&](uint32_t at, uint32_t n) { store_run<0>(p + 4 * W, at, n, t); });
+  }
+  shift_words<W>(w, 16 - off);
+#pragma unroll
+  for (int i = 0; i < W / 4; ++i) {
+    if (i == 0 && !joined)
+      upper_runs(off, [&](uint32_t at, uint32_t n) { store_run<0>(p, at, n, w); });
+    else
+      reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  }
+}
 
 template <typename TX>
 __global__ void __launch_bounds__(kQ8Threads)
     q8_save_any_kernel(const void *x, int64_t ldx, int64_t rows, int64_t cols, Q8Ref ck) {
   griddep_launch_dependents();
   griddep_wait();
+  const int64_t halves = (cols + 31) / 32 * 2, items = rows * halves, step = (int64_t)gridDim.x * kQ8Threads;
   const int lane = threadIdx.x & 31;
-  const int64_t runs = (cols + 32 * kRun - 1) / (32 * kRun), items = rows * runs;
-  const int64_t step = (int64_t)gridDim.x * (kQ8Threads / 32);
-  for (int64_t t = (int64_t)blockIdx.x * (kQ8Threads / 32) + (threadIdx.x >> 5); t < items; t += step) {
-    const int64_t r = t / runs, c0 = (t - r * runs) * (32 * kRun) + lane;
-    float v[kRun];
-#pragma unroll
-    for (int k = 0; k < kRun; ++k) v[k] = c0 + 32 * k < cols ? load_value<TX>(x, r * ldx + c0 + 32 * k) : 0.f;
-    int8_t *q = ck.q + r * ck.ldq;
-    uint8_t *ex = ck.e + r * ck.lde;
-#pragma unroll
-    for (int k = 0; k < kRun; ++k) {
-      const int64_t c = c0 + 32 * k;
-      const uint32_t e = q8_exponent(__reduce_max_sync(0xffffffffu, __float_as_uint(v[k]) & 0x7FFFFFFFu));
-      if (c < cols) q[c] = (int8_t)q8_byte(v[k], q8_inverse(e), e);
-      if (lane == 0 && c < cols) ex[c >> 5] = (uint8_t)e;
-    }
+  for (int64_t h0 = (int64_t)blockIdx.x * kQ8Threads; h0 < items; h0 += step) {
+    const int64_t h = h0 + threadIdx.x;
+    const bool live = h < items;
+    int64_t r, c;
+    half_block(live ? h : items - 1, halves, &r, &c);
+    const int n = !live || c >= cols ? 0 : (int)min((int64_t)16, cols - c);
+    const TX *row = static_cast<const TX *>(x) + r * ldx;
+    Chunk<TX, 16> raw;
+    if (n == 16)
+      load_half(row + c, c == 0, (cols - c - 16) * (int64_t)sizeof(TX), raw.w);
+    else
+      raw.load_part(row, c, n);
+    const Q8Half b = q8_half(raw);
+    int8_t *q = ck.q + r * ck.ldq + c;
+    store_half(q, n == 16, lane > 0 && c > 0, lane < 31 && c + 32 <= cols, b.w);
+    if (n < 16) store_bytes(q, b.w, n);
+    if (live && (h & 1) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)b.e;
   }
 }
 
@@ -153,24 +294,40 @@ __global__ void __launch_bounds__(kQ8Threads)
     q8_restore_any_kernel(Q8Ref ck, void *x, int64_t ldx, int64_t rows, int64_t cols) {
   griddep_launch_dependents();
   griddep_wait();
+  const int64_t halves = (cols + 31) / 32 * 2, items = rows * halves, step = (int64_t)gridDim.x * kQ8Threads;
   const int lane = threadIdx.x & 31;
-  const int64_t runs = (cols + 32 * kRun - 1) / (32 * kRun), items = rows * runs;
-  const int64_t step = (int64_t)gridDim.x * (kQ8Threads / 32);
-  for (int64_t t = (int64_t)blockIdx.x * (kQ8Threads / 32) + (threadIdx.x >> 5); t < items; t += step) {
-    const int64_t r = t / runs, c0 = (t - r * runs) * (32 * kRun) + lane;
+  for (int64_t h0 = (int64_t)blockIdx.x * kQ8Threads; h0 < items; h0 += step) {
+    const int64_t h = h0 + threadIdx.x;
+    const bool live = h < items;
+    int64_t r, c;
+    half_block(live ? h : items - 1, halves, &r, &c);
+    const int n = !live || c >= cols ? 0 : (int)min((int64_t)16, cols - c);
     const int8_t *q = ck.q + r * ck.ldq;
-    const uint8_t *ex = ck.e + r * ck.lde;
-    float v[kRun];
-    uint32_t e[kRun];
+    const float scale = n > 0 ? q8_scale(ck.e[r * ck.lde + (c >> 5)]) : 0.f;
+    Chunk<Q8, 16> raw;
+    if (n == 16)
+      load_half(q + c, c == 0, cols - c - 16, raw.w);
+    else
+      raw.load_part(q, c, n);
+    TX *row = static_cast<TX *>(x) + r * ldx;
+    uint32_t o[4 * sizeof(TX)];
+    if constexpr (sizeof(TX) == 2) {
+      q8_restored(raw, scale, o);
+    } else {
 #pragma unroll
-    for (int k = 0; k < kRun; ++k) {
-      const int64_t c = c0 + 32 * k;
-      v[k] = c < cols ? (float)q[c] : 0.f;
-      e[k] = c < cols ? ex[c >> 5] : 0u;
+      for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(raw.get(i) * scale);
     }
+    store_half(row + c, n == 16, lane > 0 && c > 0, lane < 31 && c + 32 <= cols, o);
+    if (n < 16) {
 #pragma unroll
-    for (int k = 0; k < kRun; ++k)
-      if (c0 + 32 * k < cols) store_value<TX>(x, r * ldx + c0 + 32 * k, v[k] * q8_scale(e[k]));
+      for (int i = 0; i < 16; ++i)
+        if (i < n) {
+          if constexpr (sizeof(TX) == 2)
+            reinterpret_cast<uint16_t *>(row)[c + i] = (uint16_t)(o[i / 2] >> (16 * (i & 1)));
+          else
+            reinterpret_cast<uint32_t *>(row)[c + i] = o[i];
+        }
+    }
   }
 }
 
@@ -187,8 +344,7 @@ Q8Launch plan_q8(const Q8Ref &ck, const void *x, int64_t ldx, int x_type, int64_
     l.cols = rows * cols;
     l.rows = 1;
   }
-  const int64_t items = l.vec ? l.rows * ((l.cols + 31) / 32 * 2)
-                              : l.rows * ((l.cols + 32 * kRun - 1) / (32 * kRun)) * 32;
+  const int64_t items = l.rows * ((l.cols + 31) / 32 * 2);
   const int64_t blocks = (items + kQ8Threads - 1) / kQ8Threads;
   l.grid.x = (unsigned)(blocks < (1 << 30) ? blocks : (1 << 30));
   return l;
