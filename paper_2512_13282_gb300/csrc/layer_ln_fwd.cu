@@ -13,6 +13,8 @@
 // two thirds busy.
 #include <atomic>
 
+#include <type_traits>
+
 #include "layer_rows.cuh"
 
 namespace gb300 {
@@ -70,47 +72,46 @@ __global__ void __launch_bounds__(kAnyThreads) ln_forward_any_kernel(const LnFor
 }
 
 
-// A lane's 8 consecutive results, rounded to y's type and stored, and their part
-// of the checkpoint of y as stored (four lanes hold a block).  All lanes of the
-// warp call it, those past the row's end with `in` false.
-template <typename TY>
-__device__ __forceinline__ void store_eighth(TY *y, const Q8Ref &ck, int64_t r, int c, const float2 (&v)[4], bool in) {
+// A lane's 8 consecutive results (zero past the row's end), rounded to y's type
+// and stored, and their part of the checkpoint of y as stored (four lanes hold
+// a block).  All lanes of the warp call it, also those past the row's end.
+template <typename TY, bool SHIFT>
+__device__ __forceinline__ void store_eighth(TY *y, const Q8Ref &ck, int64_t r, int c, int cols, const float2 (&v)[4]) {
+  const bool in = c < cols;
   float2 o[4];
-  uint32_t top;
+  uint32_t top = 0, h[2 * sizeof(TY)];
   if constexpr (sizeof(TY) == 2) {
-    uint32_t h[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) h[j] = pack_bf16x2(v[j].x, v[j].y);
-    if (in) *reinterpret_cast<uint4 *>(y + c) = make_uint4(h[0], h[1], h[2], h[3]);
-    if (!ck.q) return;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) h[2 * j] = __float_as_uint(v[j].x), h[2 * j + 1] = __float_as_uint(v[j].y);
+  }
+  store_group<TY, SHIFT>(y, c, cols, h);
+  if (!ck.q) return;
+  if constexpr (sizeof(TY) == 2) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] = make_float2(__uint_as_float(h[j] << 16), __uint_as_float(h[j] & 0xFFFF0000u));
     top = max_magnitude_bf16<4>(h);
   } else {
-    if (in) {
-      float4 *d = reinterpret_cast<float4 *>(y + c);
-      d[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
-      d[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
-    }
-    if (!ck.q) return;
-    top = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       o[j] = v[j];
-      top = max(top, max(__float_as_uint(v[j].x) & 0x7FFFFFFFu, __float_as_uint(v[j].y) & 0x7FFFFFFFu));
+      top = max(top, max(h[2 * j] & 0x7FFFFFFFu, h[2 * j + 1] & 0x7FFFFFFFu));
     }
   }
   if (!in) top = 0;  // not in the block
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   const uint32_t e = q8_exponent(top);
-  const uint2 w = q8_pack8(o, e);
-  if (!in) return;
-  *reinterpret_cast<uint2 *>(ck.q + r * ck.ldq + c) = w;
-  if ((c & 31) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
+  const uint2 q = q8_pack8(o, e);
+  if (!SHIFT && !in) return;
+  const uint32_t w[2] = {q.x, q.y};
+  store_group<int8_t, SHIFT>(ck.q + r * ck.ldq, c, cols, w);
+  if (in && (c & 31) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
 }
 
-// Rows of up to THREADS * NV * 8 values, at least 64 where V = 1, read once and
+// Rows of up to THREADS * NV * 8 values, at least 64 where V is not 8, read once and
 // kept in registers until they are written.  A block of threads walks rows
 // gridDim.x apart, which come through a ring of slots that bulk copies fill
 // (SlotRow); one row ahead in registers instead was not enough in flight (3
@@ -125,6 +126,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
     ln_forward_ring_kernel(const LnForward p, const int stages, const uint32_t x_bytes, const int params_shared,
                            uint32_t *err, const uint64_t wait_limit_ns) {
   constexpr bool kKeep = NV == 1;
+  static_assert(kKeep || V != 1, "parameters in shared memory are for groups of eight");
+  using Row = std::conditional_t<V == kShifted, ShiftedRow<TX>, SlotRow<TX, V == 1 ? 1 : 8, THREADS>>;
   extern __shared__ __align__(128) uint8_t slots[];
   __shared__ __align__(16) float sm[2][32];
   __shared__ __align__(8) uint64_t bars[kMaxStages];
@@ -132,7 +135,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
   griddep_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t ring = smem_addr(slots), bar0 = smem_addr(bars);
-  float *shared_gamma = reinterpret_cast<float *>(slots + stages * x_bytes), *shared_beta = shared_gamma + p.cols;
+  const int param_cols = (p.cols + 7) / 8 * 8;
+  float *shared_gamma = reinterpret_cast<float *>(slots + stages * x_bytes), *shared_beta = shared_gamma + param_cols;
   RingPlace use, put;  // put: thread 0's
   const float inv_n = 1.0f / (float)p.cols;
   if (threadIdx.x == 0) {
@@ -149,21 +153,28 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
   const auto fill = [&](int64_t i) {
     const uint32_t dst = ring + put.slot * x_bytes, bar = bar0 + 8u * put.slot;
     put.advance(stages);
-    const uint32_t bytes = SlotRow<TX, V, THREADS>::copy_bytes(x_row(i), p.cols);
+    const uint32_t bytes = Row::copy_bytes(x_row(i), p.cols);
     mbar_arrive_expect_tx(bar, bytes);
-    SlotRow<TX, V, THREADS>::copy(dst, x_row(i), bytes, bar);
+    Row::copy(dst, x_row(i), bytes, bar);
   };
   int64_t filled = mine < stages ? mine : stages;
   if (threadIdx.x == 0)
     for (int64_t i = 0; i < filled; ++i) fill(i);
-  SlotRow<TX, V, THREADS> xr;
-  xr.init(p.cols);
-  xr.fetch_ends(x_row(0));
+  Row xr;
+  if constexpr (V == kShifted) {
+    // a row's ends go into its slot while the row before is worked on
+    xr.fetch_ends(x_row(0), p.cols);
+    xr.put_ends(slots, xr.offset(x_row(0)), p.cols);
+    if (mine > 1) xr.fetch_ends(x_row(1), p.cols);
+    __syncthreads();
+  } else {
+    xr.init(p.cols);
+    xr.fetch_ends(x_row(0));
+  }
   const auto gamma_at = [&](int c) { return c < p.cols ? load_param(p.gamma, p.param_type, c, 1.f) : 0.f; };
-  // place of column c's parameters in shared memory: where a lane takes eight,
-  // the first four of every eight and then the others, so that a warp's 16-byte
-  // reads follow one another
-  const auto param_at = [&](int c) { return V == 8 ? ((c >> 2) & 1) * (p.cols / 2) + (c >> 3) * 4 + (c & 3) : c; };
+  // place of column c's parameters in shared memory: the first four of every
+  // eight and then the others, so that a warp's 16-byte reads follow one another
+  const auto param_at = [&](int c) { return ((c >> 2) & 1) * (param_cols / 2) + (c >> 3) * 4 + (c & 3); };
   const auto beta_at = [&](int c) { return c < p.cols ? load_param(p.beta, p.param_type, c, 0.f) : 0.f; };
   float2 gamma[kKeep ? NV * 4 : 1], beta[kKeep ? NV * 4 : 1];
   if constexpr (kKeep) {
@@ -177,7 +188,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
       }
   } else if (params_shared) {
     // read past the first row's barriers; eight columns in flight a thread
-    for (int c0 = threadIdx.x; c0 < p.cols; c0 += 8 * blockDim.x) {
+    for (int c0 = threadIdx.x; c0 < param_cols; c0 += 8 * blockDim.x) {
       float g[8], b[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -187,7 +198,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const int c = c0 + k * (int)blockDim.x;
-        if (c < p.cols) shared_gamma[param_at(c)] = g[k], shared_beta[param_at(c)] = b[k];
+        if (c < param_cols) shared_gamma[param_at(c)] = g[k], shared_beta[param_at(c)] = b[k];
       }
     }
   }
@@ -201,6 +212,13 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
     if constexpr (V == 1) {
       if (ok) xr.put_ends(slot, off);
       if (i + 1 < mine) xr.fetch_ends(x_row(i + 1));
+    }
+    if constexpr (V == kShifted) {
+      // (that slot's last reads came before the barrier of the row before)
+      RingPlace next = use;
+      next.advance(stages);
+      if (i + 1 < mine) xr.put_ends(slots + next.slot * x_bytes, xr.offset(x_row(i + 1)), p.cols);
+      if (i + 2 < mine) xr.fetch_ends(x_row(i + 2), p.cols);
     }
     float2 x[NV * 4], s2 = both(0.f);
 #pragma unroll
@@ -226,16 +244,20 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
     float2 v2 = both(0.f);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      float2 t = both(0.f);
+      float2 t = both(0.f), d[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        float2 d = add2(x[v * 4 + j], both(-mean));
+        d[j] = add2(x[v * 4 + j], both(-mean));
         if constexpr (V == 1) {
-          if (group_col<V, THREADS>(v, 2 * j) >= p.cols) d.x = 0.f;
-          if (group_col<V, THREADS>(v, 2 * j + 1) >= p.cols) d.y = 0.f;
+          if (group_col<V, THREADS>(v, 2 * j) >= p.cols) d[j].x = 0.f;
+          if (group_col<V, THREADS>(v, 2 * j + 1) >= p.cols) d[j].y = 0.f;
         }
-        x[v * 4 + j] = d;
-        t = fma2(d, d, t);
+      }
+      if (V == kShifted && group_col<V, THREADS>(v, 8) > p.cols) zero_from(d, p.cols - group_col<V, THREADS>(v, 0));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[v * 4 + j] = d[j];
+        t = fma2(d[j], d[j], t);
       }
       v2 = add2(v2, V == 1 || group_col<V, THREADS>(v, 0) < p.cols ? t : both(0.f));
     }
@@ -258,8 +280,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
 #pragma unroll
         for (int j = 0; j < 4; ++j) g[j] = gamma[v * 4 + j], b[j] = beta[v * 4 + j];
       } else {
-        if (V == 8 && params_shared) {
-          const int at = c0 < p.cols ? param_at(c0) : 0, half = p.cols / 2;
+        if (params_shared) {
+          const int at = c0 < p.cols ? param_at(c0) : 0, half = param_cols / 2;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const float4 gq = *reinterpret_cast<const float4 *>(shared_gamma + at + h * half);
@@ -270,19 +292,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
         } else {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int c = group_col<V, THREADS>(v, 2 * j), d = group_col<V, THREADS>(v, 2 * j + 1);
-            const int cs = c < p.cols ? c : 0, ds = d < p.cols ? d : 0;
-            g[j] = params_shared ? make_float2(shared_gamma[cs], shared_gamma[ds])
-                                 : make_float2(gamma_at(c), gamma_at(d));
-            b[j] = params_shared ? make_float2(shared_beta[cs], shared_beta[ds])
-                                 : make_float2(beta_at(c), beta_at(d));
+            g[j] = make_float2(gamma_at(c0 + 2 * j), gamma_at(c0 + 2 * j + 1));
+            b[j] = make_float2(beta_at(c0 + 2 * j), beta_at(c0 + 2 * j + 1));
           }
         }
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] = fma2(mul2(x[v * 4 + j], both(rstd)), g[j], b[j]);
-      if constexpr (V == 8) {
-        store_eighth<TY>(y, p.ck, r, c0, o, c0 < p.cols);
+      if constexpr (V != 1) {
+        store_eighth<TY, V == kShifted>(y, p.ck, r, c0, p.cols, o);
       } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -326,14 +344,15 @@ cudaError_t run_ring(const LnForward &p, const OpContext &c) {
   static std::atomic<uint64_t> known{0};
   const auto kern = ln_forward_ring_kernel<TX, TY, NV, THREADS, V>;
   const int eights = (p.cols + 7) / 8, threads = V == 1 ? THREADS : ((eights + NV - 1) / NV + 31) / 32 * 32;
-  const uint32_t x_bytes = slot_bytes(p.cols, sizeof(TX), V == 8);
+  const uint32_t x_bytes =
+      V == kShifted ? shifted_slot_bytes(p.cols, sizeof(TX)) : slot_bytes(p.cols, sizeof(TX), V == 8);
   // the rings of the blocks that registers allow share the memory, with the
   // parameters where those stay in it; fewer blocks where two slots would not
   // fit beside them (8192 x 4096 float32: 98 us with four blocks that read the
   // parameters from global memory for every row, 46.7 with three)
   int want = 1024 / threads;
   if (want > 16) want = 16;
-  int64_t param_bytes = NV > 1 ? 8 * (int64_t)p.cols : 0;
+  int64_t param_bytes = NV > 1 ? 64 * (int64_t)eights : 0;
   while (want > 1 && param_bytes && kRingBytes / want - param_bytes < 2 * (int64_t)x_bytes) --want;
   const int64_t room = kRingBytes / want;
   if (room - param_bytes < 2 * (int64_t)x_bytes) param_bytes = 0;
@@ -347,20 +366,18 @@ cudaError_t run_ring(const LnForward &p, const OpContext &c) {
                    smem, c.st, 1, p, (int)stages, x_bytes, param_bytes ? 1 : 0, c.err, c.wait_limit_ns);
 }
 
-// The narrowest block that holds the row; where V = 1, whose blocks are not cut
-// to the row, in more steps (3543 x 5690 bf16: 54 us in 512 threads, 42 in 384).
+// Rows of up to 128 eights, at any alignment, are a value a lane at a time (V =
+// 1: 2560 x 777 bf16 7.1 us, shifted 9.0), wider ones shifted (3543 x 5690 bf16,
+// with checkpoint: 42 us, 69; shifted 35.5, 51; float32 without one 42 and 48).
 template <typename TX, typename TY, int V>
 cudaError_t run_width(const LnForward &p, const OpContext &c) {
   const int eights = (p.cols + 7) / 8;
   if (V == 1 && eights <= 32) return run_ring<TX, TY, 1, 32, 1>(p, c);
   if (V == 1 && eights <= 64) return run_ring<TX, TY, 1, 64, 1>(p, c);
   if (eights <= 128) return run_ring<TX, TY, 1, 128, V>(p, c);
-  if (V == 1 && eights <= 256) return run_ring<TX, TY, 2, 128, 1>(p, c);
-  if (eights <= 512) return run_ring<TX, TY, 2, 256, V>(p, c);
-  if (V == 1 && eights <= 768) return run_ring<TX, TY, 2, 384, 1>(p, c);
-  if (eights <= 1024) return run_ring<TX, TY, 2, 512, V>(p, c);
-  if (V == 1 && eights <= 1536) return run_ring<TX, TY, 2, 768, 1>(p, c);
-  return run_ring<TX, TY, 2, 1024, V>(p, c);
+  constexpr int W = V == 1 ? kShifted : V;
+  if (eights <= 512) return run_ring<TX, TY, 2, 256, W>(p, c);
+  return eights <= 1024 ? run_ring<TX, TY, 2, 512, W>(p, c) : run_ring<TX, TY, 2, 1024, W>(p, c);
 }
 
 template <typename TX, typename TY>

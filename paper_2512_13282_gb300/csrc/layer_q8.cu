@@ -133,50 +133,12 @@ __global__ void __launch_bounds__(kQ8Threads)
   }
 }
 
-// Rows at any alignment: the same half blocks, their bytes shifted between
-// registers and the 16-byte pieces of memory that they lie in (one more than
-// fill them where the row does not start on 16 bytes).  A piece is read whole
-// where it lies inside the row, else (the row's ends) in 1, 2, 4 and 8 bytes.
-// A piece that two half blocks share is written by the later one's lane, which
-// has the earlier one's bytes from its neighbour; where there is no such
-// neighbour, both write their part.  1792 x 10471 bf16: save 16.5 us, restore
-// 15.3; a warp per 256 values of a row, a lane one value of each 32, took 36.4
-// and 23.6.
+// Rows at any alignment: the same half blocks, shifted between registers and
+// the 16-byte pieces of memory that they lie in (shift_words, store_shifted).
+// 1792 x 10471 bf16: save 16.5 us, restore 15.3; a warp per 256 values of a
+// row, a lane one value of each 32, took 36.4 and 23.6.
 
-// The words from byte `by` (0 .. 15) of w on.
-template <int W>
-__device__ __forceinline__ void shift_words(uint32_t (&w)[W + 4], uint32_t by) {
-#pragma unroll
-  for (int i = 0; i < W + 2; ++i) w[i] = by & 8u ? w[i + 2] : w[i];
-#pragma unroll
-  for (int i = 0; i < W + 1; ++i) w[i] = by & 4u ? w[i + 1] : w[i];
-#pragma unroll
-  for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (by & 3u) * 8);
-}
-
-// Bytes [b, 16) and [0, b) of a 16-byte piece as naturally aligned runs of 1,
-// 2, 4 and 8: f(first byte, bytes).
-template <typename F>
-__device__ __forceinline__ void upper_runs(uint32_t b, F f) {
-#pragma unroll
-  for (uint32_t n = 1; n <= 8; n *= 2)
-    if (b & n) {
-      f(b, n);
-      b += n;
-    }
-}
-template <typename F>
-__device__ __forceinline__ void lower_runs(uint32_t b, F f) {
-  uint32_t at = 0;
-#pragma unroll
-  for (uint32_t n = 8; n >= 1; n /= 2)
-    if (b & n) {
-      f(at, n);
-      at += n;
-    }
-}
-
-// A run of the piece at p into its words w[AT ..] (zero before), and back.
+// A run of the piece at p into its words w[AT ..] (zero before).
 template <int AT, int N>
 __device__ __forceinline__ void load_run(const char *p, uint32_t at, uint32_t n, uint32_t (&w)[N]) {
   uint2 v = make_uint2(0, 0);
@@ -190,22 +152,9 @@ __device__ __forceinline__ void load_run(const char *p, uint32_t at, uint32_t n,
 #pragma unroll
   for (uint32_t k = 0; k < 4; ++k) w[AT + k] |= at >> 2 == k ? v.x : n == 8 && (at >> 2) + 1 == k ? v.y : 0u;
 }
-template <int AT, int N>
-__device__ __forceinline__ void store_run(char *p, uint32_t at, uint32_t n, const uint32_t (&w)[N]) {
-  const uint32_t i = at >> 2, lo = i & 1u ? w[AT + 1] : w[AT], hi = i & 1u ? w[AT + 3] : w[AT + 2];
-  const uint32_t v = (i & 2u ? hi : lo) >> (8 * (at & 3u));
-  if (n == 8)
-    *reinterpret_cast<uint2 *>(p + at) = at ? make_uint2(w[AT + 2], w[AT + 3]) : make_uint2(w[AT], w[AT + 1]);
-  else if (n == 4)
-    *reinterpret_cast<uint32_t *>(p + at) = v;
-  else if (n == 2)
-    *reinterpret_cast<uint16_t *>(p + at) = (uint16_t)v;
-  else
-    *reinterpret_cast<uint8_t *>(p + at) = (uint8_t)v;
-}
 
-// A half block's W words at src.  first: the row starts with it; after: bytes
-// of the row that follow it.
+// A half block's W words at src.  Pieces that reach past the row (first: it
+// starts with this half block; after: its bytes that follow) are read in runs.
 template <int W>
 __device__ __forceinline__ void load_half(const void *src, bool first, int64_t after, uint32_t (&out)[W]) {
   const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(src) & 15u;
@@ -214,52 +163,17 @@ __device__ __forceinline__ void load_half(const void *src, bool first, int64_t a
 #pragma unroll
   for (int i = 0; i <= W / 4; ++i) {
     if (i == 0 && first && off) {
-      upper_runs(off, [&](uint32_t at, uint32_t n) { load_run<0>(p, at, n, w); });
+      upper_runs<16>(off, [&](uint32_t at, uint32_t n) { load_run<0>(p, at, n, w); });
     } else if (i == W / 4 && after < 16 - (int)off) {
-      lower_runs(off, [&](uint32_t at, uint32_t n) { load_run<W>(p + 4 * W, at, n, w); });
+      lower_runs<16>(off, [&](uint32_t at, uint32_t n) { load_run<W>(p + 4 * W, at, n, w); });
     } else if (i < W / 4 || off) {
       const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
       w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
     }
   }
-  shift_words<W>(w, off);
+  shift_words<W, 4>(w, off);
 #pragma unroll
   for (int i = 0; i < W; ++i) out[i] = w[i];
-}
-
-// A half block's W words to dst; all lanes of the warp call it, the half
-// blocks of neighbouring ones following one another.  whole: the lane has one
-// to store; joined: the lane before has the one before it in its row; taken:
-// the lane after has the one after it, whole.
-template <int W>
-__device__ __forceinline__ void store_half(void *dst, bool whole, bool joined, bool taken, const uint32_t (&in)[W]) {
-  const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(dst) & 15u;
-  char *p = static_cast<char *>(dst) - off;
-  uint32_t w[W + 4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(0xffffffffu, in[W - 4 + i], 1);
-  if (!whole) return;
-#pragma unroll
-  for (int i = 0; i < W; ++i) w[4 + i] = in[i];
-  if (off == 0) {
-#pragma unroll
-    for (int i = 0; i < W / 4; ++i)
-      reinterpret_cast<uint4 *>(p)[i] = make_uint4(in[4 * i], in[4 * i + 1], in[4 * i + 2], in[4 * i + 3]);
-    return;
-  }
-  if (!taken) {  // bytes [0, off) of the last piece
-    uint32_t t[8] = {in[W - 4], in[W - 3], in[W - 2], in[W - 1]};
-    shift_words<4>(t, 16 - off);
-    lower_runs(off, [&](uint32_t at, uint32_t n) { store_run<0>(p + 4 * W, at, n, t); });
-  }
-  shift_words<W>(w, 16 - off);
-#pragma unroll
-  for (int i = 0; i < W / 4; ++i) {
-    if (i == 0 && !joined)
-      upper_runs(off, [&](uint32_t at, uint32_t n) { store_run<0>(p, at, n, w); });
-    else
-      reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-  }
 }
 
 template <typename TX>
@@ -283,7 +197,7 @@ __global__ void __launch_bounds__(kQ8Threads)
       raw.load_part(row, c, n);
     const Q8Half b = q8_half(raw);
     int8_t *q = ck.q + r * ck.ldq + c;
-    store_half(q, n == 16, lane > 0 && c > 0, lane < 31 && c + 32 <= cols, b.w);
+    store_shifted<4>(q, n == 16, lane > 0 && c > 0, lane < 31 && c + 32 <= cols, b.w);
     if (n < 16) store_bytes(q, b.w, n);
     if (live && (h & 1) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)b.e;
   }
@@ -317,7 +231,7 @@ __global__ void __launch_bounds__(kQ8Threads)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(raw.get(i) * scale);
     }
-    store_half(row + c, n == 16, lane > 0 && c > 0, lane < 31 && c + 32 <= cols, o);
+    store_shifted<4>(row + c, n == 16, lane > 0 && c > 0, lane < 31 && c + 32 <= cols, o);
     if (n < 16) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)

@@ -244,6 +244,106 @@ __device__ __forceinline__ void store_chunk(void *row, int64_t c, const float *v
   }
 }
 
+// Rows at any alignment.  A lane's values fill pieces of 16 bytes (P = 4 words;
+// 8 bytes, P = 2, where they are no more), but lie in one piece more where the
+// row does not start on a piece: what is loaded from whole pieces is shifted
+// down, what is stored is shifted up.
+
+// W words from byte `by` (below a piece's size) of w on.
+template <int W, int P>
+__device__ __forceinline__ void shift_words(uint32_t (&w)[W + P], uint32_t by) {
+  if constexpr (P == 4) {
+#pragma unroll
+    for (int i = 0; i < W + 2; ++i) w[i] = by & 8u ? w[i + 2] : w[i];
+  }
+#pragma unroll
+  for (int i = 0; i < W + 1; ++i) w[i] = by & 4u ? w[i + 1] : w[i];
+#pragma unroll
+  for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (by & 3u) * 8);
+}
+
+// Bytes [b, SIZE) and [0, b) of a piece as naturally aligned runs of a power of
+// two: f(first byte, bytes).
+template <uint32_t SIZE, typename F>
+__device__ __forceinline__ void upper_runs(uint32_t b, F f) {
+#pragma unroll
+  for (uint32_t n = 1; n < SIZE; n *= 2)
+    if (b & n) {
+      f(b, n);
+      b += n;
+    }
+}
+template <uint32_t SIZE, typename F>
+__device__ __forceinline__ void lower_runs(uint32_t b, F f) {
+  uint32_t at = 0;
+#pragma unroll
+  for (uint32_t n = SIZE / 2; n >= 1; n /= 2)
+    if (b & n) {
+      f(at, n);
+      at += n;
+    }
+}
+// A run of the piece w[0 .. P - 1] to its place in the piece at p.
+template <int P, int N>
+__device__ __forceinline__ void store_run(char *p, uint32_t at, uint32_t n, const uint32_t (&w)[N]) {
+  const uint32_t i = at >> 2;
+  uint32_t v = i & 1u ? w[1] : w[0];
+  if constexpr (P == 4) v = i & 2u ? (i & 1u ? w[3] : w[2]) : v;
+  v >>= 8 * (at & 3u);
+  if (P == 4 && n == 8)
+    *reinterpret_cast<uint2 *>(p + at) = at ? make_uint2(w[P - 2], w[P - 1]) : make_uint2(w[0], w[1]);
+  else if (n == 4)
+    *reinterpret_cast<uint32_t *>(p + at) = v;
+  else if (n == 2)
+    *reinterpret_cast<uint16_t *>(p + at) = (uint16_t)v;
+  else
+    *reinterpret_cast<uint8_t *>(p + at) = (uint8_t)v;
+}
+
+// A lane's W words to dst, any address that its type allows.  All lanes of the
+// warp call it, what neighbouring ones hold being neighbours in memory.  whole:
+// the lane has words to store; joined: the lane before it has the words before
+// them; taken: the lane after it has the words after them.  The later lane
+// writes a piece shared by two; where there is none, each writes its part.
+template <int P, int W>
+__device__ __forceinline__ void store_shifted(void *dst, bool whole, bool joined, bool taken, const uint32_t (&in)[W]) {
+  constexpr uint32_t kSize = 4 * P;
+  const auto store_piece = [](char *p, const uint32_t *w) {
+    if constexpr (P == 4)
+      *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    else
+      *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+  };
+  const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(dst) & (kSize - 1);
+  char *p = static_cast<char *>(dst) - off;
+  uint32_t w[W + P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) w[i] = __shfl_up_sync(0xffffffffu, in[W - P + i], 1);
+  if (!whole) return;
+  if (off == 0) {
+#pragma unroll
+    for (int i = 0; i < W / P; ++i) store_piece(p + i * kSize, in + i * P);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) w[P + i] = in[i];
+  if (!taken) {  // bytes [0, off) of the last piece
+    uint32_t t[2 * P] = {};
+#pragma unroll
+    for (int i = 0; i < P; ++i) t[i] = in[W - P + i];
+    shift_words<P, P>(t, kSize - off);
+    lower_runs<kSize>(off, [&](uint32_t at, uint32_t n) { store_run<P>(p + 4 * W, at, n, t); });
+  }
+  shift_words<W, P>(w, kSize - off);
+#pragma unroll
+  for (int i = 0; i < W / P; ++i) {
+    if (i == 0 && !joined)
+      upper_runs<kSize>(off, [&](uint32_t at, uint32_t n) { store_run<P>(p, at, n, w); });
+    else
+      store_piece(p + i * kSize, w + i * P);
+  }
+}
+
 // A parameter vector of either type, or absent.
 __device__ __forceinline__ float load_param(const void *p, int type, int c, float absent) {
   if (!p) return absent;
@@ -314,6 +414,43 @@ struct RingPlace {
 __device__ __forceinline__ void ring_drain(uint32_t bars, int stages, RingPlace use, int64_t pending) {
   for (; pending > 0; --pending, use.advance(stages))
     mbar_wait_drain(bars + 8u * use.slot, use.parity, 200ull * 1000 * 1000);
+}
+
+// Elements n .. 7 of a group to zero.
+__device__ __forceinline__ void zero_from(float2 (&x)[4], int n) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = make_float2(2 * j < n ? x[j].x : 0.f, 2 * j + 1 < n ? x[j].y : 0.f);
+}
+// A group's words, as stored in a row of T at column c of `cols`: in one piece
+// where the row is aligned, else shifted; a row's last few values one by one.
+// All lanes of the warp call it.
+template <typename T, bool SHIFT>
+__device__ __forceinline__ void store_group(T *row, int c, int cols, const uint32_t (&w)[2 * sizeof(T)]) {
+  constexpr int W = 2 * (int)sizeof(T), P = W < 4 ? 2 : 4;
+  if constexpr (!SHIFT) {
+    if (c >= cols) return;
+    if constexpr (P == 2)
+      *reinterpret_cast<uint2 *>(row + c) = make_uint2(w[0], w[1]);
+    else
+#pragma unroll
+      for (int i = 0; i < W / 4; ++i)
+        reinterpret_cast<uint4 *>(row + c)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  } else {
+    const int lane = threadIdx.x & 31;
+    store_shifted<P>(row + c, c + 8 <= cols, lane > 0, lane < 31 && c + 16 <= cols, w);
+    if (c < cols && c + 8 > cols) {
+#pragma unroll
+      for (int i = 0; i < 7; ++i)
+        if (c + i < cols) {
+          if constexpr (sizeof(T) == 4)
+            reinterpret_cast<uint32_t *>(row)[c + i] = w[i];
+          else if constexpr (sizeof(T) == 2)
+            reinterpret_cast<uint16_t *>(row)[c + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+          else
+            reinterpret_cast<uint8_t *>(row)[c + i] = (uint8_t)(w[i / 4] >> (8 * (i & 3)));
+        }
+    }
+  }
 }
 
 // A row of T values on its way through a ring slot, its elements taken in
@@ -410,11 +547,73 @@ struct SlotRow {
 // Column of value i of group v (see SlotRow).
 template <int V, int THREADS>
 __device__ __forceinline__ int group_col(int v, int i) {
-  return V == 8 ? (v * (int)blockDim.x + (int)threadIdx.x) * 8 + i : (v * 8 + i) * THREADS + (int)threadIdx.x;
+  return V != 1 ? (v * (int)blockDim.x + (int)threadIdx.x) * 8 + i : (v * 8 + i) * THREADS + (int)threadIdx.x;
 }
+
+// The same for groups of eight consecutive values at any alignment (V = kShifted;
+// columns as with V = 8), rows of at least 2 * kEdge values.  The ends are put
+// into the slot by the block's first threads, a barrier before it is read; a
+// group is read in whole 16-byte pieces and shifted into place.
+constexpr int kShifted = 0;
+template <typename T>
+struct ShiftedRow {
+  static constexpr int kSize = (int)sizeof(T), kEdge = 16 / kSize;
+  static_assert(kSize > 1, "a group fills pieces of 16 bytes");
+  using Any = SlotRow<T, 1, 32>;
+  uint32_t end;  // bits of the end value fetched ahead
+  __device__ __forceinline__ static uint32_t offset(const void *row) { return Any::offset(row); }
+  __device__ __forceinline__ static uint32_t copy_bytes(const void *row, int cols) { return Any::copy_bytes(row, cols); }
+  __device__ __forceinline__ static void copy(uint32_t dst, const void *row, uint32_t bytes, uint32_t bar) {
+    Any::copy(dst, row, bytes, bar);
+  }
+  // The end value of this thread: threads 0 .. kEdge - 1 have the row's first
+  // values, the next kEdge its last.
+  __device__ __forceinline__ static int end_col(int cols) {
+    const int t = (int)threadIdx.x;
+    return t < kEdge ? t : cols - 2 * kEdge + t;
+  }
+  __device__ __forceinline__ void fetch_ends(const void *row, int cols) {
+    if (threadIdx.x < 2 * kEdge) end = Any::bits(row, end_col(cols));
+  }
+  // Into the slot of that row, where the copy does not bring the value; no
+  // thread reads the slot's former row any more.  The fence orders the write
+  // before the copy that will refill the slot.
+  __device__ __forceinline__ void put_ends(uint8_t *slot, uint32_t off, int cols) const {
+    if (threadIdx.x >= 2 * kEdge) return;
+    const uint32_t at = off + (uint32_t)end_col(cols) * kSize, last = (off + (uint32_t)cols * kSize) & ~15u;
+    if ((off == 0 || at >= 16) && at < last) return;
+    Any::put(slot + at, end);
+    fence_proxy_async_smem();
+  }
+  // Group v of the row, zero past its end (the group at column 0 for a thread
+  // whose group starts past it, for the caller to leave out).
+  __device__ __forceinline__ static void load(const uint8_t *slot, uint32_t off, int v, int cols, float2 (&x)[4]) {
+    constexpr int W = 2 * kSize;
+    const int c = (v * (int)blockDim.x + (int)threadIdx.x) * 8, at = c < cols ? c : 0;
+    const uint4 *p = reinterpret_cast<const uint4 *>(slot + (uint32_t)at * kSize);
+    uint32_t w[W + 4];
+#pragma unroll
+    for (int i = 0; i <= W / 4; ++i) {
+      const uint4 u = p[i];
+      w[4 * i] = u.x, w[4 * i + 1] = u.y, w[4 * i + 2] = u.z, w[4 * i + 3] = u.w;
+    }
+    shift_words<W, 4>(w, off);
+    Chunk<T, 8> raw;
+#pragma unroll
+    for (int i = 0; i < W; ++i) raw.w[i] = w[i];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = raw.get2(j);
+    if (at + 8 > cols) zero_from(x, cols - at);
+  }
+};
+
 // Bytes of a slot for a row of cols values of `size` bytes.
 inline uint32_t slot_bytes(int64_t cols, int size, bool aligned) {
   return (uint32_t)(aligned ? cols * size : (cols * size + 30) / 16 * 16);
+}
+// The same for ShiftedRow: whole groups, and the piece more that they reach into.
+inline uint32_t shifted_slot_bytes(int64_t cols, int size) {
+  return (uint32_t)(((cols + 7) / 8 * 8 * size + 31) / 16 * 16);
 }
 
 constexpr int kMaxStages = 8;
