@@ -56,8 +56,9 @@ typedef enum {
  * Layer norm of the rows of x: with mu and var the mean and the (biased)
  * variance of a row,
  *     y = (x - mu) * rstd * gamma + beta,   rstd = 1 / sqrt(var + eps),
- * computed in float32 (the variance from the differences x - mu) and rounded
- * once to y's type.
+ * computed in float32 (the variance from the differences x - mu; a mean far
+ * above the deviations costs y none of their digits) and rounded once to y's
+ * type.
  *   x: rows x cols, pitch ldx, of x_type.  y: rows x cols, pitch ldy, of
  *   y_type.  gamma, beta: cols values of param_type; NULL stands for ones and
  *   zeros.  eps >= 0.

@@ -2,8 +2,13 @@
 // checkpoint:
 //     y = (x - mu) * rstd * gamma + beta,  rstd = 1 / sqrt(var + eps),
 // mu and var of a row, var from the differences x - mu (a second sum over the
-// row, held in registers, so that a mean far above the deviations costs no
-// digits).  Sums are float32; y is rounded once, to its type.
+// row, held in registers).  Sums are float32; y is rounded once, to its type.
+//
+// A mean far above the deviations costs no digits: the sum of x times 1/n, m,
+// is off by roundings of the size of |x|, and where that exceeds the
+// deviations (far_mean) a third sum, over d = x - m, takes them out again.  Its
+// average c is off by roundings of the size of the deviations only, and
+//     mu = m + c,  x - mu = d - c,  var = avg(d^2) - c^2.
 //
 // HBM bounds it: each value read once and written once, 4 bytes in bf16, and 1
 // more for the checkpoint.  Measured, back to back, bf16, against a plain copy
@@ -21,14 +26,25 @@ namespace gb300 {
 
 namespace {
 
-constexpr int kAnyThreads = 256;
+// Whether a row's mean is more than two standard deviations from zero, so that
+// its roundings matter beside those of the deviations (`squares`: the average
+// of d^2).  False for a row with a NaN.  Taking the average of d for every row,
+// in the same sum as d^2, cost 9 % (32768 x 1024 bf16: 33.0 us, without 30.3).
+__device__ __forceinline__ bool far_mean(float mean, float squares) { return mean * mean > 4.f * squares; }
+// avg(d^2) - c^2, not below zero by roundings (a NaN stays one).
+__device__ __forceinline__ float variance(float squares, float c) {
+  const float v = fmaf(-c, c, squares);
+  return v < 0.f ? 0.f : v;
+}
+
+constexpr int kAnyThreads = 256, kAnyBlocks = 8;  // blocks an SM
 
 // Any width, pitch and alignment: a block per row, the row read three times
 // (mean, variance, result), the second and third time from L1 or L2.  For rows
 // above 16384 values and unaligned ones below 64 only: 8192 x 4096 with its
 // checkpoint takes 300 us here.
 template <typename TX, typename TY>
-__global__ void __launch_bounds__(kAnyThreads) ln_forward_any_kernel(const LnForward p) {
+__global__ void __launch_bounds__(kAnyThreads, kAnyBlocks) ln_forward_any_kernel(const LnForward p) {
   __shared__ float2 sm[2][32];
   griddep_launch_dependents();
   griddep_wait();
@@ -44,9 +60,18 @@ __global__ void __launch_bounds__(kAnyThreads) ln_forward_any_kernel(const LnFor
       const float d = load_value<TX>(x, c) - mean;
       v = fmaf(d, d, v);
     }
-    const float rstd = rsqrtf(block_sum2(v, 0.f, sm, 1).x * inv_n + p.eps);
+    float var = block_sum2(v, 0.f, sm, 1).x * inv_n, rest = 0.f;
+    if (far_mean(mean, var)) {
+      float t = 0.f;
+      for (int c = threadIdx.x; c < p.cols; c += kAnyThreads) t += load_value<TX>(x, c) - mean;
+      // (the buffer's last reads came before the barrier of the sum between)
+      rest = block_sum2(t, 0.f, sm, 0).x * inv_n;
+      var = variance(var, rest);
+      __syncthreads();  // the next row writes the same buffer
+    }
+    const float rstd = rsqrtf(var + p.eps), shift = -rest * rstd;
     if (threadIdx.x == 0) {
-      if (p.mean) p.mean[r] = mean;
+      if (p.mean) p.mean[r] = mean + rest;
       if (p.rstd) p.rstd[r] = rstd;
     }
     TY *y = static_cast<TY *>(p.y) + r * p.ldy;
@@ -56,7 +81,7 @@ __global__ void __launch_bounds__(kAnyThreads) ln_forward_any_kernel(const LnFor
       const int c = c0 + lane;
       float out = 0.f;
       if (c < p.cols) {
-        out = fmaf((load_value<TX>(x, c) - mean) * rstd, load_param(p.gamma, p.param_type, c, 1.f),
+        out = fmaf(fmaf(load_value<TX>(x, c) - mean, rstd, shift), load_param(p.gamma, p.param_type, c, 1.f),
                    load_param(p.beta, p.param_type, c, 0.f));
         store_value<TY>(y, c, out);
       }
@@ -117,7 +142,7 @@ __device__ __forceinline__ void store_eighth(TY *y, const Q8Ref &ck, int64_t r, 
 // (SlotRow); one row ahead in registers instead was not enough in flight (3
 // blocks of 8 KB rows an SM: 24 KB, where the copy rate times the latency asks
 // for 40).  The first of a row's two barriers, the sums for its mean and its
-// variance, frees its slot.  gamma and beta stay in registers (NV = 1), else in
+// variance (a third with far_mean), frees its slot.  gamma and beta stay in registers (NV = 1), else in
 // shared memory as float32 where the rings leave room (params_shared), so that
 // 1024 threads share an SM whatever the width: with 16 parameters a thread in
 // registers half as many fit (8192 x 8192 with checkpoint: 77.4 us, now 72.4).
@@ -129,7 +154,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
   static_assert(kKeep || V != 1, "parameters in shared memory are for groups of eight");
   using Row = std::conditional_t<V == kShifted, ShiftedRow<TX>, SlotRow<TX, V == 1 ? 1 : 8, THREADS>>;
   extern __shared__ __align__(128) uint8_t slots[];
-  __shared__ __align__(16) float sm[2][32];
+  __shared__ __align__(16) float sm[3][32];
   __shared__ __align__(8) uint64_t bars[kMaxStages];
   __shared__ volatile uint32_t abort_flag;
   griddep_launch_dependents();
@@ -144,7 +169,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
     abort_flag = 0;
     fence_mbar_init();
   }
-  if (threadIdx.x < 32) sm[0][threadIdx.x] = sm[1][threadIdx.x] = 0.f;
+  if (threadIdx.x < 32) sm[0][threadIdx.x] = sm[1][threadIdx.x] = sm[2][threadIdx.x] = 0.f;
   __syncthreads();
   griddep_wait();
   const int64_t mine = (p.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // rows of this block, at least one
@@ -261,12 +286,27 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
       }
       v2 = add2(v2, V == 1 || group_col<V, THREADS>(v, 0) < p.cols ? t : both(0.f));
     }
-    const float var = warp_sum(v2.x + v2.y);
-    if (lane == 0) sm[1][warp] = var;
+    const float squares = warp_sum(v2.x + v2.y);
+    if (lane == 0) sm[1][warp] = squares;
     __syncthreads();
-    const float rstd = rsqrtf(sum_over_warps<THREADS / 32>(sm[1]) * inv_n + p.eps);
+    float var = sum_over_warps<THREADS / 32>(sm[1]) * inv_n, rest = 0.f;
+    if (far_mean(mean, var)) {  // the same for every thread
+      float2 c2 = both(0.f);
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const float2 t = add2(add2(x[v * 4], x[v * 4 + 1]), add2(x[v * 4 + 2], x[v * 4 + 3]));
+        c2 = add2(c2, V == 1 || group_col<V, THREADS>(v, 0) < p.cols ? t : both(0.f));
+      }
+      const float c = warp_sum(c2.x + c2.y);
+      if (lane == 0) sm[2][warp] = c;
+      __syncthreads();
+      rest = sum_over_warps<THREADS / 32>(sm[2]) * inv_n;
+      var = variance(var, rest);
+    }
+    const float rstd = rsqrtf(var + p.eps);
+    const float2 shift = both(-rest * rstd);
     if (threadIdx.x == 0) {
-      if (p.mean) p.mean[r] = mean;
+      if (p.mean) p.mean[r] = mean + rest;
       if (p.rstd) p.rstd[r] = rstd;
     }
     TY *y = static_cast<TY *>(p.y) + r * p.ldy;
@@ -298,7 +338,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
         }
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = fma2(mul2(x[v * 4 + j], both(rstd)), g[j], b[j]);
+      for (int j = 0; j < 4; ++j) o[j] = fma2(fma2(x[v * 4 + j], both(rstd), shift), g[j], b[j]);
       if constexpr (V != 1) {
         store_eighth<TY, V == kShifted>(y, p.ck, r, c0, p.cols, o);
       } else {
@@ -385,7 +425,7 @@ cudaError_t run_types(const LnForward &p, const OpContext &c) {
   const bool vec = p.cols % 8 == 0 && rows_on(p.x, p.ldx, sizeof(TX), 16) && rows_on(p.y, p.ldy, sizeof(TY), 16) &&
                    (!p.ck.q || rows_on(p.ck.q, p.ck.ldq, 1, 8));
   if (p.cols > 16384 || (!vec && p.cols < 64)) {
-    const int64_t most = (int64_t)c.sms * 8;
+    const int64_t most = (int64_t)c.sms * kAnyBlocks;
     return launch_ex(ln_forward_any_kernel<TX, TY>, dim3((unsigned)(p.rows < most ? p.rows : most)), dim3(kAnyThreads),
                      0, c.st, 1, p);
   }
