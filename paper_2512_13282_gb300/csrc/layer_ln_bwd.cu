@@ -2,9 +2,11 @@
 // g = dy * gamma, by rows
 //     dx = rstd * (g - avg(g) - xh * avg(g * xh)),
 // and over the rows dgamma = sum(dy * xh), dbeta = sum(dy).  Sums are float32,
-// in an order that the sizes fix: no atomics.  xh is formed as x * rstd -
-// mean * rstd with one rounding, and from a checkpoint's byte with the scale
-// folded into rstd (a power of two: exact).
+// in an order that the sizes fix: no atomics.  xh is the rounded difference
+// x - mean times rstd, two roundings relative to xh itself (x * rstd - mean *
+// rstd would carry one relative to mean * rstd, the same for a whole row); a
+// checkpoint's byte is scaled and the mean subtracted in one operation, the
+// product with a power of two being exact.
 //
 // HBM bounds it: x and dy read once and dx written once, 6 bytes a value in
 // bf16.  Measured, back to back, bf16: 8192 x 12288 96 us (6.3 TB/s, 0.93 of
@@ -157,13 +159,6 @@ __global__ void __launch_bounds__(THREADS) ln_param_sum_kernel(const float *part
   }
 }
 
-// Row r's mean and 1/std as the factors of xh = x * rstd - mean * rstd.
-struct RowStats {
-  float rstd, shift;
-  __device__ __forceinline__ explicit RowStats(float2 mean_rstd)
-      : rstd(mean_rstd.y), shift(-mean_rstd.x * mean_rstd.y) {}
-};
-
 // Rows of up to 512 * NV * 8 values, at least 64 where V = 1.  A block walks
 // rows gridDim.x apart.  Their x and dy come through a ring of row slots in shared memory, filled by bulk
 // copies that run as far ahead as the ring is deep (SlotRow): dgamma and dbeta
@@ -306,21 +301,19 @@ __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
     }
     // x as xh and dy of group v of row r of the step
     const auto load = [&](int r, int v, float2(&xh)[4], float2(&d)[4]) {
-      const RowStats stats(st[r]);
+      const float2 minus_mean = both(-st[r].x), rstd = both(st[r].y);
       xr.load(slot[r], x_off[r], v, p.cols, xh);
       yr.load(slot[r] + x_bytes, y_off[r], v, p.cols, d);
-      float2 scale = both(stats.rstd);
-      if constexpr (kQ8 && V == 8) {
-        scale = both(stats.rstd * q8_scale(exp_rows[r][group_col<V, THREADS>(v, 0) >> 5]));
-      }
+      float2 scale = both(1.f);
+      if constexpr (kQ8 && V == 8) scale = both(q8_scale(exp_rows[r][group_col<V, THREADS>(v, 0) >> 5]));
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if constexpr (kQ8 && V == 1) {
           const int c = group_col<V, THREADS>(v, 2 * j), e = group_col<V, THREADS>(v, 2 * j + 1);
-          scale = make_float2(stats.rstd * q8_scale(exp_rows[r][c < p.cols ? c >> 5 : 0]),
-                              stats.rstd * q8_scale(exp_rows[r][e < p.cols ? e >> 5 : 0]));
+          scale = make_float2(q8_scale(exp_rows[r][c < p.cols ? c >> 5 : 0]),
+                              q8_scale(exp_rows[r][e < p.cols ? e >> 5 : 0]));
         }
-        xh[j] = fma2(xh[j], scale, both(stats.shift));
+        xh[j] = mul2(kQ8 ? fma2(xh[j], scale, minus_mean) : add2(xh[j], minus_mean), rstd);
       }
     };
     float a[R], b[R];

@@ -70,3 +70,59 @@ def test_layernorm_forward_of_a_mean_far_above_the_deviations(cols, spread):
             within(mean, m, bm)
             within(rstd, s, bs)
             within(y, want, by)
+
+
+def backward_bounds(x, mean, rstd, gamma, dy, dx_type):
+    """(dx, dgamma, dbeta) error bounds with xh two roundings of x - mean and its
+    product with rstd (each relative to xh), and the sums over the rows at most
+    a chain of all of them."""
+    dx, _, _ = R.ln_backward(x, mean, rstd, gamma, dy)
+    x, dy, m, s = (a.astype(np.float64) for a in (x, dy, mean, rstd))
+    rows, depth = x.shape[0], R._depth(x.shape[1])
+    s = s[:, None]
+    xh = np.abs((x - m[:, None]) * s)
+    xh_err = 2.01 * U * xh
+    g = np.abs(dy * gamma)
+    b = (g * xh).mean(1, keepdims=True)
+    a_err = (depth + 4) * U * g.mean(1, keepdims=True)
+    b_err = (depth + 6) * U * b + (g * xh_err).mean(1, keepdims=True)
+    err = s * (6 * U * (g + g.mean(1, keepdims=True) + xh * b) + a_err + xh * b_err + xh_err * b)
+    err = err + (np.abs(dx) + err) * U_OUT[dx_type]
+    return (err, (np.abs(dy) * ((rows + 1) * U * xh + xh_err)).sum(0) * 1.01,
+            (rows + 1) * U * np.abs(dy).sum(0) * 1.01)
+
+
+@pytest.mark.parametrize("cols", WIDTHS)
+@pytest.mark.parametrize("xt,gt,ot", [("f32", "bf16", "f32"), ("f32", "f32", "f32"), ("bf16", "bf16", "bf16"),
+                                      ("q8", "bf16", "f32")])
+def test_layernorm_backward_of_a_mean_far_above_the_deviations(cols, xt, gt, ot):
+    """xh has the digits of x - mean, not those of mean: dgamma of one row is
+    dy * xh, of a few rows their sum."""
+    rng = np.random.default_rng(cols + 1)
+    for rows in (1, 3, 40):
+        for pad, off in PLACES:
+            X = Q = E = None
+            if xt == "q8":
+                q = rng.integers(90, 128, size=(rows, cols)).astype(np.int8)
+                e = np.full((rows, -(-cols // 32)), 127, np.uint8)
+                x = R.q8_values(q, e)
+                Q, E = Mat(rows, cols, "s8", pad, off, q), Mat(rows, e.shape[1], "u8", pad, off, e)
+            else:
+                x = levels(rng, rows, cols, 1.0) if xt == "f32" else as_kind(100 + rng.normal(size=(rows, cols)), xt)
+                X = Mat(rows, cols, xt, pad, off, x)
+            gamma = as_kind(1 + 0.2 * rng.normal(size=cols), "f32")
+            _, m, s = R.ln_forward(x, gamma, 0, 1e-5)
+            # the statistics with full mantissas, as a forward pass gives them
+            m, s = (m * (1 + 2.0 ** -20 * rng.uniform(size=rows))).astype(np.float32), s.astype(np.float32)
+            dy = as_kind(rng.normal(size=(rows, cols)), gt)
+            D, O = Mat(rows, cols, gt, pad, off, dy), Mat(rows, cols, ot, pad, off)
+            dg, db = Mat(1, cols, "f32"), Mat(1, cols, "f32")
+            done(L.gemm_layernorm_backward(
+                rows, cols, X.ptr if X else None, X.ld if X else 0, TYPES[ot], Q.ptr if Q else None, Q.ld if Q else 0,
+                E.ptr if E else None, E.ld if E else 0, vec(gamma, "f32"), TYPES["f32"], vec(m, "f32"), vec(s, "f32"),
+                D.ptr, D.ld, TYPES[gt], O.ptr, O.ld, TYPES[ot], dg.ptr, db.ptr))
+            want = R.ln_backward(x, m, s, gamma, dy)
+            bound = backward_bounds(x, m, s, gamma, dy, ot)
+            within(dg.host()[0], want[1], bound[1])
+            within(db.host()[0], want[2], bound[2])
+            within(O.host(), want[0], bound[0])
