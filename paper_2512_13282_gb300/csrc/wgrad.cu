@@ -17,6 +17,11 @@ inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // 777 x 1501): 8.1e-8, 1.1e-7, 2.2e-7 and 5.1e-7 with slabs of 2, 4, 8 and 16
 // k-blocks; 16 also breaks the header's bound per element.
 constexpr int kSlabKb = 8;
+// The same of a bf16 result: 8192 tokens, whose additions lose at most a tenth
+// of what its last rounding may (without a limit, millions of tokens lost more
+// than that).  4096 x 4096: 16384 tokens 329 us, in one chain 327; 32768 tokens
+// 665 and 671.
+constexpr int kSlabKbBf16 = 128;
 
 // Most k-blocks for which base comes through shared memory: its blocks displace
 // two stages of operands, which longer reductions miss.  4096 x 4096 bf16 with
@@ -256,7 +261,7 @@ size_t wgrad_partial_bytes(const WgradPlan &pl) {
 
 cudaError_t launch_wgrad(const WgradTile &tile, const WgradMaps &m, const WgradParams &p, int grid, cudaStream_t st) {
   WgradParams q = p;
-  q.tc.slab_kb = p.out_bf16 ? p.tc.num_kb : kSlabKb;
+  q.tc.slab_kb = p.out_bf16 ? kSlabKbBf16 : kSlabKb;
   if (tile.pair) return launch_tile<256, true>(m, q, grid, st);
   return tile.bn == 128 ? launch_tile<128, false>(m, q, grid, st) : launch_tile<64, false>(m, q, grid, st);
 }

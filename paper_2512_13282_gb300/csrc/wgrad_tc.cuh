@@ -12,12 +12,12 @@
 // gemm_tc2.cuh (PAIR: 256 x BN tiles, each CTA holding 128 rows of A^T and
 // half of B) and gemm_tc.cuh (one CTA, 128 x BN tiles).
 //
-// Float32 results are summed in slabs of p.tc.slab_kb k-blocks: the tensor
-// core accumulates a slab in TMEM, and the epilogue warps add the slabs'
-// sums in registers with round-to-nearest.  The tensor core's own additions
-// lose low bits in one direction, so that a chain's error grows with its
-// length; slabs bound the chain.  bf16 results, whose last rounding is far
-// coarser, take the whole sum as one slab.
+// Results are summed in slabs of p.tc.slab_kb k-blocks: the tensor core
+// accumulates a slab in TMEM, and the epilogue warps add the slabs' sums in
+// registers with round-to-nearest.  The tensor core's own additions cut what
+// lies below 2^-25 of the larger of the sum and the products, so that a chain's
+// error grows with its length; slabs bound the chain.  bf16 results, whose last
+// rounding is far coarser, take longer slabs.
 //
 // The tensor cores bound it for many tokens (8192 tokens, 4096 x 11008,
 // float32: 417 us alone, 1.77 PFLOP/s; 475 us back to back with X's restore,
