@@ -118,8 +118,16 @@ gemm_status_t gemm_q8_restore(int64_t rows, int64_t cols, const int8_t *q, int64
  *   ldbase, to which this one is added; it may be dW itself (base == dW with
  *   ldbase == ldw), which accumulates over micro-batches.
  * T == 0 leaves dW = base (zero without one); K == 0 or N == 0 is a no-op.
- * Accuracy contract for float32 dW: |dW - ref| <= 2^-24 |ref| + 2^-20 *
- * (|base| + sum_t |X(t, k) * dY(t, n)|) per element, ref the exact value.
+ * Accuracy contract, per element, with ref the exact value and
+ * S = |base| + sum_t |X(t, k) * dY(t, n)|:
+ *     float32 dW:  |dW - ref| <= 2^-24 |ref| + c(512) S,
+ *     bf16 dW:     |dW - ref| <= 2^-8 |ref| + c(8192) S,
+ *     c(L) = (min(T, L) + T / L + 32) * 2^-24
+ * (and the last rounding of that error).  The tensor core adds chains of L
+ * tokens, cutting what lies below 2^-25 of the larger of the running sum and
+ * the products; the chains are joined in float32 with round-to-nearest.  The
+ * worst inputs have one large product among many small ones; of products
+ * whose signs are random a float32 dW measures within 2^-20 S.
  */
 gemm_status_t gemm_q8_weight_grad(int64_t T, int64_t K, int64_t N, const int8_t *q, int64_t ldq,
                                   const uint8_t *e, int64_t lde, const uint16_t *dY, int64_t lddy,

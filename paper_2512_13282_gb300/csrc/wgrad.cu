@@ -15,7 +15,8 @@ inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Longest chain of tensor-core additions of a float32 result, in k-blocks
 // of 64 tokens.  Measured error of dW against 64 bits (2-norm, 1000 tokens of
 // 777 x 1501): 8.1e-8, 1.1e-7, 2.2e-7 and 5.1e-7 with slabs of 2, 4, 8 and 16
-// k-blocks; 16 also breaks the header's bound per element.
+// k-blocks; with 16 an element of random products is off by more than 2^-20 of
+// their magnitudes' sum.  (The header's bound is of 8.)
 constexpr int kSlabKb = 8;
 // The same of a bf16 result: 8192 tokens, whose additions lose at most a tenth
 // of what its last rounding may (without a limit, millions of tokens lost more

@@ -50,3 +50,34 @@ def test_bf16_weight_grad_of_many_tokens(T, K, N, nk):
         ref, mag = R.weight_grad(R.q8_values(q, e), dy, base, nk)
         within(W.host(), ref, R.weight_grad_bound(ref, mag, "bf16"))
         assert W.guarded()
+
+
+def contract(T, ref, total, w_type):
+    """The header's bound: chains of L tokens, of which 16 at a time cut 17 terms
+    to 2^-25 of the largest and their sum to a float32, 10.5 * 2^-24 of the
+    magnitudes' sum at most; a rounding for each chain, split part and base."""
+    chain = {"f32": 512, "bf16": 8192}[w_type]
+    err = (min(T, chain) + T / chain + 32) * 2.0 ** -24 * total
+    return err + (np.abs(ref) + err) * R.U_OUT[w_type]
+
+
+@pytest.mark.parametrize("T,K,N", [(16, 64, 64), (48, 96, 130), (512, 64, 96), (513, 32, 200), (512, 2048, 1100),
+                                   (2000, 160, 480), (8192, 64, 64), (20000, 64, 64)])
+@pytest.mark.parametrize("wt", ["f32", "bf16"])
+@pytest.mark.parametrize("with_base", [False, True])
+def test_weight_grad_of_one_large_and_many_small_products(T, K, N, wt, with_base):
+    """X = 1; each column of dY has 1 at some token and 0.98 * 2^-s elsewhere, s
+    from 20 to 31, in all four pairs of signs: what the additions cut adds up."""
+    rng = np.random.default_rng(T + N)
+    j = np.arange(N)
+    dy = np.broadcast_to((63 / 64) * 2.0 ** -(20.0 + j % 12) * np.where(j // 12 % 2, -1, 1), (T, N)).copy()
+    dy[rng.integers(0, T, size=N), j] = np.where(j // 24 % 2, -1, 1)
+    if T > 100:
+        dy[0, : N // 2] = 1                         # in the first step of the chain
+    base = as_kind(rng.normal(size=(K, N)), wt) if with_base else np.zeros((K, N), np.float32)
+    Q, E = Mat(T, K, "s8", fill=np.full((T, K), 64, np.int8)), Mat(T, K // 32, "u8", fill=np.full((T, K // 32), 121))
+    D, W, B = Mat(T, N, "bf16", fill=dy), Mat(K, N, wt), Mat(K, N, wt, fill=base)
+    done(L.gemm_q8_weight_grad(T, K, N, Q.ptr, K, E.ptr, K // 32, D.ptr, N, B.ptr if with_base else None, N, W.ptr, N,
+                               L.GEMM_B_ROW_MAJOR_KxN, TYPES[wt]))
+    ref, total = dy.sum(0) + base.astype(np.float64), np.abs(dy).sum(0) + np.abs(base.astype(np.float64))
+    within(W.host(), ref, contract(T, ref, total, wt))
