@@ -25,6 +25,18 @@ from . import layer as L
 _TYPE = {torch.float32: L.GEMM_TYPE_F32, torch.bfloat16: L.GEMM_TYPE_BF16}
 
 
+def _pitch(x, rows, cols, device, types=tuple(_TYPE)):
+    """Elements from one row of x to the next, for the library, which takes
+    addresses and sizes on trust: ValueError unless x is rows x cols of one of
+    the types on the device, with contiguous rows that do not overlap."""
+    if tuple(x.shape) != (rows, cols) or x.dtype not in types or x.device != device:
+        raise ValueError(f"expected {rows} x {cols} of {' or '.join(map(str, types))} on {device}, "
+                         f"got {tuple(x.shape)} of {x.dtype} on {x.device}")
+    if (cols > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) < cols):
+        raise ValueError(f"expected contiguous rows, got strides {x.stride()} of {tuple(x.shape)}")
+    return x.stride(0) if rows > 1 else cols
+
+
 class Checkpoint:
     """An activation held in 8 bits on the device (see gb300_layer.h)."""
 
@@ -42,19 +54,23 @@ class Checkpoint:
         return self.q.numel() + self.e.numel()
 
     def save(self, x):
-        L.check(L.gemm_q8_save(self.rows, self.cols, x, x.stride(0), _TYPE[x.dtype], *self.args))
+        ld = _pitch(x, self.rows, self.cols, self.q.device)
+        L.check(L.gemm_q8_save(self.rows, self.cols, x, ld, _TYPE[x.dtype], *self.args))
         return self
 
     def restore(self, dtype=torch.bfloat16):
+        if dtype not in _TYPE:
+            raise ValueError(f"restores to {' or '.join(map(str, _TYPE))}, not {dtype}")
         x = torch.empty((self.rows, self.cols), dtype=dtype, device=self.q.device)
-        L.check(L.gemm_q8_restore(self.rows, self.cols, *self.args, x, x.stride(0), _TYPE[dtype]))
+        L.check(L.gemm_q8_restore(self.rows, self.cols, *self.args, x, self.cols, _TYPE[dtype]))
         return x
 
 
 class ProjectionBlock:
     """Parameters, float32 gradients (accumulated until ``zero_grad``) and the
     two passes.  x may be bf16 or float32 (a residual stream); W is bf16,
-    K x N row-major."""
+    K x N row-major.  A pass raises ValueError for a tensor of another shape,
+    type or device, or without contiguous rows."""
 
     def __init__(self, width, out, generator=None, eps=1e-5):
         dev = dict(device="cuda", generator=generator)
@@ -71,13 +87,14 @@ class ProjectionBlock:
             g.zero_()
 
     def forward(self, x):
-        T, K, N = x.shape[0], self.width, self.out
-        y = torch.empty((T, K), dtype=torch.bfloat16, device="cuda")
-        mean, rstd = (torch.empty(T, device="cuda") for _ in range(2))
-        cx, cy = Checkpoint(T, K).save(x), Checkpoint(T, K)
-        L.check(L.gemm_layernorm_forward(T, K, x, x.stride(0), _TYPE[x.dtype], self.gamma, self.beta,
+        T, K, N, dev = x.shape[0], self.width, self.out, self.weight.device
+        ldx = _pitch(x, T, K, dev)
+        y = torch.empty((T, K), dtype=torch.bfloat16, device=dev)
+        mean, rstd = (torch.empty(T, device=dev) for _ in range(2))
+        cx, cy = Checkpoint(T, K, dev).save(x), Checkpoint(T, K, dev)
+        L.check(L.gemm_layernorm_forward(T, K, x, ldx, _TYPE[x.dtype], self.gamma, self.beta,
                                          L.GEMM_TYPE_F32, self.eps, y, K, L.GEMM_TYPE_BF16, mean, rstd, *cy.args))
-        o = torch.empty((T, N), dtype=torch.bfloat16, device="cuda")
+        o = torch.empty((T, N), dtype=torch.bfloat16, device=dev)
         G.check(G.gemm_bf16_f32acc_bf16(T, N, K, y, K, self.weight, N, G.GEMM_B_ROW_MAJOR_KxN, o, N))
         self._held = (cx, cy, mean, rstd, x.dtype)
         return o
@@ -89,15 +106,19 @@ class ProjectionBlock:
         return cx.nbytes + cy.nbytes + 4 * (mean.numel() + rstd.numel())
 
     def backward(self, do):
-        """dx of the last forward pass (of x's type); adds to the gradients."""
+        """dx of the last forward pass (of x's type) from do, a row for each of
+        its rows, bf16; adds to the gradients."""
+        if self._held is None:
+            raise RuntimeError("backward takes what a forward pass holds, once")
         cx, cy, mean, rstd, dtype = self._held
-        T, K, N = do.shape[0], self.width, self.out
+        T, K, N, dev = cx.rows, self.width, self.out, self.weight.device
+        lddo = _pitch(do, T, N, dev, (torch.bfloat16,))
         # do . W^T: W as stored (K x N) is the transposed factor N x K, column-major
-        dy = torch.empty((T, K), dtype=torch.bfloat16, device="cuda")
-        G.check(G.gemm_bf16_f32acc_bf16(T, K, N, do, do.stride(0), self.weight, N, G.GEMM_B_COL_MAJOR_NxK, dy, K))
-        L.check(L.gemm_q8_weight_grad(T, K, N, *cy.args, do, do.stride(0), self.dweight, N, self.dweight, N,
+        dy = torch.empty((T, K), dtype=torch.bfloat16, device=dev)
+        G.check(G.gemm_bf16_f32acc_bf16(T, K, N, do, lddo, self.weight, N, G.GEMM_B_COL_MAJOR_NxK, dy, K))
+        L.check(L.gemm_q8_weight_grad(T, K, N, *cy.args, do, lddo, self.dweight, N, self.dweight, N,
                                       L.GEMM_B_ROW_MAJOR_KxN, L.GEMM_TYPE_F32))
-        dx = torch.empty((T, K), dtype=dtype, device="cuda")
+        dx = torch.empty((T, K), dtype=dtype, device=dev)
         dgamma, dbeta = torch.empty_like(self.gamma), torch.empty_like(self.beta)
         L.check(L.gemm_layernorm_backward(T, K, None, 0, L.GEMM_TYPE_F32, *cx.args, self.gamma, L.GEMM_TYPE_F32, mean,
                                           rstd, dy, K, L.GEMM_TYPE_BF16, dx, K, _TYPE[dtype], dgamma, dbeta))
