@@ -58,7 +58,7 @@ struct LnBackward {
   float *partials;        // ln_backward_partials() floats, or null
 };
 // Floats of workspace a backward pass wants for its partial parameter
-// gradients (0: it computes none).
+// gradients (0: it computes none, or has no partial ones).
 size_t ln_backward_partials(const LnBackward &p, int sms);
 // *launches is increased by the kernels launched.
 cudaError_t launch_ln_backward(const LnBackward &p, const OpContext &c, int *launches);

@@ -429,6 +429,9 @@ struct LnPlan {
   uint32_t x_bytes, dy_bytes;  // of a slot
 };
 
+// The ring kernel's only block writes dgamma and dbeta itself.
+bool writes_whole_sums(const LnPlan &l) { return l.path == kLnRing && l.grid == 1; }
+
 // Blocks that walk `rows` rows, `per_sm` at a time on an SM: every SM one
 // while there are few rows, more where each still has two rows to set against
 // the partial row that it writes and another kernel reads (1000 rows of 1500
@@ -544,7 +547,7 @@ cudaError_t run_types(const LnBackward &p, const OpContext &c, int *launches) {
       e = launch_ex(ln_backward_any_kernel<TX, TDY, TDX>, grid, dim3(kRowThreads), 0, c.st, 1, p);
     if (e != cudaSuccess) return e;
   }
-  if (!p.partials || (l.path == kLnRing && l.grid == 1)) return e;
+  if (!p.partials || writes_whole_sums(l)) return e;
   const int strips = (int)ceil_div64(p.cols, 32);
   if (l.path == kLnAny) {
     ++*launches;
@@ -561,7 +564,9 @@ cudaError_t run_types(const LnBackward &p, const OpContext &c, int *launches) {
 }  // namespace
 
 size_t ln_backward_partials(const LnBackward &p, int sms) {
-  return p.dgamma || p.dbeta ? (size_t)2 * plan_ln_backward(p, sms).parts * partial_pitch(p.cols) : 0;
+  if (!p.dgamma && !p.dbeta) return 0;
+  const LnPlan l = plan_ln_backward(p, sms);
+  return writes_whole_sums(l) ? 0 : (size_t)2 * l.parts * partial_pitch(p.cols);
 }
 
 cudaError_t launch_ln_backward(const LnBackward &p, const OpContext &c, int *launches) {
