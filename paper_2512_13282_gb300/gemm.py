@@ -104,9 +104,13 @@ def _ptr(x) -> int:
 def _stream(s) -> int:
     if s is None:
         import torch
-        # the handle itself: a torch.cuda.Stream object around it costs 2.8 us
-        # a call on GB300's host, a third of a small call's time, this 0.3 us
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        # the handle itself, where torch has this function, which is not public:
+        # a torch.cuda.Stream object around it costs 2.8 us a call on GB300's
+        # host, a third of a small call's time, this 0.3 us
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is None:
+            return int(torch.cuda.current_stream().cuda_stream)
+        return raw(torch.cuda.current_device())
     if isinstance(s, int):
         return s
     return int(s.cuda_stream)
