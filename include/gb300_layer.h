@@ -31,7 +31,9 @@
  * x / 2^E and q * 2^E are exact, so the checkpoint is determined bit for bit,
  * and every value it stands for is a bf16 number, so that a bf16 tensor core
  * multiplies checkpointed activations without a further rounding.  The error
- * of a value is at most 2^(E-1), below top / 126 (2^E at E = 122).
+ * of a value is at most 2^(E-1), which is below top / 126 for -126 < E < 122;
+ * at E = -126 it is at most 2^-127 whatever top is (a value below that is held
+ * as 0), at E = 122 at most 2^E.
  */
 #ifndef GB300_LAYER_H
 #define GB300_LAYER_H

@@ -9,9 +9,9 @@
 // product with a power of two being exact.
 //
 // HBM bounds it: x and dy read once and dx written once, 6 bytes a value in
-// bf16.  Measured, back to back, bf16: 8192 x 12288 96 us (6.3 TB/s, 0.93 of
-// the copy rate), 8192 x 4096 38 us (5.3 TB/s), 2048 x 4096 19 us (a row's
-// latency times seven rows a block, and the second launch), 65536 x 512 45 us.
+// bf16.  Measured, back to back, bf16: 8192 x 12288 98 us (6.2 TB/s, 0.91 of
+// the copy rate), 8192 x 4096 40 us (5.0 TB/s), 2048 x 4096 19 us (a row's
+// latency times seven rows a block, and the second launch), 65536 x 512 47 us.
 #include "layer_rows.cuh"
 
 namespace gb300 {
@@ -49,8 +49,9 @@ __device__ __forceinline__ float ln_input(const LnBackward &p, int64_t r, int c)
 
 // Any width, pitch and alignment: dx, a block per row, the row's x and dy
 // read twice (the two averages, then dx).  For what the ring kernel does not
-// take: rows above 16384 values, unaligned ones below 64.  2048 x 4096 bf16
-// takes 37 us this way.
+// take: rows above 16384 values, or above 12800 of float32 x and dy, of which
+// two do not fit in its ring (4096 x 12800 146 us, 4096 x 16384 429), and
+// unaligned ones below 64.  2048 x 4096 bf16 takes 37 us this way.
 template <typename TX, typename TDY, typename TDX>
 __global__ void __launch_bounds__(kRowThreads) ln_backward_any_kernel(const LnBackward p) {
   __shared__ float2 sm[2][32];
@@ -159,11 +160,11 @@ __global__ void __launch_bounds__(THREADS) ln_param_sum_kernel(const float *part
   }
 }
 
-// Rows of up to 512 * NV * 8 values, at least 64 where V = 1.  A block walks
-// rows gridDim.x apart.  Their x and dy come through a ring of row slots in shared memory, filled by bulk
-// copies that run as far ahead as the ring is deep (SlotRow): dgamma and dbeta
-// are summed in registers (16 values a thread and NV), which leaves none for
-// rows in flight.  A row is read from its slot twice, for the two averages and
+// Rows of up to 512 * NV * 8 values of which two fit in the ring, at least 64
+// where V = 1.  A block walks rows gridDim.x apart.  Their x and dy come through
+// a ring of row slots in shared memory, filled by bulk copies that run as far
+// ahead as the ring is deep (SlotRow): dgamma and dbeta are summed in registers
+// (16 values a thread and NV), which leaves none for rows in flight.  A row is read from its slot twice, for the two averages and
 // for the results; the block-wide barrier between, passed by every thread once
 // it has finished with the row before, also frees that row's slot, which
 // thread 0 refills.  `step` rows are taken between two barriers.  One partial
@@ -457,13 +458,15 @@ LnPlan plan_ln_backward(const LnBackward &p, int sms) {
               rows_on(x, ldx, sx, 16) && rows_on(p.dy, p.lddy, sg, 16) && rows_on(p.dx, p.lddx, so, 16);
   // few threads with more values each: a row's fixed costs (its barrier, the
   // sums over lanes and warps) are paid by every warp.  32768 x 1024: 51 us
-  // with 8 values a thread, 44 with 16; 32768 x 4096: 131 us with 16, 126 with
-  // 32, which take three blocks an SM where 16 take two, and so many rows that
-  // the third's partial sums do not matter (2048 x 4096: 19.8 and 21.5 us).
+  // with 8 values a thread, 44 with 16; 8192 x 4096: 41.7 us with 16, 39.8 with
+  // 32 (from a checkpoint 48.8 and 44.9), which take three blocks an SM where 16
+  // take two, and so many rows that the third's partial sums do not matter (2048
+  // x 4096: 18.9 and 19.9 us).  Four times as many rows lose a little: 32768 x
+  // 4096 132 and 140 us.
   l.nv = eights <= (l.aligned ? 32 : 128) ? 1 : eights <= 2 * kRingThreads ? 2 : (int)ceil_div64(eights, kRingThreads);
   if (l.aligned && eights > 256 && eights <= 512 && p.rows >= (int64_t)32 * sms) l.nv = 4;
   // two blocks of up to 256 threads an SM instead of one of up to 384, where
-  // both have four slots (8192 x 5120 bf16: 57.8 us with one, 50.7 with two;
+  // both have four slots (8192 x 5120 bf16: 57.8 us with one, then 50.7 with two;
   // 3543 x 5690, unaligned: 49.9 and 39.8)
   if (eights > 512 && eights <= 768 &&
       kRingBytes / 2 / (slot_bytes(p.cols, sx, l.aligned) + slot_bytes(p.cols, sg, l.aligned)) >= 4)

@@ -12,10 +12,10 @@
 //
 // HBM bounds it: each value read once and written once, 4 bytes in bf16, and 1
 // more for the checkpoint.  Measured, back to back, bf16, against a plain copy
-// of as many bytes: 8192 x 4096 28.3 us (4.7 TB/s; copy 23.1), with the
-// checkpoint 38.5 us; 32768 x 4096 96 us (5.6 TB/s; copy 82).  What is left is
-// issue: 22 instructions a value (32 with the checkpoint) keep the schedulers
-// two thirds busy.
+// of as many bytes: 8192 x 4096 28.6 us (4.7 TB/s; copy 23.1), with the
+// checkpoint 38.6 us; 32768 x 4096 97 us (5.5 TB/s; copy 82).  What is left is
+// a row's two block-wide sums, one after the other: neither issue (64 % of the
+// cycles with the checkpoint) nor the HBM is full.
 #include <atomic>
 
 #include <type_traits>
@@ -145,7 +145,7 @@ __device__ __forceinline__ void store_eighth(TY *y, const Q8Ref &ck, int64_t r, 
 // variance (a third with far_mean), frees its slot.  gamma and beta stay in registers (NV = 1), else in
 // shared memory as float32 where the rings leave room (params_shared), so that
 // 1024 threads share an SM whatever the width: with 16 parameters a thread in
-// registers half as many fit (8192 x 8192 with checkpoint: 77.4 us, now 72.4).
+// registers half as many fit (8192 x 8192 with checkpoint: 77.4 us, so 72.4).
 template <typename TX, typename TY, int NV, int THREADS, int V>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
     ln_forward_ring_kernel(const LnForward p, const int stages, const uint32_t x_bytes, const int params_shared,
@@ -389,7 +389,7 @@ cudaError_t run_ring(const LnForward &p, const OpContext &c) {
   // the rings of the blocks that registers allow share the memory, with the
   // parameters where those stay in it; fewer blocks where two slots would not
   // fit beside them (8192 x 4096 float32: 98 us with four blocks that read the
-  // parameters from global memory for every row, 46.7 with three)
+  // parameters from global memory for every row, 45.4 with three)
   int want = 1024 / threads;
   if (want > 16) want = 16;
   int64_t param_bytes = NV > 1 ? 64 * (int64_t)eights : 0;

@@ -56,7 +56,8 @@ __device__ __forceinline__ uint32_t q8_exponent(uint32_t top) {
   return top >= 0x7F800000u ? 255u : static_cast<uint32_t>(max(e, 1));
 }
 // 2^-E for that exponent, by which a block is multiplied (exactly) before
-// rounding; 0 for a block of NaN, whose bytes are 0.  E lies in -126 .. 122.
+// rounding.  E lies in -126 .. 122; what it gives for a block of NaN (e = 255,
+// minus infinity) stands for nothing: the callers make that block's bytes 0.
 __device__ __forceinline__ float q8_inverse(uint32_t e) { return __uint_as_float((254u - e) << 23); }
 
 // Float bits of the largest magnitude among 2 * N bf16 values, two to a word;

@@ -196,8 +196,8 @@ __global__ void __launch_bounds__(256) wgrad_base_kernel(const WgradParams wp) {
 // share of the memory.  The narrow tiles move twice and four times the operand
 // bytes a flop, which shared memory paces; with few tokens, where the output
 // sets the time, they fill the device in rounds that leave less of it idle
-// (128 tokens, 4096 x 4096 float32 with base: 27.4 us, pairs 34.0; 2048
-// tokens: 85 us, pairs 62).  192-wide pairs take as long a k-block as 256-wide
+// (128 tokens, 4096 x 4096 float32 with base: 27.2 us, pairs 34.0; 2048 tokens:
+// 88 us, pairs 76; without base 83 and 61).  192-wide pairs take as long a k-block as 256-wide
 // ones and are not compiled.
 struct TileCost {
   WgradTile tile;
