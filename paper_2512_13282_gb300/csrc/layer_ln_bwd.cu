@@ -164,11 +164,12 @@ __global__ void __launch_bounds__(THREADS) ln_param_sum_kernel(const float *part
 // where V = 1.  A block walks rows gridDim.x apart.  Their x and dy come through
 // a ring of row slots in shared memory, filled by bulk copies that run as far
 // ahead as the ring is deep (SlotRow): dgamma and dbeta are summed in registers
-// (16 values a thread and NV), which leaves none for rows in flight.  A row is read from its slot twice, for the two averages and
-// for the results; the block-wide barrier between, passed by every thread once
-// it has finished with the row before, also frees that row's slot, which
-// thread 0 refills.  `step` rows are taken between two barriers.  One partial
-// row of dgamma and of dbeta a block goes to the workspace.
+// (16 values a thread and NV), which leaves none for rows in flight.  A row is
+// read from its slot twice, for the two averages and for the results; the
+// block-wide barrier between, passed by every thread once it has finished with
+// the row before, also frees that row's slot, which thread 0 refills.  `step`
+// rows are taken between two barriers.  One partial row of dgamma and of dbeta a
+// block goes to the workspace.
 template <typename TX, typename TDY, typename TDX, int NV, int V, int THREADS>
 __global__ void __launch_bounds__(THREADS, ring_blocks(NV, V, THREADS))
     ln_backward_ring_kernel(const LnBackward p, const int stages, const int step, const uint32_t x_bytes,

@@ -145,7 +145,8 @@ __device__ __forceinline__ void store_eighth(TY *y, const Q8Ref &ck, int64_t r, 
 // variance (a third with far_mean), frees its slot.  gamma and beta stay in registers (NV = 1), else in
 // shared memory as float32 where the rings leave room (params_shared), so that
 // 1024 threads share an SM whatever the width: with 16 parameters a thread in
-// registers half as many fit (8192 x 8192 with checkpoint: 77.4 us, so 72.4).
+// registers half as many fit (8192 x 8192 with checkpoint: 77.4 us, from shared
+// memory 72.4).
 template <typename TX, typename TY, int NV, int THREADS, int V>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
     ln_forward_ring_kernel(const LnForward p, const int stages, const uint32_t x_bytes, const int params_shared,
