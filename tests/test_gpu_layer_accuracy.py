@@ -126,3 +126,21 @@ def test_layernorm_backward_of_a_mean_far_above_the_deviations(cols, xt, gt, ot)
             within(dg.host()[0], want[1], bound[1])
             within(db.host()[0], want[2], bound[2])
             within(O.host(), want[0], bound[0])
+
+
+@pytest.mark.parametrize("rows,cols", [(5000, 96), (4000, 777), (3000, 1536), (2000, 5120), (1500, 5121), (700, 12288)])
+def test_layernorm_forward_of_rows_of_both_kinds(rows, cols):
+    """Blocks walk many rows, some with a mean far above their deviations, in
+    no order: each keeps its own digits, and its own statistics."""
+    rng = np.random.default_rng(rows)
+    x = rng.normal(size=(rows, cols)).astype(np.float32)
+    far = rng.random(rows) < 0.4
+    x[far] = levels(rng, int(far.sum()), cols, 0.5)
+    x[rng.integers(0, rows, size=20)] = 1234.567
+    gamma, beta = as_kind(1 + 0.2 * rng.normal(size=cols), "f32"), as_kind(0.2 * rng.normal(size=cols), "f32")
+    y, mean, rstd = forward(x, "f32", "f32", gamma, beta, 1e-5, 0, 0)
+    want, m, s = R.ln_forward(x, gamma, beta, 1e-5)
+    by, bm, bs = forward_bounds(x, gamma, beta, 1e-5, "f32")
+    within(mean, m, bm)
+    within(rstd, s, bs)
+    within(y, want, by)
