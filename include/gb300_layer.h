@@ -1,10 +1,12 @@
 /*
  * gb300_layer.h -- C ABI of the operators a training step runs around its
  * projection GEMMs (gb300_gemm.h): layer norm forward and backward, 8-bit
- * activation checkpoints, and a projection's weight gradient taken from such
- * a checkpoint.  With C = A . B of gb300_gemm.h they make a pre-norm
- * projection block, y = layer_norm(x), o = y . W, and its backward pass
- * dy = do . W^T, dW = y^T . do, dx = layer_norm'(dy).
+ * activation checkpoints, a projection's weight gradient taken from such
+ * a checkpoint, the gated feed-forward block's two projections with their gate
+ * and its gradient, and dropout.  With C = A . B of gb300_gemm.h they make a
+ * pre-norm projection block, y = layer_norm(x), o = y . W, and its backward
+ * pass dy = do . W^T, dW = y^T . do, dx = layer_norm'(dy); and a gated
+ * feed-forward block (at the end of this file).
  *
  * Conventions are those of gb300_gemm.h: device pointers owned by the caller,
  * leading dimensions in elements, calls asynchronous on `stream`, status
@@ -135,6 +137,110 @@ gemm_status_t gemm_q8_weight_grad(int64_t T, int64_t K, int64_t N, const int8_t 
                                   const uint8_t *e, int64_t lde, const uint16_t *dY, int64_t lddy,
                                   const void *base, int64_t ldbase, void *dW, int64_t ldw, int w_layout,
                                   int w_type, gemm_stream_t stream);
+
+/*
+ * Gated feed-forward block.  Of T tokens X (T x K), with the gate and up
+ * projections Wg, Wu (K x F), the down projection Wd (F x N) and an activation
+ * applied element by element,
+ *
+ *     G = X . Wg,  U = X . Wu,  H = act(G) * U,  O = H . Wd;
+ *
+ * back from dO,  dH = dO . Wd^T,  dG = dH * U * act'(G),  dU = dH * act(G).
+ * The calls here take the projections with the gate, and the gate's gradient
+ * with or without the down projection's product; the rest are GEMMs and weight
+ * gradients above.  With Wg and Wu the halves of one K x 2F matrix W, and dG
+ * and dU those of a T x 2F matrix, dX is one GEMM with W^T and dW one
+ * gemm_q8_weight_grad.
+ */
+typedef enum {
+  GEMM_ACT_SILU = 0,      /* g / (1 + exp(-g)) */
+  GEMM_ACT_GELU = 1,      /* g * P(g), P the normal distribution function */
+  GEMM_ACT_GELU_TANH = 2, /* g * (1 + tanh(sqrt(2 / pi) * (g + 0.044715 g^3))) / 2 */
+  GEMM_ACT_RELU = 3       /* max(g, 0); slope 0 at 0 */
+} gemm_activation_t;
+
+/*
+ * H = act(X . Wg) * (X . Wu), all bf16 bit patterns, for one token or many.
+ *   X: T x K, pitch ldx.  Wg, Wu: of w_layout, a weight's layout as in the
+ *   GEMM calls: GEMM_B_ROW_MAJOR_KxN has Wg(k, f) at Wg[k * ldwg + f],
+ *   GEMM_B_COL_MAJOR_NxK at Wg[f * ldwg + k].
+ *   H: T x F, pitch ldh.  G, U: T x F, pitches ldg, ldu, kept for the backward
+ *   pass; both or neither.
+ * The sums are float32, H is taken from them unrounded, and H, G and U are
+ * rounded once.  T == 0 or F == 0 is a no-op; K == 0 writes zeros.
+ * Accuracy contract, per element, with g, u the exact sums and Sg, Su those of
+ * the products' magnitudes: G and U as gemm_bf16_f32acc_bf16's C, and
+ *     |H - act(g) u| <= 2^-8 |act(g) u| + 2^-20 (1.2 Sg |u| + |act(g)| Su)
+ *                       + 2^-18 |g u|
+ * (and the product of the two sums' errors).  Infinite or NaN sums give what
+ * the formulas give in float32; act of -infinity is NaN except for relu.
+ */
+gemm_status_t gemm_gated_forward(int64_t T, int64_t K, int64_t F, const uint16_t *X, int64_t ldx,
+                                 const uint16_t *Wg, int64_t ldwg, const uint16_t *Wu, int64_t ldwu, int w_layout,
+                                 int activation, uint16_t *H, int64_t ldh, uint16_t *G, int64_t ldg, uint16_t *U,
+                                 int64_t ldu, gemm_stream_t stream);
+
+/*
+ * The gate's gradient from dH: dG = dH * U * act'(G), dU = dH * act(G), in
+ * float32, each rounded once to bf16.
+ *   dH, G, U: T x F bf16, pitches lddh, ldg, ldu.  dG, dU: T x F bf16, pitches
+ *   lddg, lddu; dG may be G and dU may be U (the same address and pitch).
+ *   q, ldq, e, lde: when q and e are not NULL, the checkpoint of the float32
+ *   values act(G) * U, as gemm_q8_save writes it: H for the down projection's
+ *   weight gradient, dWd = H^T . dO, without H having been kept.
+ * T == 0 or F == 0 is a no-op.
+ */
+gemm_status_t gemm_gated_backward(int64_t T, int64_t F, const uint16_t *dH, int64_t lddh, const uint16_t *G,
+                                  int64_t ldg, const uint16_t *U, int64_t ldu, int activation, uint16_t *dG,
+                                  int64_t lddg, uint16_t *dU, int64_t lddu, int8_t *q, int64_t ldq, uint8_t *e,
+                                  int64_t lde, gemm_stream_t stream);
+
+/*
+ * The same with dH = dO . Wd^T taken in the same kernel, in float32 and not
+ * rounded in between.
+ *   dO: T x N bf16, pitch lddo.  Wd: the down projection, O = H . Wd, of
+ *   w_layout: GEMM_B_ROW_MAJOR_KxN has Wd(f, n) at Wd[f * ldwd + n],
+ *   GEMM_B_COL_MAJOR_NxK at Wd[n * ldwd + f].
+ * N == 0 takes dH as zero.
+ */
+gemm_status_t gemm_gated_down_backward(int64_t T, int64_t N, int64_t F, const uint16_t *dO, int64_t lddo,
+                                       const uint16_t *Wd, int64_t ldwd, int w_layout, const uint16_t *G, int64_t ldg,
+                                       const uint16_t *U, int64_t ldu, int activation, uint16_t *dG, int64_t lddg,
+                                       uint16_t *dU, int64_t lddu, int8_t *q, int64_t ldq, uint8_t *e, int64_t lde,
+                                       gemm_stream_t stream);
+
+/*
+ * Dropout, into a residual stream if asked, and its gradient:
+ *     y = residual + keep * x / (1 - P),    dx = keep * dy / (1 - P),
+ * in float32, rounded once.  What is kept is a function of (seed, the call's
+ * step, row, column) alone -- not of types, pitches or the launch -- so that
+ * the backward pass finds it again and no mask is stored.
+ *   p: 0 .. 1, taken as the nearest multiple P of 1 / 65536 (ties to even);
+ *   P = 1 keeps nothing.  A value that is not kept contributes 0 whatever it
+ *   is, a NaN included.
+ *   seed: the generator's key.  The call's step is `step`, plus *step_device
+ *   where that is not NULL: 8 bytes of device memory (8-byte aligned) read
+ *   when the kernel runs, so that a captured graph draws anew at each launch
+ *   if something on its stream counts the word up between them.  The two add
+ *   modulo 2^64.
+ *   x: rows x cols of x_type, pitch ldx.  residual: rows x cols of y_type,
+ *   pitch ldr, or NULL (zero).  y: rows x cols of y_type, pitch ldy; it may be
+ *   the residual, or x where the types are the same (the same address and
+ *   pitch).  dy, dx: of dy_type, dx_type; dx may be dy likewise.  The residual's
+ *   gradient is dy itself.
+ * rows == 0 or cols == 0 is a no-op.
+ * The generator is Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel
+ * random numbers: as easy as 1, 2, 3", 2011) with key (low, high word of seed)
+ * and counter (column / 8, row, low, high word of the step): bits 16 i .. 16 i
+ * + 15 of its 128 are the number of the value in column 8 * (column / 8) + i,
+ * which is kept where that number is at least 65536 P.
+ */
+gemm_status_t gemm_dropout_forward(int64_t rows, int64_t cols, const void *x, int64_t ldx, int x_type,
+                                   const void *residual, int64_t ldr, void *y, int64_t ldy, int y_type, float p,
+                                   uint64_t seed, uint64_t step, const uint64_t *step_device, gemm_stream_t stream);
+gemm_status_t gemm_dropout_backward(int64_t rows, int64_t cols, const void *dy, int64_t lddy, int dy_type, void *dx,
+                                    int64_t lddx, int dx_type, float p, uint64_t seed, uint64_t step,
+                                    const uint64_t *step_device, gemm_stream_t stream);
 
 #if defined(__GNUC__)
 #pragma GCC visibility pop

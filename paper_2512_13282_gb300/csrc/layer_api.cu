@@ -1,5 +1,7 @@
 // layer_api.cu -- the C ABI of include/gb300_layer.h: argument checks,
 // scratch and launches of the layer operators.
+#include <cmath>
+
 #include "gb300_layer.h"
 #include "layer_internal.h"
 
@@ -31,6 +33,35 @@ gemm_status_t launched(cudaError_t e) { return e == cudaSuccess ? GEMM_OK : GEMM
 gemm_status_t extents(int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 0) return GEMM_ERR_INVALID_ARG;
   return rows > INT32_MAX || cols > kMaxExtent ? GEMM_ERR_UNSUPPORTED : GEMM_OK;
+}
+
+bool bf16_ok(const void *p, int64_t ld, int64_t cols) { return matrix_ok(p, GEMM_TYPE_BF16, ld, cols); }
+
+// A gate's gradient: everything but where dH comes from.
+bool gate_backward_ok(const GatedBackward &p, int64_t F) {
+  return bf16_ok(p.g, p.ldg, F) && bf16_ok(p.u, p.ldu, F) && bf16_ok(p.dg, p.lddg, F) && bf16_ok(p.du, p.lddu, F) &&
+         !p.ck.q == !p.ck.e && (!p.ck.q || checkpoint_ok(p.ck.q, p.ck.ldq, p.ck.e, p.ck.lde, F));
+}
+inline bool known_layout(int l) { return l == GEMM_B_ROW_MAJOR_KxN || l == GEMM_B_COL_MAJOR_NxK; }
+inline bool known_activation(int a) { return a >= GEMM_ACT_SILU && a <= GEMM_ACT_RELU; }
+
+gemm_status_t dropout(int64_t rows, int64_t cols, const void *x, int64_t ldx, int x_type, const void *residual,
+                      int64_t ldr, void *y, int64_t ldy, int y_type, float p, uint64_t seed, uint64_t step,
+                      const uint64_t *step_device, gemm_stream_t stream) {
+  gemm_status_t s = extents(rows, cols);
+  if (s == GEMM_ERR_INVALID_ARG || !known_type(x_type) || !known_type(y_type) || !(p >= 0.f && p <= 1.f))
+    return GEMM_ERR_INVALID_ARG;
+  if (rows == 0 || cols == 0) return GEMM_OK;
+  if (!matrix_ok(x, x_type, ldx, cols) || !matrix_ok(y, y_type, ldy, cols) ||
+      (residual && !matrix_ok(residual, y_type, ldr, cols)) || !aligned_to(step_device, 8))
+    return GEMM_ERR_INVALID_ARG;
+  if (s != GEMM_OK) return s;
+  OpContext c;
+  if ((s = op_context(reinterpret_cast<cudaStream_t>(stream), &c)) != GEMM_OK) return s;
+  count_launches(1);
+  return launched(launch_dropout(Dropout{rows, cols, x, ldx, x_type, residual, ldr, y, ldy, y_type,
+                                         (uint32_t)std::lrintf(p * 65536.f), seed, step, step_device},
+                                 c.st));
 }
 
 }  // namespace
@@ -222,6 +253,77 @@ gemm_status_t gemm_q8_weight_grad(int64_t T, int64_t K, int64_t N, const int8_t 
     }
     return GEMM_OK;
   });
+}
+
+gemm_status_t gemm_gated_forward(int64_t T, int64_t K, int64_t F, const uint16_t *X, int64_t ldx,
+                                 const uint16_t *Wg, int64_t ldwg, const uint16_t *Wu, int64_t ldwu, int w_layout,
+                                 int activation, uint16_t *H, int64_t ldh, uint16_t *G, int64_t ldg, uint16_t *U,
+                                 int64_t ldu, gemm_stream_t stream) {
+  if (T < 0 || K < 0 || F < 0 || !known_layout(w_layout) || !known_activation(activation))
+    return GEMM_ERR_INVALID_ARG;
+  if (T == 0 || F == 0) return GEMM_OK;
+  const bool kn = w_layout == GEMM_B_ROW_MAJOR_KxN;
+  const int64_t w_cols = kn ? F : K;
+  if (!bf16_ok(H, ldh, F) || !G != !U || (G && (!bf16_ok(G, ldg, F) || !bf16_ok(U, ldu, F))))
+    return GEMM_ERR_INVALID_ARG;
+  if (K > 0 && (!bf16_ok(X, ldx, K) || !bf16_ok(Wg, ldwg, w_cols) || !bf16_ok(Wu, ldwu, w_cols)))
+    return GEMM_ERR_INVALID_ARG;
+  if (T > kMaxExtent || K > kMaxExtent || F > kMaxExtent || ceil_div64(T, kBM) * ceil_div64(F, 32) > kMaxExtent)
+    return GEMM_ERR_UNSUPPORTED;
+  return with_scratch(reinterpret_cast<cudaStream_t>(stream), [&](const OpContext &c) -> gemm_status_t {
+    const GatedForward p{T, (int)K, (int)F, X, ldx, Wg, Wu, ldwg, ldwu, !kn, activation, H, ldh, G, U, ldg, ldu};
+    count_launches(1);
+    return launched(launch_gated_forward(p, c));
+  });
+}
+
+gemm_status_t gemm_gated_backward(int64_t T, int64_t F, const uint16_t *dH, int64_t lddh, const uint16_t *G,
+                                  int64_t ldg, const uint16_t *U, int64_t ldu, int activation, uint16_t *dG,
+                                  int64_t lddg, uint16_t *dU, int64_t lddu, int8_t *q, int64_t ldq, uint8_t *e,
+                                  int64_t lde, gemm_stream_t stream) {
+  gemm_status_t s = extents(T, F);
+  if (s == GEMM_ERR_INVALID_ARG || !known_activation(activation)) return GEMM_ERR_INVALID_ARG;
+  if (T == 0 || F == 0) return GEMM_OK;
+  const GatedBackward p{T, (int)F, dH, lddh, G, U, ldg, ldu, activation, dG, dU, lddg, lddu, Q8Ref{q, ldq, e, lde}};
+  if (!bf16_ok(dH, lddh, F) || !gate_backward_ok(p, F)) return GEMM_ERR_INVALID_ARG;
+  if (s != GEMM_OK) return s;
+  OpContext c;
+  if ((s = op_context(reinterpret_cast<cudaStream_t>(stream), &c)) != GEMM_OK) return s;
+  count_launches(1);
+  return launched(launch_gated_backward(p, c.st));
+}
+
+gemm_status_t gemm_gated_down_backward(int64_t T, int64_t N, int64_t F, const uint16_t *dO, int64_t lddo,
+                                       const uint16_t *Wd, int64_t ldwd, int w_layout, const uint16_t *G, int64_t ldg,
+                                       const uint16_t *U, int64_t ldu, int activation, uint16_t *dG, int64_t lddg,
+                                       uint16_t *dU, int64_t lddu, int8_t *q, int64_t ldq, uint8_t *e, int64_t lde,
+                                       gemm_stream_t stream) {
+  if (T < 0 || N < 0 || F < 0 || !known_layout(w_layout) || !known_activation(activation))
+    return GEMM_ERR_INVALID_ARG;
+  if (T == 0 || F == 0) return GEMM_OK;
+  const bool kn = w_layout == GEMM_B_ROW_MAJOR_KxN;
+  const GatedBackward b{T, (int)F, nullptr, 0, G, U, ldg, ldu, activation, dG, dU, lddg, lddu, Q8Ref{q, ldq, e, lde}};
+  if (!gate_backward_ok(b, F) || (N > 0 && (!bf16_ok(dO, lddo, N) || !bf16_ok(Wd, ldwd, kn ? N : F))))
+    return GEMM_ERR_INVALID_ARG;
+  if (T > kMaxExtent || N > kMaxExtent || F > kMaxExtent || ceil_div64(T, kBM) * ceil_div64(F, 32) > kMaxExtent)
+    return GEMM_ERR_UNSUPPORTED;
+  return with_scratch(reinterpret_cast<cudaStream_t>(stream), [&](const OpContext &c) -> gemm_status_t {
+    count_launches(1);
+    if (N == 0) return launched(launch_gated_backward(b, c.st));
+    return launched(launch_gated_down_backward(GatedDownBackward{b, (int)N, dO, lddo, Wd, ldwd, kn}, c));
+  });
+}
+
+gemm_status_t gemm_dropout_forward(int64_t rows, int64_t cols, const void *x, int64_t ldx, int x_type,
+                                   const void *residual, int64_t ldr, void *y, int64_t ldy, int y_type, float p,
+                                   uint64_t seed, uint64_t step, const uint64_t *step_device, gemm_stream_t stream) {
+  return dropout(rows, cols, x, ldx, x_type, residual, ldr, y, ldy, y_type, p, seed, step, step_device, stream);
+}
+
+gemm_status_t gemm_dropout_backward(int64_t rows, int64_t cols, const void *dy, int64_t lddy, int dy_type, void *dx,
+                                    int64_t lddx, int dx_type, float p, uint64_t seed, uint64_t step,
+                                    const uint64_t *step_device, gemm_stream_t stream) {
+  return dropout(rows, cols, dy, lddy, dy_type, nullptr, 0, dx, lddx, dx_type, p, seed, step, step_device, stream);
 }
 
 }  // extern "C"

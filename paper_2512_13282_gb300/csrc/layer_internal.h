@@ -111,4 +111,63 @@ cudaError_t launch_wgrad_base(const WgradParams &p, int sms, cudaStream_t st);
 // and stored.
 cudaError_t launch_wgrad_reduce(const WgradTile &tile, const WgradParams &p, cudaStream_t st);
 
+// Gated feed-forward block (layer_gate.cu).  T x F matrices of bf16.
+struct GatedForward {
+  int64_t T;
+  int K, F;
+  const uint16_t *x;
+  int64_t ldx;
+  const uint16_t *wg, *wu;
+  int64_t ldwg, ldwu;
+  bool w_kmajor;  // W's k index contiguous
+  int act;
+  uint16_t *h;
+  int64_t ldh;
+  uint16_t *g, *u;  // both null: not kept
+  int64_t ldg, ldu;
+};
+cudaError_t launch_gated_forward(const GatedForward &p, const OpContext &c);
+
+struct GatedBackward {
+  int64_t T;
+  int F;
+  const uint16_t *dh;  // null: zero
+  int64_t lddh;
+  const uint16_t *g, *u;
+  int64_t ldg, ldu;
+  int act;
+  uint16_t *dg, *du;  // may be g, u
+  int64_t lddg, lddu;
+  Q8Ref ck;  // checkpoint of act(g) * u, or ck.q null
+};
+cudaError_t launch_gated_backward(const GatedBackward &p, cudaStream_t st);
+// dh = dO . Wd^T over N columns; b.dh is not used.
+struct GatedDownBackward {
+  GatedBackward b;
+  int N;
+  const uint16_t *d;
+  int64_t ldd;
+  const uint16_t *w;
+  int64_t ldw;
+  bool w_kmajor;  // Wd's n index contiguous
+};
+cudaError_t launch_gated_down_backward(const GatedDownBackward &p, const OpContext &c);
+
+// Dropout (layer_dropout.cu), forward or backward (without a residual).
+struct Dropout {
+  int64_t rows, cols;
+  const void *x;
+  int64_t ldx;
+  int x_type;
+  const void *residual;  // null: none
+  int64_t ldr;
+  void *y;
+  int64_t ldy;
+  int y_type;
+  uint32_t threshold;  // numbers below it are dropped, 0 .. 65536
+  uint64_t seed, step;
+  const uint64_t *step_device;  // null: none
+};
+cudaError_t launch_dropout(const Dropout &p, cudaStream_t st);
+
 }  // namespace gb300
