@@ -62,7 +62,7 @@ struct ActTag {
   static constexpr int value = A;
 };
 template <typename F>
-__host__ __device__ __forceinline__ void with_activation(int act, F &&f) {
+__device__ __forceinline__ void with_activation(int act, F &&f) {
   switch (act) {
     case GEMM_ACT_SILU: f(ActTag<GEMM_ACT_SILU>{}); break;
     case GEMM_ACT_GELU: f(ActTag<GEMM_ACT_GELU>{}); break;

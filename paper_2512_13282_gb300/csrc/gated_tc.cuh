@@ -1,0 +1,507 @@
+// gated_tc.cuh -- the persistent tcgen05 kernel of the gated feed-forward block,
+// forward (H = act(X Wg) * (X Wu)) and backward (the gate's gradient from
+// dH = dO Wd^T).
+//
+// Both are C = A . B with A row-major and a B of either layout, and run as
+// gemm_tc2.cuh does (PAIR: a CTA pair per 256-row tile, each CTA holding 128
+// rows of A and half of B; else one CTA per 128-row tile): a TMA producer, an
+// MMA issuer and eight epilogue warps, two accumulators in TMEM.  What differs:
+//
+// Forward.  A tile's BN columns are BN / 2 of the gate's projection and the
+// same BN / 2 of the up projection's, so that one lane of the epilogue finds g
+// and u of an element in its own TMEM lane, BN / 2 columns apart, and H leaves
+// the kernel without G and U having been stored.  In a pair, one CTA's half of
+// B is Wg's, the other's Wu's.
+//
+// Backward.  The epilogue reads G and U of its 32 x 32 blocks itself, a block
+// ahead (the first of a tile while the tensor core still works on it), takes
+// the gradient from dH in registers, and the checkpoint of act(G) U: a lane
+// holds 32 consecutive values of a row, which is one block of the checkpoint,
+// so that needs no exchange between lanes.  dH is never stored: 8192 x 11008
+// would cost 360 MB of traffic, 53 us.
+#pragma once
+#include "gate_math.cuh"
+#include "layer_rows.cuh"
+#include "gemm_tc2.cuh"
+
+namespace gb300 {
+
+constexpr int kGatedEpiWarps = 8;
+constexpr int kGatedThreads = (2 + kGatedEpiWarps) * 32;
+
+template <int BN, bool PAIR, bool BWD>
+struct GatedCfg {
+  static constexpr int kTileM = PAIR ? 2 * kBM : kBM;
+  static constexpr int kTileF = BWD ? BN : BN / 2;   // features of a tile
+  static constexpr int kCtaN = PAIR ? BN / 2 : BN;   // columns of B a CTA loads
+  static constexpr int kPartN = BWD || PAIR ? kCtaN : kCtaN / 2;  // ... of one weight
+  static_assert(kPartN % 64 == 0 && BN <= 256, "operands are assembled from 64-wide boxes");
+  static constexpr int kOuts = BWD ? 2 : 3;
+  static constexpr uint32_t kBBytes = kCtaN * kRowBytes;
+  static constexpr uint32_t kStageBytes = kABytes + kBBytes;
+  static constexpr uint32_t kEpiWarpBytes = kOuts * 2048u;  // a 32 x 32 block of bf16 for each output
+  static constexpr int kStages =
+      (int)((232448u - 1024u - 256u - kGatedEpiWarps * kEpiWarpBytes) / kStageBytes);
+  static constexpr uint32_t kTmemCols = pow2_at_least(2 * BN);
+  static constexpr int kChunks = kTileF / 32 / (kGatedEpiWarps / 4);  // 32-column blocks of an epilogue warp
+  static_assert(kChunks >= 1, "each of the two warpgroups has a block");
+  static constexpr uint32_t kEpiOffset = kStages * kStageBytes;
+  static constexpr uint32_t kBarOffset = kEpiOffset + kGatedEpiWarps * kEpiWarpBytes;
+  static constexpr uint32_t kNumBars = 2 * kStages + 4 + 1;
+  static constexpr uint32_t kSmemBytes = kBarOffset + kNumBars * 8 + 16 + 1024;
+  static_assert(kNumBars * 8 + 16 <= 256 && kSmemBytes <= 232448, "shared memory per CTA is 227 KB");
+  static_assert(kTmemCols <= 512, "TMEM has 512 columns");
+};
+
+// Blocks of 32 x 32 bf16 in an epilogue warp's shared memory, as a tensor map
+// with 64-byte swizzle has them: chunk j (16 bytes) of row r at chunk j ^
+// ((r / 2) % 4).
+__device__ __forceinline__ uint32_t block_chunk(uint32_t buf, int row, int j) {
+  return buf + row * 64 + ((j ^ ((row >> 1) & 3)) << 4);
+}
+__device__ __forceinline__ void put_row(uint32_t buf, int lane, const uint32_t (&h)[16]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    st_shared_v4(block_chunk(buf, lane, j), h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
+}
+__device__ __forceinline__ uint32_t block_element(uint32_t buf, int row, int col) {
+  return block_chunk(buf, row, col >> 3) + (col & 7) * 2;
+}
+__device__ __forceinline__ void st_shared_u16(uint32_t addr, uint16_t v) {
+  asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(v) : "memory");
+}
+__device__ __forceinline__ uint16_t ld_shared_u16(uint32_t addr) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t ld_shared_u8(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// The block at (y0, x) between memory of any alignment and shared memory,
+// along rows (lane = column): a lane's own row would be 32 lines touched by
+// every access.
+__device__ __forceinline__ void copy_in(const uint16_t *m, int64_t ld, uint32_t buf, int lane, int y0, int x, int T,
+                                        int F) {
+  const int c = x + lane, rows = min(32, T - y0);
+  uint16_t v[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = c < F && i < rows ? m[(int64_t)(y0 + i) * ld + c] : (uint16_t)0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) st_shared_u16(block_element(buf, i, lane), v[i]);
+}
+__device__ __forceinline__ void copy_out(uint16_t *m, int64_t ld, uint32_t buf, int lane, int y0, int x, int T, int F) {
+  const int c = x + lane, rows = min(32, T - y0);
+  if (c >= F) return;
+#pragma unroll 8
+  for (int i = 0; i < rows; ++i) m[(int64_t)(y0 + i) * ld + c] = ld_shared_u16(block_element(buf, i, lane));
+}
+
+// 32 values of the lane's row from column x on, F a multiple of 8 and the row
+// on 16 bytes; zero past F.
+__device__ __forceinline__ void load_row32(const uint16_t *row, int x, int F, bool live, uint32_t (&w)[16]) {
+  const uint4 *p = reinterpret_cast<const uint4 *>(row + x);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (live && x + 8 * j < F) v = p[j];
+    w[4 * j] = v.x, w[4 * j + 1] = v.y, w[4 * j + 2] = v.z, w[4 * j + 3] = v.w;
+  }
+}
+__device__ __forceinline__ float bf16_at(const uint32_t (&w)[16], int i) {
+  return __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+}
+
+// Gradient of 32 elements of a row from dh (float32 bits): g and u become dg
+// and du, dh becomes act(g) * u.
+template <int ACT>
+__device__ __forceinline__ void gate_backward32(uint32_t (&dh)[32], uint32_t (&g)[16], uint32_t (&u)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float dg[2], du[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float d = __uint_as_float(dh[2 * i + k]), uu = bf16_at(u, 2 * i + k);
+      const GateValue v = gate<ACT, true>(bf16_at(g, 2 * i + k));
+      dg[k] = d * uu * v.slope;
+      du[k] = d * v.a;
+      dh[2 * i + k] = __float_as_uint(v.a * uu);
+    }
+    g[i] = pack_bf16x2(dg[0], dg[1]);
+    u[i] = pack_bf16x2(du[0], du[1]);
+  }
+}
+
+// The checkpoint of 32 float32 values: their bytes, and the exponent.
+__device__ __forceinline__ uint32_t q8_block32(const uint32_t (&h)[32], uint32_t (&q)[8]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) top = max(top, h[i] & 0x7FFFFFFFu);
+  const uint32_t e = q8_exponent(top);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float2 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      v[i] = make_float2(__uint_as_float(h[8 * j + 2 * i]), __uint_as_float(h[8 * j + 2 * i + 1]));
+    const uint2 w = q8_pack8(v, e);
+    q[2 * j] = w.x, q[2 * j + 1] = w.y;
+  }
+  return e;
+}
+
+template <int BN, bool PAIR, bool KM, bool BWD>
+__global__ void __launch_bounds__(kGatedThreads, 1)
+    gated_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB0,
+                    const __grid_constant__ CUtensorMap tmB1, const __grid_constant__ CUtensorMap tmOut0,
+                    const __grid_constant__ CUtensorMap tmOut1, const __grid_constant__ CUtensorMap tmOut2,
+                    const GatedTcParams p) {
+  using Cfg = GatedCfg<BN, PAIR, BWD>;
+  constexpr int STAGES = Cfg::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_addr(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;  // swizzle atoms need 1024-byte alignment
+  uint8_t *base_ptr = smem_raw + (base - raw);
+  const uint32_t sA = base;
+  const uint32_t sB = base + STAGES * kABytes;
+  const uint32_t bars = base + Cfg::kBarOffset;
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(base_ptr + Cfg::kBarOffset + Cfg::kNumBars * 8);
+  volatile uint32_t *abort_flag = tmem_slot + 1;
+
+  auto full_bar = [&](uint32_t s) { return bars + 8u * s; };
+  auto empty_bar = [&](uint32_t s) { return bars + 8u * (STAGES + s); };
+  auto accf_bar = [&](uint32_t b) { return bars + 8u * (2 * STAGES + b); };
+  auto acce_bar = [&](uint32_t b) { return bars + 8u * (2 * STAGES + 2 + b); };
+  const uint32_t drain_bar = bars + 8u * (2 * STAGES + 4);
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
+  const bool leader = rank == 0;
+  const int first_tile = PAIR ? blockIdx.x >> 1 : blockIdx.x;
+  const int tile_step = PAIR ? gridDim.x >> 1 : gridDim.x;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(accf_bar(b), 1);
+      mbar_init(acce_bar(b), (PAIR ? 2 : 1) * kGatedEpiWarps * 32);
+    }
+    mbar_init(drain_bar, 1);
+    *abort_flag = 0u;
+    fence_mbar_init();
+    tma_prefetch_desc(&tmA);
+    tma_prefetch_desc(&tmB0);
+    if (!BWD) tma_prefetch_desc(&tmB1);
+    if (p.tma) {
+      tma_prefetch_desc(&tmOut0);
+      if (BWD || p.out[1]) tma_prefetch_desc(&tmOut1);
+      if (!BWD && p.out[1]) tma_prefetch_desc(&tmOut2);
+    }
+  }
+  __syncwarp();
+  if (warp == 1) {
+    if constexpr (PAIR)
+      tmem_alloc_pair<Cfg::kTmemCols>(smem_addr(tmem_slot));
+    else
+      tmem_alloc<Cfg::kTmemCols>(smem_addr(tmem_slot));
+  }
+  tc_fence_before_sync();
+  if constexpr (PAIR)
+    cluster_sync_all();  // barriers of both CTAs initialised, TMEM allocated
+  else
+    __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  // Nothing above touched global memory, so it may overlap the previous
+  // kernel of the stream.
+  griddep_wait();
+
+  const int num_tiles = p.tiles_m * p.tiles_n;
+  constexpr uint64_t kDrainNs = 200ull * 1000 * 1000;
+
+  if (warp == 0) {
+    // -------------------------------------------------------- TMA producer
+    if (lane == 0) {
+      uint32_t g = 0;
+      bool ok = true;
+      for (int t = first_tile; ok && t < num_tiles; t += tile_step) {
+        int tm, tn;
+        raster_tile(t, p.tiles_m, p.tiles_n, p.group_m, &tm, &tn);
+        const int m0 = tm * Cfg::kTileM + (int)rank * kBM;
+        for (int kb = 0; kb < p.num_kb; ++kb) {
+          const uint32_t s = g % STAGES, ph = (g / STAGES) & 1u;
+          if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.err, p.wait_limit_ns)) {
+            ok = false;
+            break;
+          }
+          if (leader) mbar_arrive_expect_tx(full_bar(s), (PAIR ? 2 : 1) * Cfg::kStageBytes);
+          const uint32_t fb = PAIR ? mapa_shared(full_bar(s), 0) : full_bar(s);
+          const auto load = [&](uint32_t dst, const CUtensorMap *m, int c0, int c1) {
+            if constexpr (PAIR)
+              tma_load_2d_pair(dst, m, c0, c1, fb);
+            else
+              tma_load_2d(dst, m, c0, c1, fb);
+          };
+          load(sA + s * kABytes, &tmA, kb * kBK, m0);
+          // kPartN columns of a weight from feature f0 on
+          const auto load_b = [&](uint32_t dst, const CUtensorMap *m, int f0) {
+            if constexpr (KM) {
+              load(dst, m, kb * kBK, f0);
+            } else {
+#pragma unroll
+              for (int j = 0; j < Cfg::kPartN / 64; ++j) load(dst + j * (kBK * 128), m, f0 + 64 * j, kb * kBK);
+            }
+          };
+          const uint32_t b_dst = sB + s * Cfg::kBBytes;
+          const int f0 = tn * Cfg::kTileF;
+          if constexpr (BWD) {
+            load_b(b_dst, &tmB0, f0 + (int)rank * Cfg::kCtaN);
+          } else if constexpr (PAIR) {
+            load_b(b_dst, leader ? &tmB0 : &tmB1, f0);
+          } else {
+            load_b(b_dst, &tmB0, f0);
+            load_b(b_dst + Cfg::kPartN * kRowBytes, &tmB1, f0);
+          }
+          ++g;
+        }
+      }
+      // Every load has landed before the CTA may exit (the peer's loads
+      // complete on the leader's barriers: it waits until their stages have
+      // been released).
+      const uint32_t first = g > (uint32_t)STAGES ? g - STAGES : 0u;
+      for (uint32_t i = first; i < g; ++i)
+        mbar_wait_drain(leader ? full_bar(i % STAGES) : empty_bar(i % STAGES), (i / STAGES) & 1u, kDrainNs);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // -------------------------------------------------- MMA issuer (leader)
+    if (lane == 0 && leader) {
+      constexpr uint32_t idesc = idesc_bf16_f32(Cfg::kTileM, BN, !KM);
+      uint32_t g = 0, acc_cnt = 0;
+      bool ok = true;
+      for (int t = first_tile; ok && t < num_tiles; t += tile_step) {
+        const uint32_t b = acc_cnt & 1u, aph = (acc_cnt >> 1) & 1u;
+        if (!mbar_wait(acce_bar(b), aph ^ 1u, abort_flag, p.err, p.wait_limit_ns)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after_sync();
+        const uint32_t d_tmem = tmem_base + b * BN;
+        for (int kb = 0; kb < p.num_kb; ++kb) {
+          const uint32_t s = g % STAGES, ph = (g / STAGES) & 1u;
+          if (!mbar_wait(full_bar(s), ph, abort_flag, p.err, p.wait_limit_ns)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after_sync();
+          const uint32_t a0 = sA + s * kABytes;
+          const uint32_t b0 = sB + s * Cfg::kBBytes;
+#pragma unroll
+          for (int k = 0; k < kBK / 16; ++k) {
+            const uint64_t ad = smem_desc_sw128(a0 + k * 32, 16, 1024);
+            const uint64_t bd = KM ? smem_desc_sw128(b0 + k * 32, 16, 1024)
+                                   : smem_desc_sw128(b0 + k * 2048, kBK * 128, 1024);
+            const uint32_t acc = (kb > 0 || k > 0) ? 1u : 0u;
+            if constexpr (PAIR)
+              tc_mma_bf16_pair(d_tmem, ad, bd, idesc, acc);
+            else
+              tc_mma_bf16(d_tmem, ad, bd, idesc, acc);
+          }
+          if constexpr (PAIR)
+            tc_commit_pair_multicast(empty_bar(s));
+          else
+            tc_commit(empty_bar(s));
+          ++g;
+        }
+        if (!ok) break;
+        if constexpr (PAIR)
+          tc_commit_pair_multicast(accf_bar(b));
+        else
+          tc_commit(accf_bar(b));
+        ++acc_cnt;
+      }
+      // all MMAs complete before TMEM is released
+      if constexpr (PAIR)
+        tc_commit_pair_multicast(drain_bar);
+      else
+        tc_commit(drain_bar);
+      mbar_wait_drain(drain_bar, 0, kDrainNs);
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------ epilogue
+    const int ew = warp - 2;
+    const int quad = warp & 3;  // a warp may only touch TMEM lanes 32*(warp%4) ..
+    const int colpart = ew >> 2;
+    const uint32_t ebuf = base + Cfg::kEpiOffset + ew * Cfg::kEpiWarpBytes;
+    uint32_t acc_cnt = 0;
+    for (int t = first_tile; t < num_tiles; t += tile_step) {
+      int tm, tn;
+      raster_tile(t, p.tiles_m, p.tiles_n, p.group_m, &tm, &tn);
+      const int y0 = tm * Cfg::kTileM + (int)rank * kBM + quad * 32;  // first row of this warp
+      const int y = y0 + lane;
+      const int col0 = colpart * (Cfg::kChunks * 32);
+      const int x0 = tn * Cfg::kTileF + col0;
+      const uint32_t b = acc_cnt & 1u, aph = (acc_cnt >> 1) & 1u;
+      const uint32_t t0 = tmem_base + b * BN + ((uint32_t)(quad * 32) << 16) + col0;
+      // Outputs of the block at (y0, x), staged by the lanes' rows: to memory.
+      const auto emit = [&](int outs, int x) {
+        if (p.tma) {
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_2d(&tmOut0, ebuf, x, y0);
+            if (outs > 1) tma_store_2d(&tmOut1, ebuf + 2048, x, y0);
+            if (outs > 2) tma_store_2d(&tmOut2, ebuf + 4096, x, y0);
+            bulk_commit();
+          }
+        } else {
+          __syncwarp();
+#pragma unroll 1
+          for (int o = 0; o < outs; ++o) copy_out(p.out[o], p.ldout[o], ebuf + o * 2048, lane, y0, x, p.T, p.F);
+          __syncwarp();
+        }
+      };
+      if constexpr (!BWD) {
+        if (!__all_sync(0xffffffffu, mbar_wait(accf_bar(b), aph, abort_flag, p.err, p.wait_limit_ns))) break;
+        tc_fence_after_sync();
+#pragma unroll 1
+        for (int c = 0; c < Cfg::kChunks; ++c) {
+          const int x = x0 + c * 32;
+          uint32_t g[32], u[32], h[16];
+          tmem_ld_32x32b_x32(t0 + c * 32, g);
+          tmem_ld_32x32b_x32(t0 + Cfg::kTileF + c * 32, u);
+          tmem_ld_wait();
+          if (y0 >= p.T || x >= p.F) continue;
+          with_activation(p.act, [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              h[i] = pack_bf16x2(gate<ACT, false>(__uint_as_float(g[2 * i])).a * __uint_as_float(u[2 * i]),
+                                 gate<ACT, false>(__uint_as_float(g[2 * i + 1])).a * __uint_as_float(u[2 * i + 1]));
+          });
+          if (lane == 0) bulk_wait_read_all();
+          __syncwarp();
+          put_row(ebuf, lane, h);
+          if (p.out[1]) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) h[i] = pack_bf16x2(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1]));
+            put_row(ebuf + 2048, lane, h);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) h[i] = pack_bf16x2(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
+            put_row(ebuf + 4096, lane, h);
+          }
+          emit(p.out[1] ? 3 : 1, x);
+        }
+      } else {
+        const bool live = y < p.T;
+        const uint16_t *grow = p.gate + (int64_t)y * p.ldgate, *urow = p.up + (int64_t)y * p.ldup;
+        uint32_t ga[16], ua[16];  // the next block's gate and up values
+        if (p.tma) {
+          load_row32(grow, x0, p.F, live, ga);
+          load_row32(urow, x0, p.F, live, ua);
+        }
+        if (!__all_sync(0xffffffffu, mbar_wait(accf_bar(b), aph, abort_flag, p.err, p.wait_limit_ns))) break;
+        tc_fence_after_sync();
+        uint32_t es = 0;  // exponents of the row's blocks
+#pragma unroll 1
+        for (int c = 0; c < Cfg::kChunks; ++c) {
+          const int x = x0 + c * 32;
+          uint32_t dh[32], g[16], u[16];
+          tmem_ld_32x32b_x32(t0 + c * 32, dh);
+          if (p.tma) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) g[i] = ga[i], u[i] = ua[i];
+            if (c + 1 < Cfg::kChunks) {
+              load_row32(grow, x + 32, p.F, live, ga);
+              load_row32(urow, x + 32, p.F, live, ua);
+            }
+          }
+          tmem_ld_wait();
+          if (y0 >= p.T || x >= p.F) continue;
+          if (!p.tma) {
+            copy_in(p.gate, p.ldgate, ebuf, lane, y0, x, p.T, p.F);
+            copy_in(p.up, p.ldup, ebuf + 2048, lane, y0, x, p.T, p.F);
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint4 a = ld_shared_v4(block_chunk(ebuf, lane, j)), d = ld_shared_v4(block_chunk(ebuf + 2048, lane, j));
+              g[4 * j] = a.x, g[4 * j + 1] = a.y, g[4 * j + 2] = a.z, g[4 * j + 3] = a.w;
+              u[4 * j] = d.x, u[4 * j + 1] = d.y, u[4 * j + 2] = d.z, u[4 * j + 3] = d.w;
+            }
+          }
+          with_activation(p.act, [&](auto act) { gate_backward32<decltype(act)::value>(dh, g, u); });
+          if (lane == 0) bulk_wait_read_all();
+          __syncwarp();
+          put_row(ebuf, lane, g);
+          put_row(ebuf + 2048, lane, u);
+          emit(2, x);
+          if (p.ck.q) {
+            uint32_t q[8];
+            es |= q8_block32(dh, q) << (8 * c);
+            if (p.q_vec && x + 32 <= p.F) {
+              if (live) store_32_bytes(p.ck.q + (int64_t)y * p.ck.ldq + x, q);
+            } else {
+              // along rows, through the block that dG just left
+              if (lane == 0) bulk_wait_read_all();
+              __syncwarp();
+              st_shared_v4(ebuf + lane * 32, q[0], q[1], q[2], q[3]);
+              st_shared_v4(ebuf + lane * 32 + 16, q[4], q[5], q[6], q[7]);
+              __syncwarp();
+              if (x + lane < p.F) {
+                const int rows = min(32, p.T - y0);
+#pragma unroll 8
+                for (int i = 0; i < rows; ++i)
+                  p.ck.q[(int64_t)(y0 + i) * p.ck.ldq + x + lane] = (int8_t)ld_shared_u8(ebuf + i * 32 + lane);
+              }
+              __syncwarp();
+            }
+          }
+        }
+        if (p.ck.q && live) {
+          uint8_t *e = p.ck.e + (int64_t)y * p.ck.lde + (x0 >> 5);
+          const int n = min(Cfg::kChunks, (p.F - x0 + 31) >> 5);  // blocks that exist (may be below 1)
+          if (Cfg::kChunks == 4 && n == 4 && (reinterpret_cast<uintptr_t>(e) & 3) == 0) {
+            *reinterpret_cast<uint32_t *>(e) = es;
+          } else {
+#pragma unroll
+            for (int i = 0; i < Cfg::kChunks; ++i)
+              if (i < n) e[i] = (uint8_t)(es >> (8 * i));
+          }
+        }
+      }
+      tc_fence_before_sync();
+      if constexpr (PAIR)
+        mbar_arrive_cluster(mapa_shared(acce_bar(b), 0));
+      else
+        mbar_arrive(acce_bar(b));
+      ++acc_cnt;
+    }
+    if (lane == 0) bulk_wait_all();  // this warp's TMA stores have landed
+  }
+
+  griddep_launch_dependents();
+  __syncwarp();
+  tc_fence_before_sync();
+  if constexpr (PAIR)
+    cluster_sync_all();  // no remote arrival or load may target a CTA that has left
+  else
+    __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after_sync();
+    if constexpr (PAIR)
+      tmem_dealloc_pair<Cfg::kTmemCols>(tmem_base);
+    else
+      tmem_dealloc<Cfg::kTmemCols>(tmem_base);
+  }
+}
+
+}  // namespace gb300

@@ -1,0 +1,19 @@
+// gated_tc_bwd.cu -- the backward instantiations of the gated feed-forward
+// block's tensor-core kernel.
+#include "gated_tc_launch.cuh"
+
+namespace gb300 {
+
+cudaError_t launch_gated_tc_bwd(const GatedTile &tile, bool km, const GatedMaps &m, const GatedTcParams &p, int grid,
+                                cudaStream_t st) {
+  if (tile.pair)
+    return km ? launch_gated_kernel<256, true, true, true>(m, p, grid, st)
+              : launch_gated_kernel<256, true, false, true>(m, p, grid, st);
+  if (tile.bn == 128)
+    return km ? launch_gated_kernel<128, false, true, true>(m, p, grid, st)
+              : launch_gated_kernel<128, false, false, true>(m, p, grid, st);
+  return km ? launch_gated_kernel<64, false, true, true>(m, p, grid, st)
+            : launch_gated_kernel<64, false, false, true>(m, p, grid, st);
+}
+
+}  // namespace gb300

@@ -272,8 +272,7 @@ gemm_status_t gemm_gated_forward(int64_t T, int64_t K, int64_t F, const uint16_t
     return GEMM_ERR_UNSUPPORTED;
   return with_scratch(reinterpret_cast<cudaStream_t>(stream), [&](const OpContext &c) -> gemm_status_t {
     const GatedForward p{T, (int)K, (int)F, X, ldx, Wg, Wu, ldwg, ldwu, !kn, activation, H, ldh, G, U, ldg, ldu};
-    count_launches(1);
-    return launched(launch_gated_forward(p, c));
+    return gated_forward(p, c);
   });
 }
 
@@ -308,9 +307,11 @@ gemm_status_t gemm_gated_down_backward(int64_t T, int64_t N, int64_t F, const ui
   if (T > kMaxExtent || N > kMaxExtent || F > kMaxExtent || ceil_div64(T, kBM) * ceil_div64(F, 32) > kMaxExtent)
     return GEMM_ERR_UNSUPPORTED;
   return with_scratch(reinterpret_cast<cudaStream_t>(stream), [&](const OpContext &c) -> gemm_status_t {
-    count_launches(1);
-    if (N == 0) return launched(launch_gated_backward(b, c.st));
-    return launched(launch_gated_down_backward(GatedDownBackward{b, (int)N, dO, lddo, Wd, ldwd, kn}, c));
+    if (N == 0) {
+      count_launches(1);
+      return launched(launch_gated_backward(b, c.st));
+    }
+    return gated_down_backward(GatedDownBackward{b, (int)N, dO, lddo, Wd, ldwd, kn}, c);
   });
 }
 

@@ -1,5 +1,9 @@
-// layer_gate.cu -- the gated feed-forward block's gate: both projections with
-// it, and its gradient with and without the down projection's product.
+// layer_gate.cu -- the gated feed-forward block's gate: planning and staging of
+// the kernel that takes it with the projections (gated_tc.cuh), and the kernel
+// of its gradient alone.
+#include <atomic>
+#include <cmath>
+
 #include "gate_math.cuh"
 #include "layer_rows.cuh"
 
@@ -7,56 +11,10 @@ namespace gb300 {
 
 namespace {
 
-constexpr int kTile = 32;
+inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// A 32 x 32 tile of A . B^T (A rows x K, K contiguous; B(k, c) at b[k * sk +
-// c * sc]) a block of 16 x 16 threads, 2 x 2 sums a thread (rows ty + 16 i,
-// columns tx + 16 j).
-__device__ __forceinline__ void tile_product(const uint16_t *a, int64_t lda, int64_t rows, const uint16_t *b, int64_t sk,
-                                             int64_t sc, int cols, int K, int64_t r0, int c0, float (&acc)[2][2],
-                                             float (*as)[kTile + 1], float (*bs)[kTile + 1]) {
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  for (int k0 = 0; k0 < K; k0 += kTile) {
-    for (int i = threadIdx.x; i < kTile * kTile; i += 256) {
-      const int y = i / kTile, x = i % kTile;
-      as[y][x] = r0 + y < rows && k0 + x < K ? load_value<bf16>(a, (r0 + y) * lda + k0 + x) : 0.f;
-      const int k = sc == 1 ? y : x, c = sc == 1 ? x : y;  // along the contiguous index
-      bs[k][c] = k0 + k < K && c0 + c < cols ? load_value<bf16>(b, (k0 + k) * sk + (c0 + c) * sc) : 0.f;
-    }
-    __syncthreads();
-#pragma unroll 8
-    for (int k = 0; k < kTile; ++k)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = fmaf(as[ty + 16 * i][k], bs[k][tx + 16 * j], acc[i][j]);
-    __syncthreads();
-  }
-}
-
-template <int ACT>
-__global__ void __launch_bounds__(256) gated_forward_kernel(const GatedForward p) {
-  griddep_launch_dependents();
-  griddep_wait();
-  __shared__ float as[kTile][kTile + 1], bs[kTile][kTile + 1];
-  const int64_t r0 = (int64_t)blockIdx.x * kTile;
-  const int c0 = blockIdx.y * kTile, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float g[2][2] = {}, u[2][2] = {};
-  const auto sk = [&](int64_t ld) { return p.w_kmajor ? (int64_t)1 : ld; };
-  const auto sc = [&](int64_t ld) { return p.w_kmajor ? ld : (int64_t)1; };
-  tile_product(p.x, p.ldx, p.T, p.wg, sk(p.ldwg), sc(p.ldwg), p.F, p.K, r0, c0, g, as, bs);
-  tile_product(p.x, p.ldx, p.T, p.wu, sk(p.ldwu), sc(p.ldwu), p.F, p.K, r0, c0, u, as, bs);
-  for (int i = 0; i < 2; ++i)
-    for (int j = 0; j < 2; ++j) {
-      const int64_t r = r0 + ty + 16 * i;
-      const int c = c0 + tx + 16 * j;
-      if (r >= p.T || c >= p.F) continue;
-      store_value<bf16>(p.h, r * p.ldh + c, gate<ACT, false>(g[i][j]).a * u[i][j]);
-      if (!p.g) continue;
-      store_value<bf16>(p.g, r * p.ldg + c, g[i][j]);
-      store_value<bf16>(p.u, r * p.ldu + c, u[i][j]);
-    }
-}
+// ------------------------------------------------------- the gradient alone
 
 // Gradient of one element; returns act(g) * u.
 template <int ACT>
@@ -95,56 +53,156 @@ __global__ void __launch_bounds__(256) gated_backward_kernel(const GatedBackward
   }
 }
 
-template <int ACT>
-__global__ void __launch_bounds__(256) gated_down_backward_kernel(const GatedDownBackward p) {
-  griddep_launch_dependents();
-  griddep_wait();
-  __shared__ float as[kTile][kTile + 1], bs[kTile][kTile + 1];
-  const int64_t r0 = (int64_t)blockIdx.x * kTile;
-  const int c0 = blockIdx.y * kTile, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float dh[2][2] = {};
-  tile_product(p.d, p.ldd, p.b.T, p.w, p.w_kmajor ? 1 : p.ldw, p.w_kmajor ? p.ldw : 1, p.b.F, p.N, r0, c0, dh, as, bs);
-  for (int i = 0; i < 2; ++i)
-    for (int j = 0; j < 2; ++j) as[ty + 16 * i][tx + 16 * j] = dh[i][j];
-  __syncthreads();
-  const int c = c0 + (threadIdx.x & 31);
-  for (int y = threadIdx.x >> 5; y < kTile; y += 8) {
-    const int64_t r = r0 + y;
-    if (r >= p.b.T) break;
-    float h = 0.f;
-    if (c < p.b.F) h = gate_backward<ACT>(p.b, r, c, as[y][threadIdx.x & 31]);
-    if (p.b.ck.q) q8_by_warp(p.b.ck, r, c, p.b.F, h);
+// --------------------------------------------- with a product: tiles, staging
+
+// Modelled cost of a tile shape: microseconds per k-block of 64 and per tile
+// besides.
+struct TileCost {
+  GatedTile tile;
+  double kb_us, tile_us;
+};
+constexpr TileCost kForwardTiles[] = {{{true, 256}, 0.36, 2.0}, {{false, 128}, 0.33, 1.2}};
+constexpr TileCost kBackwardTiles[] = {{{true, 256}, 0.36, 3.0}, {{false, 128}, 0.33, 2.0}, {{false, 64}, 0.30, 1.5}};
+
+struct GatedPlan {
+  GatedTile tile;
+  int tiles_m, tiles_n, grid;
+};
+template <size_t N>
+GatedPlan plan_gated(const TileCost (&tiles)[N], int64_t T, int64_t K, int64_t F, bool forward, int sms, int pairs) {
+  GatedPlan best{};
+  double best_us = -1;
+  const int64_t num_kb = ceil_div64(K, kBK);
+  for (const TileCost &c : tiles) {
+    const int64_t slots = c.tile.pair ? pairs : sms;
+    if (slots <= 0) continue;
+    const int64_t tm = ceil_div64(T, c.tile.pair ? 2 * kBM : kBM), tn = ceil_div64(F, forward ? c.tile.bn / 2 : c.tile.bn);
+    const int64_t rounds = ceil_div64(tm * tn, slots);
+    const double us = rounds * (num_kb * c.kb_us + c.tile_us);
+    if (best_us >= 0 && us >= best_us) continue;
+    best_us = us;
+    best.tile = c.tile;
+    best.tiles_m = (int)tm;
+    best.tiles_n = (int)tn;
+    best.grid = (int)(tm * tn < slots ? tm * tn : slots) * (c.tile.pair ? 2 : 1);
   }
+  return best;
+}
+
+// An operand as TMA can read it: as it is, or (rows off 16 bytes) copied into
+// the stream's scratch at `at`.
+struct Operand {
+  const uint16_t *p;
+  int64_t rows, cols, ld;
+  bool pack() const { return !rows_on(p, ld, 2, 16); }
+  int64_t packed_ld() const { return (cols + 7) / 8 * 8; }
+  size_t bytes() const { return pack() ? align256((size_t)rows * packed_ld() * 2) : 0; }
+};
+cudaError_t stage(Operand &o, uint8_t *&at, const OpContext &c) {
+  if (!o.pack()) return cudaSuccess;
+  uint16_t *dst = reinterpret_cast<uint16_t *>(at);
+  at += o.bytes();
+  count_launches(1);
+  const cudaError_t e = launch_pack_u16(o.p, o.rows, o.cols, o.ld, dst, o.packed_ld(), c.sms, c.st);
+  o.ld = o.packed_ld();
+  o.p = dst;
+  return e;
+}
+
+// Stages the n operands (the first is A, the others weights of layout km),
+// makes their maps and the outputs', and launches.
+gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool forward, GatedTcParams &p,
+                        const OpContext &c) {
+  if (pl.grid <= 0) return GEMM_ERR_CUDA;
+  size_t need = 0;
+  for (int i = 0; i < n; ++i) need += o[i].bytes();
+  void *ws = nullptr;
+  if (need) {
+    const gemm_status_t s = op_workspace(need, c.st, &ws);
+    if (s != GEMM_OK) return s;
+  }
+  uint8_t *at = static_cast<uint8_t *>(ws);
+  for (int i = 0; i < n; ++i)
+    if (stage(o[i], at, c) != cudaSuccess) return GEMM_ERR_CUDA;
+  GatedMaps m;
+  if (!bf16_box_map(&m.a, o[0].p, (uint64_t)o[0].cols, (uint64_t)o[0].rows, (uint64_t)o[0].ld, kBK, kBM))
+    return GEMM_ERR_CUDA;
+  const int cta_n = pl.tile.pair ? pl.tile.bn / 2 : pl.tile.bn;
+  const uint32_t part = (uint32_t)(forward && !pl.tile.pair ? cta_n / 2 : cta_n);
+  for (int i = 1; i < n; ++i)
+    if (!bf16_box_map(&m.b[i - 1], o[i].p, (uint64_t)o[i].cols, (uint64_t)o[i].rows, (uint64_t)o[i].ld, km ? kBK : 64,
+                      km ? part : kBK))
+      return GEMM_ERR_CUDA;
+  if (n < 3) m.b[1] = m.b[0];
+  // outputs through TMA where their rows are whole 16-byte pieces (a clipped
+  // store would write into a row's padding), and G and U, read in such pieces
+  // then, likewise
+  p.tma = tma_store_enabled() && p.F % 8 == 0;
+  for (int i = 0; i < 3; ++i)
+    if (p.out[i]) p.tma = p.tma && rows_on(p.out[i], p.ldout[i], 2, 16);
+  if (p.gate) p.tma = p.tma && rows_on(p.gate, p.ldgate, 2, 16) && rows_on(p.up, p.ldup, 2, 16);
+  for (int i = 0; i < 3; ++i) {
+    m.out[i] = m.a;
+    if (p.tma && p.out[i] &&
+        !float_out_map(&m.out[i], true, p.out[i], (uint64_t)p.F, (uint64_t)p.T, (uint64_t)p.ldout[i], 1))
+      return GEMM_ERR_CUDA;
+  }
+  p.tiles_m = pl.tiles_m;
+  p.tiles_n = pl.tiles_n;
+  p.num_kb = (int)ceil_div64(p.K, kBK);
+  p.group_m = 8;
+  p.q_vec = p.ck.q && rows_on(p.ck.q, p.ck.ldq, 1, 16);
+  p.err = c.err;
+  p.wait_limit_ns = c.wait_limit_ns;
+  count_launches(1);
+  const cudaError_t e = forward ? launch_gated_tc_fwd(pl.tile, km, m, p, pl.grid, c.st)
+                                : launch_gated_tc_bwd(pl.tile, km, m, p, pl.grid, c.st);
+  return e == cudaSuccess ? GEMM_OK : GEMM_ERR_CUDA;
 }
 
 }  // namespace
 
-cudaError_t launch_gated_forward(const GatedForward &p, const OpContext &c) {
-  const dim3 grid((unsigned)((p.T + kTile - 1) / kTile), (unsigned)((p.F + kTile - 1) / kTile));
-  cudaError_t e = cudaSuccess;
-  with_activation(p.act, [&](auto act) {
-    e = launch_ex(gated_forward_kernel<decltype(act)::value>, grid, dim3(256), 0, c.st, 1, p);
-  });
-  return e;
+gemm_status_t gated_forward(const GatedForward &p, const OpContext &c) {
+  if (p.K == 0) {
+    uint16_t *out[3] = {p.h, p.g, p.u};
+    const int64_t ld[3] = {p.ldh, p.ldg, p.ldu};
+    for (int i = 0; i < 3; ++i) {
+      if (!out[i]) continue;
+      count_launches(1);
+      if (launch_zero_fill(out[i], p.T, p.F, ld[i], 2, c.sms, c.st) != cudaSuccess) return GEMM_ERR_CUDA;
+    }
+    return GEMM_OK;
+  }
+  const int64_t wr = p.w_kmajor ? p.F : p.K, wc = p.w_kmajor ? p.K : p.F;
+  Operand o[3] = {{p.x, p.T, p.K, p.ldx}, {p.wg, wr, wc, p.ldwg}, {p.wu, wr, wc, p.ldwu}};
+  GatedTcParams t{};
+  t.T = (int)p.T, t.F = p.F, t.K = p.K, t.act = p.act;
+  t.out[0] = p.h, t.out[1] = p.g, t.out[2] = p.u;
+  t.ldout[0] = p.ldh, t.ldout[1] = p.ldg, t.ldout[2] = p.ldu;
+  return run_gated(plan_gated(kForwardTiles, p.T, p.K, p.F, true, c.sms, pair_slots()), o, 3, p.w_kmajor, true, t, c);
+}
+
+gemm_status_t gated_down_backward(const GatedDownBackward &p, const OpContext &c) {
+  const GatedBackward &b = p.b;
+  const int64_t wr = p.w_kmajor ? b.F : p.N, wc = p.w_kmajor ? p.N : b.F;
+  Operand o[2] = {{p.d, b.T, p.N, p.ldd}, {p.w, wr, wc, p.ldw}};
+  GatedTcParams t{};
+  t.T = (int)b.T, t.F = b.F, t.K = p.N, t.act = b.act;
+  t.out[0] = b.dg, t.out[1] = b.du;
+  t.ldout[0] = b.lddg, t.ldout[1] = b.lddu;
+  t.gate = b.g, t.up = b.u, t.ldgate = b.ldg, t.ldup = b.ldu;
+  t.ck = b.ck;
+  return run_gated(plan_gated(kBackwardTiles, b.T, p.N, b.F, false, c.sms, pair_slots()), o, 2, p.w_kmajor, false, t,
+                   c);
 }
 
 cudaError_t launch_gated_backward(const GatedBackward &p, cudaStream_t st) {
   const int64_t blocks = (p.T * ((p.F + 31) / 32) + 7) / 8;
-  cudaError_t e = cudaSuccess;
-  with_activation(p.act, [&](auto act) {
-    e = launch_ex(gated_backward_kernel<decltype(act)::value>, dim3((unsigned)(blocks < (1 << 30) ? blocks : (1 << 30))),
-                  dim3(256), 0, st, 1, p);
-  });
-  return e;
-}
-
-cudaError_t launch_gated_down_backward(const GatedDownBackward &p, const OpContext &c) {
-  const dim3 grid((unsigned)((p.b.T + kTile - 1) / kTile), (unsigned)((p.b.F + kTile - 1) / kTile));
-  cudaError_t e = cudaSuccess;
-  with_activation(p.b.act, [&](auto act) {
-    e = launch_ex(gated_down_backward_kernel<decltype(act)::value>, grid, dim3(256), 0, c.st, 1, p);
-  });
-  return e;
+  const auto kern = p.act == GEMM_ACT_SILU        ? gated_backward_kernel<GEMM_ACT_SILU>
+                    : p.act == GEMM_ACT_GELU      ? gated_backward_kernel<GEMM_ACT_GELU>
+                    : p.act == GEMM_ACT_GELU_TANH ? gated_backward_kernel<GEMM_ACT_GELU_TANH>
+                                                  : gated_backward_kernel<GEMM_ACT_RELU>;
+  return launch_ex(kern, dim3((unsigned)(blocks < (1 << 30) ? blocks : (1 << 30))), dim3(256), 0, st, 1, p);
 }
 
 }  // namespace gb300

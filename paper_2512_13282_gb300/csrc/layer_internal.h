@@ -126,7 +126,8 @@ struct GatedForward {
   uint16_t *g, *u;  // both null: not kept
   int64_t ldg, ldu;
 };
-cudaError_t launch_gated_forward(const GatedForward &p, const OpContext &c);
+// Within with_scratch().
+gemm_status_t gated_forward(const GatedForward &p, const OpContext &c);
 
 struct GatedBackward {
   int64_t T;
@@ -151,7 +152,41 @@ struct GatedDownBackward {
   int64_t ldw;
   bool w_kmajor;  // Wd's n index contiguous
 };
-cudaError_t launch_gated_down_backward(const GatedDownBackward &p, const OpContext &c);
+gemm_status_t gated_down_backward(const GatedDownBackward &p, const OpContext &c);
+
+// The tensor-core kernel of both (gated_tc.cuh).
+struct GatedTcParams {
+  int T, F, K;  // rows, features, reduction length
+  int tiles_m, tiles_n, num_kb, group_m;
+  int act;
+  // forward: out[0] = H, out[1], out[2] = G, U or null; backward: out[0], out[1]
+  // = dG, dU.  tma: they go through tensor maps, and gate / up are read in
+  // 16-byte pieces; else element by element.
+  uint16_t *out[3];
+  int64_t ldout[3];
+  int tma;
+  const uint16_t *gate, *up;  // backward: G, U
+  int64_t ldgate, ldup;
+  Q8Ref ck;   // backward: or ck.q null
+  int q_vec;  // its rows start on 16 bytes
+  uint32_t *err;
+  uint64_t wait_limit_ns;
+};
+// A compiled tile shape: bn columns of the accumulator (forward: bn / 2
+// features, each with its gate and up value).
+struct GatedTile {
+  bool pair;  // a CTA pair per 256-row tile, or one CTA per 128-row tile
+  int bn;     // 256 (pair), 128, or 64 (backward)
+};
+// Tensor maps: X or dO; Wg and Wu, or Wd; the outputs (any valid map where a
+// kernel does not use one).
+struct GatedMaps {
+  CUtensorMap a, b[2], out[3];
+};
+cudaError_t launch_gated_tc_fwd(const GatedTile &tile, bool km, const GatedMaps &m, const GatedTcParams &p, int grid,
+                                cudaStream_t st);
+cudaError_t launch_gated_tc_bwd(const GatedTile &tile, bool km, const GatedMaps &m, const GatedTcParams &p, int grid,
+                                cudaStream_t st);
 
 // Dropout (layer_dropout.cu), forward or backward (without a residual).
 struct Dropout {
