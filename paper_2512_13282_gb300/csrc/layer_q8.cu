@@ -17,19 +17,6 @@ namespace {
 
 constexpr int kQ8Threads = 256;
 
-// Half block h of the matrix -> its row and first column, `halves` of them a
-// row (an even number).  With rows laid end to end the launcher makes the
-// matrix one row, and 32-bit arithmetic serves any matrix below 2^32 halves.
-__device__ __forceinline__ void half_block(int64_t h, int64_t halves, int64_t *r, int64_t *c) {
-  int64_t row;
-  if ((uint64_t)h <= 0xFFFFFFFFull && halves <= 0xFFFFFFFFll)
-    row = (uint32_t)h / (uint32_t)halves;
-  else
-    row = h / halves;
-  *r = row;
-  *c = (h - row * halves) * 16;
-}
-
 // A half block's bytes and its block's exponent (the other half is the
 // neighbouring lane's).
 struct Q8Half {
@@ -51,12 +38,6 @@ __device__ __forceinline__ Q8Half q8_half(const Chunk<TX, 16> &raw) {
   for (int j = 0; j < 4; ++j) lo[j] = raw.get2(j), hi[j] = raw.get2(4 + j);
   const uint2 wl = q8_pack8(lo, e), wh = q8_pack8(hi, e);
   return Q8Half{{wl.x, wl.y, wh.x, wh.y}, e};
-}
-// The first n of a half block's bytes.
-__device__ __forceinline__ void store_bytes(int8_t *q, const uint32_t (&w)[4], int n) {
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (i < n) q[i] = (int8_t)(w[i / 4] >> (8 * (i & 3)));
 }
 // A half block's values in bf16.
 __device__ __forceinline__ void q8_restored(const Chunk<Q8, 16> &raw, float scale, uint32_t (&o)[8]) {
@@ -134,47 +115,9 @@ __global__ void __launch_bounds__(kQ8Threads)
 }
 
 // Rows at any alignment: the same half blocks, shifted between registers and
-// the 16-byte pieces of memory that they lie in (shift_words, store_shifted).
+// the 16-byte pieces of memory that they lie in (load_half, store_shifted).
 // 1792 x 10471 bf16: save 16.5 us, restore 15.3; a warp per 256 values of a
 // row, a lane one value of each 32, took 36.4 and 23.6.
-
-// A run of the piece at p into its words w[AT ..] (zero before).
-template <int AT, int N>
-__device__ __forceinline__ void load_run(const char *p, uint32_t at, uint32_t n, uint32_t (&w)[N]) {
-  uint2 v = make_uint2(0, 0);
-  if (n == 8)
-    v = *reinterpret_cast<const uint2 *>(p + at);
-  else
-    v.x = (n == 4   ? *reinterpret_cast<const uint32_t *>(p + at)
-           : n == 2 ? *reinterpret_cast<const uint16_t *>(p + at)
-                    : *reinterpret_cast<const uint8_t *>(p + at))
-          << (8 * (at & 3u));
-#pragma unroll
-  for (uint32_t k = 0; k < 4; ++k) w[AT + k] |= at >> 2 == k ? v.x : n == 8 && (at >> 2) + 1 == k ? v.y : 0u;
-}
-
-// A half block's W words at src.  Pieces that reach past the row (first: it
-// starts with this half block; after: its bytes that follow) are read in runs.
-template <int W>
-__device__ __forceinline__ void load_half(const void *src, bool first, int64_t after, uint32_t (&out)[W]) {
-  const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(src) & 15u;
-  const char *p = static_cast<const char *>(src) - off;
-  uint32_t w[W + 4] = {};
-#pragma unroll
-  for (int i = 0; i <= W / 4; ++i) {
-    if (i == 0 && first && off) {
-      upper_runs<16>(off, [&](uint32_t at, uint32_t n) { load_run<0>(p, at, n, w); });
-    } else if (i == W / 4 && after < 16 - (int)off) {
-      lower_runs<16>(off, [&](uint32_t at, uint32_t n) { load_run<W>(p + 4 * W, at, n, w); });
-    } else if (i < W / 4 || off) {
-      const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
-      w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
-    }
-  }
-  shift_words<W, 4>(w, off);
-#pragma unroll
-  for (int i = 0; i < W; ++i) out[i] = w[i];
-}
 
 template <typename TX>
 __global__ void __launch_bounds__(kQ8Threads)

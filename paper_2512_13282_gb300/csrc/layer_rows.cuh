@@ -1,6 +1,6 @@
 // layer_rows.cuh -- element access and row sums shared by the layer
 // operators' kernels (layer_ln_fwd.cu, layer_ln_bwd.cu,
-// layer_q8.cu).
+// layer_q8.cu, layer_gate.cu, layer_dropout.cu).
 #pragma once
 #include <cuda_bf16.h>
 
@@ -345,6 +345,63 @@ __device__ __forceinline__ void store_shifted(void *dst, bool whole, bool joined
   }
 }
 
+// A run of the piece at p into its words w[AT ..] (zero before).
+template <int AT, int N>
+__device__ __forceinline__ void load_run(const char *p, uint32_t at, uint32_t n, uint32_t (&w)[N]) {
+  uint2 v = make_uint2(0, 0);
+  if (n == 8)
+    v = *reinterpret_cast<const uint2 *>(p + at);
+  else
+    v.x = (n == 4   ? *reinterpret_cast<const uint32_t *>(p + at)
+           : n == 2 ? *reinterpret_cast<const uint16_t *>(p + at)
+                    : *reinterpret_cast<const uint8_t *>(p + at))
+          << (8 * (at & 3u));
+#pragma unroll
+  for (uint32_t k = 0; k < 4; ++k) w[AT + k] |= at >> 2 == k ? v.x : n == 8 && (at >> 2) + 1 == k ? v.y : 0u;
+}
+
+// A lane's W words at src, any address.  Pieces that reach past the row (first: it
+// starts with these words; after: its bytes that follow) are read in runs.
+template <int W>
+__device__ __forceinline__ void load_half(const void *src, bool first, int64_t after, uint32_t (&out)[W]) {
+  const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(src) & 15u;
+  const char *p = static_cast<const char *>(src) - off;
+  uint32_t w[W + 4] = {};
+#pragma unroll
+  for (int i = 0; i <= W / 4; ++i) {
+    if (i == 0 && first && off) {
+      upper_runs<16>(off, [&](uint32_t at, uint32_t n) { load_run<0>(p, at, n, w); });
+    } else if (i == W / 4 && after < 16 - (int)off) {
+      lower_runs<16>(off, [&](uint32_t at, uint32_t n) { load_run<W>(p + 4 * W, at, n, w); });
+    } else if (i < W / 4 || off) {
+      const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
+      w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+    }
+  }
+  shift_words<W, 4>(w, off);
+#pragma unroll
+  for (int i = 0; i < W; ++i) out[i] = w[i];
+}
+
+// Half block h of the matrix -> its row and first column, `halves` of them a
+// row (an even number).  With rows laid end to end the launcher makes the
+// matrix one row, and 32-bit arithmetic serves any matrix below 2^32 halves.
+__device__ __forceinline__ void half_block(int64_t h, int64_t halves, int64_t *r, int64_t *c) {
+  int64_t row;
+  if ((uint64_t)h <= 0xFFFFFFFFull && halves <= 0xFFFFFFFFll)
+    row = (uint32_t)h / (uint32_t)halves;
+  else
+    row = h / halves;
+  *r = row;
+  *c = (h - row * halves) * 16;
+}
+
+// The first n of a half block's bytes.
+__device__ __forceinline__ void store_bytes(int8_t *q, const uint32_t (&w)[4], int n) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (i < n) q[i] = (int8_t)(w[i / 4] >> (8 * (i & 3)));
+}
 // A parameter vector of either type, or absent.
 __device__ __forceinline__ float load_param(const void *p, int type, int c, float absent) {
   if (!p) return absent;
