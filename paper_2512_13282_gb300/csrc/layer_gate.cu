@@ -16,41 +16,94 @@ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // ------------------------------------------------------- the gradient alone
 
-// Gradient of one element; returns act(g) * u.
-template <int ACT>
-__device__ __forceinline__ float gate_backward(const GatedBackward &p, int64_t r, int c, float dh) {
-  const float g = load_value<bf16>(p.g, r * p.ldg + c), u = load_value<bf16>(p.u, r * p.ldu + c);
-  const GateValue v = gate<ACT, true>(g);
-  store_value<bf16>(p.dg, r * p.lddg + c, dh * u * v.slope);
-  store_value<bf16>(p.du, r * p.lddu + c, dh * v.a);
-  return v.a * u;
-}
+constexpr int kThreads = 256;
 
-// The checkpoint of 32 values, one a lane (0 past the row's end).
-__device__ __forceinline__ void q8_by_warp(const Q8Ref &ck, int64_t r, int c, int cols, float h) {
-  uint32_t top = c < cols ? __float_as_uint(h) & 0x7FFFFFFFu : 0u;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (c >= cols) return;
-  const uint32_t e = q8_exponent(top);
-  ck.q[r * ck.ldq + c] = (int8_t)q8_byte(h, q8_inverse(e), e);
-  if ((c & 31) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
-}
-
-// A warp per 32 values of a row.
-template <int ACT>
-__global__ void __launch_bounds__(256) gated_backward_kernel(const GatedBackward p) {
+// A thread takes half a block of the checkpoint: 16 consecutive values of a
+// row, its neighbouring lane the other half; they exchange the largest
+// magnitude with one shuffle.  VEC: all rows start on 16 bytes; else values are
+// shifted between registers and the 16-byte pieces of memory that they lie in.
+template <int ACT, bool VEC>
+__global__ void __launch_bounds__(kThreads) gated_backward_kernel(const GatedBackward p, int64_t cols) {
   griddep_launch_dependents();
   griddep_wait();
-  const int lane = threadIdx.x & 31, groups = (p.F + 31) / 32;
-  const int64_t items = p.T * groups;
-  for (int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); t < items; t += (int64_t)gridDim.x * 8) {
-    const int64_t r = t / groups;
-    const int c = (int)(t - r * groups) * 32 + lane;
-    float h = 0.f;
-    if (c < p.F) h = gate_backward<ACT>(p, r, c, p.dh ? load_value<bf16>(p.dh, r * p.lddh + c) : 0.f);
-    if (p.ck.q) q8_by_warp(p.ck, r, c, p.F, h);
+  const int64_t halves = (cols + 31) / 32 * 2, items = p.T * halves, step = (int64_t)gridDim.x * kThreads;
+  const int lane = threadIdx.x & 31;
+  for (int64_t h0 = (int64_t)blockIdx.x * kThreads; h0 < items; h0 += step) {
+    // items is even, so both lanes of a block are in range or neither is
+    const int64_t h = h0 + threadIdx.x;
+    const bool live = h < items;
+    int64_t r, c;
+    half_block(live ? h : items - 1, halves, &r, &c);
+    const int n = !live || c >= cols ? 0 : (int)min((int64_t)16, cols - c);
+    const auto load = [&](const uint16_t *m, int64_t ld) {
+      const uint16_t *row = m + r * ld;
+      Chunk<bf16, 16> v;
+      if (n < 16)
+        v.load_part(row, c, n);
+      else if constexpr (VEC)
+        v.load(row, c);
+      else
+        load_half(row + c, c == 0, (cols - c - 16) * 2, v.w);
+      return v;
+    };
+    Chunk<bf16, 16> d;
+    if (p.dh)
+      d = load(p.dh, p.lddh);
+    else
+      d.load_part(nullptr, 0, 0);
+    const Chunk<bf16, 16> g = load(p.g, p.ldg), u = load(p.u, p.ldu);
+    uint32_t dg[8], du[8];
+    float2 v[8];  // act(g) * u
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 di = d.get2(i), gi = g.get2(i), ui = u.get2(i);
+      const GateValue a = gate<ACT, true>(gi.x), b = gate<ACT, true>(gi.y);
+      dg[i] = pack_bf16x2(di.x * ui.x * a.slope, di.y * ui.y * b.slope);
+      du[i] = pack_bf16x2(di.x * a.a, di.y * b.a);
+      v[i] = make_float2(a.a * ui.x, b.a * ui.y);
+      top = max(top, max(__float_as_uint(v[i].x) & 0x7FFFFFFFu, __float_as_uint(v[i].y) & 0x7FFFFFFFu));
+    }
+    const auto store = [&](uint16_t *m, int64_t ld, const uint32_t(&w)[8]) {
+      uint16_t *row = m + r * ld;
+      if constexpr (VEC) {
+        if (n == 16) store_32_bytes(row + c, w);
+      } else {
+        store_shifted<4>(row + c, n == 16, lane > 0 && c > 0, lane < 31 && c + 32 <= cols, w);
+      }
+      if (n < 16) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (i < n) row[c + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+      }
+    };
+    store(p.dg, p.lddg, dg);
+    store(p.du, p.lddu, du);
+    if (!p.ck.q) continue;
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    const uint32_t e = q8_exponent(top);
+    float2 lo[4], hi[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lo[j] = v[j], hi[j] = v[4 + j];
+    const uint2 wl = q8_pack8(lo, e), wh = q8_pack8(hi, e);
+    const uint32_t w[4] = {wl.x, wl.y, wh.x, wh.y};
+    int8_t *q = p.ck.q + r * p.ck.ldq + c;
+    if constexpr (VEC) {
+      if (n == 16) *reinterpret_cast<uint4 *>(q) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+      store_shifted<4>(q, n == 16, lane > 0 && c > 0, lane < 31 && c + 32 <= cols, w);
+    }
+    if (n < 16) store_bytes(q, w, n);
+    if (live && (h & 1) == 0) p.ck.e[r * p.ck.lde + (c >> 5)] = (uint8_t)e;
   }
+}
+
+template <bool VEC>
+auto backward_kernel(int act) {
+  return act == GEMM_ACT_SILU        ? gated_backward_kernel<GEMM_ACT_SILU, VEC>
+         : act == GEMM_ACT_GELU      ? gated_backward_kernel<GEMM_ACT_GELU, VEC>
+         : act == GEMM_ACT_GELU_TANH ? gated_backward_kernel<GEMM_ACT_GELU_TANH, VEC>
+                                     : gated_backward_kernel<GEMM_ACT_RELU, VEC>;
 }
 
 // --------------------------------------------- with a product: tiles, staging
@@ -113,6 +166,7 @@ cudaError_t stage(Operand &o, uint8_t *&at, const OpContext &c) {
 // makes their maps and the outputs', and launches.
 gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool forward, GatedTcParams &p,
                         const OpContext &c) {
+  const bool few = forward && p.T <= kFewTokens;
   if (pl.grid <= 0) return GEMM_ERR_CUDA;
   size_t need = 0;
   for (int i = 0; i < n; ++i) need += o[i].bytes();
@@ -125,15 +179,23 @@ gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool fo
   for (int i = 0; i < n; ++i)
     if (stage(o[i], at, c) != cudaSuccess) return GEMM_ERR_CUDA;
   GatedMaps m;
-  if (!bf16_box_map(&m.a, o[0].p, (uint64_t)o[0].cols, (uint64_t)o[0].rows, (uint64_t)o[0].ld, kBK, kBM))
+  if (!bf16_box_map(&m.a, o[0].p, (uint64_t)o[0].cols, (uint64_t)o[0].rows, (uint64_t)o[0].ld, kBK,
+                    few ? (uint32_t)gated_few_columns(p.T) : kBM))
     return GEMM_ERR_CUDA;
   const int cta_n = pl.tile.pair ? pl.tile.bn / 2 : pl.tile.bn;
-  const uint32_t part = (uint32_t)(forward && !pl.tile.pair ? cta_n / 2 : cta_n);
+  const uint32_t part = few ? 64u : (uint32_t)(forward && !pl.tile.pair ? cta_n / 2 : cta_n);
   for (int i = 1; i < n; ++i)
     if (!bf16_box_map(&m.b[i - 1], o[i].p, (uint64_t)o[i].cols, (uint64_t)o[i].rows, (uint64_t)o[i].ld, km ? kBK : 64,
                       km ? part : kBK))
       return GEMM_ERR_CUDA;
   if (n < 3) m.b[1] = m.b[0];
+  p.num_kb = (int)ceil_div64(p.K, kBK);
+  p.err = c.err;
+  p.wait_limit_ns = c.wait_limit_ns;
+  if (few) {
+    count_launches(1);
+    return launch_gated_few(km, m, p, c.sms, c.st) == cudaSuccess ? GEMM_OK : GEMM_ERR_CUDA;
+  }
   // outputs through TMA where their rows are whole 16-byte pieces (a clipped
   // store would write into a row's padding), and G and U, read in such pieces
   // then, likewise
@@ -149,11 +211,8 @@ gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool fo
   }
   p.tiles_m = pl.tiles_m;
   p.tiles_n = pl.tiles_n;
-  p.num_kb = (int)ceil_div64(p.K, kBK);
   p.group_m = 8;
   p.q_vec = p.ck.q && rows_on(p.ck.q, p.ck.ldq, 1, 16);
-  p.err = c.err;
-  p.wait_limit_ns = c.wait_limit_ns;
   count_launches(1);
   const cudaError_t e = forward ? launch_gated_tc_fwd(pl.tile, km, m, p, pl.grid, c.st)
                                 : launch_gated_tc_bwd(pl.tile, km, m, p, pl.grid, c.st);
@@ -197,12 +256,12 @@ gemm_status_t gated_down_backward(const GatedDownBackward &p, const OpContext &c
 }
 
 cudaError_t launch_gated_backward(const GatedBackward &p, cudaStream_t st) {
-  const int64_t blocks = (p.T * ((p.F + 31) / 32) + 7) / 8;
-  const auto kern = p.act == GEMM_ACT_SILU        ? gated_backward_kernel<GEMM_ACT_SILU>
-                    : p.act == GEMM_ACT_GELU      ? gated_backward_kernel<GEMM_ACT_GELU>
-                    : p.act == GEMM_ACT_GELU_TANH ? gated_backward_kernel<GEMM_ACT_GELU_TANH>
-                                                  : gated_backward_kernel<GEMM_ACT_RELU>;
-  return launch_ex(kern, dim3((unsigned)(blocks < (1 << 30) ? blocks : (1 << 30))), dim3(256), 0, st, 1, p);
+  const auto on16 = [&](const void *m, int64_t ld) { return rows_on(m, ld, 2, 16); };
+  const bool vec = (!p.dh || on16(p.dh, p.lddh)) && on16(p.g, p.ldg) && on16(p.u, p.ldu) && on16(p.dg, p.lddg) &&
+                   on16(p.du, p.lddu) && (!p.ck.q || rows_on(p.ck.q, p.ck.ldq, 1, 16));
+  const int64_t blocks = ceil_div64(p.T * (ceil_div64(p.F, 32) * 2), kThreads);
+  return launch_ex(vec ? backward_kernel<true>(p.act) : backward_kernel<false>(p.act),
+                   dim3((unsigned)(blocks < (1 << 30) ? blocks : (1 << 30))), dim3(kThreads), 0, st, 1, p, (int64_t)p.F);
 }
 
 }  // namespace gb300

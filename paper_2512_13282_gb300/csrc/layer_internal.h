@@ -185,6 +185,11 @@ struct GatedMaps {
 };
 cudaError_t launch_gated_tc_fwd(const GatedTile &tile, bool km, const GatedMaps &m, const GatedTcParams &p, int grid,
                                 cudaStream_t st);
+// The forward kernel of at most kFewTokens tokens (gated_few.cu): X in boxes of
+// 64 x gated_few_columns(T), each weight in boxes of 64 x 64.
+constexpr int kFewTokens = 128;
+int gated_few_columns(int64_t T);
+cudaError_t launch_gated_few(bool km, const GatedMaps &m, const GatedTcParams &p, int sms, cudaStream_t st);
 cudaError_t launch_gated_tc_bwd(const GatedTile &tile, bool km, const GatedMaps &m, const GatedTcParams &p, int grid,
                                 cudaStream_t st);
 
