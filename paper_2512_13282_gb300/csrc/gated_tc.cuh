@@ -13,21 +13,18 @@
 // the kernel without G and U having been stored.  In a pair, one CTA's half of
 // B is Wg's, the other's Wu's.
 //
-// Backward.  The epilogue reads G and U of its 32 x 32 blocks itself, a block
-// ahead (the first of a tile while the tensor core still works on it), takes
-// the gradient from dH in registers, and the checkpoint of act(G) U: a lane
-// holds 32 consecutive values of a row, which is one block of the checkpoint,
-// so that needs no exchange between lanes.  dH is never stored: 8192 x 11008
-// would cost 360 MB of traffic, 53 us.
+// Backward.  The epilogue warps bring blocks of G and U (32 x 32) into shared
+// memory, take the gradient from dH and leave dG and dU in their place, from
+// where they store them; and the checkpoint of act(G) U: a lane holds 32
+// consecutive values of a row, which is one block of the checkpoint, so that
+// needs no exchange between lanes.  dH is never stored: 8192 x 11008 would cost
+// 360 MB of traffic, 53 us.
 #pragma once
 #include "gate_math.cuh"
 #include "layer_rows.cuh"
 #include "gemm_tc2.cuh"
 
 namespace gb300 {
-
-constexpr int kGatedEpiWarps = 8;
-constexpr int kGatedThreads = (2 + kGatedEpiWarps) * 32;
 
 template <int BN, bool PAIR, bool BWD>
 struct GatedCfg {
@@ -36,36 +33,51 @@ struct GatedCfg {
   static constexpr int kCtaN = PAIR ? BN / 2 : BN;   // columns of B a CTA loads
   static constexpr int kPartN = BWD || PAIR ? kCtaN : kCtaN / 2;  // ... of one weight
   static_assert(kPartN % 64 == 0 && BN <= 256, "operands are assembled from 64-wide boxes");
-  static constexpr int kOuts = BWD ? 2 : 3;
+  static constexpr int kEpiWarps = !BWD || BN == 64 ? 4 : 8;
+  static constexpr int kThreads = (2 + kEpiWarps) * 32;
   static constexpr uint32_t kBBytes = kCtaN * kRowBytes;
   static constexpr uint32_t kStageBytes = kABytes + kBBytes;
-  static constexpr uint32_t kEpiWarpBytes = kOuts * 2048u;  // a 32 x 32 block of bf16 for each output
+  // a 32 x 32 block of each output; backward, of G and U, which become dG and dU
+  static constexpr uint32_t kEpiWarpBytes = (BWD ? 2 : 3) * 2048u;
   static constexpr int kStages =
-      (int)((232448u - 1024u - 256u - kGatedEpiWarps * kEpiWarpBytes) / kStageBytes);
+      (int)((232448u - 1024u - 256u - kEpiWarps * kEpiWarpBytes) / kStageBytes);
   static constexpr uint32_t kTmemCols = pow2_at_least(2 * BN);
-  static constexpr int kChunks = kTileF / 32 / (kGatedEpiWarps / 4);  // 32-column blocks of an epilogue warp
-  static_assert(kChunks >= 1, "each of the two warpgroups has a block");
+  static constexpr int kChunks = kTileF / 32 / (kEpiWarps / 4);  // 32-column blocks of an epilogue warp
+  static_assert(kChunks >= 1, "each warpgroup has a block");
   static constexpr uint32_t kEpiOffset = kStages * kStageBytes;
-  static constexpr uint32_t kBarOffset = kEpiOffset + kGatedEpiWarps * kEpiWarpBytes;
+  static constexpr uint32_t kBarOffset = kEpiOffset + kEpiWarps * kEpiWarpBytes;
   static constexpr uint32_t kNumBars = 2 * kStages + 4 + 1;
   static constexpr uint32_t kSmemBytes = kBarOffset + kNumBars * 8 + 16 + 1024;
   static_assert(kNumBars * 8 + 16 <= 256 && kSmemBytes <= 232448, "shared memory per CTA is 227 KB");
   static_assert(kTmemCols <= 512, "TMEM has 512 columns");
 };
 
-// Blocks of 32 x 32 bf16 in an epilogue warp's shared memory, as a tensor map
-// with 64-byte swizzle has them: chunk j (16 bytes) of row r at chunk j ^
-// ((r / 2) % 4).
+// Blocks of 32 x 32 bf16 in an epilogue warp's shared memory: rows of 64 bytes,
+// chunk j (16 bytes) of row r at chunk j ^ ((r / 2) % 4), so that neither a
+// lane's row nor a warp's eight rows of four chunks meet in a bank.
 __device__ __forceinline__ uint32_t block_chunk(uint32_t buf, int row, int j) {
   return buf + row * 64 + ((j ^ ((row >> 1) & 3)) << 4);
+}
+__device__ __forceinline__ uint32_t block_element(uint32_t buf, int row, int col) {
+  return block_chunk(buf, row, col >> 3) + (col & 7) * 2;
 }
 __device__ __forceinline__ void put_row(uint32_t buf, int lane, const uint32_t (&h)[16]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     st_shared_v4(block_chunk(buf, lane, j), h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
 }
-__device__ __forceinline__ uint32_t block_element(uint32_t buf, int row, int col) {
-  return block_chunk(buf, row, col >> 3) + (col & 7) * 2;
+// A lane's 16 values from column 16 * k on.
+__device__ __forceinline__ void get_row16(uint32_t buf, int lane, int k, uint32_t (&h)[8]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const uint4 v = ld_shared_v4(block_chunk(buf, lane, 2 * k + j));
+    h[4 * j] = v.x, h[4 * j + 1] = v.y, h[4 * j + 2] = v.z, h[4 * j + 3] = v.w;
+  }
+}
+__device__ __forceinline__ void put_row16(uint32_t buf, int lane, int k, const uint32_t (&h)[8]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+    st_shared_v4(block_chunk(buf, lane, 2 * k + j), h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
 }
 __device__ __forceinline__ void st_shared_u16(uint32_t addr, uint16_t v) {
   asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(v) : "memory");
@@ -75,52 +87,73 @@ __device__ __forceinline__ uint16_t ld_shared_u16(uint32_t addr) {
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ uint32_t ld_shared_u8(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return v;
-}
 
-// The block at (y0, x) between memory of any alignment and shared memory,
-// along rows (lane = column): a lane's own row would be 32 lines touched by
-// every access.
-__device__ __forceinline__ void copy_in(const uint16_t *m, int64_t ld, uint32_t buf, int lane, int y0, int x, int T,
-                                        int F) {
-  const int c = x + lane, rows = min(32, T - y0);
-  uint16_t v[32];
+// The block at (y0, x) between memory and shared memory, along rows: a lane's
+// own row would be 32 lines touched by every access.  By the warps and not by
+// TMA, whose engine the operands keep busy: blocks through it stretched a
+// 256 x 256 tile of 4096 deep from 20.9 to 25 us (G, U, dG and dU; prefetches
+// into L2 by it, to 33 to 40 us).
+//
+// Rows on 16 bytes, F a multiple of 8: 16-byte pieces, four lanes a row.
+// block_fetch only asks for them (zero past the matrix); block_arrived waits.
+__device__ __forceinline__ void block_fetch(const uint16_t *m, int64_t ld, uint32_t buf, int lane, int y0, int x, int T,
+                                            int F) {
+  const int j = lane & 3, c = x + 8 * j;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = c < F && i < rows ? m[(int64_t)(y0 + i) * ld + c] : (uint16_t)0;
-#pragma unroll
-  for (int i = 0; i < 32; ++i) st_shared_u16(block_element(buf, i, lane), v[i]);
-}
-__device__ __forceinline__ void copy_out(uint16_t *m, int64_t ld, uint32_t buf, int lane, int y0, int x, int T, int F) {
-  const int c = x + lane, rows = min(32, T - y0);
-  if (c >= F) return;
-#pragma unroll 8
-  for (int i = 0; i < rows; ++i) m[(int64_t)(y0 + i) * ld + c] = ld_shared_u16(block_element(buf, i, lane));
-}
-
-// 32 values of the lane's row from column x on, F a multiple of 8 and the row
-// on 16 bytes; zero past F.
-__device__ __forceinline__ void load_row32(const uint16_t *row, int x, int F, bool live, uint32_t (&w)[16]) {
-  const uint4 *p = reinterpret_cast<const uint4 *>(row + x);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (live && x + 8 * j < F) v = p[j];
-    w[4 * j] = v.x, w[4 * j + 1] = v.y, w[4 * j + 2] = v.z, w[4 * j + 3] = v.w;
+  for (int i = 0; i < 4; ++i) {
+    const int row = i * 8 + (lane >> 2);
+    const bool in = y0 + row < T && c < F;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(block_chunk(buf, row, j)),
+                 "l"(__cvta_generic_to_global(in ? m + (int64_t)(y0 + row) * ld + c : m)), "r"(in ? 16 : 0)
+                 : "memory");
   }
 }
-__device__ __forceinline__ float bf16_at(const uint32_t (&w)[16], int i) {
+__device__ __forceinline__ void block_arrived() {
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncwarp();
+}
+__device__ __forceinline__ void block_store(uint16_t *m, int64_t ld, uint32_t buf, int lane, int y0, int x, int T,
+                                            int F) {
+  const int j = lane & 3, c = x + 8 * j;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = i * 8 + (lane >> 2);
+    const uint4 v = ld_shared_v4(block_chunk(buf, row, j));
+    if (y0 + row < T && c < F) *reinterpret_cast<uint4 *>(m + (int64_t)(y0 + row) * ld + c) = v;
+  }
+}
+// Any alignment: element by element, lane = column.
+__device__ __forceinline__ void block_fetch_any(const uint16_t *m, int64_t ld, uint32_t buf, int lane, int y0, int x,
+                                                int T, int F) {
+  const int c = x + lane, rows = min(32, T - y0);
+  m += (int64_t)y0 * ld + c;
+#pragma unroll 1
+  for (int r = 0; r < 32; r += 16, m += 16 * ld) {
+    uint16_t v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = c < F && r + i < rows ? m[i * ld] : (uint16_t)0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) st_shared_u16(block_element(buf, r + i, lane), v[i]);
+  }
+}
+__device__ __forceinline__ void block_store_any(uint16_t *m, int64_t ld, uint32_t buf, int lane, int y0, int x, int T,
+                                                int F) {
+  const int c = x + lane, rows = min(32, T - y0);
+  if (c >= F) return;
+  m += (int64_t)y0 * ld + c;
+#pragma unroll 8
+  for (int i = 0; i < rows; ++i, m += ld) *m = ld_shared_u16(block_element(buf, i, lane));
+}
+__device__ __forceinline__ float bf16_at(const uint32_t (&w)[8], int i) {
   return __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
 }
 
-// Gradient of 32 elements of a row from dh (float32 bits): g and u become dg
+// Gradient of 16 elements of a row from dh (float32 bits): g and u become dg
 // and du, dh becomes act(g) * u.
 template <int ACT>
-__device__ __forceinline__ void gate_backward32(uint32_t (&dh)[32], uint32_t (&g)[16], uint32_t (&u)[16]) {
+__device__ __forceinline__ void gate_backward16(uint32_t (&dh)[16], uint32_t (&g)[8], uint32_t (&u)[8]) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < 8; ++i) {
     float dg[2], du[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -154,11 +187,9 @@ __device__ __forceinline__ uint32_t q8_block32(const uint32_t (&h)[32], uint32_t
 }
 
 template <int BN, bool PAIR, bool KM, bool BWD>
-__global__ void __launch_bounds__(kGatedThreads, 1)
+__global__ void __launch_bounds__(GatedCfg<BN, PAIR, BWD>::kThreads, 1)
     gated_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB0,
-                    const __grid_constant__ CUtensorMap tmB1, const __grid_constant__ CUtensorMap tmOut0,
-                    const __grid_constant__ CUtensorMap tmOut1, const __grid_constant__ CUtensorMap tmOut2,
-                    const GatedTcParams p) {
+                    const __grid_constant__ CUtensorMap tmB1, const GatedTcParams p) {
   using Cfg = GatedCfg<BN, PAIR, BWD>;
   constexpr int STAGES = Cfg::kStages;
   extern __shared__ uint8_t smem_raw[];
@@ -191,7 +222,7 @@ __global__ void __launch_bounds__(kGatedThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(accf_bar(b), 1);
-      mbar_init(acce_bar(b), (PAIR ? 2 : 1) * kGatedEpiWarps * 32);
+      mbar_init(acce_bar(b), (PAIR ? 2 : 1) * Cfg::kEpiWarps * 32);
     }
     mbar_init(drain_bar, 1);
     *abort_flag = 0u;
@@ -199,11 +230,6 @@ __global__ void __launch_bounds__(kGatedThreads, 1)
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB0);
     if (!BWD) tma_prefetch_desc(&tmB1);
-    if (p.tma) {
-      tma_prefetch_desc(&tmOut0);
-      if (BWD || p.out[1]) tma_prefetch_desc(&tmOut1);
-      if (!BWD && p.out[1]) tma_prefetch_desc(&tmOut2);
-    }
   }
   __syncwarp();
   if (warp == 1) {
@@ -342,6 +368,38 @@ __global__ void __launch_bounds__(kGatedThreads, 1)
     const int colpart = ew >> 2;
     const uint32_t ebuf = base + Cfg::kEpiOffset + ew * Cfg::kEpiWarpBytes;
     uint32_t acc_cnt = 0;
+    const auto store = [&](uint16_t *m, int64_t ld, uint32_t buf, int y, int x) {
+      if (p.vec)
+        block_store(m, ld, buf, lane, y, x, p.T, p.F);
+      else
+        block_store_any(m, ld, buf, lane, y, x, p.T, p.F);
+    };
+    // backward: blocks of G and U are asked for in the order in which they are
+    // taken, those that exist; next_t, next_c: the next one
+    int next_t = first_tile, next_c = 0;
+    const auto ask = [&]() {
+      while (next_t < num_tiles) {
+        int tm, tn;
+        raster_tile(next_t, p.tiles_m, p.tiles_n, p.group_m, &tm, &tn);
+        const int y = tm * Cfg::kTileM + (int)rank * kBM + quad * 32;
+        const int x = tn * Cfg::kTileF + (colpart * Cfg::kChunks + next_c) * 32;
+        const bool here = y < p.T && x < p.F;
+        if (++next_c == Cfg::kChunks || !here) {
+          next_c = 0;
+          next_t += tile_step;
+        }
+        if (!here) continue;
+        if (p.vec) {
+          block_fetch(p.gate, p.ldgate, ebuf, lane, y, x, p.T, p.F);
+          block_fetch(p.up, p.ldup, ebuf + 2048, lane, y, x, p.T, p.F);
+        } else {
+          block_fetch_any(p.gate, p.ldgate, ebuf, lane, y, x, p.T, p.F);
+          block_fetch_any(p.up, p.ldup, ebuf + 2048, lane, y, x, p.T, p.F);
+        }
+        return;
+      }
+    };
+    if (BWD) ask();
     for (int t = first_tile; t < num_tiles; t += tile_step) {
       int tm, tn;
       raster_tile(t, p.tiles_m, p.tiles_n, p.group_m, &tm, &tn);
@@ -351,24 +409,6 @@ __global__ void __launch_bounds__(kGatedThreads, 1)
       const int x0 = tn * Cfg::kTileF + col0;
       const uint32_t b = acc_cnt & 1u, aph = (acc_cnt >> 1) & 1u;
       const uint32_t t0 = tmem_base + b * BN + ((uint32_t)(quad * 32) << 16) + col0;
-      // Outputs of the block at (y0, x), staged by the lanes' rows: to memory.
-      const auto emit = [&](int outs, int x) {
-        if (p.tma) {
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            tma_store_2d(&tmOut0, ebuf, x, y0);
-            if (outs > 1) tma_store_2d(&tmOut1, ebuf + 2048, x, y0);
-            if (outs > 2) tma_store_2d(&tmOut2, ebuf + 4096, x, y0);
-            bulk_commit();
-          }
-        } else {
-          __syncwarp();
-#pragma unroll 1
-          for (int o = 0; o < outs; ++o) copy_out(p.out[o], p.ldout[o], ebuf + o * 2048, lane, y0, x, p.T, p.F);
-          __syncwarp();
-        }
-      };
       if constexpr (!BWD) {
         if (!__all_sync(0xffffffffu, mbar_wait(accf_bar(b), aph, abort_flag, p.err, p.wait_limit_ns))) break;
         tc_fence_after_sync();
@@ -387,8 +427,6 @@ __global__ void __launch_bounds__(kGatedThreads, 1)
               h[i] = pack_bf16x2(gate<ACT, false>(__uint_as_float(g[2 * i])).a * __uint_as_float(u[2 * i]),
                                  gate<ACT, false>(__uint_as_float(g[2 * i + 1])).a * __uint_as_float(u[2 * i + 1]));
           });
-          if (lane == 0) bulk_wait_read_all();
-          __syncwarp();
           put_row(ebuf, lane, h);
           if (p.out[1]) {
 #pragma unroll
@@ -398,81 +436,67 @@ __global__ void __launch_bounds__(kGatedThreads, 1)
             for (int i = 0; i < 16; ++i) h[i] = pack_bf16x2(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
             put_row(ebuf + 4096, lane, h);
           }
-          emit(p.out[1] ? 3 : 1, x);
+          __syncwarp();
+          store(p.out[0], p.ldout[0], ebuf, y0, x);
+          if (p.out[1]) {
+            store(p.out[1], p.ldout[1], ebuf + 2048, y0, x);
+            store(p.out[2], p.ldout[2], ebuf + 4096, y0, x);
+          }
+          __syncwarp();
         }
       } else {
         const bool live = y < p.T;
-        const uint16_t *grow = p.gate + (int64_t)y * p.ldgate, *urow = p.up + (int64_t)y * p.ldup;
-        uint32_t ga[16], ua[16];  // the next block's gate and up values
-        if (p.tma) {
-          load_row32(grow, x0, p.F, live, ga);
-          load_row32(urow, x0, p.F, live, ua);
-        }
         if (!__all_sync(0xffffffffu, mbar_wait(accf_bar(b), aph, abort_flag, p.err, p.wait_limit_ns))) break;
         tc_fence_after_sync();
         uint32_t es = 0;  // exponents of the row's blocks
 #pragma unroll 1
         for (int c = 0; c < Cfg::kChunks; ++c) {
           const int x = x0 + c * 32;
-          uint32_t dh[32], g[16], u[16];
-          tmem_ld_32x32b_x32(t0 + c * 32, dh);
-          if (p.tma) {
+          if (y0 >= p.T || x >= p.F) break;
+          uint32_t h[32];  // act(G) U of the block
+          block_arrived();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) g[i] = ga[i], u[i] = ua[i];
-            if (c + 1 < Cfg::kChunks) {
-              load_row32(grow, x + 32, p.F, live, ga);
-              load_row32(urow, x + 32, p.F, live, ua);
-            }
-          }
-          tmem_ld_wait();
-          if (y0 >= p.T || x >= p.F) continue;
-          if (!p.tma) {
-            copy_in(p.gate, p.ldgate, ebuf, lane, y0, x, p.T, p.F);
-            copy_in(p.up, p.ldup, ebuf + 2048, lane, y0, x, p.T, p.F);
-            __syncwarp();
+          for (int k = 0; k < 2; ++k) {
+            uint32_t dh[16], g[8], u[8];
+            tmem_ld_32x32b_x16(t0 + c * 32 + k * 16, dh);
+            get_row16(ebuf, lane, k, g);
+            get_row16(ebuf + 2048, lane, k, u);
+            tmem_ld_wait();
+            with_activation(p.act, [&](auto act) { gate_backward16<decltype(act)::value>(dh, g, u); });
+            put_row16(ebuf, lane, k, g);
+            put_row16(ebuf + 2048, lane, k, u);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint4 a = ld_shared_v4(block_chunk(ebuf, lane, j)), d = ld_shared_v4(block_chunk(ebuf + 2048, lane, j));
-              g[4 * j] = a.x, g[4 * j + 1] = a.y, g[4 * j + 2] = a.z, g[4 * j + 3] = a.w;
-              u[4 * j] = d.x, u[4 * j + 1] = d.y, u[4 * j + 2] = d.z, u[4 * j + 3] = d.w;
-            }
+            for (int i = 0; i < 16; ++i) h[16 * k + i] = dh[i];
           }
-          with_activation(p.act, [&](auto act) { gate_backward32<decltype(act)::value>(dh, g, u); });
-          if (lane == 0) bulk_wait_read_all();
           __syncwarp();
-          put_row(ebuf, lane, g);
-          put_row(ebuf + 2048, lane, u);
-          emit(2, x);
+          store(p.out[0], p.ldout[0], ebuf, y0, x);
+          store(p.out[1], p.ldout[1], ebuf + 2048, y0, x);
+          __syncwarp();
+          ask();  // into the block just stored
           if (p.ck.q) {
             uint32_t q[8];
-            es |= q8_block32(dh, q) << (8 * c);
-            if (p.q_vec && x + 32 <= p.F) {
-              if (live) store_32_bytes(p.ck.q + (int64_t)y * p.ck.ldq + x, q);
-            } else {
-              // along rows, through the block that dG just left
-              if (lane == 0) bulk_wait_read_all();
-              __syncwarp();
-              st_shared_v4(ebuf + lane * 32, q[0], q[1], q[2], q[3]);
-              st_shared_v4(ebuf + lane * 32 + 16, q[4], q[5], q[6], q[7]);
-              __syncwarp();
-              if (x + lane < p.F) {
-                const int rows = min(32, p.T - y0);
-#pragma unroll 8
-                for (int i = 0; i < rows; ++i)
-                  p.ck.q[(int64_t)(y0 + i) * p.ck.ldq + x + lane] = (int8_t)ld_shared_u8(ebuf + i * 32 + lane);
+            es |= q8_block32(h, q) << (8 * c);
+            if (live) {
+              int8_t *to = p.ck.q + (int64_t)y * p.ck.ldq + x;
+              if (p.q_vec && x + 32 <= p.F) {
+                store_32_bytes(to, q);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (x + i < p.F) to[i] = (int8_t)(q[i / 4] >> (8 * (i & 3)));
               }
-              __syncwarp();
             }
           }
         }
         if (p.ck.q && live) {
           uint8_t *e = p.ck.e + (int64_t)y * p.ck.lde + (x0 >> 5);
-          const int n = min(Cfg::kChunks, (p.F - x0 + 31) >> 5);  // blocks that exist (may be below 1)
-          if (Cfg::kChunks == 4 && n == 4 && (reinterpret_cast<uintptr_t>(e) & 3) == 0) {
+          constexpr int kMost = Cfg::kChunks;
+          const int n = min(kMost, (p.F - x0 + 31) >> 5);  // blocks that exist (may be below 1)
+          if (kMost == 4 && n == 4 && (reinterpret_cast<uintptr_t>(e) & 3) == 0) {
             *reinterpret_cast<uint32_t *>(e) = es;
           } else {
 #pragma unroll
-            for (int i = 0; i < Cfg::kChunks; ++i)
+            for (int i = 0; i < kMost; ++i)
               if (i < n) e[i] = (uint8_t)(es >> (8 * i));
           }
         }
@@ -484,7 +508,7 @@ __global__ void __launch_bounds__(kGatedThreads, 1)
         mbar_arrive(acce_bar(b));
       ++acc_cnt;
     }
-    if (lane == 0) bulk_wait_all();  // this warp's TMA stores have landed
+    block_arrived();  // a block asked for and not taken (after giving up only) has landed
   }
 
   griddep_launch_dependents();

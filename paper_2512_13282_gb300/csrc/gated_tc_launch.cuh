@@ -12,8 +12,8 @@ cudaError_t launch_gated_kernel(const GatedMaps &m, const GatedTcParams &p, int 
   static std::atomic<uint64_t> allowed{0};
   const cudaError_t e = allow_shared_memory((const void *)kern, Cfg::kSmemBytes, allowed);
   if (e != cudaSuccess) return e;
-  return launch_ex(kern, dim3((unsigned)grid), dim3(kGatedThreads), Cfg::kSmemBytes, st, PAIR ? 2 : 1, m.a, m.b[0],
-                   m.b[1], m.out[0], m.out[1], m.out[2], p);
+  return launch_ex(kern, dim3((unsigned)grid), dim3(Cfg::kThreads), Cfg::kSmemBytes, st, PAIR ? 2 : 1, m.a, m.b[0],
+                   m.b[1], p);
 }
 
 }  // namespace gb300

@@ -163,7 +163,7 @@ cudaError_t stage(Operand &o, uint8_t *&at, const OpContext &c) {
 }
 
 // Stages the n operands (the first is A, the others weights of layout km),
-// makes their maps and the outputs', and launches.
+// makes their maps, and launches.
 gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool forward, GatedTcParams &p,
                         const OpContext &c) {
   const bool few = forward && p.T <= kFewTokens;
@@ -196,19 +196,9 @@ gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool fo
     count_launches(1);
     return launch_gated_few(km, m, p, c.sms, c.st) == cudaSuccess ? GEMM_OK : GEMM_ERR_CUDA;
   }
-  // outputs through TMA where their rows are whole 16-byte pieces (a clipped
-  // store would write into a row's padding), and G and U, read in such pieces
-  // then, likewise
-  p.tma = tma_store_enabled() && p.F % 8 == 0;
+  p.vec = p.F % 8 == 0 && (!p.gate || (rows_on(p.gate, p.ldgate, 2, 16) && rows_on(p.up, p.ldup, 2, 16)));
   for (int i = 0; i < 3; ++i)
-    if (p.out[i]) p.tma = p.tma && rows_on(p.out[i], p.ldout[i], 2, 16);
-  if (p.gate) p.tma = p.tma && rows_on(p.gate, p.ldgate, 2, 16) && rows_on(p.up, p.ldup, 2, 16);
-  for (int i = 0; i < 3; ++i) {
-    m.out[i] = m.a;
-    if (p.tma && p.out[i] &&
-        !float_out_map(&m.out[i], true, p.out[i], (uint64_t)p.F, (uint64_t)p.T, (uint64_t)p.ldout[i], 1))
-      return GEMM_ERR_CUDA;
-  }
+    if (p.out[i]) p.vec = p.vec && rows_on(p.out[i], p.ldout[i], 2, 16);
   p.tiles_m = pl.tiles_m;
   p.tiles_n = pl.tiles_n;
   p.group_m = 8;

@@ -160,14 +160,14 @@ struct GatedTcParams {
   int tiles_m, tiles_n, num_kb, group_m;
   int act;
   // forward: out[0] = H, out[1], out[2] = G, U or null; backward: out[0], out[1]
-  // = dG, dU.  tma: they go through tensor maps, and gate / up are read in
-  // 16-byte pieces; else element by element.
+  // = dG, dU.  vec: their rows, and gate's and up's, start on 16 bytes and are
+  // whole 16-byte pieces.
   uint16_t *out[3];
   int64_t ldout[3];
-  int tma;
+  int vec;
   const uint16_t *gate, *up;  // backward: G, U
   int64_t ldgate, ldup;
-  Q8Ref ck;   // backward: or ck.q null
+  Q8Ref ck;     // backward: or ck.q null
   int q_vec;  // its rows start on 16 bytes
   uint32_t *err;
   uint64_t wait_limit_ns;
@@ -178,10 +178,9 @@ struct GatedTile {
   bool pair;  // a CTA pair per 256-row tile, or one CTA per 128-row tile
   int bn;     // 256 (pair), 128, or 64 (backward)
 };
-// Tensor maps: X or dO; Wg and Wu, or Wd; the outputs (any valid map where a
-// kernel does not use one).
+// Tensor maps: X or dO; Wg and Wu, or Wd twice.
 struct GatedMaps {
-  CUtensorMap a, b[2], out[3];
+  CUtensorMap a, b[2];
 };
 cudaError_t launch_gated_tc_fwd(const GatedTile &tile, bool km, const GatedMaps &m, const GatedTcParams &p, int grid,
                                 cudaStream_t st);
