@@ -88,6 +88,12 @@ __device__ __forceinline__ uint16_t ld_shared_u16(uint32_t addr) {
   return v;
 }
 
+__device__ __forceinline__ uint32_t ld_shared_u8(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
 // The block at (y0, x) between memory and shared memory, along rows: a lane's
 // own row would be 32 lines touched by every access.  By the warps and not by
 // TMA, whose engine the operands keep busy: blocks through it stretched a
@@ -122,18 +128,23 @@ __device__ __forceinline__ void block_store(uint16_t *m, int64_t ld, uint32_t bu
     if (y0 + row < T && c < F) *reinterpret_cast<uint4 *>(m + (int64_t)(y0 + row) * ld + c) = v;
   }
 }
-// Any alignment: element by element, lane = column.
-__device__ __forceinline__ void block_fetch_any(const uint16_t *m, int64_t ld, uint32_t buf, int lane, int y0, int x,
-                                                int T, int F) {
-  const int c = x + lane, rows = min(32, T - y0);
-  m += (int64_t)y0 * ld + c;
-#pragma unroll 1
-  for (int r = 0; r < 32; r += 16, m += 16 * ld) {
-    uint16_t v[16];
+// Any alignment: element by element, lane = column; both matrices in one batch
+// of loads.
+__device__ __forceinline__ void block_fetch_any(const uint16_t *m0, int64_t ld0, const uint16_t *m1, int64_t ld1,
+                                                uint32_t buf0, uint32_t buf1, int lane, int y0, int x, int T, int F) {
+  const int c = x + lane, rows = c < F ? min(32, T - y0) : 0;
+  m0 += (int64_t)y0 * ld0 + c;
+  m1 += (int64_t)y0 * ld1 + c;
+  uint16_t v[32], w[32];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = c < F && r + i < rows ? m[i * ld] : (uint16_t)0;
+  for (int i = 0; i < 32; ++i, m0 += ld0, m1 += ld1) {
+    v[i] = i < rows ? *m0 : (uint16_t)0;
+    w[i] = i < rows ? *m1 : (uint16_t)0;
+  }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) st_shared_u16(block_element(buf, r + i, lane), v[i]);
+  for (int i = 0; i < 32; ++i) {
+    st_shared_u16(block_element(buf0, i, lane), v[i]);
+    st_shared_u16(block_element(buf1, i, lane), w[i]);
   }
 }
 __device__ __forceinline__ void block_store_any(uint16_t *m, int64_t ld, uint32_t buf, int lane, int y0, int x, int T,
@@ -186,6 +197,40 @@ __device__ __forceinline__ uint32_t q8_block32(const uint32_t (&h)[32], uint32_t
   return e;
 }
 
+// Work unit u -> tile, k-blocks, and whether its sums are partial ones.
+struct GatedUnit {
+  int tm, tn, kb0, kb1, split, slot;
+  bool part;
+};
+__device__ __forceinline__ int gated_units(const GatedTcParams &p) {
+  const int tiles = p.tiles_m * p.tiles_n;
+  return p.tail_splits > 0 ? p.tail_first + (tiles - p.tail_first) * p.tail_splits : tiles;
+}
+__device__ __forceinline__ GatedUnit gated_unit(const GatedTcParams &p, int u) {
+  GatedUnit w{0, 0, 0, p.num_kb, 0, 0, false};
+  if (p.tail_splits > 0 && u >= p.tail_first) {
+    const int tail = p.tiles_m * p.tiles_n - p.tail_first, v = u - p.tail_first;
+    w.part = true;
+    w.split = v / tail;
+    w.slot = v - w.split * tail;
+    w.kb0 = w.split * p.tail_kb_per;
+    w.kb1 = min(p.num_kb, w.kb0 + p.tail_kb_per);
+    u = p.tail_first + w.slot;
+  }
+  raster_tile(u, p.tiles_m, p.tiles_n, p.group_m, &w.tm, &w.tn);
+  return w;
+}
+
+// A lane's 32 sums to its row of a partial block (128 bytes, a whole line).
+__device__ __forceinline__ void store_partials(float *at, const uint32_t (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t w[8] = {v[8 * j],     v[8 * j + 1], v[8 * j + 2], v[8 * j + 3],
+                           v[8 * j + 4], v[8 * j + 5], v[8 * j + 6], v[8 * j + 7]};
+    store_32_bytes(at + 8 * j, w);
+  }
+}
+
 template <int BN, bool PAIR, bool KM, bool BWD>
 __global__ void __launch_bounds__(GatedCfg<BN, PAIR, BWD>::kThreads, 1)
     gated_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB0,
@@ -212,8 +257,8 @@ __global__ void __launch_bounds__(GatedCfg<BN, PAIR, BWD>::kThreads, 1)
   const int lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
   const bool leader = rank == 0;
-  const int first_tile = PAIR ? blockIdx.x >> 1 : blockIdx.x;
-  const int tile_step = PAIR ? gridDim.x >> 1 : gridDim.x;
+  const int first_unit = PAIR ? blockIdx.x >> 1 : blockIdx.x;
+  const int unit_step = PAIR ? gridDim.x >> 1 : gridDim.x;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -249,7 +294,7 @@ __global__ void __launch_bounds__(GatedCfg<BN, PAIR, BWD>::kThreads, 1)
   // kernel of the stream.
   griddep_wait();
 
-  const int num_tiles = p.tiles_m * p.tiles_n;
+  const int num_units = gated_units(p);
   constexpr uint64_t kDrainNs = 200ull * 1000 * 1000;
 
   if (warp == 0) {
@@ -257,11 +302,10 @@ __global__ void __launch_bounds__(GatedCfg<BN, PAIR, BWD>::kThreads, 1)
     if (lane == 0) {
       uint32_t g = 0;
       bool ok = true;
-      for (int t = first_tile; ok && t < num_tiles; t += tile_step) {
-        int tm, tn;
-        raster_tile(t, p.tiles_m, p.tiles_n, p.group_m, &tm, &tn);
-        const int m0 = tm * Cfg::kTileM + (int)rank * kBM;
-        for (int kb = 0; kb < p.num_kb; ++kb) {
+      for (int t = first_unit; ok && t < num_units; t += unit_step) {
+        const GatedUnit w = gated_unit(p, t);
+        const int m0 = w.tm * Cfg::kTileM + (int)rank * kBM;
+        for (int kb = w.kb0; kb < w.kb1; ++kb) {
           const uint32_t s = g % STAGES, ph = (g / STAGES) & 1u;
           if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.err, p.wait_limit_ns)) {
             ok = false;
@@ -286,7 +330,7 @@ __global__ void __launch_bounds__(GatedCfg<BN, PAIR, BWD>::kThreads, 1)
             }
           };
           const uint32_t b_dst = sB + s * Cfg::kBBytes;
-          const int f0 = tn * Cfg::kTileF;
+          const int f0 = w.tn * Cfg::kTileF;
           if constexpr (BWD) {
             load_b(b_dst, &tmB0, f0 + (int)rank * Cfg::kCtaN);
           } else if constexpr (PAIR) {
@@ -312,7 +356,8 @@ __global__ void __launch_bounds__(GatedCfg<BN, PAIR, BWD>::kThreads, 1)
       constexpr uint32_t idesc = idesc_bf16_f32(Cfg::kTileM, BN, !KM);
       uint32_t g = 0, acc_cnt = 0;
       bool ok = true;
-      for (int t = first_tile; ok && t < num_tiles; t += tile_step) {
+      for (int t = first_unit; ok && t < num_units; t += unit_step) {
+        const GatedUnit w = gated_unit(p, t);
         const uint32_t b = acc_cnt & 1u, aph = (acc_cnt >> 1) & 1u;
         if (!mbar_wait(acce_bar(b), aph ^ 1u, abort_flag, p.err, p.wait_limit_ns)) {
           ok = false;
@@ -320,7 +365,7 @@ __global__ void __launch_bounds__(GatedCfg<BN, PAIR, BWD>::kThreads, 1)
         }
         tc_fence_after_sync();
         const uint32_t d_tmem = tmem_base + b * BN;
-        for (int kb = 0; kb < p.num_kb; ++kb) {
+        for (int kb = w.kb0; kb < w.kb1; ++kb) {
           const uint32_t s = g % STAGES, ph = (g / STAGES) & 1u;
           if (!mbar_wait(full_bar(s), ph, abort_flag, p.err, p.wait_limit_ns)) {
             ok = false;
@@ -334,7 +379,7 @@ __global__ void __launch_bounds__(GatedCfg<BN, PAIR, BWD>::kThreads, 1)
             const uint64_t ad = smem_desc_sw128(a0 + k * 32, 16, 1024);
             const uint64_t bd = KM ? smem_desc_sw128(b0 + k * 32, 16, 1024)
                                    : smem_desc_sw128(b0 + k * 2048, kBK * 128, 1024);
-            const uint32_t acc = (kb > 0 || k > 0) ? 1u : 0u;
+            const uint32_t acc = (kb > w.kb0 || k > 0) ? 1u : 0u;
             if constexpr (PAIR)
               tc_mma_bf16_pair(d_tmem, ad, bd, idesc, acc);
             else
@@ -376,42 +421,52 @@ __global__ void __launch_bounds__(GatedCfg<BN, PAIR, BWD>::kThreads, 1)
     };
     // backward: blocks of G and U are asked for in the order in which they are
     // taken, those that exist; next_t, next_c: the next one
-    int next_t = first_tile, next_c = 0;
+    int next_t = first_unit, next_c = 0;
     const auto ask = [&]() {
-      while (next_t < num_tiles) {
-        int tm, tn;
-        raster_tile(next_t, p.tiles_m, p.tiles_n, p.group_m, &tm, &tn);
-        const int y = tm * Cfg::kTileM + (int)rank * kBM + quad * 32;
-        const int x = tn * Cfg::kTileF + (colpart * Cfg::kChunks + next_c) * 32;
-        const bool here = y < p.T && x < p.F;
+      while (next_t < num_units) {
+        const GatedUnit w = gated_unit(p, next_t);
+        const int y = w.tm * Cfg::kTileM + (int)rank * kBM + quad * 32;
+        const int x = w.tn * Cfg::kTileF + (colpart * Cfg::kChunks + next_c) * 32;
+        const bool here = !w.part && y < p.T && x < p.F;
         if (++next_c == Cfg::kChunks || !here) {
           next_c = 0;
-          next_t += tile_step;
+          next_t += unit_step;
         }
         if (!here) continue;
         if (p.vec) {
           block_fetch(p.gate, p.ldgate, ebuf, lane, y, x, p.T, p.F);
           block_fetch(p.up, p.ldup, ebuf + 2048, lane, y, x, p.T, p.F);
         } else {
-          block_fetch_any(p.gate, p.ldgate, ebuf, lane, y, x, p.T, p.F);
-          block_fetch_any(p.up, p.ldup, ebuf + 2048, lane, y, x, p.T, p.F);
+          block_fetch_any(p.gate, p.ldgate, p.up, p.ldup, ebuf, ebuf + 2048, lane, y, x, p.T, p.F);
         }
         return;
       }
     };
     if (BWD) ask();
-    for (int t = first_tile; t < num_tiles; t += tile_step) {
-      int tm, tn;
-      raster_tile(t, p.tiles_m, p.tiles_n, p.group_m, &tm, &tn);
-      const int y0 = tm * Cfg::kTileM + (int)rank * kBM + quad * 32;  // first row of this warp
+    for (int t = first_unit; t < num_units; t += unit_step) {
+      const GatedUnit w = gated_unit(p, t);
+      const int y0 = w.tm * Cfg::kTileM + (int)rank * kBM + quad * 32;  // first row of this warp
       const int y = y0 + lane;
       const int col0 = colpart * (Cfg::kChunks * 32);
-      const int x0 = tn * Cfg::kTileF + col0;
+      const int x0 = w.tn * Cfg::kTileF + col0;
       const uint32_t b = acc_cnt & 1u, aph = (acc_cnt >> 1) & 1u;
       const uint32_t t0 = tmem_base + b * BN + ((uint32_t)(quad * 32) << 16) + col0;
-      if constexpr (!BWD) {
-        if (!__all_sync(0xffffffffu, mbar_wait(accf_bar(b), aph, abort_flag, p.err, p.wait_limit_ns))) break;
-        tc_fence_after_sync();
+      if (!__all_sync(0xffffffffu, mbar_wait(accf_bar(b), aph, abort_flag, p.err, p.wait_limit_ns))) break;
+      tc_fence_after_sync();
+      if (w.part) {
+        // all BN columns, as they are
+        constexpr int kCols = BN / (Cfg::kEpiWarps / 4);
+        const int64_t tail_rows = (int64_t)(p.tiles_m * p.tiles_n - p.tail_first) * Cfg::kTileM;
+        const int row = w.slot * Cfg::kTileM + (int)rank * kBM + quad * 32 + lane;
+        float *at = p.ws + (w.split * tail_rows + row) * BN + colpart * kCols;
+#pragma unroll 1
+        for (int c = 0; c < kCols; c += 32) {
+          uint32_t v[32];
+          tmem_ld_32x32b_x32(t0 - col0 + colpart * kCols + c, v);
+          tmem_ld_wait();
+          store_partials(at + c, v);
+        }
+      } else if constexpr (!BWD) {
 #pragma unroll 1
         for (int c = 0; c < Cfg::kChunks; ++c) {
           const int x = x0 + c * 32;
@@ -446,8 +501,6 @@ __global__ void __launch_bounds__(GatedCfg<BN, PAIR, BWD>::kThreads, 1)
         }
       } else {
         const bool live = y < p.T;
-        if (!__all_sync(0xffffffffu, mbar_wait(accf_bar(b), aph, abort_flag, p.err, p.wait_limit_ns))) break;
-        tc_fence_after_sync();
         uint32_t es = 0;  // exponents of the row's blocks
 #pragma unroll 1
         for (int c = 0; c < Cfg::kChunks; ++c) {
@@ -472,19 +525,31 @@ __global__ void __launch_bounds__(GatedCfg<BN, PAIR, BWD>::kThreads, 1)
           store(p.out[0], p.ldout[0], ebuf, y0, x);
           store(p.out[1], p.ldout[1], ebuf + 2048, y0, x);
           __syncwarp();
-          ask();  // into the block just stored
+          const bool q_bytes = p.ck.q && !(p.vec && p.q_align >= 8);
+          if (!q_bytes) ask();  // into the block just stored
           if (p.ck.q) {
             uint32_t q[8];
             es |= q8_block32(h, q) << (8 * c);
-            if (live) {
-              int8_t *to = p.ck.q + (int64_t)y * p.ck.ldq + x;
-              if (p.q_vec && x + 32 <= p.F) {
-                store_32_bytes(to, q);
-              } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                  if (x + i < p.F) to[i] = (int8_t)(q[i / 4] >> (8 * (i & 3)));
+            int8_t *to = p.ck.q + (int64_t)y * p.ck.ldq + x;
+            if (q_bytes) {
+              // byte by byte along rows, through the block just stored
+              st_shared_v4(ebuf + lane * 32, q[0], q[1], q[2], q[3]);
+              st_shared_v4(ebuf + lane * 32 + 16, q[4], q[5], q[6], q[7]);
+              __syncwarp();
+              if (x + lane < p.F) {
+                const int rows = min(32, p.T - y0);
+                int8_t *col = p.ck.q + (int64_t)y0 * p.ck.ldq + x + lane;
+#pragma unroll 8
+                for (int i = 0; i < rows; ++i, col += p.ck.ldq) *col = (int8_t)ld_shared_u8(ebuf + i * 32 + lane);
               }
+              __syncwarp();
+              ask();
+            } else if (p.q_align == 16 && x + 32 <= p.F) {
+              if (live) store_32_bytes(to, q);
+            } else {  // F is a multiple of 8
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (live && x + 8 * j < p.F) *reinterpret_cast<uint2 *>(to + 8 * j) = make_uint2(q[2 * j], q[2 * j + 1]);
             }
           }
         }

@@ -108,19 +108,28 @@ auto backward_kernel(int act) {
 
 // --------------------------------------------- with a product: tiles, staging
 
-// Modelled cost of a tile shape: microseconds per k-block of 64 and per tile
-// besides.
+// Modelled cost of a tile shape: microseconds per k-block of 64, per unit
+// besides, and of the last unit's epilogue, which nothing hides.
 struct TileCost {
   GatedTile tile;
-  double kb_us, tile_us;
+  double kb_us, unit_us, last_us;
 };
-constexpr TileCost kForwardTiles[] = {{{true, 256}, 0.36, 2.0}, {{false, 128}, 0.33, 1.2}};
-constexpr TileCost kBackwardTiles[] = {{{true, 256}, 0.36, 3.0}, {{false, 128}, 0.33, 2.0}, {{false, 64}, 0.30, 1.5}};
+constexpr TileCost kForwardTiles[] = {{{true, 256}, 0.345, 0.5, 5.0}, {{false, 128}, 0.31, 0.5, 3.0}};
+constexpr TileCost kBackwardTiles[] = {
+    {{true, 256}, 0.345, 4.0, 12.0}, {{false, 128}, 0.31, 2.0, 6.0}, {{false, 64}, 0.28, 1.5, 4.0}};
+// A split tail's reduction: its launch, and the partials written and read.
+constexpr double kTailFixedUs = 3.5, kTailUsPerMB = 0.36;
 
 struct GatedPlan {
   GatedTile tile;
-  int tiles_m, tiles_n, grid;
+  int tiles_m, tiles_n, num_kb, grid;
+  int tail_first, tail_splits, tail_kb_per;
+  int tile_m() const { return tile.pair ? 2 * kBM : kBM; }
+  size_t partial_bytes() const {
+    return (size_t)tail_splits * ((size_t)tiles_m * tiles_n - tail_first) * tile_m() * tile.bn * 4;
+  }
 };
+// Tile shape, split tail and grid of the least modelled time.
 template <size_t N>
 GatedPlan plan_gated(const TileCost (&tiles)[N], int64_t T, int64_t K, int64_t F, bool forward, int sms, int pairs) {
   GatedPlan best{};
@@ -129,21 +138,39 @@ GatedPlan plan_gated(const TileCost (&tiles)[N], int64_t T, int64_t K, int64_t F
   for (const TileCost &c : tiles) {
     const int64_t slots = c.tile.pair ? pairs : sms;
     if (slots <= 0) continue;
-    const int64_t tm = ceil_div64(T, c.tile.pair ? 2 * kBM : kBM), tn = ceil_div64(F, forward ? c.tile.bn / 2 : c.tile.bn);
-    const int64_t rounds = ceil_div64(tm * tn, slots);
-    const double us = rounds * (num_kb * c.kb_us + c.tile_us);
-    if (best_us >= 0 && us >= best_us) continue;
-    best_us = us;
-    best.tile = c.tile;
-    best.tiles_m = (int)tm;
-    best.tiles_n = (int)tn;
-    best.grid = (int)(tm * tn < slots ? tm * tn : slots) * (c.tile.pair ? 2 : 1);
+    const int tile_m = c.tile.pair ? 2 * kBM : kBM;
+    const int64_t tm = ceil_div64(T, tile_m), tn = ceil_div64(F, forward ? c.tile.bn / 2 : c.tile.bn), all = tm * tn;
+    const int64_t full = all / slots, rem = all % slots;
+    const double whole = num_kb * c.kb_us + c.unit_us;
+    for (int64_t s = 1; s <= 16; ++s) {
+      int64_t kb_per = num_kb, parts = 1;
+      if (s > 1) {
+        if (rem == 0 || rem * s > slots) break;
+        kb_per = ceil_div64(num_kb, s);
+        parts = ceil_div64(num_kb, kb_per);  // no part is empty
+        if (parts != s || kb_per < 4) continue;
+      }
+      double us = full * whole;
+      if (rem > 0) us += kb_per * c.kb_us + c.unit_us;
+      us += parts > 1 ? kTailFixedUs + kTailUsPerMB * (double)parts * rem * tile_m * c.tile.bn * 4e-6 : c.last_us;
+      if (best_us >= 0 && us >= best_us) continue;
+      best_us = us;
+      best.tile = c.tile;
+      best.tiles_m = (int)tm;
+      best.tiles_n = (int)tn;
+      best.num_kb = (int)num_kb;
+      best.tail_first = parts > 1 ? (int)(full * slots) : 0;
+      best.tail_splits = parts > 1 ? (int)parts : 0;
+      best.tail_kb_per = parts > 1 ? (int)kb_per : 0;
+      const int64_t units = parts > 1 ? full * slots + rem * parts : all;
+      best.grid = (int)(units < slots ? units : slots) * (c.tile.pair ? 2 : 1);
+    }
   }
   return best;
 }
 
 // An operand as TMA can read it: as it is, or (rows off 16 bytes) copied into
-// the stream's scratch at `at`.
+// the stream's scratch.
 struct Operand {
   const uint16_t *p;
   int64_t rows, cols, ld;
@@ -151,33 +178,74 @@ struct Operand {
   int64_t packed_ld() const { return (cols + 7) / 8 * 8; }
   size_t bytes() const { return pack() ? align256((size_t)rows * packed_ld() * 2) : 0; }
 };
-cudaError_t stage(Operand &o, uint8_t *&at, const OpContext &c) {
-  if (!o.pack()) return cudaSuccess;
-  uint16_t *dst = reinterpret_cast<uint16_t *>(at);
-  at += o.bytes();
+
+// The copies of up to three operands in one launch: a thread writes eight
+// values (16 bytes), read in the 16-byte pieces of memory that they lie in.
+struct PackJobs {
+  struct {
+    const uint16_t *src;
+    uint16_t *dst;
+    int64_t rows, cols, ld, ld_dst;
+  } job[3];
+  int jobs;
+};
+__global__ void __launch_bounds__(kThreads) gated_pack_kernel(const PackJobs j, int64_t items) {
+  griddep_launch_dependents();
+  griddep_wait();
+  for (int64_t t0 = (int64_t)blockIdx.x * kThreads + threadIdx.x; t0 < items; t0 += (int64_t)gridDim.x * kThreads) {
+    int64_t t = t0;
+    int i = 0;
+    for (; i + 1 < j.jobs; ++i) {
+      const int64_t n = j.job[i].rows * (j.job[i].ld_dst / 8);
+      if (t < n) break;
+      t -= n;
+    }
+    const auto &o = j.job[i];
+    const int64_t per = o.ld_dst / 8;
+    const int64_t r = t <= 0xFFFFFFFFll ? (int64_t)((uint32_t)t / (uint32_t)per) : t / per, c = (t - r * per) * 8;
+    const uint16_t *row = o.src + r * o.ld;
+    Chunk<bf16, 8> v;
+    if (c + 8 <= o.cols)
+      load_half(row + c, c == 0, (o.cols - c - 8) * 2, v.w);
+    else
+      v.load_part(row, c, (int)(o.cols - c));
+    *reinterpret_cast<uint4 *>(o.dst + r * o.ld_dst + c) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+  }
+}
+cudaError_t pack_operands(Operand *o, int n, uint8_t *at, const OpContext &c) {
+  PackJobs j{};
+  int64_t items = 0;
+  for (int i = 0; i < n; ++i) {
+    if (!o[i].pack()) continue;
+    uint16_t *dst = reinterpret_cast<uint16_t *>(at);
+    at += o[i].bytes();
+    j.job[j.jobs++] = {o[i].p, dst, o[i].rows, o[i].cols, o[i].ld, o[i].packed_ld()};
+    items += o[i].rows * (o[i].packed_ld() / 8);
+    o[i].ld = o[i].packed_ld();
+    o[i].p = dst;
+  }
+  if (j.jobs == 0) return cudaSuccess;
   count_launches(1);
-  const cudaError_t e = launch_pack_u16(o.p, o.rows, o.cols, o.ld, dst, o.packed_ld(), c.sms, c.st);
-  o.ld = o.packed_ld();
-  o.p = dst;
-  return e;
+  const int64_t blocks = ceil_div64(items, kThreads);
+  return launch_ex(gated_pack_kernel, dim3((unsigned)(blocks < (1 << 30) ? blocks : (1 << 30))), dim3(kThreads), 0, c.st,
+                   1, j, items);
 }
 
-// Stages the n operands (the first is A, the others weights of layout km),
-// makes their maps, and launches.
+// Packs what has to be of the n operands (the first is A, the others weights of
+// layout km), makes their maps, and launches.
 gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool forward, GatedTcParams &p,
                         const OpContext &c) {
   const bool few = forward && p.T <= kFewTokens;
   if (pl.grid <= 0) return GEMM_ERR_CUDA;
-  size_t need = 0;
-  for (int i = 0; i < n; ++i) need += o[i].bytes();
+  size_t packed = 0;
+  for (int i = 0; i < n; ++i) packed += o[i].bytes();
+  const size_t need = packed + (few ? 0 : pl.partial_bytes());
   void *ws = nullptr;
   if (need) {
     const gemm_status_t s = op_workspace(need, c.st, &ws);
     if (s != GEMM_OK) return s;
   }
-  uint8_t *at = static_cast<uint8_t *>(ws);
-  for (int i = 0; i < n; ++i)
-    if (stage(o[i], at, c) != cudaSuccess) return GEMM_ERR_CUDA;
+  if (pack_operands(o, n, static_cast<uint8_t *>(ws), c) != cudaSuccess) return GEMM_ERR_CUDA;
   GatedMaps m;
   if (!bf16_box_map(&m.a, o[0].p, (uint64_t)o[0].cols, (uint64_t)o[0].rows, (uint64_t)o[0].ld, kBK,
                     few ? (uint32_t)gated_few_columns(p.T) : kBM))
@@ -189,7 +257,7 @@ gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool fo
                       km ? part : kBK))
       return GEMM_ERR_CUDA;
   if (n < 3) m.b[1] = m.b[0];
-  p.num_kb = (int)ceil_div64(p.K, kBK);
+  p.num_kb = pl.num_kb;
   p.err = c.err;
   p.wait_limit_ns = c.wait_limit_ns;
   if (few) {
@@ -199,14 +267,23 @@ gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool fo
   p.vec = p.F % 8 == 0 && (!p.gate || (rows_on(p.gate, p.ldgate, 2, 16) && rows_on(p.up, p.ldup, 2, 16)));
   for (int i = 0; i < 3; ++i)
     if (p.out[i]) p.vec = p.vec && rows_on(p.out[i], p.ldout[i], 2, 16);
+  p.q_align = !p.ck.q ? 1 : rows_on(p.ck.q, p.ck.ldq, 1, 16) ? 16 : rows_on(p.ck.q, p.ck.ldq, 1, 8) ? 8 : 1;
   p.tiles_m = pl.tiles_m;
   p.tiles_n = pl.tiles_n;
   p.group_m = 8;
-  p.q_vec = p.ck.q && rows_on(p.ck.q, p.ck.ldq, 1, 16);
+  p.tail_first = pl.tail_first;
+  p.tail_splits = pl.tail_splits;
+  p.tail_kb_per = pl.tail_kb_per;
+  p.ws = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + packed);
   count_launches(1);
   const cudaError_t e = forward ? launch_gated_tc_fwd(pl.tile, km, m, p, pl.grid, c.st)
                                 : launch_gated_tc_bwd(pl.tile, km, m, p, pl.grid, c.st);
-  return e == cudaSuccess ? GEMM_OK : GEMM_ERR_CUDA;
+  if (e != cudaSuccess) return GEMM_ERR_CUDA;
+  if (pl.tail_splits > 0) {
+    count_launches(1);
+    if (launch_gated_tail(pl.tile, forward, p, c.st) != cudaSuccess) return GEMM_ERR_CUDA;
+  }
+  return GEMM_OK;
 }
 
 }  // namespace

@@ -158,6 +158,12 @@ gemm_status_t gated_down_backward(const GatedDownBackward &p, const OpContext &c
 struct GatedTcParams {
   int T, F, K;  // rows, features, reduction length
   int tiles_m, tiles_n, num_kb, group_m;
+  // split tail, as in TcParams: the tiles from raster position tail_first on are
+  // split into tail_splits (0: none) ranges of tail_kb_per k-blocks, whose sums
+  // go to ws (float32): plane s has tile i's block of tile rows x bn words at row
+  // i * tile rows, pitch bn
+  int tail_first, tail_splits, tail_kb_per;
+  float *ws;
   int act;
   // forward: out[0] = H, out[1], out[2] = G, U or null; backward: out[0], out[1]
   // = dG, dU.  vec: their rows, and gate's and up's, start on 16 bytes and are
@@ -168,7 +174,7 @@ struct GatedTcParams {
   const uint16_t *gate, *up;  // backward: G, U
   int64_t ldgate, ldup;
   Q8Ref ck;     // backward: or ck.q null
-  int q_vec;  // its rows start on 16 bytes
+  int q_align;  // its rows start on 16 or 8 bytes, or (1) anywhere
   uint32_t *err;
   uint64_t wait_limit_ns;
 };
@@ -191,6 +197,9 @@ int gated_few_columns(int64_t T);
 cudaError_t launch_gated_few(bool km, const GatedMaps &m, const GatedTcParams &p, int sms, cudaStream_t st);
 cudaError_t launch_gated_tc_bwd(const GatedTile &tile, bool km, const GatedMaps &m, const GatedTcParams &p, int grid,
                                 cudaStream_t st);
+// The split tail's tiles: partial sums added in split order, then as the kernel
+// does (gated_tail.cu).
+cudaError_t launch_gated_tail(const GatedTile &tile, bool forward, const GatedTcParams &p, cudaStream_t st);
 
 // Dropout (layer_dropout.cu), forward or backward (without a residual).
 struct Dropout {
