@@ -1,13 +1,15 @@
-// gated_few.cu -- the gated feed-forward block's projections for few tokens (a
-// batch of sequences a token each): H = act(X Wg) * (X Wu), T <= 128.
+// gated_few.cu -- the gated feed-forward block for few tokens (a batch of
+// sequences a token each), T <= 64: H = act(X Wg) * (X Wu), and the gate's
+// gradient from dH = dO Wd^T.
 //
-// The weights' bytes bound it (4 K F, read once), so the tile is turned round:
-// the tensor core's 128 rows are 64 gate and the same 64 up features, streamed
-// by TMA in either layout of the weights, and its columns are the tokens, 16 to
-// 128 of them.  A cluster of up to eight CTAs shares a tile's reduction, so that
-// a layer with few tiles still fills the device; their sums meet in distributed
-// shared memory, added in the order of the CTAs, and the gate is taken there:
-// one launch, no scratch, no atomics.
+// The weights' bytes bound both (4 K F or 2 N F, read once), so the tile is
+// turned round: the tensor core's 128 rows are features -- 64 gate and the same
+// 64 up features, or 128 of Wd's -- streamed by TMA in either layout of the
+// weights, and its columns are the tokens, 16 to 64 of them.  A cluster of up
+// to eight CTAs shares a tile's reduction, so that a layer with few tiles still
+// fills the device; their sums meet in distributed shared memory, added in the
+// order of the CTAs, and the gate or its gradient is taken there: one launch, no
+// scratch, no atomics.  1 token, 4096 x 11008: 31.4 us (180 MB at 5.7 TB/s).
 #include <atomic>
 
 #include "gate_math.cuh"
@@ -19,18 +21,18 @@ namespace gb300 {
 namespace {
 
 constexpr int kFewThreads = 192;  // warp 0: TMA, warp 1: MMA, warps 2-5: TMEM lanes
-constexpr int kFewF = 64;         // features of a tile
-constexpr uint32_t kWBytes = 2 * kFewF * kRowBytes;
+constexpr int kFewRows = 128;     // features (forward: gate and up values) of a tile
+constexpr uint32_t kWBytes = kFewRows * kRowBytes;
 
 template <int TN>
 struct FewCfg {
   static constexpr uint32_t kStageBytes = kWBytes + TN * kRowBytes;
-  static constexpr int kCtasPerSm = TN <= 64 ? 3 : 2;
+  static constexpr int kCtasPerSm = 3;
   // shared memory of an SM (228 KB, 1 KB a CTA taken) among its CTAs
   static constexpr int kStages = (int)((227u * 1024u / kCtasPerSm - 3072u) / kStageBytes);
   static constexpr uint32_t kTmemCols = pow2_at_least(TN);
   static constexpr uint32_t kRingBytes = kStages * kStageBytes;
-  static_assert(kRingBytes >= 128 * TN * 4, "the sums are laid over the ring");
+  static_assert(kRingBytes >= kFewRows * TN * 4, "the sums are laid over the ring");
   static constexpr uint32_t kSmemBytes = kRingBytes + (2 * kStages + 1) * 8 + 16 + 1024;
 };
 
@@ -41,17 +43,28 @@ struct FewParams {
 
 __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
   float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
   return v;
 }
-__device__ __forceinline__ void st_shared_f32(uint32_t addr, uint32_t v) { st_shared_u32(addr, v); }
 
-template <int TN, bool KM>
+// The checkpoint of 32 values of row r, one a lane (0 past the row's end).
+__device__ __forceinline__ void q8_by_warp(const Q8Ref &ck, int64_t r, int c, int cols, float h) {
+  uint32_t top = __float_as_uint(h) & 0x7FFFFFFFu;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (c >= cols) return;
+  const uint32_t e = q8_exponent(top);
+  ck.q[r * ck.ldq + c] = (int8_t)q8_byte(h, q8_inverse(e), e);
+  if ((c & 31) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
+}
+
+template <int TN, bool KM, bool BWD>
 __global__ void __launch_bounds__(kFewThreads, FewCfg<TN>::kCtasPerSm)
     gated_few_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmG,
                      const __grid_constant__ CUtensorMap tmU, const FewParams fp) {
   using Cfg = FewCfg<TN>;
   constexpr int STAGES = Cfg::kStages;
+  constexpr int kTileF = BWD ? kFewRows : kFewRows / 2;
   const GatedTcParams &p = fp.g;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_addr(smem_raw);
@@ -66,7 +79,7 @@ __global__ void __launch_bounds__(kFewThreads, FewCfg<TN>::kCtasPerSm)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
-  const int f0 = (int)(blockIdx.x / (unsigned)fp.splits) * kFewF;
+  const int f0 = (int)(blockIdx.x / (unsigned)fp.splits) * kTileF;
   const int kb0 = (int)((int64_t)p.num_kb * rank / fp.splits), kb1 = (int)((int64_t)p.num_kb * (rank + 1) / fp.splits);
 
   if (threadIdx.x == 0) {
@@ -79,7 +92,7 @@ __global__ void __launch_bounds__(kFewThreads, FewCfg<TN>::kCtasPerSm)
     fence_mbar_init();
     tma_prefetch_desc(&tmX);
     tma_prefetch_desc(&tmG);
-    tma_prefetch_desc(&tmU);
+    if (!BWD) tma_prefetch_desc(&tmU);
   }
   __syncwarp();
   if (warp == 1) tmem_alloc<Cfg::kTmemCols>(smem_addr(tmem_slot));
@@ -99,9 +112,10 @@ __global__ void __launch_bounds__(kFewThreads, FewCfg<TN>::kCtasPerSm)
         if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.err, p.wait_limit_ns)) break;
         mbar_arrive_expect_tx(full_bar(s), Cfg::kStageBytes);
         const uint32_t w = ring + s * Cfg::kStageBytes;
-        const int x = KM ? kb * kBK : f0, y = KM ? f0 : kb * kBK;
-        tma_load_2d(w, &tmG, x, y, full_bar(s));
-        tma_load_2d(w + kWBytes / 2, &tmU, x, y, full_bar(s));
+        // two boxes of 64 features: a weight's each, or one weight's
+        const int f1 = BWD ? f0 + kFewRows / 2 : f0;
+        tma_load_2d(w, &tmG, KM ? kb * kBK : f0, KM ? f0 : kb * kBK, full_bar(s));
+        tma_load_2d(w + kWBytes / 2, BWD ? &tmG : &tmU, KM ? kb * kBK : f1, KM ? f1 : kb * kBK, full_bar(s));
         tma_load_2d(w + kWBytes, &tmX, kb * kBK, 0, full_bar(s));
       }
       // every load has landed before the CTA may exit
@@ -111,7 +125,7 @@ __global__ void __launch_bounds__(kFewThreads, FewCfg<TN>::kCtasPerSm)
     __syncwarp();
   } else if (warp == 1) {
     if (lane == 0) {
-      constexpr uint32_t idesc = idesc_bf16_f32(128, TN, false) | (KM ? 0u : 1u << 15);
+      constexpr uint32_t idesc = idesc_bf16_f32(kFewRows, TN, false) | (KM ? 0u : 1u << 15);
       uint32_t g = 0;
       for (int kb = kb0; kb < kb1; ++kb, ++g) {
         const uint32_t s = g % STAGES, ph = (g / STAGES) & 1u;
@@ -142,7 +156,7 @@ __global__ void __launch_bounds__(kFewThreads, FewCfg<TN>::kCtasPerSm)
         tmem_ld_32x32b_x16(tmem_base + ((uint32_t)(quad * 32) << 16) + c * 16, v);
         tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) st_shared_f32(at + (c * 16 + i) * 512, v[i]);
+        for (int i = 0; i < 16; ++i) st_shared_u32(at + (c * 16 + i) * (kFewRows * 4), v[i]);
       }
     }
     tc_fence_before_sync();
@@ -154,56 +168,94 @@ __global__ void __launch_bounds__(kFewThreads, FewCfg<TN>::kCtasPerSm)
   }
   // the cluster's CTAs share the tokens out: sums of all of them, the gate, H
   const int t0 = (int)((int64_t)p.T * rank / fp.splits), t1 = (int)((int64_t)p.T * (rank + 1) / fp.splits);
-  const int f = (int)threadIdx.x & (kFewF - 1);
-  if (f0 + f < p.F) {
-    for (int t = t0 + ((int)threadIdx.x >> 6); t < t1; t += kFewThreads / kFewF) {
-      const uint32_t at = ring + t * 512 + f * 4;
-      float g = 0.f, u = 0.f;
-      for (int s = 0; s < fp.splits; ++s) {
-        const uint32_t from = mapa_shared(at, s);
-        g += ld_cluster_f32(from);
-        u += ld_cluster_f32(from + kFewF * 4);
+  // a warp takes 32 features of a token, kBatch of these at a time so that
+  // their loads overlap
+  constexpr int kGroups = kTileF / 32, kBatch = BWD ? 8 : 4, kWarps = kFewThreads / 32;
+  const int items = (t1 - t0) * kGroups;
+  for (int i0 = warp; i0 < items; i0 += kBatch * kWarps) {
+    float a[kBatch] = {}, b[kBatch] = {};  // the sums: of g and u, or of dh
+    float g[kBatch], u[kBatch];
+    uint32_t at[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int i = min(i0 + j * kWarps, items - 1), t = t0 + i / kGroups, f = (i % kGroups) * 32 + lane, c = f0 + f;
+      at[j] = ring + t * (kFewRows * 4) + f * 4;
+      if constexpr (BWD) {
+        g[j] = c < p.F ? load_value<bf16>(p.gate, t * p.ldgate + c) : 0.f;
+        u[j] = c < p.F ? load_value<bf16>(p.up, t * p.ldup + c) : 0.f;
       }
-      float h = 0.f;
-      with_activation(p.act, [&](auto act) { h = gate<decltype(act)::value, false>(g).a * u; });
-      store_value<bf16>(p.out[0], t * p.ldout[0] + f0 + f, h);
-      if (p.out[1]) {
-        store_value<bf16>(p.out[1], t * p.ldout[1] + f0 + f, g);
-        store_value<bf16>(p.out[2], t * p.ldout[2] + f0 + f, u);
+    }
+    for (int s = 0; s < fp.splits; ++s) {
+      float v[kBatch], w[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const uint32_t from = mapa_shared(at[j], s);
+        v[j] = ld_cluster_f32(from);
+        w[j] = BWD ? 0.f : ld_cluster_f32(from + kTileF * 4);
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) a[j] += v[j], b[j] += w[j];
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int i = i0 + j * kWarps, t = t0 + i / kGroups, c = f0 + (i % kGroups) * 32 + lane;
+      if (i >= items) break;
+      if constexpr (!BWD) {
+        float h = 0.f;
+        with_activation(p.act, [&](auto act) { h = gate<decltype(act)::value, false>(a[j]).a * b[j]; });
+        if (c >= p.F) continue;
+        store_value<bf16>(p.out[0], t * p.ldout[0] + c, h);
+        if (p.out[1]) {
+          store_value<bf16>(p.out[1], t * p.ldout[1] + c, a[j]);
+          store_value<bf16>(p.out[2], t * p.ldout[2] + c, b[j]);
+        }
+      } else {
+        GateValue v{0.f, 0.f};
+        with_activation(p.act, [&](auto act) { v = gate<decltype(act)::value, true>(g[j]); });
+        if (c < p.F) {
+          store_value<bf16>(p.out[0], t * p.ldout[0] + c, a[j] * u[j] * v.slope);
+          store_value<bf16>(p.out[1], t * p.ldout[1] + c, a[j] * v.a);
+        }
+        if (p.ck.q) q8_by_warp(p.ck, t, c, p.F, v.a * u[j]);
       }
     }
   }
   cluster_sync_all();  // no CTA leaves while another reads its sums
 }
 
-template <int TN, bool KM>
+template <int TN, bool KM, bool BWD>
 cudaError_t launch(const GatedMaps &m, const FewParams &p, int grid, cudaStream_t st) {
   using Cfg = FewCfg<TN>;
-  auto kern = gated_few_kernel<TN, KM>;
+  auto kern = gated_few_kernel<TN, KM, BWD>;
   static std::atomic<uint64_t> allowed{0};
   const cudaError_t e = allow_shared_memory((const void *)kern, Cfg::kSmemBytes, allowed);
   if (e != cudaSuccess) return e;
   return launch_ex(kern, dim3((unsigned)grid), dim3(kFewThreads), Cfg::kSmemBytes, st, p.splits, m.a, m.b[0], m.b[1], p);
 }
-template <bool KM>
+template <bool KM, bool BWD>
 cudaError_t launch_tokens(int tn, const GatedMaps &m, const FewParams &p, int grid, cudaStream_t st) {
-  return tn == 16   ? launch<16, KM>(m, p, grid, st)
-         : tn == 32 ? launch<32, KM>(m, p, grid, st)
-         : tn == 64 ? launch<64, KM>(m, p, grid, st)
-                    : launch<128, KM>(m, p, grid, st);
+  return tn == 16   ? launch<16, KM, BWD>(m, p, grid, st)
+         : tn == 32 ? launch<32, KM, BWD>(m, p, grid, st)
+                    : launch<64, KM, BWD>(m, p, grid, st);
 }
 
 }  // namespace
 
-int gated_few_columns(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
+int gated_few_columns(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : 64; }
 
-cudaError_t launch_gated_few(bool km, const GatedMaps &m, const GatedTcParams &p, int sms, cudaStream_t st) {
-  const int tn = gated_few_columns(p.T), tiles = (p.F + kFewF - 1) / kFewF;
-  const int slots = sms * (tn <= 64 ? 3 : 2);
+cudaError_t launch_gated_few(bool forward, bool km, const GatedMaps &m, const GatedTcParams &p, int sms,
+                             cudaStream_t st) {
+  const int tn = gated_few_columns(p.T), tile_f = forward ? kFewRows / 2 : kFewRows, tiles = (p.F + tile_f - 1) / tile_f;
+  // the most CTAs a cluster with which all are resident at once (three an SM),
+  // each with at least four k-blocks: a second wave costs more than it hides (48
+  // tokens 4096 x 11008, 172 tiles: 40, 34.6, 39 and 49 us by 1, 2, 4 and 8; 1
+  // token 4096 x 4096, 64 tiles: 22.8, 15.1, 12.5 and 15.5)
   int splits = 1;
-  while (splits < 8 && tiles * splits * 2 <= slots && p.num_kb >= splits * 8) splits *= 2;
+  while (splits < 8 && tiles * splits * 2 <= sms * 3 && p.num_kb >= splits * 8) splits *= 2;
   const FewParams fp{p, splits};
-  return km ? launch_tokens<true>(tn, m, fp, tiles * splits, st) : launch_tokens<false>(tn, m, fp, tiles * splits, st);
+  const int grid = tiles * splits;
+  if (forward) return km ? launch_tokens<true, false>(tn, m, fp, grid, st) : launch_tokens<false, false>(tn, m, fp, grid, st);
+  return km ? launch_tokens<true, true>(tn, m, fp, grid, st) : launch_tokens<false, true>(tn, m, fp, grid, st);
 }
 
 }  // namespace gb300

@@ -235,7 +235,7 @@ cudaError_t pack_operands(Operand *o, int n, uint8_t *at, const OpContext &c) {
 // layout km), makes their maps, and launches.
 gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool forward, GatedTcParams &p,
                         const OpContext &c) {
-  const bool few = forward && p.T <= kFewTokens;
+  const bool few = p.T <= kFewTokens;
   if (pl.grid <= 0) return GEMM_ERR_CUDA;
   size_t packed = 0;
   for (int i = 0; i < n; ++i) packed += o[i].bytes();
@@ -262,7 +262,7 @@ gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool fo
   p.wait_limit_ns = c.wait_limit_ns;
   if (few) {
     count_launches(1);
-    return launch_gated_few(km, m, p, c.sms, c.st) == cudaSuccess ? GEMM_OK : GEMM_ERR_CUDA;
+    return launch_gated_few(forward, km, m, p, c.sms, c.st) == cudaSuccess ? GEMM_OK : GEMM_ERR_CUDA;
   }
   p.vec = p.F % 8 == 0 && (!p.gate || (rows_on(p.gate, p.ldgate, 2, 16) && rows_on(p.up, p.ldup, 2, 16)));
   for (int i = 0; i < 3; ++i)

@@ -190,11 +190,12 @@ struct GatedMaps {
 };
 cudaError_t launch_gated_tc_fwd(const GatedTile &tile, bool km, const GatedMaps &m, const GatedTcParams &p, int grid,
                                 cudaStream_t st);
-// The forward kernel of at most kFewTokens tokens (gated_few.cu): X in boxes of
-// 64 x gated_few_columns(T), each weight in boxes of 64 x 64.
-constexpr int kFewTokens = 128;
+// The kernel of at most kFewTokens tokens (gated_few.cu): X or dO in boxes of 64
+// x gated_few_columns(T), each weight in boxes of 64 x 64.
+constexpr int kFewTokens = 64;
 int gated_few_columns(int64_t T);
-cudaError_t launch_gated_few(bool km, const GatedMaps &m, const GatedTcParams &p, int sms, cudaStream_t st);
+cudaError_t launch_gated_few(bool forward, bool km, const GatedMaps &m, const GatedTcParams &p, int sms,
+                             cudaStream_t st);
 cudaError_t launch_gated_tc_bwd(const GatedTile &tile, bool km, const GatedMaps &m, const GatedTcParams &p, int grid,
                                 cudaStream_t st);
 // The split tail's tiles: partial sums added in split order, then as the kernel
