@@ -147,8 +147,9 @@ gemm_status_t gemm_q8_weight_grad(int64_t T, int64_t K, int64_t N, const int8_t 
  *
  * back from dO,  dH = dO . Wd^T,  dG = dH * U * act'(G),  dU = dH * act(G).
  * The calls here take the projections with the gate, and the gate's gradient
- * with or without the down projection's product; the rest are GEMMs and weight
- * gradients above.  With Wg and Wu the halves of one K x 2F matrix W, and dG
+ * with or without the down projection's product (those with a product use the
+ * stream's scratch where rows are not 16-byte aligned and where a last round of
+ * tiles is split); the rest are GEMMs and weight gradients above.  With Wg and Wu the halves of one K x 2F matrix W, and dG
  * and dU those of a T x 2F matrix, dX is one GEMM with W^T and dW one
  * gemm_q8_weight_grad.
  */
@@ -168,12 +169,17 @@ typedef enum {
  *   pass; both or neither.
  * The sums are float32, H is taken from them unrounded, and H, G and U are
  * rounded once.  T == 0 or F == 0 is a no-op; K == 0 writes zeros.
- * Accuracy contract, per element, with g, u the exact sums and Sg, Su those of
- * the products' magnitudes: G and U as gemm_bf16_f32acc_bf16's C, and
- *     |H - act(g) u| <= 2^-8 |act(g) u| + 2^-20 (1.2 Sg |u| + |act(g)| Su)
- *                       + 2^-18 |g u|
- * (and the product of the two sums' errors).  Infinite or NaN sums give what
- * the formulas give in float32; act of -infinity is NaN except for relu.
+ * Accuracy contract, per element, with g, u the exact sums, Sg, Su those of
+ * the products' magnitudes and c = (K + 32) * 2^-24:
+ *     |G - g| <= 2^-8 |g| + c Sg,   |U - u| <= 2^-8 |u| + c Su,
+ *     |H - act(g) u| <= 2^-8 |act(g) u| + c (1.13 Sg |u| + |act(g)| Su)
+ *                       + 1.13 c^2 Sg Su + 2^-18 |g u|
+ * (and the last rounding of that error).  As in the weight gradient, c allows
+ * for what the tensor core cuts of its additions, worst for one large product
+ * among many small ones; of products whose signs are random the sums measure
+ * within 2^-20 Sg.  1.13 is the activations' largest slope.  Infinite or NaN
+ * sums give what the formulas give in float32: act of -infinity is NaN, except
+ * of relu.
  */
 gemm_status_t gemm_gated_forward(int64_t T, int64_t K, int64_t F, const uint16_t *X, int64_t ldx,
                                  const uint16_t *Wg, int64_t ldwg, const uint16_t *Wu, int64_t ldwu, int w_layout,
@@ -188,6 +194,7 @@ gemm_status_t gemm_gated_forward(int64_t T, int64_t K, int64_t F, const uint16_t
  *   q, ldq, e, lde: when q and e are not NULL, the checkpoint of the float32
  *   values act(G) * U, as gemm_q8_save writes it: H for the down projection's
  *   weight gradient, dWd = H^T . dO, without H having been kept.
+ * act and act' are off by at most 2^-18 |G| and 2^-18 before the products.
  * T == 0 or F == 0 is a no-op.
  */
 gemm_status_t gemm_gated_backward(int64_t T, int64_t F, const uint16_t *dH, int64_t lddh, const uint16_t *G,
@@ -197,7 +204,8 @@ gemm_status_t gemm_gated_backward(int64_t T, int64_t F, const uint16_t *dH, int6
 
 /*
  * The same with dH = dO . Wd^T taken in the same kernel, in float32 and not
- * rounded in between.
+ * rounded in between; dH is off by at most (N + 32) * 2^-24 of its products'
+ * magnitudes' sum.
  *   dO: T x N bf16, pitch lddo.  Wd: the down projection, O = H . Wd, of
  *   w_layout: GEMM_B_ROW_MAJOR_KxN has Wd(f, n) at Wd[f * ldwd + n],
  *   GEMM_B_COL_MAJOR_NxK at Wd[n * ldwd + f].
