@@ -47,17 +47,6 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
   return v;
 }
 
-// The checkpoint of 32 values of row r, one a lane (0 past the row's end).
-__device__ __forceinline__ void q8_by_warp(const Q8Ref &ck, int64_t r, int c, int cols, float h) {
-  uint32_t top = __float_as_uint(h) & 0x7FFFFFFFu;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (c >= cols) return;
-  const uint32_t e = q8_exponent(top);
-  ck.q[r * ck.ldq + c] = (int8_t)q8_byte(h, q8_inverse(e), e);
-  if ((c & 31) == 0) ck.e[r * ck.lde + (c >> 5)] = (uint8_t)e;
-}
-
 template <int TN, bool KM, bool BWD>
 __global__ void __launch_bounds__(kFewThreads, FewCfg<TN>::kCtasPerSm)
     gated_few_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmG,
@@ -166,23 +155,23 @@ __global__ void __launch_bounds__(kFewThreads, FewCfg<TN>::kCtasPerSm)
     tc_fence_after_sync();
     tmem_dealloc<Cfg::kTmemCols>(tmem_base);
   }
-  // the cluster's CTAs share the tokens out: sums of all of them, the gate, H
+  // The cluster's CTAs share the tokens out: sums of all of them, the gate,
+  // results.  A warp takes 32 features of a token, kBatch of these at a time so
+  // that their loads overlap.
+  constexpr int kGroups = kTileF / 32, kBatch = 4, kWarps = kFewThreads / 32;
   const int t0 = (int)((int64_t)p.T * rank / fp.splits), t1 = (int)((int64_t)p.T * (rank + 1) / fp.splits);
-  // a warp takes 32 features of a token, kBatch of these at a time so that
-  // their loads overlap
-  constexpr int kGroups = kTileF / 32, kBatch = BWD ? 8 : 4, kWarps = kFewThreads / 32;
   const int items = (t1 - t0) * kGroups;
   for (int i0 = warp; i0 < items; i0 += kBatch * kWarps) {
     float a[kBatch] = {}, b[kBatch] = {};  // the sums: of g and u, or of dh
-    float g[kBatch], u[kBatch];
+    float gate_in[kBatch], up_in[kBatch];
     uint32_t at[kBatch];
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       const int i = min(i0 + j * kWarps, items - 1), t = t0 + i / kGroups, f = (i % kGroups) * 32 + lane, c = f0 + f;
       at[j] = ring + t * (kFewRows * 4) + f * 4;
       if constexpr (BWD) {
-        g[j] = c < p.F ? load_value<bf16>(p.gate, t * p.ldgate + c) : 0.f;
-        u[j] = c < p.F ? load_value<bf16>(p.up, t * p.ldup + c) : 0.f;
+        gate_in[j] = c < p.F ? load_value<bf16>(p.gate, t * p.ldgate + c) : 0.f;
+        up_in[j] = c < p.F ? load_value<bf16>(p.up, t * p.ldup + c) : 0.f;
       }
     }
     for (int s = 0; s < fp.splits; ++s) {
@@ -196,27 +185,53 @@ __global__ void __launch_bounds__(kFewThreads, FewCfg<TN>::kCtasPerSm)
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) a[j] += v[j], b[j] += w[j];
     }
+    // act and the checkpoint's exponents of the batch together: chains that
+    // would take 0.4 us an item one after the other
+    if constexpr (!BWD) {
+      float h[kBatch];
+      with_activation(p.act, [&](auto act) {
 #pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
-      const int i = i0 + j * kWarps, t = t0 + i / kGroups, c = f0 + (i % kGroups) * 32 + lane;
-      if (i >= items) break;
-      if constexpr (!BWD) {
-        float h = 0.f;
-        with_activation(p.act, [&](auto act) { h = gate<decltype(act)::value, false>(a[j]).a * b[j]; });
-        if (c >= p.F) continue;
-        store_value<bf16>(p.out[0], t * p.ldout[0] + c, h);
+        for (int j = 0; j < kBatch; ++j) h[j] = gate<decltype(act)::value, false>(a[j]).a * b[j];
+      });
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int i = i0 + j * kWarps, t = t0 + i / kGroups, c = f0 + (i % kGroups) * 32 + lane;
+        if (i >= items || c >= p.F) continue;
+        store_value<bf16>(p.out[0], t * p.ldout[0] + c, h[j]);
         if (p.out[1]) {
           store_value<bf16>(p.out[1], t * p.ldout[1] + c, a[j]);
           store_value<bf16>(p.out[2], t * p.ldout[2] + c, b[j]);
         }
-      } else {
-        GateValue v{0.f, 0.f};
-        with_activation(p.act, [&](auto act) { v = gate<decltype(act)::value, true>(g[j]); });
-        if (c < p.F) {
-          store_value<bf16>(p.out[0], t * p.ldout[0] + c, a[j] * u[j] * v.slope);
-          store_value<bf16>(p.out[1], t * p.ldout[1] + c, a[j] * v.a);
+      }
+    } else {
+      float h[kBatch], g[kBatch], u[kBatch];  // act(G) U (0 past F), dG, dU
+      uint32_t top[kBatch];
+      with_activation(p.act, [&](auto act) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          const GateValue v = gate<decltype(act)::value, true>(gate_in[j]);
+          h[j] = v.a * up_in[j];
+          g[j] = a[j] * up_in[j] * v.slope;
+          u[j] = a[j] * v.a;
+          top[j] = __float_as_uint(h[j]) & 0x7FFFFFFFu;
         }
-        if (p.ck.q) q8_by_warp(p.ck, t, c, p.F, v.a * u[j]);
+      });
+      if (p.ck.q) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+          for (int j = 0; j < kBatch; ++j) top[j] = max(top[j], __shfl_xor_sync(0xffffffffu, top[j], o));
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int i = i0 + j * kWarps, t = t0 + i / kGroups, c = f0 + (i % kGroups) * 32 + lane;
+        if (i >= items || c >= p.F) continue;
+        store_value<bf16>(p.out[0], t * p.ldout[0] + c, g[j]);
+        store_value<bf16>(p.out[1], t * p.ldout[1] + c, u[j]);
+        if (!p.ck.q) continue;
+        const uint32_t e = q8_exponent(top[j]);
+        p.ck.q[t * p.ck.ldq + c] = (int8_t)q8_byte(h[j], q8_inverse(e), e);
+        if (lane == 0) p.ck.e[t * p.ck.lde + (c >> 5)] = (uint8_t)e;
       }
     }
   }
@@ -246,12 +261,15 @@ int gated_few_columns(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : 64; }
 cudaError_t launch_gated_few(bool forward, bool km, const GatedMaps &m, const GatedTcParams &p, int sms,
                              cudaStream_t st) {
   const int tn = gated_few_columns(p.T), tile_f = forward ? kFewRows / 2 : kFewRows, tiles = (p.F + tile_f - 1) / tile_f;
-  // the most CTAs a cluster with which all are resident at once (three an SM),
-  // each with at least four k-blocks: a second wave costs more than it hides (48
-  // tokens 4096 x 11008, 172 tiles: 40, 34.6, 39 and 49 us by 1, 2, 4 and 8; 1
-  // token 4096 x 4096, 64 tiles: 22.8, 15.1, 12.5 and 15.5)
+  // The split: up to a CTA an SM or a quarter more, at least one k-block each
+  // (eight CTAs of a cluster: eight); where that leaves 32 k-blocks or more to
+  // each, twice as many, as long as all are resident at once (three an SM).
+  // Forward in us by 1, 2, 4 and 8: 16 tokens 4096 x 2048 (32 tiles) 20.4, 11.7,
+  // 7.9, 9.7; 64 tokens 768 x 4096 (64) 8.5, 6.4, 8.5, 15.6; 48 tokens 4096 x
+  // 11008 (172) 40, 34.6, 39, 49.
   int splits = 1;
-  while (splits < 8 && tiles * splits * 2 <= sms * 3 && p.num_kb >= splits * 8) splits *= 2;
+  while (splits < 8 && tiles * splits * 2 <= sms * 5 / 4 && p.num_kb >= (splits == 4 ? 64 : splits * 2)) splits *= 2;
+  if (splits < 8 && p.num_kb >= splits * 32 && tiles * splits * 2 <= sms * 3) splits *= 2;
   const FewParams fp{p, splits};
   const int grid = tiles * splits;
   if (forward) return km ? launch_tokens<true, false>(tn, m, fp, grid, st) : launch_tokens<false, false>(tn, m, fp, grid, st);

@@ -289,7 +289,7 @@ gemm_status_t gemm_gated_backward(int64_t T, int64_t F, const uint16_t *dH, int6
   OpContext c;
   if ((s = op_context(reinterpret_cast<cudaStream_t>(stream), &c)) != GEMM_OK) return s;
   count_launches(1);
-  return launched(launch_gated_backward(p, c.st));
+  return launched(launch_gated_backward(p, c));
 }
 
 gemm_status_t gemm_gated_down_backward(int64_t T, int64_t N, int64_t F, const uint16_t *dO, int64_t lddo,
@@ -309,7 +309,7 @@ gemm_status_t gemm_gated_down_backward(int64_t T, int64_t N, int64_t F, const ui
   return with_scratch(reinterpret_cast<cudaStream_t>(stream), [&](const OpContext &c) -> gemm_status_t {
     if (N == 0) {
       count_launches(1);
-      return launched(launch_gated_backward(b, c.st));
+      return launched(launch_gated_backward(b, c));
     }
     return gated_down_backward(GatedDownBackward{b, (int)N, dO, lddo, Wd, ldwd, kn}, c);
   });

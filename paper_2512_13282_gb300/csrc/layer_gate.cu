@@ -18,45 +18,49 @@ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 constexpr int kThreads = 256;
 
-// A thread takes half a block of the checkpoint: 16 consecutive values of a
-// row, its neighbouring lane the other half; they exchange the largest
-// magnitude with one shuffle.  VEC: all rows start on 16 bytes; else values are
-// shifted between registers and the 16-byte pieces of memory that they lie in.
-template <int ACT, bool VEC>
+// A thread takes V = 16 or 8 consecutive values of a row, two or four
+// neighbouring lanes a block of the checkpoint; they exchange its largest
+// magnitude with shuffles.  VEC: all rows start on 16 bytes (the checkpoint's on
+// 8); else values are shifted between registers and the 16-byte pieces of memory
+// that they lie in.
+// The bytes bound many values (8192 x 11008 silu with the checkpoint: 139 us, 6.6
+// TB/s), a thread's own chain of instructions few, for which V is 8.
+template <int ACT, bool VEC, int V>
 __global__ void __launch_bounds__(kThreads) gated_backward_kernel(const GatedBackward p, int64_t cols) {
   griddep_launch_dependents();
   griddep_wait();
-  const int64_t halves = (cols + 31) / 32 * 2, items = p.T * halves, step = (int64_t)gridDim.x * kThreads;
+  constexpr int kLanes = 32 / V;  // of a block
+  const int64_t pieces = (cols + 31) / 32 * kLanes, items = p.T * pieces, step = (int64_t)gridDim.x * kThreads;
   const int lane = threadIdx.x & 31;
   for (int64_t h0 = (int64_t)blockIdx.x * kThreads; h0 < items; h0 += step) {
-    // items is even, so both lanes of a block are in range or neither is
+    // items is a multiple of kLanes, so the lanes of a block are all in range or none
     const int64_t h = h0 + threadIdx.x;
     const bool live = h < items;
     int64_t r, c;
-    half_block(live ? h : items - 1, halves, &r, &c);
-    const int n = !live || c >= cols ? 0 : (int)min((int64_t)16, cols - c);
+    row_piece<V>(live ? h : items - 1, pieces, &r, &c);
+    const int n = !live || c >= cols ? 0 : (int)min((int64_t)V, cols - c);
     const auto load = [&](const uint16_t *m, int64_t ld) {
       const uint16_t *row = m + r * ld;
-      Chunk<bf16, 16> v;
-      if (n < 16)
+      Chunk<bf16, V> v;
+      if (n < V)
         v.load_part(row, c, n);
       else if constexpr (VEC)
         v.load(row, c);
       else
-        load_half(row + c, c == 0, (cols - c - 16) * 2, v.w);
+        load_half(row + c, c == 0, (cols - c - V) * 2, v.w);
       return v;
     };
-    Chunk<bf16, 16> d;
+    Chunk<bf16, V> d;
     if (p.dh)
       d = load(p.dh, p.lddh);
     else
       d.load_part(nullptr, 0, 0);
-    const Chunk<bf16, 16> g = load(p.g, p.ldg), u = load(p.u, p.ldu);
-    uint32_t dg[8], du[8];
-    float2 v[8];  // act(g) * u
+    const Chunk<bf16, V> g = load(p.g, p.ldg), u = load(p.u, p.ldu);
+    uint32_t dg[V / 2], du[V / 2];
+    float2 v[V / 2];  // act(g) * u
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < V / 2; ++i) {
       const float2 di = d.get2(i), gi = g.get2(i), ui = u.get2(i);
       const GateValue a = gate<ACT, true>(gi.x), b = gate<ACT, true>(gi.y);
       dg[i] = pack_bf16x2(di.x * ui.x * a.slope, di.y * ui.y * b.slope);
@@ -64,46 +68,62 @@ __global__ void __launch_bounds__(kThreads) gated_backward_kernel(const GatedBac
       v[i] = make_float2(a.a * ui.x, b.a * ui.y);
       top = max(top, max(__float_as_uint(v[i].x) & 0x7FFFFFFFu, __float_as_uint(v[i].y) & 0x7FFFFFFFu));
     }
-    const auto store = [&](uint16_t *m, int64_t ld, const uint32_t(&w)[8]) {
+    const bool joined = lane > 0 && c > 0, taken = lane < 31 && c + 2 * V <= cols;
+    const auto store = [&](uint16_t *m, int64_t ld, const uint32_t(&w)[V / 2]) {
       uint16_t *row = m + r * ld;
-      if constexpr (VEC) {
-        if (n == 16) store_32_bytes(row + c, w);
-      } else {
-        store_shifted<4>(row + c, n == 16, lane > 0 && c > 0, lane < 31 && c + 32 <= cols, w);
+      if constexpr (!VEC) {
+        store_shifted<4>(row + c, n == V, joined, taken, w);
+      } else if (n == V) {
+        if constexpr (V == 16)
+          store_32_bytes(row + c, w);
+        else
+          *reinterpret_cast<uint4 *>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
       }
-      if (n < 16) {
+      if (n < V) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
+        for (int i = 0; i < V; ++i)
           if (i < n) row[c + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
       }
     };
     store(p.dg, p.lddg, dg);
     store(p.du, p.lddu, du);
     if (!p.ck.q) continue;
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    const uint32_t e = q8_exponent(top);
-    float2 lo[4], hi[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) lo[j] = v[j], hi[j] = v[4 + j];
-    const uint2 wl = q8_pack8(lo, e), wh = q8_pack8(hi, e);
-    const uint32_t w[4] = {wl.x, wl.y, wh.x, wh.y};
-    int8_t *q = p.ck.q + r * p.ck.ldq + c;
-    if constexpr (VEC) {
-      if (n == 16) *reinterpret_cast<uint4 *>(q) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-      store_shifted<4>(q, n == 16, lane > 0 && c > 0, lane < 31 && c + 32 <= cols, w);
+    for (int o = 1; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const uint32_t e = q8_exponent(top);
+    uint32_t w[V / 4];
+#pragma unroll
+    for (int k = 0; k < V / 8; ++k) {
+      const float2 eight[4] = {v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]};
+      const uint2 q = q8_pack8(eight, e);
+      w[2 * k] = q.x, w[2 * k + 1] = q.y;
     }
-    if (n < 16) store_bytes(q, w, n);
-    if (live && (h & 1) == 0) p.ck.e[r * p.ck.lde + (c >> 5)] = (uint8_t)e;
+    int8_t *q = p.ck.q + r * p.ck.ldq + c;
+    if constexpr (!VEC) {
+      store_shifted<V / 4>(q, n == V, joined, taken, w);
+    } else if (n == V) {
+      if (V == 16 && (reinterpret_cast<uintptr_t>(q) & 15) == 0) {
+        *reinterpret_cast<uint4 *>(q) = make_uint4(w[0], w[1], w[V / 4 - 2], w[V / 4 - 1]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < V / 8; ++k) reinterpret_cast<uint2 *>(q)[k] = make_uint2(w[2 * k], w[2 * k + 1]);
+      }
+    }
+    if (n < V) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (i < n) q[i] = (int8_t)(w[i / 4] >> (8 * (i & 3)));
+    }
+    if (live && (c & 31) == 0) p.ck.e[r * p.ck.lde + (c >> 5)] = (uint8_t)e;
   }
 }
 
-template <bool VEC>
+template <bool VEC, int V>
 auto backward_kernel(int act) {
-  return act == GEMM_ACT_SILU        ? gated_backward_kernel<GEMM_ACT_SILU, VEC>
-         : act == GEMM_ACT_GELU      ? gated_backward_kernel<GEMM_ACT_GELU, VEC>
-         : act == GEMM_ACT_GELU_TANH ? gated_backward_kernel<GEMM_ACT_GELU_TANH, VEC>
-                                     : gated_backward_kernel<GEMM_ACT_RELU, VEC>;
+  return act == GEMM_ACT_SILU        ? gated_backward_kernel<GEMM_ACT_SILU, VEC, V>
+         : act == GEMM_ACT_GELU      ? gated_backward_kernel<GEMM_ACT_GELU, VEC, V>
+         : act == GEMM_ACT_GELU_TANH ? gated_backward_kernel<GEMM_ACT_GELU_TANH, VEC, V>
+                                     : gated_backward_kernel<GEMM_ACT_RELU, VEC, V>;
 }
 
 // --------------------------------------------- with a product: tiles, staging
@@ -327,13 +347,19 @@ gemm_status_t gated_down_backward(const GatedDownBackward &p, const OpContext &c
                    c);
 }
 
-cudaError_t launch_gated_backward(const GatedBackward &p, cudaStream_t st) {
+cudaError_t launch_gated_backward(const GatedBackward &p, const OpContext &c) {
   const auto on16 = [&](const void *m, int64_t ld) { return rows_on(m, ld, 2, 16); };
   const bool vec = (!p.dh || on16(p.dh, p.lddh)) && on16(p.g, p.ldg) && on16(p.u, p.ldu) && on16(p.dg, p.lddg) &&
-                   on16(p.du, p.lddu) && (!p.ck.q || rows_on(p.ck.q, p.ck.ldq, 1, 16));
-  const int64_t blocks = ceil_div64(p.T * (ceil_div64(p.F, 32) * 2), kThreads);
-  return launch_ex(vec ? backward_kernel<true>(p.act) : backward_kernel<false>(p.act),
-                   dim3((unsigned)(blocks < (1 << 30) ? blocks : (1 << 30))), dim3(kThreads), 0, st, 1, p, (int64_t)p.F);
+                   on16(p.du, p.lddu) && (!p.ck.q || rows_on(p.ck.q, p.ck.ldq, 1, 8));
+  // eight values a thread while each has one piece: 100 x 1024 1.9 us (16: 2.25),
+  // 2928 x 776 the same.  Unaligned, whose pieces overlap, only for very few: 56 x
+  // 290 4.3 us (16: 5.5), 1000 x 1501 11.3 (8.4)
+  const bool small = p.T * ceil_div64(p.F, 32) * 4 <= (int64_t)c.sms * (vec ? 2048 : 256);
+  const int64_t blocks = ceil_div64(p.T * ceil_div64(p.F, 32) * (small ? 4 : 2), kThreads);
+  const auto kern = small ? vec ? backward_kernel<true, 8>(p.act) : backward_kernel<false, 8>(p.act)
+                          : vec ? backward_kernel<true, 16>(p.act) : backward_kernel<false, 16>(p.act);
+  return launch_ex(kern, dim3((unsigned)(blocks < (1 << 30) ? blocks : (1 << 30))), dim3(kThreads), 0, c.st, 1, p,
+                   (int64_t)p.F);
 }
 
 }  // namespace gb300

@@ -141,7 +141,7 @@ struct GatedBackward {
   int64_t lddg, lddu;
   Q8Ref ck;  // checkpoint of act(g) * u, or ck.q null
 };
-cudaError_t launch_gated_backward(const GatedBackward &p, cudaStream_t st);
+cudaError_t launch_gated_backward(const GatedBackward &p, const OpContext &c);
 // dh = dO . Wd^T over N columns; b.dh is not used.
 struct GatedDownBackward {
   GatedBackward b;

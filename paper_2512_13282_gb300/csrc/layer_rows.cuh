@@ -383,17 +383,22 @@ __device__ __forceinline__ void load_half(const void *src, bool first, int64_t a
   for (int i = 0; i < W; ++i) out[i] = w[i];
 }
 
-// Half block h of the matrix -> its row and first column, `halves` of them a
-// row (an even number).  With rows laid end to end the launcher makes the
-// matrix one row, and 32-bit arithmetic serves any matrix below 2^32 halves.
-__device__ __forceinline__ void half_block(int64_t h, int64_t halves, int64_t *r, int64_t *c) {
+// Piece h of the matrix, V columns, -> its row and first column, `pieces` of them
+// a row.  With rows laid end to end a launcher may make the matrix one row, and
+// 32-bit arithmetic serves any matrix below 2^32 pieces.
+template <int V>
+__device__ __forceinline__ void row_piece(int64_t h, int64_t pieces, int64_t *r, int64_t *c) {
   int64_t row;
-  if ((uint64_t)h <= 0xFFFFFFFFull && halves <= 0xFFFFFFFFll)
-    row = (uint32_t)h / (uint32_t)halves;
+  if ((uint64_t)h <= 0xFFFFFFFFull && pieces <= 0xFFFFFFFFll)
+    row = (uint32_t)h / (uint32_t)pieces;
   else
-    row = h / halves;
+    row = h / pieces;
   *r = row;
-  *c = (h - row * halves) * 16;
+  *c = (h - row * pieces) * V;
+}
+// Half block h of a checkpoint (`halves` is even).
+__device__ __forceinline__ void half_block(int64_t h, int64_t halves, int64_t *r, int64_t *c) {
+  row_piece<16>(h, halves, r, c);
 }
 
 // The first n of a half block's bytes.

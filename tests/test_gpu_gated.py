@@ -158,7 +158,7 @@ def gate_grad(T, F, act, pad=0, off=0, held=True, in_place=False):
 
 
 BACKWARD = [(1, 1), (1, 11008), (2, 31), (3, 32), (5, 33), (7, 64), (40, 777), (129, 1501), (64, 2048), (1000, 96),
-            (33, 4096), (2, 40008)]
+            (33, 4096), (2, 40008), (2000, 1001), (700, 4104)]
 
 
 @pytest.mark.parametrize("T,F", BACKWARD)
