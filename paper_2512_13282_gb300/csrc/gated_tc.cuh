@@ -5,7 +5,8 @@
 // Both are C = A . B with A row-major and a B of either layout, and run as
 // gemm_tc2.cuh does (PAIR: a CTA pair per 256-row tile, each CTA holding 128
 // rows of A and half of B; else one CTA per 128-row tile): a TMA producer, an
-// MMA issuer and eight epilogue warps, two accumulators in TMEM.  What differs:
+// MMA issuer and epilogue warps (four forward, eight backward), two accumulators
+// in TMEM.  What differs:
 //
 // Forward.  A tile's BN columns are BN / 2 of the gate's projection and the
 // same BN / 2 of the up projection's, so that one lane of the epilogue finds g

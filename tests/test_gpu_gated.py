@@ -173,7 +173,8 @@ def test_backward(T, F, act):
 
 DOWN = [(1, 1, 1), (1, 4096, 640), (3, 777, 33), (16, 64, 64), (40, 328, 200), (100, 1000, 129), (128, 128, 256),
         (129, 96, 777), (256, 512, 320), (300, 777, 301), (513, 64, 264), (1000, 136, 130), (70, 2048, 1376),
-        (300, 4096, 520), (600, 2048, 1504), (130, 3000, 1000), (2100, 256, 2008)]
+        (300, 4096, 520), (600, 2048, 1504), (130, 3000, 1000), (2100, 256, 2008), (90, 100, 32), (300, 64, 96),
+        (1000, 520, 480), (2100, 256, 2016), (129, 4096, 544), (300, 4096, 352)]
 
 
 def down_grad(T, N, F, act, layout, pad=0, off=0, held=True, in_place=False):
