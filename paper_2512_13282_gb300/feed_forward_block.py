@@ -36,7 +36,8 @@ class FeedForwardBlock:
     two passes.  x and y are bf16 or float32 (a residual stream); the weights
     are bf16, row-major: W is width x 2 hidden (Wg, then Wu), Wd hidden x width.
     ``drop`` is dropout's share, ``seed`` its key; each forward pass draws with
-    the next step.  A pass raises ValueError for a tensor of another shape, type
+    the next step; the replays of a captured pass draw as it did, each the
+    same.  A pass raises ValueError for a tensor of another shape, type
     or device, or without contiguous rows."""
 
     def __init__(self, width, hidden, act="silu", drop=0.0, generator=None, eps=1e-5, seed=0):
@@ -91,6 +92,7 @@ class FeedForwardBlock:
         cx, cn, mean, rstd, gu, dtype, step = self._held
         T, K, F, dev = cx.rows, self.width, self.hidden, self.weight.device
         lddy = _pitch(dy, T, K, dev, (dtype,))
+        self._held = None  # G and U are written over: held once, also by a pass that fails
         do = torch.empty((T, K), dtype=_BF16, device=dev)
         L.check(L.gemm_dropout_backward(T, K, dy, lddy, _TYPE[dtype], do, K, L.GEMM_TYPE_BF16, self.drop, self.seed,
                                         step))
@@ -110,7 +112,6 @@ class FeedForwardBlock:
                                           rstd, dn, K, L.GEMM_TYPE_BF16, dx, K, _TYPE[dtype], dgamma, dbeta))
         self.dgamma += dgamma
         self.dbeta += dbeta
-        self._held = None
         return dx.add_(dy)
 
 

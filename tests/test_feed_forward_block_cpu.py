@@ -45,6 +45,15 @@ def test_backward_refuses(dy):
     assert b._held is not None, "the activations stay held"
 
 
+def test_a_backward_pass_that_fails_holds_nothing():
+    """It may have written over G and U."""
+    b = block(BF16)
+    with pytest.raises(AssertionError, match="library"):
+        b.backward(torch.zeros((T, K), dtype=BF16))
+    with pytest.raises(RuntimeError):
+        b.backward(torch.zeros((T, K), dtype=BF16))
+
+
 def test_backward_without_a_forward_pass():
     with pytest.raises(RuntimeError):
         block().backward(torch.zeros((T, K), dtype=BF16))
