@@ -29,7 +29,7 @@ struct FewCfg {
   static constexpr uint32_t kStageBytes = kWBytes + TN * kRowBytes;
   static constexpr int kCtasPerSm = 3;
   // shared memory of an SM (228 KB, 1 KB a CTA taken) among its CTAs
-  static constexpr int kStages = (int)((227u * 1024u / kCtasPerSm - 3072u) / kStageBytes);
+  static constexpr int kStages = (int)((227u * 1024u / kCtasPerSm - 3u * 1024u) / kStageBytes);
   static constexpr uint32_t kTmemCols = pow2_at_least(TN);
   static constexpr uint32_t kRingBytes = kStages * kStageBytes;
   static_assert(kRingBytes >= kFewRows * TN * 4, "the sums are laid over the ring");

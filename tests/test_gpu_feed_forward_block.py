@@ -24,7 +24,9 @@ def values(c):
 @pytest.mark.parametrize("T,K,F,act,drop,dtype", [(200, 128, 192, "silu", 0.1, torch.bfloat16),
                                                   (77, 130, 101, "gelu", 0.25, torch.float32),
                                                   (40, 64, 96, "relu", 0.0, torch.bfloat16),
-                                                  (300, 96, 160, "gelu_tanh", 0.5, torch.float32)])
+                                                  (300, 96, 160, "gelu_tanh", 0.5, torch.float32),
+                                                  (1, 72, 40, "silu", 0.1, torch.bfloat16),
+                                                  (65, 33, 47, "silu", 0.1, torch.float32)])
 def test_gradients(T, K, F, act, drop, dtype, monkeypatch):
     """Each gradient against the 64-bit formula on what its call read, so that a
     bound is that call's alone: what the block hands from call to call is taken
@@ -145,3 +147,40 @@ def test_steps_draw_apart_and_the_backward_pass_draws_the_same():
         k = A.keep(16, 64, 0.5, 3, step)
         assert (dropped.cpu().numpy() | k).all() and not (kept[-1] & ~k).any()
     assert (kept[0] != kept[1]).any()
+
+
+def test_no_tokens():
+    b = FB.FeedForwardBlock(64, 96, drop=0.1)
+    x = torch.empty((0, 64), device="cuda")
+    assert b.forward(x).shape == (0, 64) and b.backward(x).shape == (0, 64)
+    assert not any(g.any() for g in (b.dgamma, b.dbeta, b.dweight, b.ddown))
+
+
+def test_a_captured_pass():
+    """Both passes in a graph, with a block that runs eagerly beside it: the
+    replay gives what the eager passes give, of the inputs it finds then."""
+    T, K, F = 200, 64, 96
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    b = FB.FeedForwardBlock(K, F, "silu", 0.25, gen, seed=9)
+    x, dy = (torch.randn((T, K), device="cuda", generator=gen) for _ in range(2))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        b.forward(x)
+        b.backward(dy)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            b.step = 5
+            b.zero_grad()
+            y = b.forward(x)
+            dx = b.backward(dy)
+        for _ in range(2):
+            x.copy_(torch.randn((T, K), device="cuda", generator=gen))
+            graph.replay()
+            got = [t.clone() for t in (y, dx, b.dweight, b.ddown, b.dgamma, b.dbeta)]
+            b.step = 5
+            b.zero_grad()
+            want = [b.forward(x), b.backward(dy), b.dweight, b.ddown, b.dgamma, b.dbeta]
+            assert all(torch.equal(g, w) for g, w in zip(got, want))
+    torch.cuda.current_stream().wait_stream(side)

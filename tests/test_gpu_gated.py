@@ -52,7 +52,8 @@ def check_forward(T, K, F, act, layout, pad=0, off=0, save=True, scale=1.0):
 FORWARD = [(1, 1, 1), (1, 64, 64), (1, 4096, 1000), (2, 777, 129), (3, 72, 65), (8, 512, 2048), (15, 200, 96),
            (16, 1500, 192), (17, 64, 31), (33, 328, 777), (48, 1024, 1376), (64, 130, 512), (65, 96, 64), (100, 4096, 256),
            (127, 64, 1501), (128, 520, 640), (129, 256, 200), (200, 1000, 136), (256, 64, 384), (300, 777, 301),
-           (513, 192, 264), (1000, 128, 130), (129, 4096, 264), (600, 2048, 1504), (2100, 256, 2000)]
+           (513, 192, 264), (1000, 128, 130), (129, 4096, 264), (600, 2048, 1504), (2100, 256, 2000), (20000, 3, 5),
+           (9000, 8, 8)]
 
 
 @pytest.mark.parametrize("layout", [KN, NK], ids=NAMES.get)
@@ -174,7 +175,7 @@ def test_backward(T, F, act):
 DOWN = [(1, 1, 1), (1, 4096, 640), (3, 777, 33), (16, 64, 64), (40, 328, 200), (100, 1000, 129), (128, 128, 256),
         (129, 96, 777), (256, 512, 320), (300, 777, 301), (513, 64, 264), (1000, 136, 130), (70, 2048, 1376),
         (300, 4096, 520), (600, 2048, 1504), (130, 3000, 1000), (2100, 256, 2008), (90, 100, 32), (300, 64, 96),
-        (1000, 520, 480), (2100, 256, 2016), (129, 4096, 544), (300, 4096, 352)]
+        (1000, 520, 480), (2100, 256, 2016), (129, 4096, 544), (300, 4096, 352), (20000, 3, 5), (9000, 8, 8)]
 
 
 def down_grad(T, N, F, act, layout, pad=0, off=0, held=True, in_place=False):
