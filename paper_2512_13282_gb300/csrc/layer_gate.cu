@@ -140,9 +140,13 @@ constexpr TileCost kForwardTiles[] = {{{true, 256}, 0.345, 0.5, 5.0}, {{false, 1
 constexpr TileCost kBackwardTiles[] = {
     {{true, 256}, 0.345, 4.5, 12.0}, {{false, 128}, 0.31, 2.0, 6.0}, {{false, 64}, 0.28, 1.5, 4.0}};
 // A split tail besides: the reduction's launch, the partials written and read.
-// 2048 tokens 4096 x 11008 forward: 214 us whole, 204 with a tail; 300 tokens 776
-// x 1504 backward: 15.9 and 19.
-constexpr double kTailFixedUs = 6.0, kTailUsPerMB = 0.36;
+// After whole rounds its units wait for the slowest of them; where the tail is
+// all there is they start at once, and backward the reduction takes the
+// epilogue too, on all SMs.  2048 tokens 4096 x 11008 forward: 214 us whole, 204
+// with a tail; one round of tiles, whole and split: 80 tokens 2048 x 1024 forward
+// 12.6, 9.5, backward of 256 tokens 2048 x 1024 15.4, 10.2, 512 tokens 4096 x
+// 2048 25.2, 21.8.
+constexpr double kTailFixedUs = 6.0, kTailAloneForwardUs = 2.0, kTailAloneBackwardUs = 0.0, kTailUsPerMB = 0.36;
 
 struct GatedPlan {
   GatedTile tile;
@@ -177,7 +181,8 @@ GatedPlan plan_gated(const TileCost (&tiles)[N], int64_t T, int64_t K, int64_t F
       double us = full * whole;
       if (rem > 0) us += kb_per * c.kb_us + c.unit_us;
       us += c.last_us;
-      if (parts > 1) us += kTailFixedUs + kTailUsPerMB * (double)parts * rem * tile_m * c.tile.bn * 4e-6;
+      const double tail_us = full > 0 ? kTailFixedUs : forward ? kTailAloneForwardUs : kTailAloneBackwardUs;
+      if (parts > 1) us += tail_us + kTailUsPerMB * (double)parts * rem * tile_m * c.tile.bn * 4e-6;
       if (best_us >= 0 && us >= best_us) continue;
       best_us = us;
       best.tile = c.tile;
