@@ -9,7 +9,10 @@
 //              slope s + g s (1 - s) 2 z'
 //   relu       g where g > 0, else 0; slope 1 there, else 0
 // In these forms nothing cancels at the negative end, where the values are
-// small, so float32 keeps their relative accuracy.  A NaN stays one.
+// small, and the quotients' divisors lie in 1 .. 5 there, so that they keep their
+// relative accuracy (2^-14, mostly the exponential's of a large argument) as far
+// down as act(g) is a normal number: g = -91.8, -13.1 and -10.1 of the first
+// three.  A NaN stays one.
 #pragma once
 #include "layer_internal.h"
 
@@ -20,14 +23,16 @@ struct GateValue {
   float slope;  // act'(g)
 };
 
-// s(x) and 1 - s(x), which is not taken as a difference where it is small (a
-// unit in s's last place would come back multiplied by x).
+// s(x) and 1 - s(x).  With e = exp(-|x|) one of them is 1 / (1 + e) and the other
+// e / (1 + e): neither a difference where it is small (a unit in s's last place
+// would come back multiplied by x) nor the inverse of a divisor above 2^126, of
+// which __fdividef gives 0.
 struct Logistic {
   float s, t;
 };
 __device__ __forceinline__ Logistic logistic(float x) {
-  const float e = __expf(-x), s = __fdividef(1.f, 1.f + e);
-  return Logistic{s, x > 0.f ? e * s : 1.f - s};
+  const float e = __expf(-fabsf(x)), r = __fdividef(1.f, 1.f + e), er = e * r;
+  return x > 0.f ? Logistic{r, er} : Logistic{er, r};
 }
 
 // P(g) and exp(-g^2 / 2).  The upper tail past x = |g| is exp(-x^2 / 2) R(x) with
