@@ -106,13 +106,17 @@ class FeedForwardBlock:
         # [dG dU] . W^T: W as stored is the transposed factor, column-major
         dn = torch.empty((T, K), dtype=_BF16, device=dev)
         G.check(G.gemm_bf16_f32acc_bf16(T, K, 2 * F, gu, 2 * F, self.weight, 2 * F, G.GEMM_B_COL_MAJOR_NxK, dn, K))
-        dx = torch.empty((T, K), dtype=dtype, device=dev)
+        # layer_norm'(dn) stays float32 until dy has been added (dropout's call with a
+        # share of 0 is that sum), so that a bf16 dx is rounded once
+        dl = torch.empty((T, K), device=dev)
         dgamma, dbeta = torch.empty_like(self.gamma), torch.empty_like(self.beta)
         L.check(L.gemm_layernorm_backward(T, K, None, 0, L.GEMM_TYPE_F32, *cx.args, self.gamma, L.GEMM_TYPE_F32, mean,
-                                          rstd, dn, K, L.GEMM_TYPE_BF16, dx, K, _TYPE[dtype], dgamma, dbeta))
+                                          rstd, dn, K, L.GEMM_TYPE_BF16, dl, K, L.GEMM_TYPE_F32, dgamma, dbeta))
         self.dgamma += dgamma
         self.dbeta += dbeta
-        return dx.add_(dy)
+        dx = dl if dtype == torch.float32 else torch.empty((T, K), dtype=dtype, device=dev)
+        L.check(L.gemm_dropout_forward(T, K, dl, K, L.GEMM_TYPE_F32, dy, lddy, dx, K, _TYPE[dtype], 0.0, 0, 0))
+        return dx
 
 
 def train(tokens, width, hidden, steps, act="silu", drop=0.0, report=print):
