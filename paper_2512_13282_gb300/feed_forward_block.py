@@ -35,20 +35,23 @@ class FeedForwardBlock:
     """Parameters, float32 gradients (accumulated until ``zero_grad``) and the
     two passes.  x and y are bf16 or float32 (a residual stream); the weights
     are bf16, row-major: W is width x 2 hidden (Wg, then Wu), Wd hidden x width.
-    ``drop`` is dropout's share, ``seed`` its key; each forward pass draws with
-    the next step; the replays of a captured pass draw as it did, each the
-    same.  A pass raises ValueError for a tensor of another shape, type
-    or device, or without contiguous rows."""
+    ``drop`` is dropout's share, ``seed`` its key: one drawn after the weights
+    if none is given, so that blocks drop apart from one another (processes
+    whose generators are alike, as those of one set of weights are, need seeds).
+    Each forward pass draws with the next step; the replays of a captured pass
+    draw as it did, each the same.  A pass raises ValueError for a tensor of
+    another shape, type or device, or without contiguous rows."""
 
-    def __init__(self, width, hidden, act="silu", drop=0.0, generator=None, eps=1e-5, seed=0):
+    def __init__(self, width, hidden, act="silu", drop=0.0, generator=None, eps=1e-5, seed=None):
         if act not in ACTIVATIONS or not 0 <= drop < 1:
             raise ValueError(f"an activation of {', '.join(ACTIVATIONS)} and a share in [0, 1), not {act} and {drop}")
         dev = dict(device="cuda", generator=generator)
-        self.width, self.hidden, self.act, self.drop, self.eps, self.seed = width, hidden, act, drop, eps, seed
+        self.width, self.hidden, self.act, self.drop, self.eps = width, hidden, act, drop, eps
         self.gamma = torch.ones(width, device="cuda")
         self.beta = torch.zeros(width, device="cuda")
         self.weight = (torch.randn((width, 2 * hidden), **dev) / width ** 0.5).to(_BF16)
         self.down = (torch.randn((hidden, width), **dev) / hidden ** 0.5).to(_BF16)
+        self.seed = int(torch.randint(2 ** 63 - 1, (), **dev)) if seed is None else seed
         self.dgamma, self.dbeta = torch.zeros_like(self.gamma), torch.zeros_like(self.beta)
         self.dweight = torch.zeros((width, 2 * hidden), device="cuda")
         self.ddown = torch.zeros((hidden, width), device="cuda")
@@ -122,8 +125,8 @@ class FeedForwardBlock:
 def train(tokens, width, hidden, steps, act="silu", drop=0.0, report=print):
     """Losses of `steps` steps of gradient descent towards a fixed block."""
     gen = torch.Generator(device="cuda").manual_seed(1)
-    teacher = FeedForwardBlock(width, hidden, act, 0.0, gen)
-    block = FeedForwardBlock(width, hidden, act, drop, gen)
+    teacher = FeedForwardBlock(width, hidden, act, 0.0, gen, seed=0)
+    block = FeedForwardBlock(width, hidden, act, drop, gen, seed=0)
     masters = [block.weight.float(), block.down.float()]
     losses = []
     for step in range(steps):
