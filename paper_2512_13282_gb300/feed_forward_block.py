@@ -31,6 +31,11 @@ ACTIVATIONS = {"silu": L.GEMM_ACT_SILU, "gelu": L.GEMM_ACT_GELU, "gelu_tanh": L.
 _BF16 = torch.bfloat16
 
 
+def _drawn(step):
+    """Dropout's step arguments: a number, and what is added to it on the device."""
+    return step if isinstance(step, tuple) else (step, None)
+
+
 class FeedForwardBlock:
     """Parameters, float32 gradients (accumulated until ``zero_grad``) and the
     two passes.  x and y are bf16 or float32 (a residual stream); the weights
@@ -38,9 +43,15 @@ class FeedForwardBlock:
     ``drop`` is dropout's share, ``seed`` its key: one drawn after the weights
     if none is given, so that blocks drop apart from one another (processes
     whose generators are alike, as those of one set of weights are, need seeds).
-    Each forward pass draws with the next step; the replays of a captured pass
-    draw as it did, each the same.  A pass raises ValueError for a tensor of
-    another shape, type or device, or without contiguous rows."""
+    Each forward pass draws with the next ``step``, each replay of a captured one
+    too.  A pass raises ValueError for a tensor of another shape, type or device,
+    or without contiguous rows."""
+
+    # The next step is _start, which passes count up on the host; from the first
+    # captured pass on it is _start + _word, and all passes count the word up on
+    # the device, as replays do.  (That takes two launches: 30 us of an eager
+    # forward pass of few tokens, 73 without.)
+    _start, _word, _counted = 0, None, False
 
     def __init__(self, width, hidden, act="silu", drop=0.0, generator=None, eps=1e-5, seed=None):
         if act not in ACTIVATIONS or not 0 <= drop < 1:
@@ -55,8 +66,28 @@ class FeedForwardBlock:
         self.dgamma, self.dbeta = torch.zeros_like(self.gamma), torch.zeros_like(self.beta)
         self.dweight = torch.zeros((width, 2 * hidden), device="cuda")
         self.ddown = torch.zeros((hidden, width), device="cuda")
-        self.step = 0
+        self._word = torch.zeros((), dtype=torch.int64, device="cuda")
         self._held = None
+
+    def _on_device(self):
+        """Whether steps are counted on the device."""
+        if self._word is not None and not self._counted:
+            self._counted = torch.cuda.is_current_stream_capturing()
+        return self._counted
+
+    @property
+    def step(self):
+        """The step of the next forward pass, modulo 2^64.  Reading it waits for
+        the device once a pass has been captured; set within a capture, it is set
+        by every replay."""
+        return (self._start + (int(self._word) if self._counted else 0)) % 2 ** 64
+
+    @step.setter
+    def step(self, value):
+        if self._on_device():
+            self._word.fill_((value - self._start + 2 ** 63) % 2 ** 64 - 2 ** 63)
+        else:
+            self._start = value % 2 ** 64
 
     def zero_grad(self):
         for g in (self.dgamma, self.dbeta, self.dweight, self.ddown):
@@ -75,10 +106,15 @@ class FeedForwardBlock:
                                      L.GEMM_B_ROW_MAJOR_KxN, ACTIVATIONS[self.act], h, F, gu, 2 * F, gu[:, F:], 2 * F))
         o, y = torch.empty((T, K), dtype=_BF16, device=dev), torch.empty((T, K), dtype=x.dtype, device=dev)
         G.check(G.gemm_bf16_f32acc_bf16(T, K, F, h, F, self.down, K, G.GEMM_B_ROW_MAJOR_KxN, o, K))
+        # this pass's step, and its backward pass's
+        step = (self._start, self._word.clone()) if self._on_device() else self._start
         L.check(L.gemm_dropout_forward(T, K, o, K, L.GEMM_TYPE_BF16, x, ldx, y, K, _TYPE[x.dtype], self.drop, self.seed,
-                                       self.step))
-        self._held = (cx, cn, mean, rstd, gu, x.dtype, self.step)
-        self.step += 1
+                                       *_drawn(step)))
+        self._held = (cx, cn, mean, rstd, gu, x.dtype, step)
+        if self._counted:
+            self._word += 1
+        else:
+            self._start += 1
         return y
 
     @property
@@ -98,7 +134,7 @@ class FeedForwardBlock:
         self._held = None  # G and U are written over: held once, also by a pass that fails
         do = torch.empty((T, K), dtype=_BF16, device=dev)
         L.check(L.gemm_dropout_backward(T, K, dy, lddy, _TYPE[dtype], do, K, L.GEMM_TYPE_BF16, self.drop, self.seed,
-                                        step))
+                                        *_drawn(step)))
         ch = Checkpoint(T, F, dev)
         L.check(L.gemm_gated_down_backward(T, K, F, do, K, self.down, K, L.GEMM_B_ROW_MAJOR_KxN, gu, 2 * F, gu[:, F:],
                                            2 * F, ACTIVATIONS[self.act], gu, 2 * F, gu[:, F:], 2 * F, *ch.args))
