@@ -24,7 +24,7 @@ import torch
 
 from . import gemm as G
 from . import layer as L
-from .projection_block import _TYPE, Checkpoint, _pitch
+from .projection_block import _TYPE, Checkpoint, _pitch, _read_here
 
 ACTIVATIONS = {"silu": L.GEMM_ACT_SILU, "gelu": L.GEMM_ACT_GELU, "gelu_tanh": L.GEMM_ACT_GELU_TANH,
                "relu": L.GEMM_ACT_RELU}
@@ -45,13 +45,15 @@ class FeedForwardBlock:
     whose generators are alike, as those of one set of weights are, need seeds).
     Each forward pass draws with the next ``step``, each replay of a captured one
     too.  A pass raises ValueError for a tensor of another shape, type or device,
-    or without contiguous rows."""
+    or without contiguous rows.  The backward pass may run on another stream, one
+    that waits for the forward pass."""
 
     # The next step is _start, which passes count up on the host; from the first
     # captured pass on it is _start + _word, and all passes count the word up on
     # the device, as replays do.  (That takes two launches: 30 us of an eager
     # forward pass of few tokens, 73 without.)
     _start, _word, _counted = 0, None, False
+    _home = None  # the last forward pass's stream
 
     def __init__(self, width, hidden, act="silu", drop=0.0, generator=None, eps=1e-5, seed=None):
         if act not in ACTIVATIONS or not 0 <= drop < 1:
@@ -110,7 +112,7 @@ class FeedForwardBlock:
         step = (self._start, self._word.clone()) if self._on_device() else self._start
         L.check(L.gemm_dropout_forward(T, K, o, K, L.GEMM_TYPE_BF16, x, ldx, y, K, _TYPE[x.dtype], self.drop, self.seed,
                                        *_drawn(step)))
-        self._held = (cx, cn, mean, rstd, gu, x.dtype, step)
+        self._held, self._home = (cx, cn, mean, rstd, gu, x.dtype, step), G._stream(None)
         if self._counted:
             self._word += 1
         else:
@@ -132,6 +134,7 @@ class FeedForwardBlock:
         T, K, F, dev = cx.rows, self.width, self.hidden, self.weight.device
         lddy = _pitch(dy, T, K, dev, (dtype,))
         self._held = None  # G and U are written over: held once, also by a pass that fails
+        _read_here((cx.q, cx.e, cn.q, cn.e, mean, rstd, gu, _drawn(step)[1]), self._home)
         do = torch.empty((T, K), dtype=_BF16, device=dev)
         L.check(L.gemm_dropout_backward(T, K, dy, lddy, _TYPE[dtype], do, K, L.GEMM_TYPE_BF16, self.drop, self.seed,
                                         *_drawn(step)))

@@ -37,6 +37,18 @@ def _pitch(x, rows, cols, device, types=tuple(_TYPE)):
     return x.stride(0) if rows > 1 else cols
 
 
+def _read_here(tensors, home):
+    """Has torch's allocator keep the memory of tensors that a pass on the stream
+    of handle `home` has left until what the current stream has been given by then
+    is done: freed, it would go to the next allocation on `home`, whose kernels do
+    not wait for this stream's."""
+    if home is not None and G._stream(None) != home:
+        here = torch.cuda.current_stream()
+        for t in tensors:
+            if isinstance(t, torch.Tensor):
+                t.record_stream(here)
+
+
 class Checkpoint:
     """An activation held in 8 bits on the device (see gb300_layer.h)."""
 
@@ -70,7 +82,10 @@ class ProjectionBlock:
     """Parameters, float32 gradients (accumulated until ``zero_grad``) and the
     two passes.  x may be bf16 or float32 (a residual stream); W is bf16,
     K x N row-major.  A pass raises ValueError for a tensor of another shape,
-    type or device, or without contiguous rows."""
+    type or device, or without contiguous rows.  The backward pass may run on
+    another stream, one that waits for the forward pass."""
+
+    _home = None  # the last forward pass's stream
 
     def __init__(self, width, out, generator=None, eps=1e-5):
         dev = dict(device="cuda", generator=generator)
@@ -96,7 +111,7 @@ class ProjectionBlock:
                                          L.GEMM_TYPE_F32, self.eps, y, K, L.GEMM_TYPE_BF16, mean, rstd, *cy.args))
         o = torch.empty((T, N), dtype=torch.bfloat16, device=dev)
         G.check(G.gemm_bf16_f32acc_bf16(T, N, K, y, K, self.weight, N, G.GEMM_B_ROW_MAJOR_KxN, o, N))
-        self._held = (cx, cy, mean, rstd, x.dtype)
+        self._held, self._home = (cx, cy, mean, rstd, x.dtype), G._stream(None)
         return o
 
     @property
@@ -113,6 +128,7 @@ class ProjectionBlock:
         cx, cy, mean, rstd, dtype = self._held
         T, K, N, dev = cx.rows, self.width, self.out, self.weight.device
         lddo = _pitch(do, T, N, dev, (torch.bfloat16,))
+        _read_here((cx.q, cx.e, cy.q, cy.e, mean, rstd), self._home)
         # do . W^T: W as stored (K x N) is the transposed factor N x K, column-major
         dy = torch.empty((T, K), dtype=torch.bfloat16, device=dev)
         G.check(G.gemm_bf16_f32acc_bf16(T, K, N, do, lddo, self.weight, N, G.GEMM_B_COL_MAJOR_NxK, dy, K))
