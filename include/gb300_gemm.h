@@ -52,8 +52,10 @@
  *     GB300_GEMM_TINY_MAX_MACS (largest M*N*K of an int8 GEMM computed in one
  *     launch on the CUDA cores; 0 disables that kernel, and so does forcing
  *     a tile width, family or split with the variables above) and
- *     GB300_GEMM_DEBUG=1 (prints each plan to stderr).  They are read once,
- *     at the first call, and again by gemm_reload_overrides().
+ *     GB300_GEMM_DEBUG=1 (prints each plan to stderr).  The gated feed-forward
+ *     calls of gb300_layer.h follow BN, PAIR, TAIL_SPLITS (any round of tiles
+ *     that is not full counts as a last one there) and DEBUG.  They are read
+ *     once, at the first call, and again by gemm_reload_overrides().
  *     GB300_GEMM_WAIT_LIMIT_MS (read once) bounds every device-side wait
  *     (default 2000 ms).
  */

@@ -1224,6 +1224,10 @@ bool float_out_map(CUtensorMap *map, bool bf16, const void *base, uint64_t N, ui
 }
 
 bool tma_store_enabled() { return overrides().tma_store; }
+TileOverrides tile_overrides() {
+  const Overrides o = overrides();
+  return TileOverrides{o.bn, o.pair, o.tail_splits, o.debug};
+}
 
 gemm_status_t validate_s8(int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, const void *B,
                           int64_t ldb, int b_layout, const void *C, int64_t ldc) {

@@ -83,6 +83,13 @@ bool float_out_map(CUtensorMap *map, bool bf16, const void *base, uint64_t N, ui
                    uint64_t splits);
 // Whether outputs are to go through TMA stores (GB300_GEMM_TMA_STORE).
 bool tma_store_enabled();
+// The planner overrides that the gated feed-forward block's plans follow too:
+// tile width (0: none), family (-1), split tail (-1), plans printed.
+struct TileOverrides {
+  int bn, pair, tail_splits;
+  bool debug;
+};
+TileOverrides tile_overrides();
 
 // One compiled variant of the tcgen05 kernel.
 struct TcVariant {

@@ -1,8 +1,7 @@
 // layer_gate.cu -- the gated feed-forward block's gate: planning and staging of
 // the kernel that takes it with the projections (gated_tc.cuh), and the kernel
 // of its gradient alone.
-#include <atomic>
-#include <cmath>
+#include <cstdio>
 
 #include "gate_math.cuh"
 #include "layer_rows.cuh"
@@ -157,45 +156,58 @@ struct GatedPlan {
     return (size_t)tail_splits * ((size_t)tiles_m * tiles_n - tail_first) * tile_m() * tile.bn * 4;
   }
 };
-// Tile shape, split tail and grid of the least modelled time.
+// Tile shape, split tail and grid of the least modelled time, among those that
+// the planner overrides leave: first with a forced tail (a split of 2 or more
+// where the plan has a round to split), then without, then without a forced tile
+// that is not compiled.
 template <size_t N>
 GatedPlan plan_gated(const TileCost (&tiles)[N], int64_t T, int64_t K, int64_t F, bool forward, int sms, int pairs) {
   GatedPlan best{};
   double best_us = -1;
   const int64_t num_kb = ceil_div64(K, kBK);
-  for (const TileCost &c : tiles) {
-    const int64_t slots = c.tile.pair ? pairs : sms;
-    if (slots <= 0) continue;
-    const int tile_m = c.tile.pair ? 2 * kBM : kBM;
-    const int64_t tm = ceil_div64(T, tile_m), tn = ceil_div64(F, forward ? c.tile.bn / 2 : c.tile.bn), all = tm * tn;
-    const int64_t full = all / slots, rem = all % slots;
-    const double whole = num_kb * c.kb_us + c.unit_us;
-    for (int64_t s = 1; s <= 16; ++s) {
-      int64_t kb_per = num_kb, parts = 1;
-      if (s > 1) {
-        if (rem == 0 || rem * s > slots) break;
-        kb_per = ceil_div64(num_kb, s);
-        parts = ceil_div64(num_kb, kb_per);  // no part is empty
-        if (parts != s || kb_per < 4) continue;
+  const TileOverrides ovr = tile_overrides();
+  for (int pass = ovr.tail_splits >= 2 ? 0 : 1; pass < 3 && best_us < 0; ++pass) {
+    for (const TileCost &c : tiles) {
+      if (pass < 2 && ((ovr.bn > 0 && ovr.bn != c.tile.bn) || (ovr.pair >= 0 && (ovr.pair != 0) != c.tile.pair))) continue;
+      const int64_t slots = c.tile.pair ? pairs : sms;
+      if (slots <= 0) continue;
+      const int tile_m = c.tile.pair ? 2 * kBM : kBM;
+      const int64_t tm = ceil_div64(T, tile_m), tn = ceil_div64(F, forward ? c.tile.bn / 2 : c.tile.bn), all = tm * tn;
+      const int64_t full = all / slots, rem = all % slots;
+      const double whole = num_kb * c.kb_us + c.unit_us;
+      const int64_t first = pass == 0 ? ovr.tail_splits : 1, last = pass == 0 ? first : ovr.tail_splits == 0 ? 1 : 16;
+      for (int64_t s = first; s <= last; ++s) {
+        int64_t kb_per = num_kb, parts = 1;
+        if (s > 1) {
+          if (rem == 0 || rem * s > slots) break;
+          kb_per = ceil_div64(num_kb, s);
+          parts = ceil_div64(num_kb, kb_per);  // no part is empty
+          if (parts != s || kb_per < 4) continue;
+        }
+        double us = full * whole;
+        if (rem > 0) us += kb_per * c.kb_us + c.unit_us;
+        us += c.last_us;
+        const double tail_us = full > 0 ? kTailFixedUs : forward ? kTailAloneForwardUs : kTailAloneBackwardUs;
+        if (parts > 1) us += tail_us + kTailUsPerMB * (double)parts * rem * tile_m * c.tile.bn * 4e-6;
+        if (best_us >= 0 && us >= best_us) continue;
+        best_us = us;
+        best.tile = c.tile;
+        best.tiles_m = (int)tm;
+        best.tiles_n = (int)tn;
+        best.num_kb = (int)num_kb;
+        best.tail_first = parts > 1 ? (int)(full * slots) : 0;
+        best.tail_splits = parts > 1 ? (int)parts : 0;
+        best.tail_kb_per = parts > 1 ? (int)kb_per : 0;
+        const int64_t units = parts > 1 ? full * slots + rem * parts : all;
+        best.grid = (int)(units < slots ? units : slots) * (c.tile.pair ? 2 : 1);
       }
-      double us = full * whole;
-      if (rem > 0) us += kb_per * c.kb_us + c.unit_us;
-      us += c.last_us;
-      const double tail_us = full > 0 ? kTailFixedUs : forward ? kTailAloneForwardUs : kTailAloneBackwardUs;
-      if (parts > 1) us += tail_us + kTailUsPerMB * (double)parts * rem * tile_m * c.tile.bn * 4e-6;
-      if (best_us >= 0 && us >= best_us) continue;
-      best_us = us;
-      best.tile = c.tile;
-      best.tiles_m = (int)tm;
-      best.tiles_n = (int)tn;
-      best.num_kb = (int)num_kb;
-      best.tail_first = parts > 1 ? (int)(full * slots) : 0;
-      best.tail_splits = parts > 1 ? (int)parts : 0;
-      best.tail_kb_per = parts > 1 ? (int)kb_per : 0;
-      const int64_t units = parts > 1 ? full * slots + rem * parts : all;
-      best.grid = (int)(units < slots ? units : slots) * (c.tile.pair ? 2 : 1);
     }
   }
+  if (ovr.debug)
+    std::fprintf(stderr, "[gb300_gemm] gated %s %lldx%lldx%lld: %s %d, %dx%d tiles, %d in whole, tail split in %d\n",
+                 forward ? "forward" : "backward", (long long)T, (long long)K, (long long)F,
+                 best.tile.pair ? "pair" : "single", best.tile.bn, best.tiles_m, best.tiles_n,
+                 best.tail_splits ? best.tail_first : best.tiles_m * best.tiles_n, best.tail_splits);
   return best;
 }
 
