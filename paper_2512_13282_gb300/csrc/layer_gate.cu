@@ -149,7 +149,7 @@ constexpr double kTailFixedUs = 6.0, kTailAloneForwardUs = 2.0, kTailAloneBackwa
 
 struct GatedPlan {
   GatedTile tile;
-  int tiles_m, tiles_n, num_kb, grid;
+  int tiles_m, tiles_n, grid;
   int tail_first, tail_splits, tail_kb_per;
   int tile_m() const { return tile.pair ? 2 * kBM : kBM; }
   size_t partial_bytes() const {
@@ -194,7 +194,6 @@ GatedPlan plan_gated(const TileCost (&tiles)[N], int64_t T, int64_t K, int64_t F
         best.tile = c.tile;
         best.tiles_m = (int)tm;
         best.tiles_n = (int)tn;
-        best.num_kb = (int)num_kb;
         best.tail_first = parts > 1 ? (int)(full * slots) : 0;
         best.tail_splits = parts > 1 ? (int)parts : 0;
         best.tail_kb_per = parts > 1 ? (int)kb_per : 0;
@@ -276,11 +275,11 @@ cudaError_t pack_operands(Operand *o, int n, uint8_t *at, const OpContext &c) {
 }
 
 // Packs what has to be of the n operands (the first is A, the others weights of
-// layout km), makes their maps, and launches.
+// layout km), makes their maps, and launches: the kernel of few tokens, or the plan.
 gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool forward, GatedTcParams &p,
                         const OpContext &c) {
   const bool few = p.T <= kFewTokens;
-  if (pl.grid <= 0) return GEMM_ERR_CUDA;
+  if (!few && pl.grid <= 0) return GEMM_ERR_CUDA;
   size_t packed = 0;
   for (int i = 0; i < n; ++i) packed += o[i].bytes();
   const size_t need = packed + (few ? 0 : pl.partial_bytes());
@@ -301,7 +300,7 @@ gemm_status_t run_gated(const GatedPlan &pl, Operand *o, int n, bool km, bool fo
                       km ? part : kBK))
       return GEMM_ERR_CUDA;
   if (n < 3) m.b[1] = m.b[0];
-  p.num_kb = pl.num_kb;
+  p.num_kb = (int)ceil_div64(o[0].cols, kBK);
   p.err = c.err;
   p.wait_limit_ns = c.wait_limit_ns;
   if (few) {
@@ -346,10 +345,12 @@ gemm_status_t gated_forward(const GatedForward &p, const OpContext &c) {
   const int64_t wr = p.w_kmajor ? p.F : p.K, wc = p.w_kmajor ? p.K : p.F;
   Operand o[3] = {{p.x, p.T, p.K, p.ldx}, {p.wg, wr, wc, p.ldwg}, {p.wu, wr, wc, p.ldwu}};
   GatedTcParams t{};
-  t.T = (int)p.T, t.F = p.F, t.K = p.K, t.act = p.act;
+  t.T = (int)p.T, t.F = p.F, t.act = p.act;
   t.out[0] = p.h, t.out[1] = p.g, t.out[2] = p.u;
   t.ldout[0] = p.ldh, t.ldout[1] = p.ldg, t.ldout[2] = p.ldu;
-  return run_gated(plan_gated(kForwardTiles, p.T, p.K, p.F, true, c.sms, pair_slots()), o, 3, p.w_kmajor, true, t, c);
+  const GatedPlan pl =
+      p.T > kFewTokens ? plan_gated(kForwardTiles, p.T, p.K, p.F, true, c.sms, pair_slots()) : GatedPlan{};
+  return run_gated(pl, o, 3, p.w_kmajor, true, t, c);
 }
 
 gemm_status_t gated_down_backward(const GatedDownBackward &p, const OpContext &c) {
@@ -357,13 +358,14 @@ gemm_status_t gated_down_backward(const GatedDownBackward &p, const OpContext &c
   const int64_t wr = p.w_kmajor ? b.F : p.N, wc = p.w_kmajor ? p.N : b.F;
   Operand o[2] = {{p.d, b.T, p.N, p.ldd}, {p.w, wr, wc, p.ldw}};
   GatedTcParams t{};
-  t.T = (int)b.T, t.F = b.F, t.K = p.N, t.act = b.act;
+  t.T = (int)b.T, t.F = b.F, t.act = b.act;
   t.out[0] = b.dg, t.out[1] = b.du;
   t.ldout[0] = b.lddg, t.ldout[1] = b.lddu;
   t.gate = b.g, t.up = b.u, t.ldgate = b.ldg, t.ldup = b.ldu;
   t.ck = b.ck;
-  return run_gated(plan_gated(kBackwardTiles, b.T, p.N, b.F, false, c.sms, pair_slots()), o, 2, p.w_kmajor, false, t,
-                   c);
+  const GatedPlan pl =
+      b.T > kFewTokens ? plan_gated(kBackwardTiles, b.T, p.N, b.F, false, c.sms, pair_slots()) : GatedPlan{};
+  return run_gated(pl, o, 2, p.w_kmajor, false, t, c);
 }
 
 cudaError_t launch_gated_backward(const GatedBackward &p, const OpContext &c) {

@@ -156,7 +156,7 @@ gemm_status_t gated_down_backward(const GatedDownBackward &p, const OpContext &c
 
 // The tensor-core kernel of both (gated_tc.cuh).
 struct GatedTcParams {
-  int T, F, K;  // rows, features, reduction length
+  int T, F;  // rows, features
   int tiles_m, tiles_n, num_kb, group_m;
   // split tail, as in TcParams: the tiles from raster position tail_first on are
   // split into tail_splits (0: none) ranges of tail_kb_per k-blocks, whose sums
