@@ -129,8 +129,10 @@ auto backward_kernel(int act) {
 
 // Modelled cost of a tile shape: microseconds per k-block of 64, per unit
 // besides, and of the last unit's epilogue, which nothing hides.  Fitted to
-// forced plans on GB300 (19 sizes a direction, 65 to 8192 tokens): what the
-// model picks is 2 % off the fastest of them on average, 11 % at most.
+// forced plans on GB300 (19 sizes a direction).  Against all forced plans of 90
+// random sizes a direction (65 to 8192 tokens, reductions of 256 to 8192, 256 to
+// 12288 features; in graphs, on rotating operands) what the model picks is off the
+// fastest by 0.6 % forward and 2.5 % backward on average, by 11 and 22 % at most.
 struct TileCost {
   GatedTile tile;
   double kb_us, unit_us, last_us;
@@ -144,7 +146,7 @@ constexpr TileCost kBackwardTiles[] = {
 // epilogue too, on all SMs.  2048 tokens 4096 x 11008 forward: 214 us whole, 204
 // with a tail; one round of tiles, whole and split: 80 tokens 2048 x 1024 forward
 // 12.6, 9.5, backward of 256 tokens 2048 x 1024 15.4, 10.2, 512 tokens 4096 x
-// 2048 25.2, 21.8.
+// 2048 25.2, 20.9.
 constexpr double kTailFixedUs = 6.0, kTailAloneForwardUs = 2.0, kTailAloneBackwardUs = 0.0, kTailUsPerMB = 0.36;
 
 struct GatedPlan {
