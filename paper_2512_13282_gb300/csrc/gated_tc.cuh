@@ -22,7 +22,7 @@
 // 360 MB of traffic, 53 us.
 //
 // The tensor cores bound both: 8192 tokens 4096 x 11008 forward with G and U kept
-// 813 us in bursts (1.82 PFLOP/s), 925 back to back under the power cap; backward
+// 813 us in bursts (1.82 PFLOP/s), 917 back to back under the power cap; backward
 // 480 and 530, a round of tiles 25 us where a plain GEMM's takes 21, since what the
 // epilogue moves competes with the operands on their way from L2.
 #pragma once

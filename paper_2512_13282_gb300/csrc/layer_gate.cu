@@ -22,7 +22,7 @@ constexpr int kThreads = 256;
 // magnitude with shuffles.  VEC: all rows start on 16 bytes (the checkpoint's on
 // 8); else values are shifted between registers and the 16-byte pieces of memory
 // that they lie in.
-// The bytes bound many values (8192 x 11008 silu with the checkpoint: 139 us, 6.6
+// The bytes bound many values (8192 x 11008 silu with the checkpoint: 141 us, 7.1
 // TB/s), a thread's own chain of instructions few, for which V is 8.
 template <int ACT, bool VEC, int V>
 __global__ void __launch_bounds__(kThreads) gated_backward_kernel(const GatedBackward p, int64_t cols) {
