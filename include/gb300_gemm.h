@@ -134,8 +134,11 @@ gemm_status_t gemm_s8s8_s8(int64_t M, int64_t N, int64_t K,
  * nearest-even.  A, B, C are bf16 bit patterns (uint16_t).
  *   A: M x K row-major (lda >= K).  B: layout per b_layout.
  *   C: M x N row-major (ldc >= N), fully overwritten in [0,M) x [0,N).
- * Accuracy contract: |C - ref| <= 2^-8 |ref| + 2^-20 sum_k |a_ik b_kj| per
- * element, ref being the exact sum.
+ * Accuracy contract, per element, ref being the exact sum and S that of the
+ * products' magnitudes, sum_k |a_ik b_kj|: |C - ref| <= 2^-8 |ref| + 2^-20 S
+ * for products whose signs are random, and for all inputs |C - ref| <=
+ * 2^-8 |ref| + (K + 32) 2^-24 S, which allows for what the tensor core cuts of
+ * its additions, worst for large products that cancel among many small ones.
  */
 gemm_status_t gemm_bf16_f32acc_bf16(int64_t M, int64_t N, int64_t K,
                                     const uint16_t *A, int64_t lda,
